@@ -1,6 +1,7 @@
 /*
  * tkphi.h -- C ABI of libtkphi: decode-step Top-K+phi residual-mass attention
- * and its prefill summary build, as hand-written CUDA kernels for sm_100a.
+ * and its prefill summary build, and the append / attention calls of a paged cache,
+ * as hand-written CUDA kernels for sm_100a.
  *
  * Method (arXiv 2604.05438, "Residual-Mass Accounting for Partial-KV Decoding"):
  * for one attention layer and each decode query head the library
@@ -284,6 +285,122 @@ tkphi_status tkphi_decode_step_mlp(const tkphi_kv_desc* kv, const tkphi_mlp_desc
                                    uint32_t flags, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
+ * ---------------------------------------------------------------------------------------------
+ * Paged cache: writing it, attention over all of it, attention over selected pages.
+ *
+ * The calls above read a cache that somebody has filled and that lies in one piece per head.  The calls below serve
+ * the rest of a serving step on a cache kept in pages: rotate and append the new tokens' keys and values, attend from
+ * the new tokens to the whole cache (prefill, chunks of a prompt, decoding), or to the pages that a cheap bound selects.
+ * (The paper has no counterpart; exact attention is its baseline y = nu / Z over all keys, Sec. 3, and page selection
+ * is one more partial-KV selector beside the exhaustive Top-K of Sec. 5.1.)  A contiguous cache of this library is
+ * also a paged one if its sequences start at multiples of page_size rows: page = row / page_size.
+ *
+ * One descriptor is one step of `batch` sequences.  kv_lens[b] is the sequence's cache length with this step's new
+ * tokens, cu_q[b] .. cu_q[b+1]-1 are the rows of its new tokens in k_new, v_new, q and y; they are its last
+ * q_len = cu_q[b+1] - cu_q[b] cache positions (q_len 0: the sequence takes no part).  Position t of sequence b is slot
+ * t % page_size of page page_table[b][t / page_size]; element (page, head, slot, dim) of k and v is at
+ * base + page*stride_page + head*stride_head + slot*stride_token + dim (16-bit elements).
+ * Requirements: 1 <= batch <= 1024; head_dim 64 or 128; n_q_heads a multiple of n_kv_heads, at most 16 query heads per
+ * KV head; page_size 16, 32, 64 or 128; k, v (and key_bounds) 16-byte aligned; strides multiples of 8 elements that
+ * give every element memory of its own (in any order of page, head and slot); cu_q[0] = 0, non-decreasing;
+ * 0 <= q_len <= kv_len <= max_pages * page_size (TKPHI_FLAG_FULL_CONTEXT lifts q_len <= kv_len), kv_len < 2^31 - 1024.
+ * Host and device copies as in the general rules, with one addition for captured graphs: the launches are sized by
+ * the host copy of kv_lens, and a replayed graph may find other device lengths as long as each is at most the captured
+ * host value and still at least q_len; cu_q must be the captured one.
+ *  - Page table: entries behind a sequence's last page are not read.  An entry outside [0, n_pages) is never followed:
+ *    its rows are not written, or count as unspecified values, and *status is set to TKPHI_ERR_INVALID_ARG.  Pages that
+ *    receive rows must belong to one sequence of the batch; pages that are only read may be shared.
+ *  - status: a device int32 owned by the caller and set to 0 by it; the kernels store an error there (a bad page, or
+ *    TKPHI_ERR_TIMEOUT) and never clear it.  Required.
+ *  - Slots at or behind a sequence's length may hold anything, NaN included: nothing read from them reaches a result.
+ *  - key_bounds (optional; needed by tkphi_paged_block_attention): [n_pages][n_kv_heads][2][head_dim] in the cache's
+ *    type, the element-wise minimum and maximum of each page's keys.
+ */
+enum { TKPHI_DTYPE_BF16 = 0, TKPHI_DTYPE_FP16 = 1 };
+typedef struct {
+  int32_t batch, n_q_heads, n_kv_heads, head_dim;
+  int32_t dtype;                  /* TKPHI_DTYPE_*: of the cache, q, y, k_new, v_new and key_bounds */
+  int32_t page_size, n_pages, max_pages;
+  void* k;                        /* device; written by tkphi_paged_append only */
+  void* v;
+  int64_t stride_page, stride_head, stride_token;
+  const int32_t* page_table;      /* device, [batch][max_pages] */
+  const int64_t* kv_lens_host;    /* host,   [batch] */
+  const int64_t* kv_lens_dev;     /* device, [batch] */
+  const int64_t* cu_q_host;       /* host,   [batch+1] */
+  const int64_t* cu_q_dev;        /* device, [batch+1] */
+  void* key_bounds;               /* device or NULL */
+  int32_t* status;                /* device */
+} tkphi_paged_desc;
+
+/* New tokens of one step.  Element (token row t, head h, dim c) of k_new is at t*stride_token + h*stride_head + c, and
+ * so on; all pointers 16-byte aligned, all strides multiples of 8 elements (a fused projection's slices work as they
+ * are).  q and q_out (both or neither): the step's queries, rotated into q_out, which may be q itself (same strides)
+ * and otherwise must not overlap it. */
+typedef struct {
+  const void* k_new; int64_t k_stride_token, k_stride_head;  /* [total_q][n_kv_heads][head_dim] */
+  const void* v_new; int64_t v_stride_token, v_stride_head;
+  const void* q;     int64_t q_stride_token, q_stride_head;  /* [total_q][n_q_heads][head_dim] or NULL */
+  void* q_out;       int64_t o_stride_token, o_stride_head;
+  const float* inv_freq;          /* device, [rot_dim / 2] angle per position; NULL if rot_dim is 0 */
+  int32_t rot_dim;                /* dims rotated, from dim 0: a multiple of 16, at most head_dim; 0: none */
+  int32_t pairs;                  /* 0: dim c turns with dim c + rot_dim/2; 1: dim 2c with dim 2c + 1 */
+  const int64_t* positions;       /* device, [total_q] positions of the rotation, or NULL: the cache positions */
+} tkphi_append_desc;
+
+/*
+ * Rotates the new keys (and queries) by their positions and writes keys and values into the cache's pages:
+ * (a, c) -> (a cos w - c sin w, c cos w + a sin w) with w = position * inv_freq in 64 bits, the products in 32, rounded
+ * once.  With key_bounds, the bounds of every page that receives a row are recomputed from its rows below the new
+ * length (so they are right after a rollback of drafted tokens, too).  No workspace.
+ */
+tkphi_status tkphi_paged_append(const tkphi_paged_desc* kv, const tkphi_append_desc* step, void* cuda_stream);
+
+/* Flag of tkphi_paged_attention: every new token sees all kv_len rows of its sequence instead of those up to its own
+ * position.  A sequence may then be shorter than its number of new tokens, or empty. */
+enum { TKPHI_FLAG_FULL_CONTEXT = 2 };
+
+/* Workspace kinds of tkphi_paged_workspace_bytes. */
+enum { TKPHI_WS_PAGED_ATTENTION = 4, TKPHI_WS_PAGED_BLOCK_ATTENTION = 5 };
+
+/* Pages that tkphi_paged_block_attention reads for a token that sees n pages (its own is the last): the first
+ * n_sink_pages, the last n_tail_pages (>= 1), and of those between the topk_pages with the largest bounds. */
+typedef struct {
+  int32_t n_sink_pages, n_tail_pages, topk_pages;
+} tkphi_page_selection;
+
+/* Bytes of workspace (256-byte aligned device memory, contents irrelevant) of the paged calls; selection may be NULL
+ * for TKPHI_WS_PAGED_ATTENTION.  0 on invalid arguments.  Enough for all shorter kv_lens of the same cu_q, too. */
+size_t tkphi_paged_workspace_bytes(const tkphi_paged_desc* kv, const tkphi_page_selection* selection, int which);
+
+/*
+ * Attention of the new tokens over their sequences' caches: y = softmax(scale q.k) v over the visible keys (the
+ * token's own position included), all new tokens of all sequences in one call, whatever mix of lengths.
+ *   q     [total_q][n_q_heads][head_dim], y_out likewise, both in the cache's type, contiguous, 16-byte aligned.
+ *   lse   fp32 [total_q][n_q_heads] or NULL: log of the softmax denominator, log sum exp(scale q.k), with which
+ *         results over disjoint sets of keys can be joined.  A token that sees nothing gets y = 0, lse = -inf.
+ *   scale 0 for 1/sqrt(head_dim), else finite and positive.
+ *   flags TKPHI_FLAG_FULL_CONTEXT or 0.
+ */
+tkphi_status tkphi_paged_attention(const tkphi_paged_desc* kv, const void* q, void* y_out, float* lse_out, float scale,
+                                   uint32_t flags, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Attention over selected pages.  For every new token and KV head the middle pages are ordered by the largest score
+ * that a key within their bounds could have with one of the group's query heads,
+ *   bound = max over the group of sum_c max(q_c lo_c, q_c hi_c)
+ * (evaluated in 64 bits; equal bounds go to the lower page), and attention runs exactly over the rows of the selected
+ * pages up to the token's position.  A token that sees no more than n_sink_pages + n_tail_pages + topk_pages pages
+ * gets plain attention.
+ *   page_idx_out  int32 [total_q][n_kv_heads][n_sink_pages + n_tail_pages + topk_pages] or NULL: the selected pages
+ *                 (indices into the sequence's page table row), ascending, padded with -1.
+ * Other arguments as for tkphi_paged_attention.
+ */
+tkphi_status tkphi_paged_block_attention(const tkphi_paged_desc* kv, const tkphi_page_selection* selection,
+                                         const void* q, void* y_out, float* lse_out, int32_t* page_idx_out, float scale,
+                                         void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
  * Reads the device status word that the kernels of the last call using this
  * workspace set (0 = fine; TKPHI_ERR_TIMEOUT if a bounded wait ran out).  Waits
  * for the stream.  *status_out is a host int.
@@ -321,7 +438,11 @@ enum {
   TKPHI_KERNEL_MEMSET = 4,          /* clearing counters when there is nothing to score */
   TKPHI_KERNEL_CACHED_Z = 5,        /* <phi_q, cached phi_k row> of the retrieved tokens (phi_k_cache given) */
   TKPHI_KERNEL_MLP = 6,             /* the layers of the MLP key feature map (weight conversion included) */
-  TKPHI_KERNEL_KINDS = 7
+  TKPHI_KERNEL_PAGED_APPEND = 7,    /* rotation and append to a paged cache */
+  TKPHI_KERNEL_PAGED_SELECT = 8,    /* page bounds and selection */
+  TKPHI_KERNEL_PAGED_ROWS = 9,      /* attention of few query rows over a paged cache, and its join */
+  TKPHI_KERNEL_PAGED_TILES = 10,    /* attention of many query rows over a paged cache, and its join */
+  TKPHI_KERNEL_KINDS = 11
 };
 void tkphi_kernel_timing_enable(int32_t on);
 tkphi_status tkphi_kernel_timing_read(float* ms_out, int32_t* count_out);

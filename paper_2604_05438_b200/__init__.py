@@ -1,4 +1,4 @@
-"""Top-K+phi residual-mass decode attention for B200 (sm_100a).
+"""Top-K+phi residual-mass decode attention for B200 (sm_100a), and the append and attention calls of a paged cache.
 
 Thin Python binding over the C-ABI library ``libtkphi.so`` (see ``include/tkphi.h``).
 Every step of the method runs in the library's CUDA kernels; this package only
@@ -14,6 +14,16 @@ from .binding import (  # noqa: F401
     build_summaries_cached,
     decode_step_mlp,
     WS_MLP_KEY_FEATURES,
+    PagedKVCache,
+    RotaryMap,
+    PageSelection,
+    paged_workspace_bytes,
+    paged_append,
+    paged_attention,
+    paged_block_attention,
+    WS_PAGED_ATTENTION,
+    WS_PAGED_BLOCK_ATTENTION,
+    FLAG_FULL_CONTEXT,
     load_library,
     library_path,
     workspace_bytes,

@@ -14,7 +14,8 @@ _LIB_PATH = os.path.join(_HERE, "libtkphi.so")
 _lib = None
 
 WS_BUILD, WS_TOPK_DECODE, WS_DECODE_STEP, WS_MLP_KEY_FEATURES = 0, 1, 2, 3
-FLAG_NONE, FLAG_NOSUB = 0, 1
+WS_PAGED_ATTENTION, WS_PAGED_BLOCK_ATTENTION = 4, 5
+FLAG_NONE, FLAG_NOSUB, FLAG_FULL_CONTEXT = 0, 1, 2
 
 EXPORTED_SYMBOLS = (
     "tkphi_workspace_bytes", "tkphi_build_summaries", "tkphi_topk_decode", "tkphi_decode_step",
@@ -23,9 +24,11 @@ EXPORTED_SYMBOLS = (
     "tkphi_build_summaries_static", "tkphi_static_last_error", "tkphi_static_device_status",
     "tkphi_selftest_timeout",
     "tkphi_mlp_key_features", "tkphi_build_summaries_cached", "tkphi_decode_step_mlp",
+    "tkphi_paged_workspace_bytes", "tkphi_paged_append", "tkphi_paged_attention", "tkphi_paged_block_attention",
 )
 STATIC_SCRATCH_BYTES = 8 << 20
-KERNEL_KINDS = ("score", "select", "exact_residual", "build", "memset", "cached_z", "mlp")
+KERNEL_KINDS = ("score", "select", "exact_residual", "build", "memset", "cached_z", "mlp", "paged_append", "paged_select",
+                "paged_rows", "paged_tiles")
 ERR_TIMEOUT = -5
 
 
@@ -52,6 +55,27 @@ class _MlpDesc(C.Structure):
     _fields_ = [("d_emb", C.c_int32), ("n_heads", C.c_int32), ("w_s", C.c_void_p), ("b_s", C.c_void_p),
                 ("w_1", C.c_void_p), ("b_1", C.c_void_p), ("w_2", C.c_void_p), ("b_2", C.c_void_p),
                 ("alpha", C.c_void_p), ("w_o", C.c_void_p), ("b_o", C.c_void_p)]
+
+
+class _PagedDesc(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("stride_page", C.c_int64), ("stride_head", C.c_int64),
+                ("stride_token", C.c_int64), ("page_table", C.c_void_p), ("kv_lens_host", C.c_void_p),
+                ("kv_lens_dev", C.c_void_p), ("cu_q_host", C.c_void_p), ("cu_q_dev", C.c_void_p),
+                ("key_bounds", C.c_void_p), ("status", C.c_void_p)]
+
+
+class _AppendDesc(C.Structure):
+    _fields_ = [("k_new", C.c_void_p), ("k_stride_token", C.c_int64), ("k_stride_head", C.c_int64),
+                ("v_new", C.c_void_p), ("v_stride_token", C.c_int64), ("v_stride_head", C.c_int64),
+                ("q", C.c_void_p), ("q_stride_token", C.c_int64), ("q_stride_head", C.c_int64),
+                ("q_out", C.c_void_p), ("o_stride_token", C.c_int64), ("o_stride_head", C.c_int64),
+                ("inv_freq", C.c_void_p), ("rot_dim", C.c_int32), ("pairs", C.c_int32), ("positions", C.c_void_p)]
+
+
+class _PageSelection(C.Structure):
+    _fields_ = [("n_sink_pages", C.c_int32), ("n_tail_pages", C.c_int32), ("topk_pages", C.c_int32)]
 
 
 def library_path() -> str:
@@ -97,6 +121,16 @@ def load_library():
     lib.tkphi_decode_step_mlp.argtypes = [C.POINTER(_KvDesc), C.POINTER(_MlpDesc), C.c_void_p, C.c_void_p, C.c_void_p,
                                           C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                           C.c_void_p, C.c_uint32, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.tkphi_paged_workspace_bytes.restype = C.c_size_t
+    lib.tkphi_paged_workspace_bytes.argtypes = [C.POINTER(_PagedDesc), C.POINTER(_PageSelection), C.c_int]
+    lib.tkphi_paged_append.restype = C.c_int
+    lib.tkphi_paged_append.argtypes = [C.POINTER(_PagedDesc), C.POINTER(_AppendDesc), C.c_void_p]
+    lib.tkphi_paged_attention.restype = C.c_int
+    lib.tkphi_paged_attention.argtypes = [C.POINTER(_PagedDesc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
+                                          C.c_uint32, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.tkphi_paged_block_attention.restype = C.c_int
+    lib.tkphi_paged_block_attention.argtypes = [C.POINTER(_PagedDesc), C.POINTER(_PageSelection), C.c_void_p, C.c_void_p,
+                                                C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_size_t, C.c_void_p]
     lib.tkphi_device_status.restype = C.c_int
     lib.tkphi_device_status.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(C.c_int32)]
     lib.tkphi_kernel_timing_enable.restype = None
@@ -211,6 +245,106 @@ class MlpMaps:
         return _MlpDesc(self.w_1.shape[1], self.w_s.shape[0], *[t.data_ptr() for t in ts])
 
 
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1}
+
+
+class PagedKVCache:
+    """One step of a batch of sequences over a paged K/V cache, as the library sees it (no copies of the cache are made).
+
+    k, v: device tensors of one 16-bit type addressed as [page, head, slot, dim] through their (equal) strides; a cache
+    stored [page, slot, head, dim] is passed as its ``transpose(1, 2)``.  page_table: int32 device [batch, max_pages].
+    kv_lens: int64 host [batch], cache lengths with this step's new tokens; cu_q: int64 host [batch+1], the new tokens'
+    rows; device copies are kept alongside.  key_bounds: [n_pages, n_kv_heads, 2, head_dim] or None.  status: device
+    int32 word in which the kernels leave errors (made here, zero, unless given); ``device_status()`` reads it.
+    """
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, kv_lens, cu_q, n_q_heads: int,
+                 key_bounds: Optional[torch.Tensor] = None, kv_lens_dev: Optional[torch.Tensor] = None,
+                 cu_q_dev: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+        dev = k.device
+        self.k, self.v, self.page_table, self.key_bounds, self.n_q_heads = k, v, page_table, key_bounds, n_q_heads
+        self.kv_lens = np.ascontiguousarray(kv_lens, dtype=np.int64)
+        self.cu_q = np.ascontiguousarray(cu_q, dtype=np.int64)
+        assert k.dtype in _DTYPES and v.dtype == k.dtype and k.dim() == 4 and v.shape == k.shape
+        assert k.stride() == v.stride() and k.stride(3) == 1
+        assert self.kv_lens.ndim == 1 and self.cu_q.shape == (len(self.kv_lens) + 1,)
+        assert page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.is_contiguous()
+        assert page_table.shape[0] == len(self.kv_lens)
+        if key_bounds is not None:
+            assert key_bounds.dtype == k.dtype and key_bounds.is_contiguous()
+            assert key_bounds.shape == (k.shape[0], k.shape[1], 2, k.shape[3])
+        self.kv_lens_dev = torch.from_numpy(self.kv_lens).to(dev) if kv_lens_dev is None else kv_lens_dev
+        self.cu_q_dev = torch.from_numpy(self.cu_q).to(dev) if cu_q_dev is None else cu_q_dev
+        self.status = torch.zeros(1, dtype=torch.int32, device=dev) if status is None else status
+        assert self.kv_lens_dev.dtype == torch.int64 and self.kv_lens_dev.shape == self.kv_lens.shape
+        assert self.cu_q_dev.dtype == torch.int64 and self.cu_q_dev.shape == self.cu_q.shape
+        assert self.status.dtype == torch.int32 and self.status.numel() == 1
+        for t in (v, page_table, key_bounds, self.kv_lens_dev, self.cu_q_dev, self.status):
+            assert t is None or t.device == dev, "the cache, its page table and its lengths must be on one device"
+        self.total_q = int(self.cu_q[-1])
+        self._desc = _PagedDesc(len(self.kv_lens), n_q_heads, k.shape[1], k.shape[3], _DTYPES[k.dtype], k.shape[2],
+                                k.shape[0], page_table.shape[1], k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
+                                k.stride(2), page_table.data_ptr(), self.kv_lens.ctypes.data, self.kv_lens_dev.data_ptr(),
+                                self.cu_q.ctypes.data, self.cu_q_dev.data_ptr(),
+                                None if key_bounds is None else key_bounds.data_ptr(), self.status.data_ptr())
+
+    @property
+    def batch(self) -> int:
+        return len(self.kv_lens)
+
+    def desc(self) -> _PagedDesc:
+        return self._desc
+
+    def device_status(self) -> int:
+        """0, or the error that a call on this descriptor's status word left there (waits for the device)."""
+        return int(self.status.item())
+
+    def _take(self, t: torch.Tensor, heads: int, contiguous: bool = True) -> int:
+        """Pointer of a [total_q, heads, head_dim] tensor of the cache's type on the cache's device."""
+        k = self.k
+        if t.dtype != k.dtype or t.device != k.device or t.shape != (self.total_q, heads, k.shape[3]):
+            raise ValueError(f"expected {k.dtype} [{self.total_q}, {heads}, {k.shape[3]}] on {k.device}, got {t.dtype} "
+                             f"{list(t.shape)} on {t.device}")
+        if not (t.is_contiguous() if contiguous else t.stride(2) == 1):
+            raise ValueError("tensor must be contiguous" if contiguous else "the last dim must be contiguous")
+        return t.data_ptr()
+
+
+@dataclass
+class RotaryMap:
+    """Position rotation: fp32 device inv_freq [rot_dim / 2] (angle per position); pairs: neighbouring dims are partners
+    (otherwise dim c and dim c + rot_dim / 2)."""
+    inv_freq: torch.Tensor
+    pairs: bool = False
+
+    def __post_init__(self):
+        assert self.inv_freq.dtype == torch.float32 and self.inv_freq.dim() == 1 and self.inv_freq.is_contiguous()
+
+
+@dataclass
+class PageSelection:
+    """Pages that paged_block_attention reads: the first n_sink_pages, the last n_tail_pages, topk_pages between."""
+    n_sink_pages: int
+    n_tail_pages: int
+    topk_pages: int
+
+    @property
+    def n_pages(self) -> int:
+        return self.n_sink_pages + self.n_tail_pages + self.topk_pages
+
+    def desc(self) -> _PageSelection:
+        return _PageSelection(self.n_sink_pages, self.n_tail_pages, self.topk_pages)
+
+
+def _on_device(t: torch.Tensor, call, stream):
+    """call(stream pointer) with t's device current: launches go to the device that holds the data."""
+    index = t.device.index
+    if index is None or index == torch.cuda.current_device():
+        return call(_stream_ptr(stream))
+    with torch.cuda.device(index):
+        return call(_stream_ptr(stream))
+
+
 def _topk_host(topk) -> np.ndarray:
     return np.ascontiguousarray(topk, dtype=np.int32)
 
@@ -313,6 +447,89 @@ def decode_step(kv: KVCache, phi: PhiMaps, q: torch.Tensor, topk_host, topk_dev:
                                  int(topk_max), S.data_ptr(), u.data_ptr(), _ptr(idx_out), y_out.data_ptr(),
                                  _ptr(dbg_out), int(flags), workspace.data_ptr(),
                                  workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+
+
+def paged_workspace_bytes(kv: PagedKVCache, which: int, selection: Optional[PageSelection] = None) -> int:
+    lib = load_library()
+    sel = None if selection is None else C.byref(selection.desc())
+    with torch.cuda.device(kv.k.device):          # the plan goes by the device's multiprocessors
+        n = lib.tkphi_paged_workspace_bytes(C.byref(kv.desc()), sel, which)
+    if n == 0:
+        raise TkphiError(-1, lib.tkphi_last_error().decode())
+    return int(n)
+
+
+def paged_append(kv: PagedKVCache, k_new: torch.Tensor, v_new: torch.Tensor, rotary: Optional[RotaryMap] = None,
+                 q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                 positions: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Rotates the new keys (and q into q_out) by their positions and writes keys and values into the cache's pages;
+    key bounds of the touched pages follow.  k_new, v_new, q, q_out: [total_q, heads, head_dim], any token and head
+    strides."""
+    lib = load_library()
+    hkv = kv.k.shape[1]
+    d = _AppendDesc()
+    d.k_new, d.k_stride_token, d.k_stride_head = kv._take(k_new, hkv, False), k_new.stride(0), k_new.stride(1)
+    d.v_new, d.v_stride_token, d.v_stride_head = kv._take(v_new, hkv, False), v_new.stride(0), v_new.stride(1)
+    if q is not None:
+        d.q, d.q_stride_token, d.q_stride_head = kv._take(q, kv.n_q_heads, False), q.stride(0), q.stride(1)
+    if q_out is not None:
+        d.q_out, d.o_stride_token, d.o_stride_head = kv._take(q_out, kv.n_q_heads, False), q_out.stride(0), q_out.stride(1)
+    if rotary is not None:
+        assert rotary.inv_freq.device == kv.k.device
+        d.inv_freq, d.rot_dim, d.pairs = rotary.inv_freq.data_ptr(), 2 * rotary.inv_freq.numel(), int(rotary.pairs)
+    if positions is not None:
+        assert positions.dtype == torch.int64 and positions.shape == (kv.total_q,) and positions.is_contiguous()
+        assert positions.device == kv.k.device
+        d.positions = positions.data_ptr()
+    _check(_on_device(kv.k, lambda s: lib.tkphi_paged_append(C.byref(kv._desc), C.byref(d), s), stream))
+
+
+def _lse_ptr(kv: PagedKVCache, lse: Optional[torch.Tensor]) -> Optional[int]:
+    if lse is None:
+        return None
+    if lse.dtype != torch.float32 or lse.shape != (kv.total_q, kv.n_q_heads) or not lse.is_contiguous() or lse.device != kv.k.device:
+        raise ValueError(f"lse_out must be contiguous float32 [{kv.total_q}, {kv.n_q_heads}] on {kv.k.device}")
+    return lse.data_ptr()
+
+
+def paged_attention(kv: PagedKVCache, q: torch.Tensor, y_out: torch.Tensor, lse_out: Optional[torch.Tensor],
+                    scale: Optional[float], flags: int, workspace: torch.Tensor, stream=None) -> None:
+    """Attention of the step's new tokens over their sequences' whole caches; q, y_out [total_q, n_q_heads, head_dim],
+    lse_out fp32 [total_q, n_q_heads] or None, scale None for 1/sqrt(head_dim), flags FLAG_NONE or FLAG_FULL_CONTEXT."""
+    lib = load_library()
+    args = (C.byref(kv._desc), kv._take(q, kv.n_q_heads), kv._take(y_out, kv.n_q_heads), _lse_ptr(kv, lse_out),
+            0.0 if scale is None else _positive(scale), flags, _ws_ptr(kv, workspace), workspace.numel() * workspace.element_size())
+    _check(_on_device(kv.k, lambda s: lib.tkphi_paged_attention(*args, s), stream))
+
+
+def paged_block_attention(kv: PagedKVCache, selection: PageSelection, q: torch.Tensor, y_out: torch.Tensor,
+                          lse_out: Optional[torch.Tensor], page_idx_out: Optional[torch.Tensor], scale: Optional[float],
+                          workspace: torch.Tensor, stream=None) -> None:
+    """Attention over the pages that ``selection`` takes for each new token and KV head; page_idx_out int32
+    [total_q, n_kv_heads, selection.n_pages] or None gets them."""
+    lib = load_library()
+    idx = None
+    if page_idx_out is not None:
+        want = (kv.total_q, kv.k.shape[1], selection.n_pages)
+        if page_idx_out.dtype != torch.int32 or page_idx_out.shape != want or not page_idx_out.is_contiguous() or page_idx_out.device != kv.k.device:
+            raise ValueError(f"page_idx_out must be contiguous int32 {list(want)} on {kv.k.device}")
+        idx = page_idx_out.data_ptr()
+    sel = selection.desc()
+    args = (C.byref(kv._desc), C.byref(sel), kv._take(q, kv.n_q_heads), kv._take(y_out, kv.n_q_heads), _lse_ptr(kv, lse_out),
+            idx, 0.0 if scale is None else _positive(scale), _ws_ptr(kv, workspace), workspace.numel() * workspace.element_size())
+    _check(_on_device(kv.k, lambda s: lib.tkphi_paged_block_attention(*args, s), stream))
+
+
+def _positive(scale: float) -> float:
+    if not scale > 0:
+        raise ValueError(f"scale must be positive, got {scale}")
+    return float(scale)
+
+
+def _ws_ptr(kv: PagedKVCache, workspace: torch.Tensor) -> int:
+    if workspace.device != kv.k.device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous on {kv.k.device}")
+    return workspace.data_ptr()
 
 
 def device_status(workspace: torch.Tensor, stream=None) -> int:

@@ -1,6 +1,6 @@
 // C ABI of libtkphi: argument validation, workspace layout, launches.
 #include "../../include/tkphi.h"
-#include "common.cuh"
+#include "host.cuh"
 
 #include <cmath>
 #include <cstdarg>
@@ -11,8 +11,12 @@
 using namespace tkphi;
 
 namespace {
-
 thread_local char g_err[512] = "";
+}
+
+namespace tkphi {
+
+void clear_error() { g_err[0] = 0; }
 
 tkphi_status fail(tkphi_status st, const char* fmt, ...) {
   va_list ap;
@@ -22,7 +26,47 @@ tkphi_status fail(tkphi_status st, const char* fmt, ...) {
   return st;
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+EncodeTiledFn encode_fn() {
+  static EncodeTiledFn fn = nullptr;
+  if (!fn) {
+    void* ptr = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &qres) == cudaSuccess &&
+        qres == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<EncodeTiledFn>(ptr);
+  }
+  return fn;
+}
+
+// ---- optional per-kernel timing (off by default): CUDA events around every launch
+bool g_timing = false;
+std::vector<TimedSpan> g_spans;
+
+ScopedSpan::ScopedSpan(cudaStream_t s, int k) : st(s), kind(k) {
+  if (!g_timing) return;
+  if (cudaEventCreate(&a) != cudaSuccess || cudaEventCreate(&b) != cudaSuccess) { a = b = nullptr; return; }
+  cudaEventRecord(a, st);
+}
+ScopedSpan::~ScopedSpan() {
+  if (!a) return;
+  cudaEventRecord(b, st);
+  try { g_spans.push_back({a, b, kind}); } catch (...) { cudaEventDestroy(a); cudaEventDestroy(b); }   // no exception leaves a C entry
+}
+
+tkphi_status check_ws(void* ws, size_t have, size_t need) {
+  if (!ws) return fail(TKPHI_ERR_WORKSPACE, "workspace is NULL");
+  if (reinterpret_cast<uintptr_t>(ws) & 255u) return fail(TKPHI_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (have < need) return fail(TKPHI_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", have, need);
+  return TKPHI_OK;
+}
+
+tkphi_status cuda_fail(cudaError_t e, const char* what) {
+  return fail(TKPHI_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+
+}  // namespace tkphi
+
+namespace {
 
 struct Shape {
   long long total_tokens;
@@ -168,22 +212,6 @@ void build_layout(const tkphi_kv_desc* kv, const Shape& sh, WsLayout* L) {
   L->total = o;
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  if (!fn) {
-    void* ptr = nullptr;
-    cudaDriverEntryPointQueryResult qres;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &qres) == cudaSuccess &&
-        qres == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(ptr);
-  }
-  return fn;
-}
-
 // 3-D view [head][row][dim] of a K or V cache; box = 64 dims x box_rows rows of one head,
 // stored with the 128-byte swizzle (head_dim 128 takes two boxes per tile).
 tkphi_status make_tensor_map(const tkphi_kv_desc* kv, const void* base, int box_rows, long long total_tokens,
@@ -230,36 +258,6 @@ int make_gather_map(const tkphi_kv_desc* kv, const void* base, long long total_t
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? mode : -1;
-}
-
-// ---- optional per-kernel timing (off by default): CUDA events around every launch
-struct TimedSpan { cudaEvent_t a, b; int kind; };
-bool g_timing = false;
-std::vector<TimedSpan> g_spans;
-
-struct ScopedSpan {
-  cudaStream_t st; int kind; cudaEvent_t a = nullptr, b = nullptr;
-  ScopedSpan(cudaStream_t s, int k) : st(s), kind(k) {
-    if (!g_timing) return;
-    if (cudaEventCreate(&a) != cudaSuccess || cudaEventCreate(&b) != cudaSuccess) { a = b = nullptr; return; }
-    cudaEventRecord(a, st);
-  }
-  ~ScopedSpan() {
-    if (!a) return;
-    cudaEventRecord(b, st);
-    g_spans.push_back({a, b, kind});
-  }
-};
-
-tkphi_status check_ws(void* ws, size_t have, size_t need) {
-  if (!ws) return fail(TKPHI_ERR_WORKSPACE, "workspace is NULL");
-  if (reinterpret_cast<uintptr_t>(ws) & 255u) return fail(TKPHI_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-  if (have < need) return fail(TKPHI_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", have, need);
-  return TKPHI_OK;
-}
-
-tkphi_status cuda_fail(cudaError_t e, const char* what) {
-  return fail(TKPHI_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
 // Workspace of tkphi_mlp_key_features: status word, bf16 copies of the weights, three bf16 activation

@@ -1,0 +1,560 @@
+// Attention of few query rows over a paged cache: decoding (one token per sequence), a few drafted tokens, and the
+// page-selected form, where every token of a KV head reads a page list of its own.
+//
+//   y = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale * q.k_t - m),  lse = m + log sum_t p_t   over the visible keys t
+//
+// in one pass with the running maximum m and sum.  A unit is up to 16 query rows of one KV head (tokens x query heads
+// of the group), so that the group's heads share every key and value read.  Bound: memory, 2 * 2 * head_dim bytes per
+// key against 16 rows of work.  The 16-row mma.sync tile is therefore the right size of matrix instruction (a
+// tcgen05 tile has 64 rows at least, and its accumulators would have to come back from tensor memory for every
+// tile); what carries the kernel is the TMA ring that keeps copies in flight:
+//   - one producer warp: a tile of 64 keys and their values is a handful of page boxes (lane = one box); page ids are
+//     read 32 at a time, one batch ahead;
+//   - four compute warps, each with 16 keys of the tile and a running softmax of its own, so that nothing is exchanged
+//     between warps until a unit ends; rows are rescaled only when a maximum moved.
+// Probabilities enter the second product as hi + lo pairs of the element type (2^-16 relative for bf16): that costs
+// 16 extra matrix instructions per tile, which the kernel has time for, and leaves the output's own rounding as the
+// only one of its size.
+// Work is dealt out evenly: the tiles of all units form one line, cut into as many equal pieces as there are resident
+// CTAs; a unit that is cut leaves partial results, joined in a fixed order by a second, dependent kernel.
+#include "paged.cuh"
+
+namespace tkphi {
+
+constexpr int kRowWarps = 4;
+constexpr int kRowThreads = (kRowWarps + 1) * 32;
+
+template <int D>
+struct RowCfg {
+  static constexpr int HALVES = D / 64;
+  static constexpr int HALF = kRowKeys * 128;               // bytes of one 64-dim half of a 64-key tile
+  static constexpr int TILE = HALVES * HALF;                // keys or values of a tile
+  static constexpr int STAGE = 2 * TILE;
+  static constexpr int NS = D == 128 ? 3 : 6;
+  static constexpr size_t red = (size_t)NS * STAGE;         // [4 warps][16 rows][64 dims] fp32
+  static constexpr size_t stat = red + kRowWarps * kRowTile * 64 * 4;   // [4][16][2]
+  static constexpr size_t bars = stat + kRowWarps * kRowTile * 2 * 4;
+  static constexpr size_t total = bars + (2 * NS) * 8 + 16;
+};
+size_t paged_rows_smem(int d) { return d == 128 ? RowCfg<128>::total : RowCfg<64>::total; }
+
+// The pieces of one CTA: (unit, tile range) one after the other.  Every warp runs its own copy.
+template <bool BLOCK>
+struct RowWalk {
+  const PagedProblem& p;
+  // current piece
+  int b, h, tok0, rows, len, pos0;      // sequence, KV head, first token of the unit (global), rows, cache length, position of row 0
+  int r_first;                          // first row of the unit within its sequence (0 in the block form)
+  int t0, t1, tiles;                    // tile range of the piece, tiles of the unit
+  int unit;                             // block form: token * hkv + head
+  int n_list;                           // block form: pages of the unit's list
+  // line position
+  int f, f1, seq_start, seq_end, seq_tiles, seq_rows, seq_tok0, seq_len, seq_q;
+
+  __device__ __forceinline__ void load_seq(int s) {
+    seq_tiles = 0; seq_rows = 0; seq_tok0 = 0; seq_len = 0; seq_q = 0;
+    if (s < p.batch) {
+      seq_tok0 = (int)__ldg(p.cu_q + s);
+      seq_q = paged_q_len(p, s);
+      seq_len = paged_kv_len(p, s);
+      seq_rows = seq_q > 0 ? seq_q * p.group : 0;
+      if (seq_rows > p.rows_limit) seq_rows = 0;
+      seq_tiles = seq_len > 0 ? (seq_len + kRowKeys - 1) / kRowKeys : 1;
+    }
+  }
+  __device__ __forceinline__ int seq_weight() const { return seq_tiles * p.hkv * ((seq_rows + kRowTile - 1) / kRowTile); }
+
+  __device__ __forceinline__ RowWalk(const PagedProblem& pr, int cta) : p(pr) {
+    const int lane = threadIdx.x & 31;
+    f = f1 = 0;
+    if (BLOCK) {
+      unit = cta / p.n_split;
+      const int part = cta % p.n_split, tok = unit / p.hkv;
+      h = unit % p.hkv;
+      b = paged_seq_of(p, tok);
+      len = paged_kv_len(p, b);
+      tok0 = tok; rows = p.group; r_first = 0;
+      pos0 = len - paged_q_len(p, b) + (tok - (int)__ldg(p.cu_q + b));
+      if (pos0 < 0) pos0 = 0;                           // (a device length below the new tokens' number)
+      const int seen = (pos0 >> p.page_shift) + 1;
+      n_list = seen < p.n_keep ? seen : p.n_keep;
+      tiles = ((n_list << p.page_shift) + kRowKeys - 1) / kRowKeys;
+      const int per = (tiles + p.n_split - 1) / p.n_split;
+      t0 = part * per;
+      t1 = t0 + per < tiles ? t0 + per : tiles;
+      f1 = t0 < t1 ? 1 : 0;
+      return;
+    }
+    // the line: sequence by sequence, in a sequence row tile by row tile, head by head
+    if (p.row_ctas == 0) {                              // one CTA per unit (sequences of one row tile)
+      b = cta / p.hkv;
+      load_seq(b);
+      seq_start = 0;
+      f = (cta % p.hkv) * seq_tiles;
+      seq_end = seq_weight();
+      f1 = seq_rows > 0 ? f + seq_tiles : f;
+      return;
+    }
+    int total = 0;
+    for (int s = 0; s < p.batch; s += 32) {
+      load_seq(s + lane);
+      total += __reduce_add_sync(0xffffffffu, seq_weight());
+    }
+    const int per = (total + p.row_ctas - 1) / p.row_ctas;
+    f = per * cta < total ? per * cta : total;
+    f1 = f + per < total ? f + per : total;
+    if (f >= f1) return;
+    int base = 0;
+    b = 0;
+    for (int s = 0; s < p.batch; s += 32) {
+      load_seq(s + lane);
+      const int w = seq_weight(), incl = warp_inclusive_scan(w) + base;
+      const unsigned hit = __ballot_sync(0xffffffffu, incl > f);
+      if (hit) {
+        const int l = __ffs(hit) - 1;
+        b = s + l;
+        seq_start = __shfl_sync(0xffffffffu, incl - w, l);
+        break;
+      }
+      base = __shfl_sync(0xffffffffu, incl, 31);
+    }
+    load_seq(b);
+    seq_end = seq_start + seq_weight();
+  }
+  __device__ __forceinline__ bool next() {
+    if (f >= f1) return false;
+    if (BLOCK) { f = f1; return true; }
+    while (f >= seq_end) {
+      load_seq(++b);
+      seq_start = seq_end;
+      seq_end += seq_weight();
+    }
+    const int local = f - seq_start, u = local / seq_tiles;
+    tiles = seq_tiles;
+    t0 = local % seq_tiles;
+    t1 = t0 + (f1 - f) < tiles ? t0 + (f1 - f) : tiles;
+    f += t1 - t0;
+    h = u % p.hkv;
+    r_first = (u / p.hkv) * kRowTile;
+    rows = seq_rows - r_first < kRowTile ? seq_rows - r_first : kRowTile;
+    tok0 = seq_tok0;
+    len = seq_len;
+    pos0 = seq_len - seq_q;
+    return true;
+  }
+  __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == tiles; }
+  __device__ __forceinline__ int slot(int cta) const { return BLOCK ? cta : 2 * cta + (t0 == 0 ? 1 : 0); }
+};
+
+template <typename T, int D, bool BLOCK>
+__global__ void __launch_bounds__(kRowThreads, 2)
+paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                  const __grid_constant__ PagedProblem p) {
+  using C = RowCfg<D>;
+  constexpr int NS = C::NS;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  float* red = reinterpret_cast<float*>(smem + C::red);
+  float* stat = reinterpret_cast<float*>(smem + C::stat);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::bars);
+  uint64_t* empty = full + NS;
+  volatile int* s_abort = reinterpret_cast<int*>(empty + NS);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int cta = blockIdx.x;
+
+  if (tid == 0) {
+    for (int s = 0; s < NS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], kRowWarps); }
+    mbar_fence_init();
+    *s_abort = 0;
+  }
+  __syncthreads();
+  pdl_launch_next();
+  if (BLOCK) pdl_wait();                       // the page lists come from the kernel before
+
+  if (warp == kRowWarps) {
+    // ================================================================ TMA producer
+    RowWalk<BLOCK> w(p, cta);
+    const int ps = 1 << p.page_shift;
+    const int npg = ps < kRowKeys ? kRowKeys >> p.page_shift : 1;             // pages of a tile
+    const int box_rows = ps < kRowKeys ? ps : kRowKeys;
+    const int copies = 2 * C::HALVES * npg;
+    const int which = lane / (C::HALVES * npg), half = (lane / npg) % C::HALVES, pg = lane % npg;
+    const CUtensorMap* tm = which ? &tmap_v : &tmap_k;
+    const uint64_t pol = BLOCK ? l2_policy_normal() : l2_policy_evict_first();
+    const uint32_t dst_off = which * C::TILE + half * C::HALF + pg * box_rows * 128;
+    int it = 0;
+    bool ok = true;
+    int issued[NS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) issued[s] = -1;
+    while (ok && w.next()) {
+      const int n_pages_unit = BLOCK ? w.n_list : (w.len + ps - 1) >> p.page_shift;
+      const int* list = BLOCK ? p.page_list + (size_t)w.unit * p.n_keep : p.table + (size_t)w.b * p.max_pages;
+      int batch0 = ((w.t0 * kRowKeys) >> p.page_shift) & ~31;
+      int id = batch0 + lane < n_pages_unit ? (BLOCK ? __ldcg(list + batch0 + lane) : __ldg(list + batch0 + lane)) : p.n_pages;
+      int id_next = batch0 + 32 + lane < n_pages_unit ? (BLOCK ? __ldcg(list + batch0 + 32 + lane) : __ldg(list + batch0 + 32 + lane)) : p.n_pages;
+      for (int t = w.t0; t < w.t1; ++t, ++it) {
+        const int stage = it % NS;
+        const int first = (t * kRowKeys) >> p.page_shift;
+        if (first >= batch0 + 32) {
+          batch0 += 32;
+          id = id_next;
+          id_next = batch0 + 32 + lane < n_pages_unit ? (BLOCK ? __ldcg(list + batch0 + 32 + lane) : __ldg(list + batch0 + 32 + lane)) : p.n_pages;
+        }
+        int page = __shfl_sync(0xffffffffu, id, (first + pg) & 31);
+        if (page < 0 || page > p.n_pages || (page == p.n_pages && first + pg < n_pages_unit)) {
+          if (lane < npg) atomicExch(p.status, kStatusBadPage);
+          page = p.n_pages;                     // a box outside the tensor arrives as zeros
+        }
+        ok = __all_sync(0xffffffffu, mbar_wait(&empty[stage], ((uint32_t)(it / NS) & 1u) ^ 1u, s_abort));
+        if (!ok) break;
+        if (lane == 0) mbar_expect_tx(&full[stage], C::STAGE);
+        __syncwarp();
+        if (lane < copies)
+          tma_load_4d(smem + (size_t)stage * C::STAGE + dst_off, tm, &full[stage], half * 64,
+                      ps > kRowKeys ? (t & 1) * kRowKeys : 0, w.h, page, pol);
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+          if (s == stage) issued[s] = it;
+      }
+    }
+    if (*s_abort) {
+      // every copy that was issued must land before shared memory is released
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+        for (uint32_t n = 0; issued[s] >= 0 && n < kWaitPolls; ++n) {
+          if (mbar_try_wait(&full[s], (uint32_t)(issued[s] / NS) & 1u)) break;
+          __nanosleep(64);
+        }
+    }
+  } else {
+    // ================================================================ compute
+    RowWalk<BLOCK> w(p, cta);
+    const int ps = 1 << p.page_shift;
+    const int rA = lane >> 2, rB = rA + 8, cc = 2 * (lane & 3);
+    bool ok = true;
+    int it = 0;
+    while (w.next()) {
+      // ---- the unit's queries as A operands: row r, dims 16 k ..
+      uint32_t qf[D / 16][4];
+      {
+        const uint32_t* qa = nullptr;
+        const uint32_t* qb = nullptr;
+        const uint32_t* q = static_cast<const uint32_t*>(p.q);
+        if (rA < w.rows) {
+          const int r = w.r_first + rA;
+          qa = q + ((size_t)(w.tok0 + r / p.group) * p.hq + w.h * p.group + r % p.group) * (D / 2);
+        }
+        if (rB < w.rows) {
+          const int r = w.r_first + rB;
+          qb = q + ((size_t)(w.tok0 + r / p.group) * p.hq + w.h * p.group + r % p.group) * (D / 2);
+        }
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          qf[k][0] = qa ? __ldg(qa + k * 8 + (cc >> 1)) : 0u;
+          qf[k][1] = qb ? __ldg(qb + k * 8 + (cc >> 1)) : 0u;
+          qf[k][2] = qa ? __ldg(qa + k * 8 + 4 + (cc >> 1)) : 0u;
+          qf[k][3] = qb ? __ldg(qb + k * 8 + 4 + (cc >> 1)) : 0u;
+        }
+      }
+      // last visible position of this thread's rows; -1: no such row
+      int limA = -1, limB = -1;
+      if (rA < w.rows) limA = BLOCK ? w.pos0 : p.causal ? w.pos0 + (w.r_first + rA) / p.group : w.len - 1;
+      if (rB < w.rows) limB = BLOCK ? w.pos0 : p.causal ? w.pos0 + (w.r_first + rB) / p.group : w.len - 1;
+      // keys up to lim_all are visible to every row of the unit
+      const int lim_all = BLOCK ? w.pos0 : p.causal ? w.pos0 + w.r_first / p.group : w.len - 1;
+      float o[D / 8][4];
+#pragma unroll
+      for (int n = 0; n < D / 8; ++n) { o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f; }
+      float mA = -INFINITY, mB = -INFINITY, lA = 0.f, lB = 0.f;
+
+      for (int t = w.t0; t < w.t1; ++t, ++it) {
+        const int stage = it % NS;
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&full[stage], (uint32_t)(it / NS) & 1u, s_abort));
+        if (!ok) continue;                                // the barriers below are still met
+        unsigned char* ks = smem + (size_t)stage * C::STAGE;
+        unsigned char* vs = ks + C::TILE;
+        // position of this warp's first key (its 16 keys never straddle a page); in the block form only the last
+        // page of a list can be partly visible, everything before it is
+        int key0 = t * kRowKeys + warp * 16;
+        if (BLOCK) {
+          const int entry = key0 >> p.page_shift;
+          if (entry < w.n_list - 1) key0 = 0 - 16;                          // all visible
+          else if (entry == w.n_list - 1) key0 = ((w.pos0 >> p.page_shift) << p.page_shift) + (key0 & (ps - 1));
+          else key0 = w.len;                                                // past the list
+        }
+        const bool skip = key0 > (BLOCK ? w.pos0 : p.causal ? w.pos0 + (w.r_first + w.rows - 1) / p.group : w.len - 1);
+        if (!skip) {
+          float s[2][4];
+#pragma unroll
+          for (int n = 0; n < 2; ++n) { s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f; }
+          {
+            const int row = warp * 16 + ((lane >> 4) << 3) + (lane & 7), sub = (lane >> 3) & 1;
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+              uint32_t bf[4];
+              ldmatrix_x4(bf, smem_u32(ks) + (k >> 2) * C::HALF + swz128(row, (2 * k + sub) & 7));
+              T::mma(s[0], qf[k], bf[0], bf[1]);
+              T::mma(s[1], qf[k], bf[2], bf[3]);
+            }
+          }
+          if (key0 + 15 > lim_all) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const int key = key0 + n * 8 + cc + e;
+                if (key > limA) s[n][e] = -INFINITY;
+                if (key > limB) s[n][2 + e] = -INFINITY;
+              }
+            // rows of the tile at or behind the sequence's end may hold anything: they must not reach the product
+            const int keep = w.len - key0;                  // >= 1 here
+            if (keep < 16) {
+              constexpr int CPR = D / 8;                    // 16-byte pieces of a row
+              for (int i = lane; i < (16 - keep) * CPR; i += 32) {
+                const int row = warp * 16 + keep + i / CPR, c = i % CPR;
+                *reinterpret_cast<uint4*>(vs + (c >> 3) * C::HALF + swz128(row, c & 7)) = make_uint4(0, 0, 0, 0);
+              }
+              fence_proxy_async_smem();                     // before the slot's next copy
+              __syncwarp();
+            }
+          }
+          float tA = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
+          float tB = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
+#pragma unroll
+          for (int d = 1; d < 4; d <<= 1) {
+            tA = fmaxf(tA, __shfl_xor_sync(0xffffffffu, tA, d));
+            tB = fmaxf(tB, __shfl_xor_sync(0xffffffffu, tB, d));
+          }
+          const float nA = fmaxf(mA, tA * p.scale_log2), nB = fmaxf(mB, tB * p.scale_log2);
+          if (__any_sync(0xffffffffu, nA > mA || nB > mB)) {
+            const float fA = nA > mA ? ex2_approx(mA - nA) : 1.f, fB = nB > mB ? ex2_approx(mB - nB) : 1.f;
+            lA *= fA; lB *= fB;
+#pragma unroll
+            for (int n = 0; n < D / 8; ++n) { o[n][0] *= fA; o[n][1] *= fA; o[n][2] *= fB; o[n][3] *= fB; }
+            mA = nA; mB = nB;
+          }
+          // a row that has seen nothing yet: every term exp2(-inf - 0) = 0
+          const float uA = mA == -INFINITY ? 0.f : mA, uB = mB == -INFINITY ? 0.f : mB;
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              s[n][e] = ex2_approx(fmaf(s[n][e], p.scale_log2, -uA));
+              s[n][2 + e] = ex2_approx(fmaf(s[n][2 + e], p.scale_log2, -uB));
+              lA += s[n][e];
+              lB += s[n][2 + e];
+            }
+          uint32_t ph[4], pl[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {                      // A operand: (row, keys 0-7), (row + 8, 0-7), (row, 8-15), (row + 8, 8-15)
+            const float x = s[j >> 1][(j & 1) * 2], y = s[j >> 1][(j & 1) * 2 + 1];
+            ph[j] = T::pack(x, y);
+            pl[j] = T::pack(x - T::lo(ph[j]), y - T::hi(ph[j]));
+          }
+          {
+            const int row = warp * 16 + (((lane >> 3) & 1) << 3) + (lane & 7), sub = lane >> 4;
+#pragma unroll
+            for (int n = 0; n < D / 16; ++n) {
+              uint32_t bf[4];
+              ldmatrix_x4_trans(bf, smem_u32(vs) + (n >> 2) * C::HALF + swz128(row, (2 * n + sub) & 7));
+              T::mma(o[2 * n], ph, bf[0], bf[1]);
+              T::mma(o[2 * n + 1], ph, bf[2], bf[3]);
+              T::mma(o[2 * n], pl, bf[0], bf[1]);
+              T::mma(o[2 * n + 1], pl, bf[2], bf[3]);
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&empty[stage]);
+      }
+
+      // ---- the four warps' softmaxes joined; a thread ends up with 8 dims of one row
+#pragma unroll
+      for (int d = 1; d < 4; d <<= 1) {
+        lA += __shfl_xor_sync(0xffffffffu, lA, d);
+        lB += __shfl_xor_sync(0xffffffffu, lB, d);
+      }
+      if ((lane & 3) == 0) {
+        stat[(warp * kRowTile + rA) * 2] = mA; stat[(warp * kRowTile + rA) * 2 + 1] = lA;
+        stat[(warp * kRowTile + rB) * 2] = mB; stat[(warp * kRowTile + rB) * 2 + 1] = lB;
+      }
+      named_barrier(1, kRowWarps * 32);
+      float MA = -INFINITY, MB = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kRowWarps; ++i) {
+        MA = fmaxf(MA, stat[(i * kRowTile + rA) * 2]);
+        MB = fmaxf(MB, stat[(i * kRowTile + rB) * 2]);
+      }
+      const float sA = mA == -INFINITY ? 0.f : ex2_approx(mA - MA), sB = mB == -INFINITY ? 0.f : ex2_approx(mB - MB);
+      const int row = tid >> 3, d8 = (tid & 7) * 8;
+      float M = -INFINITY, L = 0.f;
+#pragma unroll
+      for (int i = 0; i < kRowWarps; ++i) M = fmaxf(M, stat[(i * kRowTile + row) * 2]);
+#pragma unroll
+      for (int i = 0; i < kRowWarps; ++i) {
+        const float m = stat[(i * kRowTile + row) * 2];
+        if (m != -INFINITY) L += stat[(i * kRowTile + row) * 2 + 1] * ex2_approx(m - M);
+      }
+      const bool fin = w.whole();
+      const int slot = w.slot(cta);
+      const int r = w.r_first + row;
+      const size_t out_row = (size_t)(w.tok0 + r / p.group) * p.hq + w.h * p.group + r % p.group;
+#pragma unroll
+      for (int x = 0; x < C::HALVES; ++x) {
+        // rows of 64 floats, 8-float pieces rotated by the row so that the column accesses spread over the banks
+        float* mine = red + warp * kRowTile * 64;
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+          const int pa = ((n + rA) & 7) * 8 + cc, pb = ((n + rB) & 7) * 8 + cc;
+          *reinterpret_cast<float2*>(mine + rA * 64 + pa) = make_float2(o[x * 8 + n][0] * sA, o[x * 8 + n][1] * sA);
+          *reinterpret_cast<float2*>(mine + rB * 64 + pb) = make_float2(o[x * 8 + n][2] * sB, o[x * 8 + n][3] * sB);
+        }
+        named_barrier(1, kRowWarps * 32);
+        float a[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kRowWarps; ++i) {
+          const float4* src = reinterpret_cast<const float4*>(red + (i * kRowTile + row) * 64 + (((tid & 7) + row) & 7) * 8);
+          const float4 u = src[0], v = src[1];
+          a[0] += u.x; a[1] += u.y; a[2] += u.z; a[3] += u.w;
+          a[4] += v.x; a[5] += v.y; a[6] += v.z; a[7] += v.w;
+        }
+        if (row < w.rows) {
+          if (fin) {
+            const float inv = L > 0.f ? 1.f / L : 0.f;
+            uint4 y;
+            y.x = T::pack(a[0] * inv, a[1] * inv); y.y = T::pack(a[2] * inv, a[3] * inv);
+            y.z = T::pack(a[4] * inv, a[5] * inv); y.w = T::pack(a[6] * inv, a[7] * inv);
+            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.y) + out_row * D + x * 64 + d8) = y;
+          } else {
+            float4* dst = reinterpret_cast<float4*>(p.row_part + ((size_t)slot * kRowTile + row) * D + x * 64 + d8);
+            dst[0] = make_float4(a[0], a[1], a[2], a[3]);
+            dst[1] = make_float4(a[4], a[5], a[6], a[7]);
+          }
+        }
+        named_barrier(1, kRowWarps * 32);
+      }
+      if ((tid & 7) == 0 && row < w.rows) {
+        if (fin) {
+          if (p.lse) p.lse[out_row] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+        } else {
+          p.row_stat[((size_t)slot * kRowTile + row) * 2] = M;
+          p.row_stat[((size_t)slot * kRowTile + row) * 2 + 1] = L;
+        }
+      }
+    }
+  }
+  __syncthreads();
+  if (*s_abort && tid == 0) atomicExch(p.status, kStatusTimeout);
+}
+
+// Joins the partial results of the units that were cut: a CTA per (unit, row), a thread per pair of dims; the parts
+// are added in the order of their keys.
+template <typename T, int D, bool BLOCK>
+__global__ void __launch_bounds__(D / 2) paged_rows_merge_kernel(const __grid_constant__ PagedProblem p) {
+  pdl_wait();
+  const int lane = threadIdx.x & 31, row = blockIdx.y;
+  int first, count, step, rows, tok0, h, r;
+  if (BLOCK) {
+    const int unit = blockIdx.x, tok = unit / p.hkv;
+    h = unit % p.hkv;
+    const int b = paged_seq_of(p, tok);
+    int pos = paged_kv_len(p, b) - paged_q_len(p, b) + (tok - (int)__ldg(p.cu_q + b));
+    if (pos < 0) pos = 0;
+    const int seen = (pos >> p.page_shift) + 1, n_list = seen < p.n_keep ? seen : p.n_keep;
+    const int tiles = ((n_list << p.page_shift) + kRowKeys - 1) / kRowKeys, per = (tiles + p.n_split - 1) / p.n_split;
+    count = (tiles + per - 1) / per;
+    first = unit * p.n_split;
+    step = 1;
+    rows = p.group; tok0 = tok; r = row;
+  } else {
+    // the line as the row kernel cut it
+    const int unit = blockIdx.x, b = unit / p.hkv;
+    h = unit % p.hkv;
+    int before = 0, total = 0, mine = 0, my_tiles = 1;
+    for (int s = 0; s < p.batch; s += 32) {
+      int w = 0, tl = 1;
+      if (s + lane < p.batch) {
+        const int q = paged_q_len(p, s + lane), len = paged_kv_len(p, s + lane);
+        int rw = q > 0 ? q * p.group : 0;
+        if (rw > p.rows_limit) rw = 0;
+        tl = len > 0 ? (len + kRowKeys - 1) / kRowKeys : 1;
+        w = tl * p.hkv * ((rw + kRowTile - 1) / kRowTile);
+        if (s + lane == b) mine = rw;
+      }
+      total += __reduce_add_sync(0xffffffffu, w);
+      before += __reduce_add_sync(0xffffffffu, s + lane < b ? w : 0);
+      if (b >= s && b < s + 32) { mine = __shfl_sync(0xffffffffu, mine, b - s); my_tiles = __shfl_sync(0xffffffffu, tl, b - s); }
+    }
+    const int rt = row / kRowTile;
+    if (row >= mine) return;
+    const int per = (total + p.row_ctas - 1) / p.row_ctas;
+    const int u0 = before + (rt * p.hkv + h) * my_tiles, u1 = u0 + my_tiles;
+    const int c0 = u0 / per, c1 = (u1 - 1) / per;
+    count = c1 - c0 + 1;
+    first = 2 * c0;                       // the first part starts at the unit's first tile: slot 2 c0 + 1, then 2 (c0 + i)
+    step = 2;
+    rows = mine; tok0 = (int)__ldg(p.cu_q + b); r = row;
+  }
+  if (count < 2 || row >= rows) return;   // written by the row kernel itself
+  const int rr = r % kRowTile;
+  auto slot_of = [&](int i) { return BLOCK ? first + i : i == 0 ? first + 1 : first + step * i; };
+  float M = -INFINITY;
+  for (int i = lane; i < count; i += 32) M = fmaxf(M, __ldcg(p.row_stat + ((size_t)slot_of(i) * kRowTile + rr) * 2));
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+  float L = 0.f, a0 = 0.f, a1 = 0.f;
+#pragma unroll 4
+  for (int i = 0; i < count; ++i) {
+    const size_t s = (size_t)slot_of(i) * kRowTile + rr;
+    const float2 st = __ldcg(reinterpret_cast<const float2*>(p.row_stat) + s);
+    const float2 v = __ldcg(reinterpret_cast<const float2*>(p.row_part + s * D) + threadIdx.x);
+    const float f = st.x == -INFINITY ? 0.f : ex2_approx(st.x - M);
+    L += st.y * f;
+    a0 += v.x * f;
+    a1 += v.y * f;
+  }
+  const float inv = L > 0.f ? 1.f / L : 0.f;
+  const size_t out_row = (size_t)(tok0 + r / p.group) * p.hq + h * p.group + r % p.group;
+  reinterpret_cast<uint32_t*>(p.y)[out_row * (D / 2) + threadIdx.x] = T::pack(a0 * inv, a1 * inv);
+  if (threadIdx.x == 0 && p.lse) p.lse[out_row] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+}
+
+template <typename T, int D, bool BLOCK>
+static cudaError_t launch_rows_t(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int grid,
+                                 bool dependent, cudaStream_t st) {
+  static PerDeviceFlag configured;
+  cudaError_t e = set_max_dynamic_smem(configured, reinterpret_cast<const void*>(paged_rows_kernel<T, D, BLOCK>), RowCfg<D>::total);
+  if (e != cudaSuccess) return e;
+  if (dependent) return launch_pdl(paged_rows_kernel<T, D, BLOCK>, dim3(grid), dim3(kRowThreads), RowCfg<D>::total, st, tk, tv, p);
+  paged_rows_kernel<T, D, BLOCK><<<grid, kRowThreads, RowCfg<D>::total, st>>>(tk, tv, p);
+  return cudaGetLastError();
+}
+
+template <typename T, int D, bool BLOCK>
+static cudaError_t launch_merge_t(const PagedProblem& p, int units, int max_rows, cudaStream_t st) {
+  return launch_pdl(paged_rows_merge_kernel<T, D, BLOCK>, dim3(units, max_rows), dim3(D / 2), 0, st, p);
+}
+
+#define TKPHI_BY_TYPE(call)                                                          \
+  (d == 64 ? (bf16 ? (block ? call(Bf16, 64, true) : call(Bf16, 64, false))           \
+                   : (block ? call(Fp16, 64, true) : call(Fp16, 64, false)))          \
+           : (bf16 ? (block ? call(Bf16, 128, true) : call(Bf16, 128, false))         \
+                   : (block ? call(Fp16, 128, true) : call(Fp16, 128, false))))
+
+cudaError_t launch_paged_rows(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int d, bool bf16,
+                              bool block, int grid, bool dependent, cudaStream_t st) {
+#define ROWS(T, D, B) launch_rows_t<T, D, B>(p, tk, tv, grid, dependent, st)
+  return TKPHI_BY_TYPE(ROWS);
+#undef ROWS
+}
+
+cudaError_t launch_paged_rows_merge(const PagedProblem& p, int d, bool bf16, bool block, int units, int max_rows,
+                                    cudaStream_t st) {
+#define MERGE(T, D, B) launch_merge_t<T, D, B>(p, units, max_rows, st)
+  return TKPHI_BY_TYPE(MERGE);
+#undef MERGE
+}
+
+}  // namespace tkphi
