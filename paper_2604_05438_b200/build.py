@@ -11,7 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtkphi.so")
 SOURCES = ["api.cu", "score.cu", "select_cluster.cu", "exact_residual.cu", "build_summaries.cu", "static_scratch.cu",
            "selftest.cu", "cached_features.cu",
-           "mlp_features.cu", "mlp_query.cu", "paged_api.cu", "paged_append.cu", "paged_rows.cu", "paged_select.cu"]
+           "mlp_features.cu", "mlp_query.cu", "paged_api.cu", "paged_append.cu", "paged_rows.cu",
+           "paged_tiles.cu", "paged_select.cu"]
 HEADERS = ["common.cuh", "sm100.cuh", "feature_jobs.cuh", "host.cuh", "paged.cuh", os.path.join("..", "..", "include", "tkphi.h")]
 
 

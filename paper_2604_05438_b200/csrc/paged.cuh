@@ -168,6 +168,8 @@ cudaError_t launch_paged_rows(const PagedProblem& p, const CUtensorMap& tk, cons
                               bool block, int grid, bool dependent, cudaStream_t st);
 cudaError_t launch_paged_rows_merge(const PagedProblem& p, int d, bool bf16, bool block, int units, int max_rows, cudaStream_t st);
 cudaError_t launch_paged_select(const PagedProblem& p, int d, bool bf16, int max_pages_seq, cudaStream_t st);
-size_t paged_rows_smem(int d);
+cudaError_t launch_paged_tiles(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int d, bool bf16, int grid,
+                               cudaStream_t st);
+cudaError_t launch_paged_tiles_merge(const PagedProblem& p, int d, bool bf16, cudaStream_t st);
 
 }  // namespace tkphi

@@ -115,31 +115,83 @@ struct AttendPlan {
   int max_rows;                  // rows of the widest sequence of the row kernel
   int64_t row_tiles;             // tiles of the row kernel
   int row_ctas, row_grid;        // row_ctas 0: one CTA per unit
-  bool any_rows;
-  size_t row_part, row_stat, total;
+  bool any_rows, any_tiles;
+  int chunk, max_chunks, tile_grid;
+  size_t row_part, row_stat, tile_part, tile_stat, total;
 };
+
+// Sequences with at most this many rows per KV head go to the row kernel.
+constexpr int kRowsLimit = 16;
+
+// Keys per CTA of the tile kernel: the whole context if the row tiles alone fill the SMs evenly, otherwise a part of it.
+// The estimate of a choice, in key tiles of one CTA: the larger of the waves' sum and the balanced share plus half of
+// the longest CTA; a CTA costs about four tiles of set-up and, if its output is partial, a thirtieth of a tile of the
+// device's time for writing and joining it.
+int choose_chunk(const tkphi_paged_desc* kv, const PagedShape& sh, int64_t longest, int n_sm) {
+  int best = 0;
+  double best_cost = 0;
+  for (int parts = 1; parts <= 64; ++parts) {
+    const int64_t per = (longest + parts - 1) / parts;
+    if (parts > 1 && per < 4) break;
+    double ctas = 0, work = 0;
+    for (int b = 0; b < kv->batch; ++b) {
+      const int64_t q = kv->cu_q_host[b + 1] - kv->cu_q_host[b], len = kv->kv_lens_host[b];
+      if (q * sh.group <= kRowsLimit) continue;
+      const double rt = (double)((q * sh.group + kTileRows - 1) / kTileRows) * kv->n_kv_heads;
+      const double seen = std::max<double>(1., ((double)len - 0.5 * (double)std::min(q, len)) / kTileKeys);   // of an average row tile
+      ctas += rt * std::max(1., seen / (double)per + (seen > (double)per ? 0.5 : 0.));
+      work += rt * seen;
+    }
+    const double mean = work / ctas + 4, joined = parts > 1 ? ctas / 30 : 0;
+    const double waves = std::ceil(ctas / n_sm) * mean, shared = (work + 4 * ctas) / n_sm + 0.5 * ((double)per + 4);
+    const double cost = std::max(waves, shared) + joined;
+    if (!best || cost < best_cost * 0.98) { best = (int)per; best_cost = cost; }
+  }
+  return best * kTileKeys;
+}
 
 tkphi_status plan_attend(const tkphi_paged_desc* kv, const PagedShape& sh, AttendPlan* pl) {
   const int n_sm = sm_count_current_device();
   *pl = AttendPlan{};
-  int64_t longest = 0;
+  int64_t longest_row = 0, longest = 0;
   for (int b = 0; b < kv->batch; ++b) {
     const int64_t q = kv->cu_q_host[b + 1] - kv->cu_q_host[b];
     if (q == 0) continue;
     const int64_t rows = q * sh.group, len = kv->kv_lens_host[b];
+    if (rows > kRowsLimit) {
+      pl->any_tiles = true;
+      longest = std::max<int64_t>(longest, len > 0 ? (len + kTileKeys - 1) / kTileKeys : 1);
+      continue;
+    }
     const int64_t tiles = len > 0 ? (len + kRowKeys - 1) / kRowKeys : 1;
     pl->any_rows = true;
     pl->max_rows = (int)std::max<int64_t>(pl->max_rows, rows);
     pl->row_tiles += tiles * kv->n_kv_heads * ((rows + kRowTile - 1) / kRowTile);
-    longest = std::max(longest, tiles);
+    longest_row = std::max(longest_row, tiles);
   }
   if (pl->row_tiles > INT_MAX / 2) return fail(TKPHI_ERR_UNSUPPORTED, "too many key tiles for one call");
   pl->row_ctas = (int)std::min<int64_t>(2 * n_sm, pl->row_tiles);
-  if (longest <= 8 && pl->max_rows <= kRowTile) pl->row_ctas = 0;       // short caches: nothing to join
+  if (longest_row <= 8 && pl->max_rows <= kRowTile) pl->row_ctas = 0;       // short caches: nothing to join
   pl->row_grid = pl->row_ctas ? pl->row_ctas : kv->batch * kv->n_kv_heads;
+  if (pl->any_tiles) {
+    pl->chunk = choose_chunk(kv, sh, longest, n_sm);
+    int64_t grid = 0;
+    for (int b = 0; b < kv->batch; ++b) {
+      const int64_t rows = (kv->cu_q_host[b + 1] - kv->cu_q_host[b]) * sh.group, len = kv->kv_lens_host[b];
+      if (rows <= kRowsLimit) continue;
+      const int64_t chunks = len > pl->chunk ? (len + pl->chunk - 1) / pl->chunk : 1;
+      pl->max_chunks = (int)std::max<int64_t>(pl->max_chunks, chunks);
+      grid += (rows + kTileRows - 1) / kTileRows * chunks * kv->n_kv_heads;
+    }
+    if (grid > INT_MAX / 2) return fail(TKPHI_ERR_UNSUPPORTED, "too many query rows for one call");
+    pl->tile_grid = (int)grid;
+  }
   size_t o = 0;
   pl->row_part = o; o = align_up(o + sizeof(float) * 2 * pl->row_ctas * kRowTile * kv->head_dim, 256);
   pl->row_stat = o; o = align_up(o + sizeof(float) * 2 * pl->row_ctas * kRowTile * 2, 256);
+  const size_t parts = pl->max_chunks > 1 ? (size_t)pl->tile_grid * kTileRows : 0;
+  pl->tile_part = o; o = align_up(o + sizeof(float) * parts * kv->head_dim, 256);
+  pl->tile_stat = o; o = align_up(o + sizeof(float) * parts * 2, 256);
   pl->total = std::max<size_t>(o, 256);
   return TKPHI_OK;
 }
@@ -299,20 +351,34 @@ tkphi_status tkphi_paged_attention(const tkphi_paged_desc* kv, const void* q, vo
   PagedProblem p = problem_of(kv, sh, q, y_out, lse_out, scale);
   p.causal = (flags & TKPHI_FLAG_FULL_CONTEXT) ? 0 : 1;
   char* w = static_cast<char*>(workspace);
-  p.rows_limit = INT_MAX;
+  p.rows_limit = kRowsLimit;
   p.row_ctas = pl.row_ctas;
   p.row_part = reinterpret_cast<float*>(w + pl.row_part);
   p.row_stat = reinterpret_cast<float*>(w + pl.row_stat);
+  p.chunk = pl.chunk;
+  p.tile_part = reinterpret_cast<float*>(w + pl.tile_part);
+  p.tile_stat = reinterpret_cast<float*>(w + pl.tile_stat);
   const bool bf16 = kv->dtype == TKPHI_DTYPE_BF16;
   cudaStream_t cs = reinterpret_cast<cudaStream_t>(cuda_stream);
-  if (pl.any_rows) {
-    ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_ROWS);
-    cudaError_t e = launch_paged_rows(p, tk, tv, kv->head_dim, bf16, false, pl.row_grid, false, cs);
-    if (e == cudaSuccess && pl.row_ctas)
-      e = launch_paged_rows_merge(p, kv->head_dim, bf16, false, kv->batch * kv->n_kv_heads, pl.max_rows, cs);
-    if (e != cudaSuccess) return cuda_fail(e, "paged attention launch");
+  // tiles, rows (may start beside the tiles' last CTAs), then the joins
+  cudaError_t e = cudaSuccess;
+  if (pl.any_tiles) {
+    ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_TILES);
+    e = launch_paged_tiles(p, tk, tv, kv->head_dim, bf16, pl.tile_grid, cs);
   }
-  return TKPHI_OK;
+  if (e == cudaSuccess && pl.any_rows) {
+    ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_ROWS);
+    e = launch_paged_rows(p, tk, tv, kv->head_dim, bf16, false, pl.row_grid, pl.any_tiles, cs);
+  }
+  if (e == cudaSuccess && pl.max_chunks > 1) {
+    ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_TILES);
+    e = launch_paged_tiles_merge(p, kv->head_dim, bf16, cs);
+  }
+  if (e == cudaSuccess && pl.any_rows && pl.row_ctas) {
+    ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_ROWS);
+    e = launch_paged_rows_merge(p, kv->head_dim, bf16, false, kv->batch * kv->n_kv_heads, pl.max_rows, cs);
+  }
+  return e == cudaSuccess ? TKPHI_OK : cuda_fail(e, "paged attention launch");
 }
 
 tkphi_status tkphi_paged_block_attention(const tkphi_paged_desc* kv, const tkphi_page_selection* selection,

@@ -36,7 +36,6 @@ struct RowCfg {
   static constexpr size_t bars = stat + kRowWarps * kRowTile * 2 * 4;
   static constexpr size_t total = bars + (2 * NS) * 8 + 16;
 };
-size_t paged_rows_smem(int d) { return d == 128 ? RowCfg<128>::total : RowCfg<64>::total; }
 
 // The pieces of one CTA: (unit, tile range) one after the other.  Every warp runs its own copy.
 template <bool BLOCK>
@@ -447,6 +446,9 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
   }
   __syncthreads();
   if (*s_abort && tid == 0) atomicExch(p.status, kStatusTimeout);
+  // (beside a tile-kernel launch this grid may run next to it: it must not be complete before that one is, because the
+  // joins that follow wait for this grid only)
+  if (!BLOCK) pdl_wait();
 }
 
 // Joins the partial results of the units that were cut: a CTA per (unit, row), a thread per pair of dims; the parts

@@ -1,0 +1,512 @@
+// Attention of many query rows over a paged cache (prefill, chunks of a prompt): the two products on tcgen05.
+//
+//   S = Q K^T (fp32, tensor memory), P = exp2(scale_log2 S - m) (16 bits), O = O + P V (fp32, tensor memory)
+//
+// with the running maximum m and sum of each row; y = O / sum.  A CTA owns 256 query rows of one KV head (tokens x
+// query heads of the group, so that the group's heads share every key and value tile) as two MMA tiles of 128 rows, and
+// a range of keys.  While the softmax warps of one tile work on its scores, the tensor pipe runs the other tile's
+// products.  Per tile of 128 keys and 128 rows: 2 * 128 * 128 * head_dim FMAs of tensor work against 16384
+// exponentials, at 16 per clock and SM as long as the tensor work at head_dim 128 and twice as long at 64.
+//   warps 0-3, 4-7  softmax of row tile 0, 1: thread = row = tensor-memory lane, so that a row's maximum and sum need
+//                   no exchange.  P is written over the scores it came from and read from there as the A operand.  The
+//                   output accumulator is rescaled only when a row's maximum has grown by more than 2^8 since it was
+//                   last used as the reference: P then stays below 2^8, and the few rescales do not need warps of
+//                   their own (S complete implies the product before it complete: one thread issues both, in order).
+//   warp 8          one thread issues the MMAs: P V of a tile as soon as its P is stored, then the next S of the tile.
+//   warp 9          TMA producer: page boxes of keys and values into one ring, in the order of their use; in the end
+//                   it zeroes the value rows behind the sequence's end (they may hold NaN, and 0 * NaN would reach the
+//                   sums).
+// fp16: P is scaled by 2^7 (2^15 at most), because without it probabilities below 2^-24 of the maximum vanish, and a
+// long context is made of those; the sum carries the same factor.
+// Rounding P to 16 bits is the only rounding besides the output's: its relative error per term is that of one 16-bit
+// rounding and averages out over the terms.  The sum is of the unrounded values.
+// Keys are cut into chunks when there are too few row tiles to fill the SMs evenly; partial outputs are joined in key
+// order by a second, dependent kernel.
+#include <climits>
+
+#include "paged.cuh"
+
+namespace tkphi {
+
+constexpr int kTileThreads = 384;
+constexpr int kWarpMma = 8, kWarpTma = 9;
+constexpr uint32_t kTileTmemCols = 512;      // S/P of the two row tiles: 128 columns each; O: head_dim columns each
+constexpr float kRescaleAt = 8.f;            // log2
+
+template <int D>
+struct TileCfg {
+  static constexpr int HALVES = D / 64;
+  static constexpr int BOX = 128 * 128;                      // bytes of one 64-dim half of 128 rows
+  static constexpr int TILE = HALVES * BOX;
+  static constexpr int NS = D == 128 ? 5 : 10;               // ring slots
+  static constexpr size_t q = 0;
+  static constexpr size_t ring = 2 * TILE;
+  static constexpr size_t bars = ring + (size_t)NS * TILE;
+  static constexpr size_t total = bars + 256;
+};
+
+__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+      "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+      "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+// kind::f16 instruction descriptor with both operands of one 16-bit type (1: bf16, 0: f16)
+__host__ __device__ constexpr uint32_t umma_idesc_16(int bf16, int M, int N, int a_mn, int b_mn) {
+  return (1u << 4) | ((uint32_t)bf16 << 7) | ((uint32_t)bf16 << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
+         ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+// CTAs of a sequence: KV heads x key chunks x row tiles.
+struct TileSeq {
+  int rows, len, chunks, row_tiles;
+};
+__device__ __forceinline__ TileSeq tile_seq_of(const PagedProblem& p, int b) {
+  TileSeq s{0, 0, 1, 0};
+  if (b >= p.batch) return s;
+  const int q = paged_q_len(p, b);
+  s.len = paged_kv_len(p, b);
+  s.rows = q > 0 ? q * p.group : 0;
+  if (s.rows <= p.rows_limit) s.rows = 0;
+  s.row_tiles = (s.rows + kTileRows - 1) / kTileRows;
+  s.chunks = s.len > p.chunk ? (s.len + p.chunk - 1) / p.chunk : 1;
+  return s;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kTileThreads, 1)
+paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                   const __grid_constant__ PagedProblem p) {
+  using C = TileCfg<D>;
+  constexpr int NS = C::NS;
+  constexpr float kShift = T::kBf16 ? 0.f : 7.f;             // P = 2^kShift exp2(..)
+  extern __shared__ __align__(1024) unsigned char smem[];
+  unsigned char* qs = smem + C::q;
+  unsigned char* ring = smem + C::ring;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::bars);   // [NS] tile landed
+  uint64_t* empty = full + NS;             // [NS] the MMAs that read the slot are complete
+  uint64_t* s_full = empty + NS;           // [2]  scores complete
+  uint64_t* p_ready = s_full + 2;          // [2]  P stored
+  uint64_t* o_full = p_ready + 2;          // [2]  last product complete
+  uint64_t* q_ready = o_full + 2;          // [1]
+  uint64_t* v_fixed = q_ready + 1;         // [1]  tail rows of the last value tile zeroed
+  uint64_t* drained = v_fixed + 1;         // [1]  after a wait that ran out: the MMAs issued so far are complete
+  int* misc = reinterpret_cast<int*>(drained + 1);
+  volatile int* s_abort = misc;
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(misc + 1);
+  int* s_find = misc + 2;                  // sequence, index within it
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int cta = blockIdx.x;
+
+  pdl_launch_next();
+  if (warp == 0) {
+    int base = 0;
+    bool found = false;
+    for (int s = 0; s < p.batch && !found; s += 32) {
+      const TileSeq q = tile_seq_of(p, s + lane);
+      const int w = q.row_tiles * q.chunks * p.hkv, incl = warp_inclusive_scan(w) + base;
+      const unsigned hit = __ballot_sync(0xffffffffu, incl > cta);
+      if (hit) {
+        const int l = __ffs(hit) - 1, first = __shfl_sync(0xffffffffu, incl - w, l);
+        if (lane == 0) { s_find[0] = s + l; s_find[1] = cta - first; }
+        found = true;
+      }
+      base = __shfl_sync(0xffffffffu, incl, 31);
+    }
+    if (!found && lane == 0) s_find[0] = -1;
+  } else if (warp == 1) {
+    tmem_alloc(s_tmem, kTileTmemCols);
+  } else if (tid == 64) {
+    for (int s = 0; s < NS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+    for (int t = 0; t < 2; ++t) { mbar_init(&s_full[t], 1); mbar_init(&p_ready[t], 128); mbar_init(&o_full[t], 1); }
+    mbar_init(q_ready, 256);
+    mbar_init(v_fixed, 1);
+    mbar_init(drained, 1);
+    mbar_fence_init();
+    *s_abort = 0;
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = *s_tmem;
+  const int b = s_find[0];
+
+  int n[2] = {0, 0};                       // key tiles of the two row tiles
+  int h = 0, c0 = 0, row0 = 0, q_len = 0;
+  TileSeq sq{0, 0, 1, 0};
+  if (b >= 0) {
+    sq = tile_seq_of(p, b);
+    q_len = paged_q_len(p, b);
+    int i = s_find[1];
+    row0 = (sq.row_tiles - 1 - i % sq.row_tiles) * kTileRows;        // the rows that see most first
+    i /= sq.row_tiles;
+    c0 = (i % sq.chunks) * p.chunk;
+    h = i / sq.chunks;
+    const int c1 = sq.len - c0 < p.chunk ? sq.len : c0 + p.chunk;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int first = row0 + t * 128, last = (first + 128 < sq.rows ? first + 128 : sq.rows) - 1;
+      if (first >= sq.rows) continue;
+      int end = p.causal ? sq.len - q_len + last / p.group + 1 : sq.len;
+      if (end > c1) end = c1;
+      n[t] = end > c0 ? (end - c0 + kTileKeys - 1) / kTileKeys : 0;
+    }
+  }
+  const int n_all = n[0] > n[1] ? n[0] : n[1];
+  const bool fix = n_all > 0 && c0 + n_all * kTileKeys > sq.len;      // the last tile reaches behind the sequence
+
+  if (warp < 8) {
+    // ================================================================ softmax: thread = row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    const int t = warp >> 2, r = tid & 127, quad = warp & 3;
+    const int row = row0 + t * 128 + r;
+    const int nt = t == 0 ? n[0] : n[1];
+    const bool live = row < sq.rows;
+    const size_t tok0 = b >= 0 ? (size_t)__ldg(p.cu_q + b) : 0;
+    const size_t out_row = live ? (tok0 + row / p.group) * p.hq + (size_t)h * p.group + row % p.group : 0;
+    const size_t slot_row = (size_t)cta * kTileRows + t * 128 + r;
+    if (n_all > 0) {
+      // queries: the tile's 128 threads copy its rows, 16 bytes at a time (rows past the last are zeros)
+      constexpr int CPR = D / 8;
+      const uint4* q = static_cast<const uint4*>(p.q);
+#pragma unroll 4
+      for (int i = r; i < 128 * CPR; i += 128) {
+        const int rr = i / CPR, c = i % CPR, g = row0 + t * 128 + rr;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (g < sq.rows) v = __ldg(q + ((tok0 + g / p.group) * p.hq + (size_t)h * p.group + g % p.group) * CPR + c);
+        *reinterpret_cast<uint4*>(qs + t * C::TILE + (c >> 3) * C::BOX + swz128(rr, c & 7)) = v;
+      }
+      fence_proxy_async_smem();
+      mbar_arrive(q_ready);
+    }
+    // last visible key; rows without a query run along unmasked and are not stored
+    const int lim = !live ? INT_MAX : p.causal ? sq.len - q_len + row / p.group : sq.len - 1;
+    const uint32_t s_addr = tmem_addr(tmem, quad * 32, t * 128);
+    const uint32_t o_addr = tmem_addr(tmem, quad * 32, 256 + t * D);
+    float m = -INFINITY, l = 0.f;
+    bool ok = true;
+    for (int j = 0; j < nt; ++j) {
+      ok = __all_sync(0xffffffffu, mbar_wait(&s_full[t], (uint32_t)j & 1u, s_abort));
+      if (!ok) break;
+      tc_fence_after_sync();
+      float s[4][32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld_x32(s_addr + c * 32, s[c]);
+      tc_wait_ld();
+      const int key0 = c0 + j * kTileKeys;
+      if (__any_sync(0xffffffffu, key0 + kTileKeys - 1 > lim)) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (key0 + c * 32 + e > lim) s[c][e] = -INFINITY;
+      }
+      float mx[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        mx[c] = fmaxf(s[c][0], s[c][1]);
+#pragma unroll
+        for (int e = 2; e < 32; e += 2) mx[c] = fmaxf(mx[c], fmaxf(s[c][e], s[c][e + 1]));
+      }
+      const float cand = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
+      const bool grow = cand > m + kRescaleAt;
+      if (__any_sync(0xffffffffu, grow)) {
+        const float f = grow ? ex2_approx(m - cand) : 1.f;   // m = -inf: 0
+        if (j > 0) {
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            float o[32];
+            tmem_ld_x32(o_addr + c * 32, o);
+            tc_wait_ld();
+            uint32_t w[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(o[e] * f);
+            tmem_st_x32(o_addr + c * 32, w);
+          }
+        }
+        l *= f;
+        if (grow) m = cand;
+      }
+      const float off = kShift - (m == -INFINITY ? 0.f : m);
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        uint32_t w[32];
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float a = ex2_approx(fmaf(s[half * 2 + c][2 * e], p.scale_log2, off));
+            const float d = ex2_approx(fmaf(s[half * 2 + c][2 * e + 1], p.scale_log2, off));
+            sum[c * 2] += a;
+            sum[c * 2 + 1] += d;
+            w[c * 16 + e] = T::pack(a, d);
+          }
+        tmem_st_x32(s_addr + half * 32, w);
+      }
+      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      tc_wait_st();
+      tc_fence_before_sync();
+      mbar_arrive(&p_ready[t]);
+    }
+    if (ok && nt > 0) ok = __all_sync(0xffffffffu, mbar_wait(&o_full[t], 0, s_abort));
+    if (ok && b >= 0) {
+      tc_fence_after_sync();
+      if (sq.chunks == 1) {
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        uint4* y = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.y) + out_row * D);
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          float o[32];
+          if (nt > 0) {                        // warp-uniform
+            tmem_ld_x32(o_addr + c * 32, o);
+            tc_wait_ld();
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (l > 0.f) {
+              v.x = T::pack(o[8 * e] * inv, o[8 * e + 1] * inv); v.y = T::pack(o[8 * e + 2] * inv, o[8 * e + 3] * inv);
+              v.z = T::pack(o[8 * e + 4] * inv, o[8 * e + 5] * inv); v.w = T::pack(o[8 * e + 6] * inv, o[8 * e + 7] * inv);
+            }
+            if (live) y[c * 4 + e] = v;
+          }
+        }
+        if (live && p.lse) p.lse[out_row] = l > 0.f ? (m - kShift + log2f(l)) * 0.6931471805599453f : -INFINITY;
+      } else {
+        if (live) reinterpret_cast<float2*>(p.tile_stat)[slot_row] = make_float2(l > 0.f ? m - kShift : -INFINITY, l);
+        if (nt > 0) {
+          float4* dst = reinterpret_cast<float4*>(p.tile_part + slot_row * D);
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            float o[32];
+            tmem_ld_x32(o_addr + c * 32, o);
+            tc_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (live) dst[c * 8 + e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+          }
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == kWarpTma && n_all > 0) {
+      // ================================================================ TMA producer
+      const int ps = 1 << p.page_shift;
+      const int box_rows = ps < 64 ? ps : 64, boxes = kTileKeys / box_rows;
+      const int copies = C::HALVES * boxes, half = lane / boxes, bx = lane % boxes;
+      const int page_off = (bx * box_rows) >> p.page_shift, row_off = (bx * box_rows) & (ps - 1);
+      const uint32_t dst_off = half * C::BOX + bx * box_rows * 128;
+      const int n_pages_seq = (sq.len + ps - 1) >> p.page_shift;
+      const int* list = p.table + (size_t)b * p.max_pages;
+      const uint64_t pol = l2_policy_normal();
+      int batch0 = (c0 >> p.page_shift) & ~31;
+      int id = batch0 + lane < n_pages_seq ? __ldg(list + batch0 + lane) : p.n_pages;
+      int id_next = batch0 + 32 + lane < n_pages_seq ? __ldg(list + batch0 + 32 + lane) : p.n_pages;
+      int issued[NS];
+#pragma unroll
+      for (int s = 0; s < NS; ++s) issued[s] = -1;
+      bool ok = true;
+      int page = p.n_pages;
+      for (int i = 0; i < 2 * n_all && ok; ++i) {             // K0, V0, K1, V1, ...
+        if ((i & 1) == 0) {
+          const int first = (c0 + (i >> 1) * kTileKeys) >> p.page_shift;
+          if (first >= batch0 + 32) {
+            batch0 += 32;
+            id = id_next;
+            id_next = batch0 + 32 + lane < n_pages_seq ? __ldg(list + batch0 + 32 + lane) : p.n_pages;
+          }
+          page = __shfl_sync(0xffffffffu, id, (first + page_off) & 31);
+          if (page < 0 || page > p.n_pages || (page == p.n_pages && first + page_off < n_pages_seq)) {
+            if (lane < boxes) atomicExch(p.status, kStatusBadPage);
+            page = p.n_pages;                                 // a box outside the tensor arrives as zeros
+          }
+        }
+        const int slot = i % NS;
+        ok = __all_sync(0xffffffffu, mbar_wait(&empty[slot], ((uint32_t)(i / NS) & 1u) ^ 1u, s_abort));
+        if (!ok) break;
+        if (lane == 0) mbar_expect_tx(&full[slot], C::TILE);
+        __syncwarp();
+        if (lane < copies)
+          tma_load_4d(ring + (size_t)slot * C::TILE + dst_off, (i & 1) ? &tmap_v : &tmap_k, &full[slot], half * 64,
+                      row_off, h, page, pol);
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+          if (s == slot) issued[s] = i;
+      }
+      if (ok && fix) {
+        // Value rows of the last tile behind the end of the sequence.  (The slot's barrier is in the phase of this
+        // copy until the wait returns, because nothing is loaded after it.)
+        const int i = 2 * n_all - 1, slot = i % NS;
+        const int keep = sq.len - (c0 + (n_all - 1) * kTileKeys);        // 1 .. 127
+        ok = __all_sync(0xffffffffu, mbar_wait(&full[slot], (uint32_t)(i / NS) & 1u, s_abort));
+        if (ok) {
+          constexpr int CPR = D / 8;
+          unsigned char* v = ring + (size_t)slot * C::TILE;
+          for (int x = lane; x < (kTileKeys - keep) * CPR; x += 32) {
+            const int row = keep + x / CPR, c = x % CPR;
+            *reinterpret_cast<uint4*>(v + (c >> 3) * C::BOX + swz128(row, c & 7)) = make_uint4(0, 0, 0, 0);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(v_fixed);
+        }
+      }
+      if (!ok) {
+        // every copy that was issued must land before shared memory is released
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+          for (uint32_t w = 0; issued[s] >= 0 && w < kWaitPolls; ++w) {
+            if (mbar_try_wait(&full[s], (uint32_t)(issued[s] / NS) & 1u)) break;
+            __nanosleep(64);
+          }
+      }
+    } else if (warp == kWarpMma && n_all > 0) {
+      // ================================================================ MMA issuer
+      if (lane == 0) {
+        constexpr uint32_t idesc_s = umma_idesc_16(T::kBf16, 128, kTileKeys, 0, 0);
+        constexpr uint32_t idesc_o = umma_idesc_16(T::kBf16, 128, D, 0, 1);
+        const uint64_t q_desc = umma_smem_desc(smem_u32(qs), 16, 1024);
+        const uint64_t k_desc = umma_smem_desc(smem_u32(ring), 16, 1024);
+        const uint64_t v_desc = umma_smem_desc(smem_u32(ring), C::BOX, 1024);   // MN-major: 64-dim blocks BOX bytes apart
+        auto scores = [&](int t, int slot) {
+          const uint64_t qd = q_desc + (uint64_t)((t * C::TILE) >> 4), kd = k_desc + (uint64_t)((slot * C::TILE) >> 4);
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const uint64_t off = (uint64_t)(((k >> 2) * C::BOX + (k & 3) * 32) >> 4);
+            umma_ss(tmem + t * 128, qd + off, kd + off, idesc_s, k ? 1u : 0u);
+          }
+          tc_commit(&s_full[t]);
+        };
+        auto product = [&](int t, int slot, bool add) {
+          const uint64_t vd = v_desc + (uint64_t)((slot * C::TILE) >> 4);
+#pragma unroll
+          for (int k = 0; k < kTileKeys / 16; ++k)
+            umma_ts(tmem + 256 + t * D, tmem + t * 128 + k * 8, vd + (uint64_t)((k * 16 * 128) >> 4), idesc_o,
+                    (add || k > 0) ? 1u : 0u);
+        };
+        bool ok = mbar_wait(q_ready, 0, s_abort) && mbar_wait(&full[0], 0, s_abort);
+        tc_fence_after_sync();
+        if (ok) {
+          if (n[0] > 0) scores(0, 0);
+          if (n[1] > 0) scores(1, 0);
+          tc_commit(&empty[0]);
+        }
+        for (int j = 0; j < n_all && ok; ++j) {
+          const int iv = 2 * j + 1, ik = 2 * j + 2, sv = iv % NS, sk = ik % NS;
+          ok = mbar_wait(&full[sv], (uint32_t)(iv / NS) & 1u, s_abort);
+          if (ok && fix && j + 1 == n_all) ok = mbar_wait(v_fixed, 0, s_abort);
+          if (ok && j + 1 < n_all) ok = mbar_wait(&full[sk], (uint32_t)(ik / NS) & 1u, s_abort);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (!ok || j >= n[t]) continue;
+            ok = mbar_wait(&p_ready[t], (uint32_t)j & 1u, s_abort);
+            if (!ok) continue;
+            tc_fence_after_sync();
+            product(t, sv, j > 0);
+            if (j + 1 < n[t]) scores(t, sk);
+            else tc_commit(&o_full[t]);
+          }
+          if (!ok) break;
+          tc_commit(&empty[sv]);
+          if (j + 1 < n_all) tc_commit(&empty[sk]);
+        }
+        if (!ok) {                             // tensor memory is released only when no MMA uses it any more
+          tc_commit(drained);
+          for (uint32_t w = 0; w < kWaitPolls && !mbar_try_wait(drained, 0); ++w) __nanosleep(64);
+        }
+      }
+    }
+  }
+  // ---- teardown
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, kTileTmemCols);
+  }
+  if (*s_abort && tid == 0) atomicExch(p.status, kStatusTimeout);
+}
+
+// Joins the key chunks of a row in key order: a warp per (token, query head).
+template <typename T, int D>
+__global__ void __launch_bounds__(256) paged_tiles_merge_kernel(const __grid_constant__ PagedProblem p) {
+  pdl_wait();
+  pdl_launch_next();
+  const int lane = threadIdx.x & 31;
+  const int idx = blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (idx >= p.total_q * p.hq) return;
+  const int tok = idx / p.hq, head = idx % p.hq, b = paged_seq_of(p, tok);
+  const TileSeq sq = tile_seq_of(p, b);
+  if (sq.rows == 0 || sq.chunks == 1) return;
+  int before = 0;
+  for (int s = 0; s < b; s += 32) {
+    const TileSeq o = tile_seq_of(p, s + lane);
+    before += __reduce_add_sync(0xffffffffu, s + lane < b ? o.row_tiles * o.chunks * p.hkv : 0);
+  }
+  const int row = (tok - (int)__ldg(p.cu_q + b)) * p.group + head % p.group;
+  const int i = sq.row_tiles - 1 - row / kTileRows;
+  const size_t first = ((size_t)before + (size_t)(head / p.group) * sq.chunks * sq.row_tiles + i) * kTileRows + row % kTileRows;
+  const size_t step = (size_t)sq.row_tiles * kTileRows;
+  const float2* stat = reinterpret_cast<const float2*>(p.tile_stat);
+  float M = -INFINITY;
+  for (int c = lane; c < sq.chunks; c += 32) M = fmaxf(M, __ldcg(stat + first + c * step).x);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+  constexpr int V = D / 32;                  // dims of a lane
+  float a[V], L = 0.f;
+#pragma unroll
+  for (int e = 0; e < V; ++e) a[e] = 0.f;
+#pragma unroll 4
+  for (int c = 0; c < sq.chunks; ++c) {
+    const size_t s = first + c * step;
+    const float2 st = __ldcg(stat + s);
+    if (st.x == -INFINITY) continue;         // (its partial output was not written)
+    const float f = ex2_approx(st.x - M);
+    L += st.y * f;
+    if (D == 128) {
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(p.tile_part + s * D) + lane);
+      a[0] += v.x * f; a[1] += v.y * f; a[V - 2] += v.z * f; a[V - 1] += v.w * f;
+    } else {
+      const float2 v = __ldcg(reinterpret_cast<const float2*>(p.tile_part + s * D) + lane);
+      a[0] += v.x * f; a[1] += v.y * f;
+    }
+  }
+  const float inv = L > 0.f ? 1.f / L : 0.f;
+  uint32_t* y = static_cast<uint32_t*>(p.y) + (size_t)idx * (D / 2) + lane * (V / 2);
+  y[0] = T::pack(a[0] * inv, a[1] * inv);
+  if (D == 128) y[1] = T::pack(a[V - 2] * inv, a[V - 1] * inv);
+  if (lane == 0 && p.lse) p.lse[idx] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+}
+
+template <typename T, int D>
+static cudaError_t launch_tiles_t(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int grid, cudaStream_t st) {
+  static PerDeviceFlag configured;
+  const cudaError_t e = set_max_dynamic_smem(configured, reinterpret_cast<const void*>(paged_tiles_kernel<T, D>), TileCfg<D>::total);
+  if (e != cudaSuccess) return e;
+  paged_tiles_kernel<T, D><<<grid, kTileThreads, TileCfg<D>::total, st>>>(tk, tv, p);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_paged_tiles(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int d, bool bf16, int grid,
+                               cudaStream_t st) {
+  if (d == 64) return bf16 ? launch_tiles_t<Bf16, 64>(p, tk, tv, grid, st) : launch_tiles_t<Fp16, 64>(p, tk, tv, grid, st);
+  return bf16 ? launch_tiles_t<Bf16, 128>(p, tk, tv, grid, st) : launch_tiles_t<Fp16, 128>(p, tk, tv, grid, st);
+}
+
+cudaError_t launch_paged_tiles_merge(const PagedProblem& p, int d, bool bf16, cudaStream_t st) {
+  const dim3 grid((p.total_q * p.hq + 7) / 8), block(256);
+  if (d == 64)
+    return bf16 ? launch_pdl(paged_tiles_merge_kernel<Bf16, 64>, grid, block, 0, st, p)
+                : launch_pdl(paged_tiles_merge_kernel<Fp16, 64>, grid, block, 0, st, p);
+  return bf16 ? launch_pdl(paged_tiles_merge_kernel<Bf16, 128>, grid, block, 0, st, p)
+              : launch_pdl(paged_tiles_merge_kernel<Fp16, 128>, grid, block, 0, st, p);
+}
+
+}  // namespace tkphi
