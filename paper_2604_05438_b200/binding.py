@@ -153,8 +153,8 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 def _stream_ptr(stream) -> Optional[int]:
-    if stream is None:
-        stream = torch.cuda.current_stream()
+    if stream is None:      # (the raw handle: building a Stream object for it takes longer than a kernel launch)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
     return stream.cuda_stream or None
 
 
@@ -282,11 +282,17 @@ class PagedKVCache:
         for t in (v, page_table, key_bounds, self.kv_lens_dev, self.cu_q_dev, self.status):
             assert t is None or t.device == dev, "the cache, its page table and its lengths must be on one device"
         self.total_q = int(self.cu_q[-1])
+        self._index = -1 if dev.type != "cuda" else torch.cuda.current_device() if dev.index is None else dev.index
+        self._q_shape = (self.total_q, n_q_heads, k.shape[3])
+        self._kv_shape = (self.total_q, k.shape[1], k.shape[3])
+        self._lse_shape = (self.total_q, n_q_heads)
+        self._dtype = k.dtype
         self._desc = _PagedDesc(len(self.kv_lens), n_q_heads, k.shape[1], k.shape[3], _DTYPES[k.dtype], k.shape[2],
                                 k.shape[0], page_table.shape[1], k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
                                 k.stride(2), page_table.data_ptr(), self.kv_lens.ctypes.data, self.kv_lens_dev.data_ptr(),
                                 self.cu_q.ctypes.data, self.cu_q_dev.data_ptr(),
                                 None if key_bounds is None else key_bounds.data_ptr(), self.status.data_ptr())
+        self._ref = C.byref(self._desc)
 
     @property
     def batch(self) -> int:
@@ -299,15 +305,23 @@ class PagedKVCache:
         """0, or the error that a call on this descriptor's status word left there (waits for the device)."""
         return int(self.status.item())
 
-    def _take(self, t: torch.Tensor, heads: int, contiguous: bool = True) -> int:
-        """Pointer of a [total_q, heads, head_dim] tensor of the cache's type on the cache's device."""
-        k = self.k
-        if t.dtype != k.dtype or t.device != k.device or t.shape != (self.total_q, heads, k.shape[3]):
-            raise ValueError(f"expected {k.dtype} [{self.total_q}, {heads}, {k.shape[3]}] on {k.device}, got {t.dtype} "
-                             f"{list(t.shape)} on {t.device}")
+    def _take(self, t: torch.Tensor, shape: tuple, contiguous: bool = True) -> int:
+        """Pointer of a tensor of the cache's type on the cache's device."""
+        if t.dtype is not self._dtype or t.shape != shape or t.get_device() != self._index:
+            raise ValueError(f"expected {self._dtype} {list(shape)} on {self.k.device}, got {t.dtype} {list(t.shape)} on {t.device}")
         if not (t.is_contiguous() if contiguous else t.stride(2) == 1):
             raise ValueError("tensor must be contiguous" if contiguous else "the last dim must be contiguous")
         return t.data_ptr()
+
+    def _call(self, fn, args, stream) -> None:
+        """fn(*args, stream) with the cache's device current: launches go to the device that holds the data."""
+        if self._index == torch.cuda.current_device():
+            st = fn(*args, _stream_ptr(stream))
+        else:
+            with torch.cuda.device(self._index):
+                st = fn(*args, _stream_ptr(stream))
+        if st != 0:
+            _check(st)
 
 
 @dataclass
@@ -334,15 +348,6 @@ class PageSelection:
 
     def desc(self) -> _PageSelection:
         return _PageSelection(self.n_sink_pages, self.n_tail_pages, self.topk_pages)
-
-
-def _on_device(t: torch.Tensor, call, stream):
-    """call(stream pointer) with t's device current: launches go to the device that holds the data."""
-    index = t.device.index
-    if index is None or index == torch.cuda.current_device():
-        return call(_stream_ptr(stream))
-    with torch.cuda.device(index):
-        return call(_stream_ptr(stream))
 
 
 def _topk_host(topk) -> np.ndarray:
@@ -465,30 +470,36 @@ def paged_append(kv: PagedKVCache, k_new: torch.Tensor, v_new: torch.Tensor, rot
     """Rotates the new keys (and q into q_out) by their positions and writes keys and values into the cache's pages;
     key bounds of the touched pages follow.  k_new, v_new, q, q_out: [total_q, heads, head_dim], any token and head
     strides."""
-    lib = load_library()
-    hkv = kv.k.shape[1]
-    d = _AppendDesc()
-    d.k_new, d.k_stride_token, d.k_stride_head = kv._take(k_new, hkv, False), k_new.stride(0), k_new.stride(1)
-    d.v_new, d.v_stride_token, d.v_stride_head = kv._take(v_new, hkv, False), v_new.stride(0), v_new.stride(1)
+    k0, k1, k2 = k_new.stride()
+    v0, v1, v2 = v_new.stride()
+    if k2 != 1 or v2 != 1:
+        raise ValueError("the last dim must be contiguous")
+    qp = op = inv = pos = None
+    q0 = q1 = o0 = o1 = rot = pairs = 0
     if q is not None:
-        d.q, d.q_stride_token, d.q_stride_head = kv._take(q, kv.n_q_heads, False), q.stride(0), q.stride(1)
+        qp = kv._take(q, kv._q_shape, False)
+        q0, q1, _ = q.stride()
     if q_out is not None:
-        d.q_out, d.o_stride_token, d.o_stride_head = kv._take(q_out, kv.n_q_heads, False), q_out.stride(0), q_out.stride(1)
+        op = kv._take(q_out, kv._q_shape, False)
+        o0, o1, _ = q_out.stride()
     if rotary is not None:
-        assert rotary.inv_freq.device == kv.k.device
-        d.inv_freq, d.rot_dim, d.pairs = rotary.inv_freq.data_ptr(), 2 * rotary.inv_freq.numel(), int(rotary.pairs)
+        if rotary.inv_freq.get_device() != kv._index:
+            raise ValueError(f"inv_freq must be on {kv.k.device}")
+        inv, rot, pairs = rotary.inv_freq.data_ptr(), 2 * rotary.inv_freq.shape[0], int(rotary.pairs)
     if positions is not None:
-        assert positions.dtype == torch.int64 and positions.shape == (kv.total_q,) and positions.is_contiguous()
-        assert positions.device == kv.k.device
-        d.positions = positions.data_ptr()
-    _check(_on_device(kv.k, lambda s: lib.tkphi_paged_append(C.byref(kv._desc), C.byref(d), s), stream))
+        if positions.dtype != torch.int64 or positions.shape != (kv.total_q,) or not positions.is_contiguous() or positions.get_device() != kv._index:
+            raise ValueError(f"positions must be contiguous int64 [{kv.total_q}] on {kv.k.device}")
+        pos = positions.data_ptr()
+    d = _AppendDesc(kv._take(k_new, kv._kv_shape, False), k0, k1, kv._take(v_new, kv._kv_shape, False), v0, v1, qp, q0, q1,
+                    op, o0, o1, inv, rot, pairs, pos)
+    kv._call(load_library().tkphi_paged_append, (kv._ref, C.byref(d)), stream)
 
 
 def _lse_ptr(kv: PagedKVCache, lse: Optional[torch.Tensor]) -> Optional[int]:
     if lse is None:
         return None
-    if lse.dtype != torch.float32 or lse.shape != (kv.total_q, kv.n_q_heads) or not lse.is_contiguous() or lse.device != kv.k.device:
-        raise ValueError(f"lse_out must be contiguous float32 [{kv.total_q}, {kv.n_q_heads}] on {kv.k.device}")
+    if lse.dtype is not torch.float32 or lse.shape != kv._lse_shape or not lse.is_contiguous() or lse.get_device() != kv._index:
+        raise ValueError(f"lse_out must be contiguous float32 {list(kv._lse_shape)} on {kv.k.device}")
     return lse.data_ptr()
 
 
@@ -496,10 +507,10 @@ def paged_attention(kv: PagedKVCache, q: torch.Tensor, y_out: torch.Tensor, lse_
                     scale: Optional[float], flags: int, workspace: torch.Tensor, stream=None) -> None:
     """Attention of the step's new tokens over their sequences' whole caches; q, y_out [total_q, n_q_heads, head_dim],
     lse_out fp32 [total_q, n_q_heads] or None, scale None for 1/sqrt(head_dim), flags FLAG_NONE or FLAG_FULL_CONTEXT."""
-    lib = load_library()
-    args = (C.byref(kv._desc), kv._take(q, kv.n_q_heads), kv._take(y_out, kv.n_q_heads), _lse_ptr(kv, lse_out),
-            0.0 if scale is None else _positive(scale), flags, _ws_ptr(kv, workspace), workspace.numel() * workspace.element_size())
-    _check(_on_device(kv.k, lambda s: lib.tkphi_paged_attention(*args, s), stream))
+    kv._call(load_library().tkphi_paged_attention,
+             (kv._ref, kv._take(q, kv._q_shape), kv._take(y_out, kv._q_shape), _lse_ptr(kv, lse_out),
+              0.0 if scale is None else _positive(scale), flags, _ws_ptr(kv, workspace),
+              workspace.numel() * workspace.element_size()), stream)
 
 
 def paged_block_attention(kv: PagedKVCache, selection: PageSelection, q: torch.Tensor, y_out: torch.Tensor,
@@ -507,17 +518,17 @@ def paged_block_attention(kv: PagedKVCache, selection: PageSelection, q: torch.T
                           workspace: torch.Tensor, stream=None) -> None:
     """Attention over the pages that ``selection`` takes for each new token and KV head; page_idx_out int32
     [total_q, n_kv_heads, selection.n_pages] or None gets them."""
-    lib = load_library()
     idx = None
     if page_idx_out is not None:
         want = (kv.total_q, kv.k.shape[1], selection.n_pages)
-        if page_idx_out.dtype != torch.int32 or page_idx_out.shape != want or not page_idx_out.is_contiguous() or page_idx_out.device != kv.k.device:
+        if page_idx_out.dtype is not torch.int32 or page_idx_out.shape != want or not page_idx_out.is_contiguous() or page_idx_out.get_device() != kv._index:
             raise ValueError(f"page_idx_out must be contiguous int32 {list(want)} on {kv.k.device}")
         idx = page_idx_out.data_ptr()
     sel = selection.desc()
-    args = (C.byref(kv._desc), C.byref(sel), kv._take(q, kv.n_q_heads), kv._take(y_out, kv.n_q_heads), _lse_ptr(kv, lse_out),
-            idx, 0.0 if scale is None else _positive(scale), _ws_ptr(kv, workspace), workspace.numel() * workspace.element_size())
-    _check(_on_device(kv.k, lambda s: lib.tkphi_paged_block_attention(*args, s), stream))
+    kv._call(load_library().tkphi_paged_block_attention,
+             (kv._ref, C.byref(sel), kv._take(q, kv._q_shape), kv._take(y_out, kv._q_shape), _lse_ptr(kv, lse_out), idx,
+              0.0 if scale is None else _positive(scale), _ws_ptr(kv, workspace),
+              workspace.numel() * workspace.element_size()), stream)
 
 
 def _positive(scale: float) -> float:
@@ -527,7 +538,7 @@ def _positive(scale: float) -> float:
 
 
 def _ws_ptr(kv: PagedKVCache, workspace: torch.Tensor) -> int:
-    if workspace.device != kv.k.device or not workspace.is_contiguous():
+    if workspace.get_device() != kv._index or not workspace.is_contiguous():
         raise ValueError(f"workspace must be contiguous on {kv.k.device}")
     return workspace.data_ptr()
 

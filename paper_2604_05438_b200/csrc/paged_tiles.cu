@@ -7,16 +7,21 @@
 // a range of keys.  While the softmax warps of one tile work on its scores, the tensor pipe runs the other tile's
 // products.  Per tile of 128 keys and 128 rows: 2 * 128 * 128 * head_dim FMAs of tensor work against 16384
 // exponentials, at 16 per clock and SM as long as the tensor work at head_dim 128 and twice as long at 64.
-//   warps 0-3, 4-7  softmax of row tile 0, 1: thread = row = tensor-memory lane, so that a row's maximum and sum need
-//                   no exchange.  P is written over the scores it came from and read from there as the A operand.  The
-//                   output accumulator is rescaled only when a row's maximum has grown by more than 2^8 since it was
-//                   last used as the reference: P then stays below 2^8, and the few rescales do not need warps of
-//                   their own (S complete implies the product before it complete: one thread issues both, in order).
-//   warp 8          one thread issues the MMAs: P V of a tile as soon as its P is stored, then the next S of the tile.
+//   warps 0-3, 4-7  softmax of row tile 0, 1: thread = row = tensor-memory lane, so that a row's sum needs no exchange.
+//                   P is written over the scores it came from and read from there as the A operand.
+//                   The reference m of a row need not be its maximum, it only has to keep P in range: it is the
+//                   maximum of the first tile, and later tiles go straight from the score to exp2(score - m) without
+//                   looking for theirs.  A tile whose row sum passes a limit (2^40; fp16: 61440, below which no term
+//                   can overflow the type) is redone with its maximum as the new reference and O rescaled; nothing of
+//                   a row is lost on the way, because m never exceeds a score the row has seen.  (One thread issues
+//                   the MMAs in order, so a complete S says that the product before it is complete, too.)
+//                   Part of the exponentials are computed on the FMA pipes (exp2_pair), which halves the time of a
+//                   tile where the 16 per clock of the special-function unit bound it.
+//   warp 8          issues the MMAs: P V of a row tile as soon as its P is stored, then the next S of the tile.
 //   warp 9          TMA producer: page boxes of keys and values into one ring, in the order of their use; in the end
 //                   it zeroes the value rows behind the sequence's end (they may hold NaN, and 0 * NaN would reach the
 //                   sums).
-// fp16: P is scaled by 2^7 (2^15 at most), because without it probabilities below 2^-24 of the maximum vanish, and a
+// fp16: P is scaled by 2^7, because without it probabilities below 2^-24 of the maximum vanish, and a
 // long context is made of those; the sum carries the same factor.
 // Rounding P to 16 bits is the only rounding besides the output's: its relative error per term is that of one 16-bit
 // rounding and averages out over the terms.  The sum is of the unrounded values.
@@ -31,7 +36,67 @@ namespace tkphi {
 constexpr int kTileThreads = 384;
 constexpr int kWarpMma = 8, kWarpTma = 9;
 constexpr uint32_t kTileTmemCols = 512;      // S/P of the two row tiles: 128 columns each; O: head_dim columns each
-constexpr float kRescaleAt = 8.f;            // log2
+constexpr float kGrow = 1.f;                 // log2: how far a tile's maximum passes the reference before it replaces it
+
+// Two fp32 values as one operand of the packed FMA instructions.
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// exp2 of two values on the FMA and integer pipes: x = n + f with n the nearest integer, |f| <= 1/2, 2^f by the
+// Chebyshev interpolation polynomial of degree 5 (relative error below 2^-22: the terms of the series beyond it,
+// (ln 2 / 2)^6 / 6! = 2.4e-6, shrink by 2^5 when the six nodes are Chebyshev's), n added to the exponent field.
+// Below -126 the result is 2^-126.
+__device__ __forceinline__ uint64_t exp2_pair(uint64_t x2) {
+  constexpr float c0 = 1.000000075e+00f, c1 = 6.931471880e-01f, c2 = 2.402210749e-01f, c3 = 5.550357114e-02f, c4 = 9.676031918e-03f, c5 = 1.339086336e-03f;
+  float x, y;
+  unpack2(x2, x, y);
+  x2 = pack2(fmaxf(x, -126.f), fmaxf(y, -126.f));
+  const uint64_t magic = pack2(12582912.f, 12582912.f), minus = pack2(-1.f, -1.f);      // 1.5 * 2^23: the sum's low bits are n
+  const uint64_t t = add2(x2, magic);
+  const uint64_t n = add2(t, pack2(-12582912.f, -12582912.f));
+  const uint64_t f = fma2(n, minus, x2);
+  uint64_t r = fma2(f, pack2(c5, c5), pack2(c4, c4));
+  r = fma2(r, f, pack2(c3, c3));
+  r = fma2(r, f, pack2(c2, c2));
+  r = fma2(r, f, pack2(c1, c1));
+  r = fma2(r, f, pack2(c0, c0));
+  float a, b, ta, tb;
+  unpack2(r, a, b);
+  unpack2(t, ta, tb);
+  return pack2(__int_as_float(__float_as_int(a) + (__float_as_int(ta) << 23)),
+               __int_as_float(__float_as_int(b) + (__float_as_int(tb) << 23)));
+}
+// Which of the 16 pairs of a 32-column piece go through exp2_pair.
+template <int D>
+__device__ __forceinline__ constexpr bool emulated(int e) { return D == 64 ? e % 8 % 3 == 0 : e % 4 == 0; }
+__device__ __forceinline__ bool elect_one() {
+  uint32_t e;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.b32 %0, 1, 0, p;\n}\n" : "=r"(e));
+  return e != 0;
+}
+// Waits for this thread's tensor-memory loads; the values are tied to the wait.
+__device__ __forceinline__ void tc_wait_ld_x32(float (&v)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                 "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
+                 "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]),
+                 "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+               :
+               : "memory");
+}
 
 template <int D>
 struct TileCfg {
@@ -85,6 +150,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   using C = TileCfg<D>;
   constexpr int NS = C::NS;
   constexpr float kShift = T::kBf16 ? 0.f : 7.f;             // P = 2^kShift exp2(..)
+  constexpr float kSumLimit = T::kBf16 ? 1.099511627776e12f : 61440.f;
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char* qs = smem + C::q;
   unsigned char* ring = smem + C::ring;
@@ -100,7 +166,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   volatile int* s_abort = misc;
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(misc + 1);
   int* s_find = misc + 2;                  // sequence, index within it
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int cta = blockIdx.x;
 
   pdl_launch_next();
@@ -123,7 +189,9 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     tmem_alloc(s_tmem, kTileTmemCols);
   } else if (tid == 64) {
     for (int s = 0; s < NS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-    for (int t = 0; t < 2; ++t) { mbar_init(&s_full[t], 1); mbar_init(&p_ready[t], 128); mbar_init(&o_full[t], 1); }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&s_full[t], 1); mbar_init(&p_ready[t], 4); mbar_init(&o_full[t], 1);
+    }
     mbar_init(q_ready, 256);
     mbar_init(v_fixed, 1);
     mbar_init(drained, 1);
@@ -194,65 +262,107 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       ok = __all_sync(0xffffffffu, mbar_wait(&s_full[t], (uint32_t)j & 1u, s_abort));
       if (!ok) break;
       tc_fence_after_sync();
-      float s[4][32];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld_x32(s_addr + c * 32, s[c]);
-      tc_wait_ld();
       const int key0 = c0 + j * kTileKeys;
-      if (__any_sync(0xffffffffu, key0 + kTileKeys - 1 > lim)) {
+      uint32_t w[64];
+      bool careful = j == 0 || __any_sync(0xffffffffu, key0 + kTileKeys - 1 > lim || m == -INFINITY);
+      if (!careful) {
+        const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), off2 = pack2(kShift - m, kShift - m);
+        uint64_t sum2[2] = {0, 0};
+        float u[32], v[32];
+        // pairs of a 32-column piece: the first kEmulated on the FMA pipes, spread between the others
+        auto piece = [&](const float (&x)[32], int c) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const uint64_t y = fma2(pack2(x[2 * e], x[2 * e + 1]), scale2, off2);
+            uint64_t r;
+            if (emulated<D>(e)) {
+              r = exp2_pair(y);
+            } else {
+              float a, d;
+              unpack2(y, a, d);
+              r = pack2(ex2_approx(a), ex2_approx(d));
+            }
+            sum2[e & 1] = add2(sum2[e & 1], r);
+            float a, d;
+            unpack2(r, a, d);
+            w[c * 16 + e] = T::pack(a, d);
+          }
+        };
+        tmem_ld_x32(s_addr, u);
+        tc_wait_ld_x32(u);
+        tmem_ld_x32(s_addr + 32, v);
+        piece(u, 0);
+        tc_wait_ld_x32(v);
+        tmem_ld_x32(s_addr + 64, u);
+        piece(v, 1);
+        tc_wait_ld_x32(u);
+        tmem_ld_x32(s_addr + 96, v);
+        piece(u, 2);
+        tc_wait_ld_x32(v);
+        piece(v, 3);
+        float a, d;
+        unpack2(add2(sum2[0], sum2[1]), a, d);
+        careful = __any_sync(0xffffffffu, !(a + d < kSumLimit));
+        if (!careful) l += a + d;
+      }
+      if (careful) {
+        float s[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld_x32(s_addr + c * 32, s[c]);
+        tc_wait_ld();
+        if (__any_sync(0xffffffffu, key0 + kTileKeys - 1 > lim)) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (key0 + c * 32 + e > lim) s[c][e] = -INFINITY;
+        }
+        float mx[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          mx[c] = fmaxf(s[c][0], s[c][1]);
+#pragma unroll
+          for (int e = 2; e < 32; e += 2) mx[c] = fmaxf(mx[c], fmaxf(s[c][e], s[c][e + 1]));
+        }
+        const float cand = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
+        const bool grow = cand > m + kGrow;
+        if (__any_sync(0xffffffffu, grow)) {
+          const float f = grow ? ex2_approx(m - cand) : 1.f;   // m = -inf: 0
+          if (j > 0) {
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+              float o[32];
+              tmem_ld_x32(o_addr + c * 32, o);
+              tc_wait_ld();
+              uint32_t x[32];
+#pragma unroll
+              for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(o[e] * f);
+              tmem_st_x32(o_addr + c * 32, x);
+            }
+          }
+          l *= f;
+          if (grow) m = cand;
+        }
+        const float off = kShift - (m == -INFINITY ? 0.f : m);
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
-          for (int e = 0; e < 32; ++e)
-            if (key0 + c * 32 + e > lim) s[c][e] = -INFINITY;
-      }
-      float mx[4];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        mx[c] = fmaxf(s[c][0], s[c][1]);
-#pragma unroll
-        for (int e = 2; e < 32; e += 2) mx[c] = fmaxf(mx[c], fmaxf(s[c][e], s[c][e + 1]));
-      }
-      const float cand = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
-      const bool grow = cand > m + kRescaleAt;
-      if (__any_sync(0xffffffffu, grow)) {
-        const float f = grow ? ex2_approx(m - cand) : 1.f;   // m = -inf: 0
-        if (j > 0) {
-#pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            float o[32];
-            tmem_ld_x32(o_addr + c * 32, o);
-            tc_wait_ld();
-            uint32_t w[32];
-#pragma unroll
-            for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(o[e] * f);
-            tmem_st_x32(o_addr + c * 32, w);
-          }
-        }
-        l *= f;
-        if (grow) m = cand;
-      }
-      const float off = kShift - (m == -INFINITY ? 0.f : m);
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        uint32_t w[32];
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const float a = ex2_approx(fmaf(s[half * 2 + c][2 * e], p.scale_log2, off));
-            const float d = ex2_approx(fmaf(s[half * 2 + c][2 * e + 1], p.scale_log2, off));
-            sum[c * 2] += a;
-            sum[c * 2 + 1] += d;
+            const float a = ex2_approx(fmaf(s[c][2 * e], p.scale_log2, off));
+            const float d = ex2_approx(fmaf(s[c][2 * e + 1], p.scale_log2, off));
+            sum[(c & 1) * 2] += a;
+            sum[(c & 1) * 2 + 1] += d;
             w[c * 16 + e] = T::pack(a, d);
           }
-        tmem_st_x32(s_addr + half * 32, w);
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      tmem_st_x32(s_addr, w);
+      tmem_st_x32(s_addr + 32, w + 32);
       tc_wait_st();
       tc_fence_before_sync();
-      mbar_arrive(&p_ready[t]);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&p_ready[t]);
     }
     if (ok && nt > 0) ok = __all_sync(0xffffffffu, mbar_wait(&o_full[t], 0, s_abort));
     if (ok && b >= 0) {
@@ -369,58 +479,88 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       }
     } else if (warp == kWarpMma && n_all > 0) {
       // ================================================================ MMA issuer
-      if (lane == 0) {
-        constexpr uint32_t idesc_s = umma_idesc_16(T::kBf16, 128, kTileKeys, 0, 0);
-        constexpr uint32_t idesc_o = umma_idesc_16(T::kBf16, 128, D, 0, 1);
-        const uint64_t q_desc = umma_smem_desc(smem_u32(qs), 16, 1024);
-        const uint64_t k_desc = umma_smem_desc(smem_u32(ring), 16, 1024);
-        const uint64_t v_desc = umma_smem_desc(smem_u32(ring), C::BOX, 1024);   // MN-major: 64-dim blocks BOX bytes apart
-        auto scores = [&](int t, int slot) {
-          const uint64_t qd = q_desc + (uint64_t)((t * C::TILE) >> 4), kd = k_desc + (uint64_t)((slot * C::TILE) >> 4);
+      // The whole warp runs this code and one elected lane issues: descriptors then stay in uniform registers, where
+      // the instruction takes them from.  (In a branch of one lane every MMA cost about 75 cycles of moves to issue, more
+      // than it took to execute.)
+      constexpr uint32_t idesc_s = umma_idesc_16(T::kBf16, 128, kTileKeys, 0, 0);
+      constexpr uint32_t idesc_o = umma_idesc_16(T::kBf16, 128, D, 0, 1);
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), base = __shfl_sync(0xffffffffu, smem_u32(smem), 0);
+      const int n0 = __shfl_sync(0xffffffffu, n[0], 0), n1 = __shfl_sync(0xffffffffu, n[1], 0), na = n0 > n1 ? n0 : n1;
+      const uint64_t q_desc = umma_smem_desc(base + (uint32_t)C::q, 16, 1024);
+      const uint64_t k_desc = umma_smem_desc(base + (uint32_t)C::ring, 16, 1024);
+      const uint64_t v_desc = umma_smem_desc(base + (uint32_t)C::ring, C::BOX, 1024);   // MN-major: 64-dim blocks BOX bytes apart
+      auto scores = [&](int t, int slot, bool release) {
+        const uint64_t qd = q_desc + (uint64_t)((t * C::TILE) >> 4), kd = k_desc + (uint64_t)((slot * C::TILE) >> 4);
+        if (elect_one()) {
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
             const uint64_t off = (uint64_t)(((k >> 2) * C::BOX + (k & 3) * 32) >> 4);
-            umma_ss(tmem + t * 128, qd + off, kd + off, idesc_s, k ? 1u : 0u);
+            umma_ss(tm + t * 128, qd + off, kd + off, idesc_s, k ? 1u : 0u);
           }
           tc_commit(&s_full[t]);
-        };
-        auto product = [&](int t, int slot, bool add) {
-          const uint64_t vd = v_desc + (uint64_t)((slot * C::TILE) >> 4);
+          if (release) tc_commit(&empty[slot]);
+        }
+        __syncwarp();
+      };
+      auto product = [&](int t, int slot, bool add, bool last, bool release) {
+        const uint64_t vd = v_desc + (uint64_t)((slot * C::TILE) >> 4);
+        if (elect_one()) {
 #pragma unroll
           for (int k = 0; k < kTileKeys / 16; ++k)
-            umma_ts(tmem + 256 + t * D, tmem + t * 128 + k * 8, vd + (uint64_t)((k * 16 * 128) >> 4), idesc_o,
+            umma_ts(tm + 256 + t * D, tm + t * 128 + k * 8, vd + (uint64_t)((k * 16 * 128) >> 4), idesc_o,
                     (add || k > 0) ? 1u : 0u);
-        };
-        bool ok = mbar_wait(q_ready, 0, s_abort) && mbar_wait(&full[0], 0, s_abort);
+          if (last) tc_commit(&o_full[t]);
+          if (release) tc_commit(&empty[slot]);
+        }
+        __syncwarp();
+      };
+      // slot and phase of the ring's tiles K0, V0, K1, V1, ..
+      int slot = 0;
+      uint32_t phase = 0;
+      auto step = [&]() { if (++slot == NS) { slot = 0; phase ^= 1u; } };
+      bool ok = mbar_wait(q_ready, 0, s_abort) && mbar_wait(&full[0], 0, s_abort);
+      ok = __all_sync(0xffffffffu, ok);
+      if (ok) {
         tc_fence_after_sync();
-        if (ok) {
-          if (n[0] > 0) scores(0, 0);
-          if (n[1] > 0) scores(1, 0);
-          tc_commit(&empty[0]);
+        if (n0 > 0) scores(0, 0, n1 == 0);
+        if (n1 > 0) scores(1, 0, true);
+        step();
+      }
+      for (int j = 0; j < na && ok; ++j) {
+        const int sv = slot;
+        ok = mbar_wait(&full[sv], phase, s_abort);
+        if (ok && fix && j + 1 == na) ok = mbar_wait(v_fixed, 0, s_abort);
+        step();
+        const int sk = slot;
+        if (j + 1 < na) {
+          if (ok) ok = mbar_wait(&full[sk], phase, s_abort);
+          step();
         }
-        for (int j = 0; j < n_all && ok; ++j) {
-          const int iv = 2 * j + 1, ik = 2 * j + 2, sv = iv % NS, sk = ik % NS;
-          ok = mbar_wait(&full[sv], (uint32_t)(iv / NS) & 1u, s_abort);
-          if (ok && fix && j + 1 == n_all) ok = mbar_wait(v_fixed, 0, s_abort);
-          if (ok && j + 1 < n_all) ok = mbar_wait(&full[sk], (uint32_t)(ik / NS) & 1u, s_abort);
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            if (!ok || j >= n[t]) continue;
-            ok = mbar_wait(&p_ready[t], (uint32_t)j & 1u, s_abort);
-            if (!ok) continue;
-            tc_fence_after_sync();
-            product(t, sv, j > 0);
-            if (j + 1 < n[t]) scores(t, sk);
-            else tc_commit(&o_full[t]);
+        // a tile of keys or values is released by the last row tile that uses it
+        if (ok && j < n0) {
+          ok = __all_sync(0xffffffffu, mbar_wait(&p_ready[0], (uint32_t)j & 1u, s_abort));
+          tc_fence_after_sync();
+          if (ok) {
+            product(0, sv, j > 0, j + 1 == n0, j >= n1);
+            if (j + 1 < n0) scores(0, sk, j + 1 >= n1);
           }
-          if (!ok) break;
-          tc_commit(&empty[sv]);
-          if (j + 1 < n_all) tc_commit(&empty[sk]);
         }
-        if (!ok) {                             // tensor memory is released only when no MMA uses it any more
+        if (ok && j < n1) {
+          ok = __all_sync(0xffffffffu, mbar_wait(&p_ready[1], (uint32_t)j & 1u, s_abort));
+          tc_fence_after_sync();
+          if (ok) {
+            product(1, sv, j > 0, j + 1 == n1, true);
+            if (j + 1 < n1) scores(1, sk, true);
+          }
+        }
+        ok = __all_sync(0xffffffffu, ok);
+      }
+      if (!ok) {                             // tensor memory is released only when no MMA uses it any more
+        if (elect_one()) {
           tc_commit(drained);
           for (uint32_t w = 0; w < kWaitPolls && !mbar_try_wait(drained, 0); ++w) __nanosleep(64);
         }
+        __syncwarp();
       }
     }
   }
