@@ -35,7 +35,7 @@ namespace tkphi {
 
 constexpr int kTileThreads = 384;
 constexpr int kWarpMma = 8, kWarpTma = 9;
-constexpr uint32_t kTileTmemCols = 512;      // S/P of the two row tiles: 128 columns each; O: head_dim columns each
+constexpr uint32_t kTileTmemCols = 512;      // S / P buffers of 128 columns, then the two outputs
 constexpr float kGrow = 1.f;                 // log2: how far a tile's maximum passes the reference before it replaces it
 
 // Two fp32 values as one operand of the packed FMA instructions.
@@ -79,9 +79,12 @@ __device__ __forceinline__ uint64_t exp2_pair(uint64_t x2) {
   return pack2(__int_as_float(__float_as_int(a) + (__float_as_int(ta) << 23)),
                __int_as_float(__float_as_int(b) + (__float_as_int(tb) << 23)));
 }
-// Which of the 16 pairs of a 32-column piece go through exp2_pair.
+// Which of the 16 pairs of a 32-column piece go through exp2_pair: a quarter at head_dim 64, where the special-function
+// unit is the bound (4096 x 32K tokens, 32 / 8 heads: 1322 us with none, 1250 with an eighth, 1187 with a quarter, 1230
+// with three eighths, 1375 with a half); none at 128, where the tensor pipe is (2048 x 32K, 24 / 8 heads: 664 us with none
+// or a quarter, 714 with a half).
 template <int D>
-__device__ __forceinline__ constexpr bool emulated(int e) { return D == 64 ? e % 8 % 3 == 0 : e % 4 == 0; }
+__device__ __forceinline__ constexpr bool emulated(int e) { return D == 64 && e % 4 == 0; }
 __device__ __forceinline__ bool elect_one() {
   uint32_t e;
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.b32 %0, 1, 0, p;\n}\n" : "=r"(e));
@@ -104,10 +107,18 @@ struct TileCfg {
   static constexpr int BOX = 128 * 128;                      // bytes of one 64-dim half of 128 rows
   static constexpr int TILE = HALVES * BOX;
   static constexpr int NS = D == 128 ? 5 : 10;               // ring slots
+  // Score buffers of 128 columns: as many as tensor memory has room for beside the two outputs.  With three, the next
+  // scores of a row tile are computed while its softmax warps still work on the ones before.
+  static constexpr int NB = D == 128 ? 2 : 3;
+  static constexpr int O_COL = NB * 128;
+  static constexpr int NV = 8;                               // more than the value tiles that the ring can hold
+  static_assert(NV > NS / 2 + 2, "a phase of v_free may not come round while the producer waits for it");
   static constexpr size_t q = 0;
   static constexpr size_t ring = 2 * TILE;
   static constexpr size_t bars = ring + (size_t)NS * TILE;
-  static constexpr size_t total = bars + 256;
+  static constexpr size_t bar_bytes = 512;                   // barriers and four words
+  static_assert((NS + NV + 2 * NB + 6) * 8 + 16 <= bar_bytes, "barriers");
+  static constexpr size_t total = bars + bar_bytes;
 };
 
 __device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t* r) {
@@ -148,18 +159,19 @@ __global__ void __launch_bounds__(kTileThreads, 1)
 paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                    const __grid_constant__ PagedProblem p) {
   using C = TileCfg<D>;
-  constexpr int NS = C::NS;
+  constexpr int NS = C::NS, NV = C::NV;
   constexpr float kShift = T::kBf16 ? 0.f : 7.f;             // P = 2^kShift exp2(..)
   constexpr float kSumLimit = T::kBf16 ? 1.099511627776e12f : 61440.f;
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char* qs = smem + C::q;
   unsigned char* ring = smem + C::ring;
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::bars);   // [NS] tile landed
-  uint64_t* empty = full + NS;             // [NS] the MMAs that read the slot are complete
-  uint64_t* s_full = empty + NS;           // [2]  scores complete
-  uint64_t* p_ready = s_full + 2;          // [2]  P stored
-  uint64_t* o_full = p_ready + 2;          // [2]  last product complete
-  uint64_t* q_ready = o_full + 2;          // [1]
+  uint64_t* v_free = full + NS;            // [NV] products of a key tile complete (key tile j: j % NV)
+  uint64_t* s_full = v_free + NV;          // [NB] scores complete
+  uint64_t* p_ready = s_full + C::NB;      // [NB] P stored
+  uint64_t* o_full = p_ready + C::NB;      // [2]  last product of the row tile complete
+  uint64_t* pv_done = o_full + 2;          // [1]  (three score buffers) products whose completion no scores tell
+  uint64_t* q_ready = pv_done + 1;         // [1]
   uint64_t* v_fixed = q_ready + 1;         // [1]  tail rows of the last value tile zeroed
   uint64_t* drained = v_fixed + 1;         // [1]  after a wait that ran out: the MMAs issued so far are complete
   int* misc = reinterpret_cast<int*>(drained + 1);
@@ -169,6 +181,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int cta = blockIdx.x;
 
+  pdl_wait();
   pdl_launch_next();
   if (warp == 0) {
     int base = 0;
@@ -188,10 +201,11 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   } else if (warp == 1) {
     tmem_alloc(s_tmem, kTileTmemCols);
   } else if (tid == 64) {
-    for (int s = 0; s < NS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-    for (int t = 0; t < 2; ++t) {
-      mbar_init(&s_full[t], 1); mbar_init(&p_ready[t], 4); mbar_init(&o_full[t], 1);
-    }
+    for (int s = 0; s < NS; ++s) mbar_init(&full[s], 1);
+    for (int s = 0; s < NV; ++s) mbar_init(&v_free[s], 1);
+    for (int i = 0; i < C::NB; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_ready[i], 4); }
+    mbar_init(&o_full[0], 1); mbar_init(&o_full[1], 1);
+    mbar_init(pv_done, 1);
     mbar_init(q_ready, 256);
     mbar_init(v_fixed, 1);
     mbar_init(drained, 1);
@@ -204,7 +218,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   const uint32_t tmem = *s_tmem;
   const int b = s_find[0];
 
-  int n[2] = {0, 0};                       // key tiles of the two row tiles
+  int n = 0, tiles = 1;                    // key tiles, row tiles of this CTA
   int h = 0, c0 = 0, row0 = 0, q_len = 0;
   TileSeq sq{0, 0, 1, 0};
   if (b >= 0) {
@@ -215,30 +229,29 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     i /= sq.row_tiles;
     c0 = (i % sq.chunks) * p.chunk;
     h = i / sq.chunks;
-    const int c1 = sq.len - c0 < p.chunk ? sq.len : c0 + p.chunk;
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int first = row0 + t * 128, last = (first + 128 < sq.rows ? first + 128 : sq.rows) - 1;
-      if (first >= sq.rows) continue;
-      int end = p.causal ? sq.len - q_len + last / p.group + 1 : sq.len;
-      if (end > c1) end = c1;
-      n[t] = end > c0 ? (end - c0 + kTileKeys - 1) / kTileKeys : 0;
-    }
+    const int rows = sq.rows - row0 < kTileRows ? sq.rows - row0 : kTileRows;
+    tiles = rows > 128 ? 2 : 1;
+    // up to the last key that the last row sees; both row tiles take all of these (the first one may see less: masked)
+    int end = p.causal ? sq.len - q_len + (row0 + rows - 1) / p.group + 1 : sq.len;
+    if (end > c0 + p.chunk) end = c0 + p.chunk;
+    n = end > c0 ? (end - c0 + kTileKeys - 1) / kTileKeys : 0;
   }
-  const int n_all = n[0] > n[1] ? n[0] : n[1];
-  const bool fix = n_all > 0 && c0 + n_all * kTileKeys > sq.len;      // the last tile reaches behind the sequence
+  const bool fix = n > 0 && c0 + n * kTileKeys > sq.len;              // the last tile reaches behind the sequence
+  // Scores, P and products run through one sequence: number i = key tile * tiles + row tile, buffer i % NB.  Keys are
+  // used `lead` tiles ahead of values: the ring holds K 0 .. K lead-1, V 0, K lead, V 1, ..
+  const int lead = (C::NB + tiles - 1) / tiles;
 
   if (warp < 8) {
     // ================================================================ softmax: thread = row
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int t = warp >> 2, r = tid & 127, quad = warp & 3;
     const int row = row0 + t * 128 + r;
-    const int nt = t == 0 ? n[0] : n[1];
+    const int nt = t < tiles ? n : 0;
     const bool live = row < sq.rows;
     const size_t tok0 = b >= 0 ? (size_t)__ldg(p.cu_q + b) : 0;
     const size_t out_row = live ? (tok0 + row / p.group) * p.hq + (size_t)h * p.group + row % p.group : 0;
     const size_t slot_row = (size_t)cta * kTileRows + t * 128 + r;
-    if (n_all > 0) {
+    if (n > 0) {
       // queries: the tile's 128 threads copy its rows, 16 bytes at a time (rows past the last are zeros)
       constexpr int CPR = D / 8;
       const uint4* q = static_cast<const uint4*>(p.q);
@@ -254,14 +267,16 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     }
     // last visible key; rows without a query run along unmasked and are not stored
     const int lim = !live ? INT_MAX : p.causal ? sq.len - q_len + row / p.group : sq.len - 1;
-    const uint32_t s_addr = tmem_addr(tmem, quad * 32, t * 128);
-    const uint32_t o_addr = tmem_addr(tmem, quad * 32, 256 + t * D);
+    const uint32_t o_addr = tmem_addr(tmem, quad * 32, C::O_COL + t * D);
+    int buf = t;
+    uint32_t phase = 0;
     float m = -INFINITY, l = 0.f;
     bool ok = true;
     for (int j = 0; j < nt; ++j) {
-      ok = __all_sync(0xffffffffu, mbar_wait(&s_full[t], (uint32_t)j & 1u, s_abort));
+      ok = __all_sync(0xffffffffu, mbar_wait(&s_full[buf], phase, s_abort));
       if (!ok) break;
       tc_fence_after_sync();
+      const uint32_t s_addr = tmem_addr(tmem, quad * 32, buf * 128);
       const int key0 = c0 + j * kTileKeys;
       uint32_t w[64];
       bool careful = j == 0 || __any_sync(0xffffffffu, key0 + kTileKeys - 1 > lim || m == -INFINITY);
@@ -329,6 +344,15 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         if (__any_sync(0xffffffffu, grow)) {
           const float f = grow ? ex2_approx(m - cand) : 1.f;   // m = -inf: 0
           if (j > 0) {
+            // The product before this one must be complete.  With two score buffers these scores were issued after it;
+            // with three, the next scores were (or, where there are none, it has a barrier of its own).
+            if (C::NB == 3) {
+              const bool next = tiles == 2 && 2 * j + t + 1 < 2 * n;
+              const int nb = buf + 1 == C::NB ? 0 : buf + 1;
+              ok = __all_sync(0xffffffffu, next ? mbar_wait(&s_full[nb], nb ? phase : phase ^ 1u, s_abort)
+                                                : mbar_wait(pv_done, tiles == 2 ? 0u : (uint32_t)(j - 1) & 1u, s_abort));
+              tc_fence_after_sync();
+            }
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
               float o[32];
@@ -362,7 +386,9 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       tc_wait_st();
       tc_fence_before_sync();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&p_ready[t]);
+      if (lane == 0) mbar_arrive(&p_ready[buf]);
+      buf += tiles;
+      if (buf >= C::NB) { buf -= C::NB; phase ^= 1u; }
     }
     if (ok && nt > 0) ok = __all_sync(0xffffffffu, mbar_wait(&o_full[t], 0, s_abort));
     if (ok && b >= 0) {
@@ -406,7 +432,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-    if (warp == kWarpTma && n_all > 0) {
+    if (warp == kWarpTma && n > 0) {
       // ================================================================ TMA producer
       const int ps = 1 << p.page_shift;
       const int box_rows = ps < 64 ? ps : 64, boxes = kTileKeys / box_rows;
@@ -416,49 +442,59 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       const int n_pages_seq = (sq.len + ps - 1) >> p.page_shift;
       const int* list = p.table + (size_t)b * p.max_pages;
       const uint64_t pol = l2_policy_normal();
-      int batch0 = (c0 >> p.page_shift) & ~31;
-      int id = batch0 + lane < n_pages_seq ? __ldg(list + batch0 + lane) : p.n_pages;
-      int id_next = batch0 + 32 + lane < n_pages_seq ? __ldg(list + batch0 + 32 + lane) : p.n_pages;
-      int issued[NS];
-#pragma unroll
-      for (int s = 0; s < NS; ++s) issued[s] = -1;
+      // page ids of the keys' and of the values' tiles: 32 at a time, the next 32 fetched ahead
+      int batch0[2], id[2], id_next[2];
+      batch0[0] = batch0[1] = (c0 >> p.page_shift) & ~31;
+      id[0] = id[1] = batch0[0] + lane < n_pages_seq ? __ldg(list + batch0[0] + lane) : p.n_pages;
+      id_next[0] = id_next[1] = batch0[0] + 32 + lane < n_pages_seq ? __ldg(list + batch0[0] + 32 + lane) : p.n_pages;
+      int slot = 0, last_slot = 0;
+      uint32_t phase = 0, last_phase = 0;
+      int issued = 0;
+      uint32_t pending = 0, parity = 0;                       // slots with a copy issued, and its phase
       bool ok = true;
-      int page = p.n_pages;
-      for (int i = 0; i < 2 * n_all && ok; ++i) {             // K0, V0, K1, V1, ...
-        if ((i & 1) == 0) {
-          const int first = (c0 + (i >> 1) * kTileKeys) >> p.page_shift;
-          if (first >= batch0 + 32) {
-            batch0 += 32;
-            id = id_next;
-            id_next = batch0 + 32 + lane < n_pages_seq ? __ldg(list + batch0 + 32 + lane) : p.n_pages;
-          }
-          page = __shfl_sync(0xffffffffu, id, (first + page_off) & 31);
-          if (page < 0 || page > p.n_pages || (page == p.n_pages && first + page_off < n_pages_seq)) {
-            if (lane < boxes) atomicExch(p.status, kStatusBadPage);
-            page = p.n_pages;                                 // a box outside the tensor arrives as zeros
-          }
+      auto load = [&](int x, int j) {                         // x: 0 keys, 1 values
+        const int first = (c0 + j * kTileKeys) >> p.page_shift;
+        if (first >= batch0[x] + 32) {
+          batch0[x] += 32;
+          id[x] = id_next[x];
+          id_next[x] = batch0[x] + 32 + lane < n_pages_seq ? __ldg(list + batch0[x] + 32 + lane) : p.n_pages;
         }
-        const int slot = i % NS;
-        ok = __all_sync(0xffffffffu, mbar_wait(&empty[slot], ((uint32_t)(i / NS) & 1u) ^ 1u, s_abort));
-        if (!ok) break;
+        int page = __shfl_sync(0xffffffffu, id[x], (first + page_off) & 31);
+        if (page < 0 || page > p.n_pages || (page == p.n_pages && first + page_off < n_pages_seq)) {
+          if (lane < boxes) atomicExch(p.status, kStatusBadPage);
+          page = p.n_pages;                                   // a box outside the tensor arrives as zeros
+        }
+        // The slot's last tile: number issued - NS of the ring's order.  Keys are free when the products of their own
+        // tile number (less the keys' lead) are complete, because all scores issued before those are, too.
+        const int old = issued++ - NS;
+        if (old >= 0) {
+          const int oj = old < lead ? 0 : ((old - lead) & 1) ? (old - lead + 1) / 2 : (old - lead) / 2;
+          ok = __all_sync(0xffffffffu, mbar_wait(&v_free[oj % NV], (uint32_t)(oj / NV) & 1u, s_abort));
+          if (!ok) return;
+        }
         if (lane == 0) mbar_expect_tx(&full[slot], C::TILE);
         __syncwarp();
         if (lane < copies)
-          tma_load_4d(ring + (size_t)slot * C::TILE + dst_off, (i & 1) ? &tmap_v : &tmap_k, &full[slot], half * 64,
-                      row_off, h, page, pol);
-#pragma unroll
-        for (int s = 0; s < NS; ++s)
-          if (s == slot) issued[s] = i;
+          tma_load_4d(ring + (size_t)slot * C::TILE + dst_off, x ? &tmap_v : &tmap_k, &full[slot], half * 64, row_off, h,
+                      page, pol);
+        pending |= 1u << slot;
+        parity = (parity & ~(1u << slot)) | (phase << slot);
+        last_slot = slot;
+        last_phase = phase;
+        if (++slot == NS) { slot = 0; phase ^= 1u; }
+      };
+      for (int jk = 0, jv = 0; jv < n && ok;) {
+        if (jk < n && jk < jv + lead) load(0, jk++);
+        else load(1, jv++);
       }
       if (ok && fix) {
         // Value rows of the last tile behind the end of the sequence.  (The slot's barrier is in the phase of this
         // copy until the wait returns, because nothing is loaded after it.)
-        const int i = 2 * n_all - 1, slot = i % NS;
-        const int keep = sq.len - (c0 + (n_all - 1) * kTileKeys);        // 1 .. 127
-        ok = __all_sync(0xffffffffu, mbar_wait(&full[slot], (uint32_t)(i / NS) & 1u, s_abort));
+        const int keep = sq.len - (c0 + (n - 1) * kTileKeys);        // 1 .. 127
+        ok = __all_sync(0xffffffffu, mbar_wait(&full[last_slot], last_phase, s_abort));
         if (ok) {
           constexpr int CPR = D / 8;
-          unsigned char* v = ring + (size_t)slot * C::TILE;
+          unsigned char* v = ring + (size_t)last_slot * C::TILE;
           for (int x = lane; x < (kTileKeys - keep) * CPR; x += 32) {
             const int row = keep + x / CPR, c = x % CPR;
             *reinterpret_cast<uint4*>(v + (c >> 3) * C::BOX + swz128(row, c & 7)) = make_uint4(0, 0, 0, 0);
@@ -470,92 +506,104 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       }
       if (!ok) {
         // every copy that was issued must land before shared memory is released
-#pragma unroll
         for (int s = 0; s < NS; ++s)
-          for (uint32_t w = 0; issued[s] >= 0 && w < kWaitPolls; ++w) {
-            if (mbar_try_wait(&full[s], (uint32_t)(issued[s] / NS) & 1u)) break;
+          for (uint32_t w = 0; (pending >> s & 1u) && w < kWaitPolls; ++w) {
+            if (mbar_try_wait(&full[s], parity >> s & 1u)) break;
             __nanosleep(64);
           }
       }
-    } else if (warp == kWarpMma && n_all > 0) {
+    } else if (warp == kWarpMma && n > 0) {
       // ================================================================ MMA issuer
       // The whole warp runs this code and one elected lane issues: descriptors then stay in uniform registers, where
       // the instruction takes them from.  (In a branch of one lane every MMA cost about 75 cycles of moves to issue, more
-      // than it took to execute.)
+      // than it took to execute.)  A wait that runs out raises the abort flag; this warp then issues the rest without
+      // waiting long, which touches only this CTA's own memory.
+      constexpr int NB = C::NB;
       constexpr uint32_t idesc_s = umma_idesc_16(T::kBf16, 128, kTileKeys, 0, 0);
       constexpr uint32_t idesc_o = umma_idesc_16(T::kBf16, 128, D, 0, 1);
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), base = __shfl_sync(0xffffffffu, smem_u32(smem), 0);
-      const int n0 = __shfl_sync(0xffffffffu, n[0], 0), n1 = __shfl_sync(0xffffffffu, n[1], 0), na = n0 > n1 ? n0 : n1;
+      const int nu = __shfl_sync(0xffffffffu, n, 0), T2 = __shfl_sync(0xffffffffu, tiles, 0), L = __shfl_sync(0xffffffffu, lead, 0);
       const uint64_t q_desc = umma_smem_desc(base + (uint32_t)C::q, 16, 1024);
       const uint64_t k_desc = umma_smem_desc(base + (uint32_t)C::ring, 16, 1024);
       const uint64_t v_desc = umma_smem_desc(base + (uint32_t)C::ring, C::BOX, 1024);   // MN-major: 64-dim blocks BOX bytes apart
-      auto scores = [&](int t, int slot, bool release) {
-        const uint64_t qd = q_desc + (uint64_t)((t * C::TILE) >> 4), kd = k_desc + (uint64_t)((slot * C::TILE) >> 4);
-        if (elect_one()) {
-#pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
-            const uint64_t off = (uint64_t)(((k >> 2) * C::BOX + (k & 3) * 32) >> 4);
-            umma_ss(tm + t * 128, qd + off, kd + off, idesc_s, k ? 1u : 0u);
-          }
-          tc_commit(&s_full[t]);
-          if (release) tc_commit(&empty[slot]);
-        }
+      auto wait_on = [&](uint64_t* bar, uint32_t parity) {
+        mbar_wait(bar, parity, s_abort);
         __syncwarp();
       };
-      auto product = [&](int t, int slot, bool add, bool last, bool release) {
-        const uint64_t vd = v_desc + (uint64_t)((slot * C::TILE) >> 4);
-        if (elect_one()) {
-#pragma unroll
-          for (int k = 0; k < kTileKeys / 16; ++k)
-            umma_ts(tm + 256 + t * D, tm + t * 128 + k * 8, vd + (uint64_t)((k * 16 * 128) >> 4), idesc_o,
-                    (add || k > 0) ? 1u : 0u);
-          if (last) tc_commit(&o_full[t]);
-          if (release) tc_commit(&empty[slot]);
-        }
-        __syncwarp();
+      // Ring slots and phases of the next key and value tiles.  In the ring's order a value tile follows every key tile
+      // from the lead-th on, until the keys run out.
+      int k_slot = 0, v_slot = 0, v_next = 0;
+      uint32_t k_phase = 0, v_phase = 0;
+      auto advance = [](int& slot, uint32_t& phase, int by) {
+        slot += by;
+        if (slot >= NS) { slot -= NS; phase ^= 1u; }
       };
-      // slot and phase of the ring's tiles K0, V0, K1, V1, ..
-      int slot = 0;
-      uint32_t phase = 0;
-      auto step = [&]() { if (++slot == NS) { slot = 0; phase ^= 1u; } };
-      bool ok = mbar_wait(q_ready, 0, s_abort) && mbar_wait(&full[0], 0, s_abort);
-      ok = __all_sync(0xffffffffu, ok);
-      if (ok) {
+      static_assert(NS > 3, "a step of the ring passes its end once at most");
+      auto issue_scores = [&](int t, int buf) {                 // (elected lane)
+        const uint64_t qd = q_desc + (uint64_t)((t * C::TILE) >> 4), kd = k_desc + (uint64_t)((k_slot * C::TILE) >> 4);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint64_t off = (uint64_t)(((k >> 2) * C::BOX + (k & 3) * 32) >> 4);
+          umma_ss(tm + buf * 128, qd + off, kd + off, idesc_s, k ? 1u : 0u);
+        }
+        tc_commit(&s_full[buf]);
+      };
+      auto wait_keys = [&](int j) {
+        if (j > 0) advance(k_slot, k_phase, j < L ? 1 : 2);
+        wait_on(&full[k_slot], k_phase);
+      };
+      auto wait_values = [&](int j) {
+        advance(v_next, v_phase, j == 0 ? (L < nu ? L : nu) : j + L <= nu ? 2 : 1);
+        wait_on(&full[v_next], v_phase);
+        if (fix && j + 1 == nu) wait_on(v_fixed, 0);
+      };
+      wait_on(q_ready, 0);
+      int sj = 0, st = 0;                                       // next scores to issue
+      for (int i = 0; i < NB && sj < nu; ++i) {
+        if (st == 0) wait_keys(sj);
         tc_fence_after_sync();
-        if (n0 > 0) scores(0, 0, n1 == 0);
-        if (n1 > 0) scores(1, 0, true);
-        step();
+        if (elect_one()) issue_scores(st, i);
+        __syncwarp();
+        if (++st == T2) { st = 0; ++sj; }
       }
-      for (int j = 0; j < na && ok; ++j) {
-        const int sv = slot;
-        ok = mbar_wait(&full[sv], phase, s_abort);
-        if (ok && fix && j + 1 == na) ok = mbar_wait(v_fixed, 0, s_abort);
-        step();
-        const int sk = slot;
-        if (j + 1 < na) {
-          if (ok) ok = mbar_wait(&full[sk], phase, s_abort);
-          step();
-        }
-        // a tile of keys or values is released by the last row tile that uses it
-        if (ok && j < n0) {
-          ok = __all_sync(0xffffffffu, mbar_wait(&p_ready[0], (uint32_t)j & 1u, s_abort));
-          tc_fence_after_sync();
-          if (ok) {
-            product(0, sv, j > 0, j + 1 == n0, j >= n1);
-            if (j + 1 < n0) scores(0, sk, j + 1 >= n1);
-          }
-        }
-        if (ok && j < n1) {
-          ok = __all_sync(0xffffffffu, mbar_wait(&p_ready[1], (uint32_t)j & 1u, s_abort));
-          tc_fence_after_sync();
-          if (ok) {
-            product(1, sv, j > 0, j + 1 == n1, true);
-            if (j + 1 < n1) scores(1, sk, true);
-          }
-        }
-        ok = __all_sync(0xffffffffu, ok);
+      if (NB == 3) {
+        wait_values(0);
+        v_slot = v_next;
+        if (st == 0 && sj < nu) wait_keys(sj);
       }
-      if (!ok) {                             // tensor memory is released only when no MMA uses it any more
+      int buf = 0;
+      uint32_t phase = 0;
+      // One burst per step: the product of a row tile, then its buffer's next scores.  What a burst needs beside P has
+      // been waited for after an earlier one, while that one's MMAs ran.
+      for (int j = 0; j < nu; ++j) {
+        if (NB == 2) {
+          wait_values(j);
+          v_slot = v_next;
+        }
+        for (int t = 0; t < T2; ++t) {
+          if (NB == 2 && st == 0 && sj < nu) wait_keys(sj);
+          wait_on(&p_ready[buf], phase);
+          const uint64_t vd = v_desc + (uint64_t)((v_slot * C::TILE) >> 4);
+          tc_fence_after_sync();
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < kTileKeys / 16; ++k)
+              umma_ts(tm + C::O_COL + t * D, tm + buf * 128 + k * 8, vd + (uint64_t)((k * 16 * 128) >> 4), idesc_o,
+                      (j > 0 || k > 0) ? 1u : 0u);
+            if (sj < nu) issue_scores(st, buf);
+            if (t + 1 == T2) tc_commit(&v_free[j % NV]);
+            if (j + 1 == nu) tc_commit(&o_full[t]);
+            if (NB == 3 && (T2 == 1 || (t == 1 && j + 2 == nu))) tc_commit(pv_done);
+          }
+          __syncwarp();
+          if (++st == T2) { st = 0; ++sj; }
+          if (NB == 3 && t + 1 == T2 && j + 1 < nu) wait_values(j + 1);
+          if (NB == 3 && st == 0 && sj < nu) wait_keys(sj);
+          if (++buf == NB) { buf = 0; phase ^= 1u; }
+        }
+        if (NB == 3) v_slot = v_next;
+      }
+      if (*s_abort) {                        // tensor memory is released only when no MMA uses it any more
         if (elect_one()) {
           tc_commit(drained);
           for (uint32_t w = 0; w < kWaitPolls && !mbar_try_wait(drained, 0); ++w) __nanosleep(64);
