@@ -161,7 +161,7 @@ struct AppendProblem {
   const long long* positions;      // [total_q] or null: the cache position of each token
   void* bounds;
   int* status;
-  int items;                       // page items of all sequences (upper bound over the positions of a page's start)
+  int items;                       // CTAs per KV head: spans of 64 positions (or a page of 128) of all sequences, at most
 };
 cudaError_t launch_paged_append(const AppendProblem& p, bool bf16, cudaStream_t st);
 cudaError_t launch_paged_rows(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int d, bool bf16,

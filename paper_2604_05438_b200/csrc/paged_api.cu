@@ -300,9 +300,10 @@ tkphi_status tkphi_paged_append(const tkphi_paged_desc* kv, const tkphi_append_d
     return fail(TKPHI_ERR_INVALID_ARG, "q_out is q with other strides");
   if (sh.total_q == 0) return TKPHI_OK;
   int64_t items = 0;
+  const int64_t span = std::max(kv->page_size, 64);          // positions of a CTA
   for (int b = 0; b < kv->batch; ++b) {
     const int64_t q = kv->cu_q_host[b + 1] - kv->cu_q_host[b];
-    if (q > 0) items += ((q + kv->page_size - 2) >> sh.page_shift) + 1;
+    if (q > 0) items += ((q + span - 2) / span) + 1;
   }
   AppendProblem p{};
   p.batch = kv->batch; p.hq = kv->n_q_heads; p.hkv = kv->n_kv_heads; p.group = sh.group; p.d = kv->head_dim;
