@@ -33,11 +33,12 @@ struct PagedProblem {
   int* status;
   // row kernel: sequences with at most rows_limit rows
   int rows_limit;
-  int row_ctas;                    // CTAs that share the tiles of all units evenly; 0: one CTA per unit
+  int row_ctas;                    // CTAs that share the tiles of all units evenly
+  int n_split;                     // CTAs per unit where units are cut evenly instead (clusters; the block form)
+  int beside;                      // launched beside the tile kernel: does not wait for it before its end
   float* row_part;                 // [2 * row_ctas or units * n_split][16][d] unnormalised partial outputs
   float* row_stat;                 // [..][16][2] their maximum (log2 units) and sum
   // page selection
-  int n_split;                     // CTAs per unit (token, KV head) of the block form
   int n_keep, n_sink, n_tail, topk;
   const void* bounds;              // [n_pages][hkv][2][d]
   unsigned long long* page_keys;   // [units][key_stride] ordered bounds of the candidate pages
@@ -165,7 +166,7 @@ struct AppendProblem {
 };
 cudaError_t launch_paged_append(const AppendProblem& p, bool bf16, cudaStream_t st);
 cudaError_t launch_paged_rows(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int d, bool bf16,
-                              bool block, int grid, bool dependent, cudaStream_t st);
+                              bool block, bool split, int grid, cudaStream_t st);
 cudaError_t launch_paged_rows_merge(const PagedProblem& p, int d, bool bf16, bool block, int units, int max_rows, cudaStream_t st);
 cudaError_t launch_paged_select(const PagedProblem& p, int d, bool bf16, int max_pages_seq, cudaStream_t st);
 cudaError_t launch_paged_tiles(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int d, bool bf16, int grid,

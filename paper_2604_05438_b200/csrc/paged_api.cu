@@ -114,7 +114,7 @@ tkphi_status make_page_map(const tkphi_paged_desc* kv, const void* base, CUtenso
 struct AttendPlan {
   int max_rows;                  // rows of the widest sequence of the row kernel
   int64_t row_tiles;             // tiles of the row kernel
-  int row_ctas, row_grid;        // row_ctas 0: one CTA per unit
+  int row_ctas, row_split, row_grid;   // row_split > 0: clusters of that many CTAs per unit, nothing to join
   bool any_rows, any_tiles;
   int chunk, max_chunks, tile_grid;
   size_t row_part, row_stat, tile_part, tile_stat, total;
@@ -150,6 +150,13 @@ int choose_chunk(const tkphi_paged_desc* kv, const PagedShape& sh, int64_t longe
   return best * kTileKeys;
 }
 
+// CTAs per unit of the row kernel's cluster form, or 0 for the line: units of at most `tiles` tiles.
+int split_rows(int64_t units, int64_t tiles, int n_sm) {
+  int split = 1;
+  while (split < 8 && tiles > split && units * split * 2 <= 2 * n_sm) split *= 2;
+  return tiles <= 16 * split ? split : 0;
+}
+
 tkphi_status plan_attend(const tkphi_paged_desc* kv, const PagedShape& sh, AttendPlan* pl) {
   const int n_sm = sm_count_current_device();
   *pl = AttendPlan{};
@@ -170,9 +177,10 @@ tkphi_status plan_attend(const tkphi_paged_desc* kv, const PagedShape& sh, Atten
     longest_row = std::max(longest_row, tiles);
   }
   if (pl->row_tiles > INT_MAX / 2) return fail(TKPHI_ERR_UNSUPPORTED, "too many key tiles for one call");
-  pl->row_ctas = (int)std::min<int64_t>(2 * n_sm, pl->row_tiles);
-  if (longest_row <= 8 && pl->max_rows <= kRowTile) pl->row_ctas = 0;       // short caches: nothing to join
-  pl->row_grid = pl->row_ctas ? pl->row_ctas : kv->batch * kv->n_kv_heads;
+  const int units = kv->batch * kv->n_kv_heads;
+  pl->row_split = split_rows(units, longest_row, n_sm);
+  pl->row_ctas = pl->row_split ? 0 : (int)std::min<int64_t>(2 * n_sm, pl->row_tiles);
+  pl->row_grid = pl->row_split ? units * pl->row_split : pl->row_ctas;
   if (pl->any_tiles) {
     pl->chunk = choose_chunk(kv, sh, longest, n_sm);
     int64_t grid = 0;
@@ -198,6 +206,7 @@ tkphi_status plan_attend(const tkphi_paged_desc* kv, const PagedShape& sh, Atten
 
 struct BlockPlan {
   int n_split, n_keep, key_stride;
+  bool cluster;                  // the CTAs of a unit are a cluster and join their pieces themselves
   size_t keys, list, part, stat, total;
 };
 
@@ -213,12 +222,14 @@ tkphi_status plan_block(const tkphi_paged_desc* kv, const PagedShape& sh, const 
   const int64_t middle = sh.max_pages_seq - sel->n_sink_pages - sel->n_tail_pages;
   pl->key_stride = (int)std::max<int64_t>(middle > sel->topk_pages ? middle : 0, 1);
   const int64_t tiles = ((std::min<int64_t>(keep, std::max<int64_t>(sh.max_pages_seq, 1)) << sh.page_shift) + kRowKeys - 1) / kRowKeys;
-  const int64_t slots = 2 * sm_count_current_device();
-  pl->n_split = (int)std::max<int64_t>(1, std::min<int64_t>((tiles + 1) / 2, units > 0 ? slots / units : 1));
+  const int n_sm = sm_count_current_device();
+  pl->n_split = split_rows(units, tiles, n_sm);
+  pl->cluster = pl->n_split > 0;
+  if (!pl->cluster) pl->n_split = (int)std::max<int64_t>(1, std::min<int64_t>((tiles + 1) / 2, units > 0 ? 2 * n_sm / units : 1));
   size_t o = 0;
   pl->keys = o; o = align_up(o + sizeof(unsigned long long) * units * pl->key_stride, 256);
   pl->list = o; o = align_up(o + sizeof(int) * units * pl->n_keep, 256);
-  const size_t parts = pl->n_split > 1 ? (size_t)units * pl->n_split : 0;
+  const size_t parts = pl->n_split > 1 && !pl->cluster ? (size_t)units * pl->n_split : 0;
   pl->part = o; o = align_up(o + sizeof(float) * parts * kRowTile * kv->head_dim, 256);
   pl->stat = o; o = align_up(o + sizeof(float) * parts * kRowTile * 2, 256);
   pl->total = std::max<size_t>(o, 256);
@@ -354,6 +365,8 @@ tkphi_status tkphi_paged_attention(const tkphi_paged_desc* kv, const void* q, vo
   char* w = static_cast<char*>(workspace);
   p.rows_limit = kRowsLimit;
   p.row_ctas = pl.row_ctas;
+  p.n_split = pl.row_split;
+  p.beside = pl.any_tiles ? 1 : 0;
   p.row_part = reinterpret_cast<float*>(w + pl.row_part);
   p.row_stat = reinterpret_cast<float*>(w + pl.row_stat);
   p.chunk = pl.chunk;
@@ -369,13 +382,13 @@ tkphi_status tkphi_paged_attention(const tkphi_paged_desc* kv, const void* q, vo
   }
   if (e == cudaSuccess && pl.any_rows) {
     ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_ROWS);
-    e = launch_paged_rows(p, tk, tv, kv->head_dim, bf16, false, pl.row_grid, pl.any_tiles, cs);
+    e = launch_paged_rows(p, tk, tv, kv->head_dim, bf16, false, pl.row_split > 0, pl.row_grid, cs);
   }
   if (e == cudaSuccess && pl.max_chunks > 1) {
     ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_TILES);
     e = launch_paged_tiles_merge(p, kv->head_dim, bf16, cs);
   }
-  if (e == cudaSuccess && pl.any_rows && pl.row_ctas) {
+  if (e == cudaSuccess && pl.any_rows && !pl.row_split) {
     ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_ROWS);
     e = launch_paged_rows_merge(p, kv->head_dim, bf16, false, kv->batch * kv->n_kv_heads, pl.max_rows, cs);
   }
@@ -424,8 +437,8 @@ tkphi_status tkphi_paged_block_attention(const tkphi_paged_desc* kv, const tkphi
   if (e != cudaSuccess) return cuda_fail(e, "page selection launch");
   {
     ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_ROWS);
-    e = launch_paged_rows(p, tk, tv, kv->head_dim, bf16, true, units * pl.n_split, true, cs);
-    if (e == cudaSuccess && pl.n_split > 1) e = launch_paged_rows_merge(p, kv->head_dim, bf16, true, units, sh.group, cs);
+    e = launch_paged_rows(p, tk, tv, kv->head_dim, bf16, true, pl.cluster, units * pl.n_split, cs);
+    if (e == cudaSuccess && pl.n_split > 1 && !pl.cluster) e = launch_paged_rows_merge(p, kv->head_dim, bf16, true, units, sh.group, cs);
   }
   if (e != cudaSuccess) return cuda_fail(e, "paged block attention launch");
   return TKPHI_OK;

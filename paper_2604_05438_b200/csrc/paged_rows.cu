@@ -15,14 +15,28 @@
 // Probabilities enter the second product as hi + lo pairs of the element type (2^-16 relative for bf16): that costs
 // 16 extra matrix instructions per tile, which the kernel has time for, and leaves the output's own rounding as the
 // only one of its size.
-// Work is dealt out evenly: the tiles of all units form one line, cut into as many equal pieces as there are resident
-// CTAs; a unit that is cut leaves partial results, joined in a fixed order by a second, dependent kernel.
+// Work is dealt out in one of two ways.  Long caches: the tiles of all units form one line, cut into as many equal pieces
+// as there are resident CTAs; a unit that is cut leaves partial results, joined in a fixed order by a second, dependent
+// kernel.  Short ones and short page lists: a unit is cut into up to eight pieces, the CTAs of one cluster, which join
+// theirs through distributed shared memory (no second launch, no trip through global memory).
 #include "paged.cuh"
 
 namespace tkphi {
 
 constexpr int kRowWarps = 4;
 constexpr int kRowThreads = (kRowWarps + 1) * 32;
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Two floats at shared-memory address p of the cluster's CTA `rank`.
+__device__ __forceinline__ float2 ld_cluster_f2(const float* p, int rank) {
+  uint32_t a;
+  float2 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
+  return v;
+}
 
 template <int D>
 struct RowCfg {
@@ -35,10 +49,14 @@ struct RowCfg {
   static constexpr size_t stat = red + kRowWarps * kRowTile * 64 * 4;   // [4][16][2]
   static constexpr size_t bars = stat + kRowWarps * kRowTile * 2 * 4;
   static constexpr size_t total = bars + (2 * NS) * 8 + 16;
+  // cluster form: [16][D] piece of this CTA and [16][2] its statistics, over the ring's first tiles (a CTA has one
+  // piece there, and writes it when its warps have read all of them)
+  static constexpr size_t keep = 0;
+  static_assert(kRowTile * (D + 2) * 4 <= NS * STAGE, "piece");
 };
 
 // The pieces of one CTA: (unit, tile range) one after the other.  Every warp runs its own copy.
-template <bool BLOCK>
+template <bool BLOCK, bool SPLIT>
 struct RowWalk {
   const PagedProblem& p;
   // current piece
@@ -63,6 +81,12 @@ struct RowWalk {
   }
   __device__ __forceinline__ int seq_weight() const { return seq_tiles * p.hkv * ((seq_rows + kRowTile - 1) / kRowTile); }
 
+  __device__ __forceinline__ void split_tiles(int part) {
+    const int per = (tiles + p.n_split - 1) / p.n_split;
+    t0 = part * per < tiles ? part * per : tiles;
+    t1 = t0 + per < tiles ? t0 + per : tiles;
+    f1 = t0 < t1 ? 1 : 0;
+  }
   __device__ __forceinline__ RowWalk(const PagedProblem& pr, int cta) : p(pr) {
     const int lane = threadIdx.x & 31;
     f = f1 = 0;
@@ -78,22 +102,20 @@ struct RowWalk {
       const int seen = (pos0 >> p.page_shift) + 1;
       n_list = seen < p.n_keep ? seen : p.n_keep;
       tiles = ((n_list << p.page_shift) + kRowKeys - 1) / kRowKeys;
-      const int per = (tiles + p.n_split - 1) / p.n_split;
-      t0 = part * per;
-      t1 = t0 + per < tiles ? t0 + per : tiles;
-      f1 = t0 < t1 ? 1 : 0;
+      split_tiles(part);
+      return;
+    }
+    if (SPLIT) {                                        // sequences of one row tile
+      const int u = cta / p.n_split;
+      b = u / p.hkv;
+      h = u % p.hkv;
+      load_seq(b);
+      tiles = seq_tiles; r_first = 0; rows = seq_rows; tok0 = seq_tok0; len = seq_len; pos0 = seq_len - seq_q;
+      t0 = t1 = 0;
+      if (rows > 0) split_tiles(cta % p.n_split);
       return;
     }
     // the line: sequence by sequence, in a sequence row tile by row tile, head by head
-    if (p.row_ctas == 0) {                              // one CTA per unit (sequences of one row tile)
-      b = cta / p.hkv;
-      load_seq(b);
-      seq_start = 0;
-      f = (cta % p.hkv) * seq_tiles;
-      seq_end = seq_weight();
-      f1 = seq_rows > 0 ? f + seq_tiles : f;
-      return;
-    }
     int total = 0;
     for (int s = 0; s < p.batch; s += 32) {
       load_seq(s + lane);
@@ -122,7 +144,7 @@ struct RowWalk {
   }
   __device__ __forceinline__ bool next() {
     if (f >= f1) return false;
-    if (BLOCK) { f = f1; return true; }
+    if (BLOCK || SPLIT) { f = f1; return true; }
     while (f >= seq_end) {
       load_seq(++b);
       seq_start = seq_end;
@@ -145,7 +167,7 @@ struct RowWalk {
   __device__ __forceinline__ int slot(int cta) const { return BLOCK ? cta : 2 * cta + (t0 == 0 ? 1 : 0); }
 };
 
-template <typename T, int D, bool BLOCK>
+template <typename T, int D, bool BLOCK, bool SPLIT>
 __global__ void __launch_bounds__(kRowThreads, 2)
 paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                   const __grid_constant__ PagedProblem p) {
@@ -157,6 +179,8 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::bars);
   uint64_t* empty = full + NS;
   volatile int* s_abort = reinterpret_cast<int*>(empty + NS);
+  float* keep = reinterpret_cast<float*>(smem + C::keep);
+  float* keep_stat = keep + kRowTile * D;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int cta = blockIdx.x;
 
@@ -166,12 +190,12 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     *s_abort = 0;
   }
   __syncthreads();
+  if (!p.beside) pdl_wait();
   pdl_launch_next();
-  if (BLOCK) pdl_wait();                       // the page lists come from the kernel before
 
   if (warp == kRowWarps) {
     // ================================================================ TMA producer
-    RowWalk<BLOCK> w(p, cta);
+    RowWalk<BLOCK, SPLIT> w(p, cta);
     const int ps = 1 << p.page_shift;
     const int npg = ps < kRowKeys ? kRowKeys >> p.page_shift : 1;             // pages of a tile
     const int box_rows = ps < kRowKeys ? ps : kRowKeys;
@@ -227,7 +251,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     }
   } else {
     // ================================================================ compute
-    RowWalk<BLOCK> w(p, cta);
+    RowWalk<BLOCK, SPLIT> w(p, cta);
     const int ps = 1 << p.page_shift;
     const int rA = lane >> 2, rB = rA + 8, cc = 2 * (lane & 3);
     bool ok = true;
@@ -394,7 +418,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         const float m = stat[(i * kRowTile + row) * 2];
         if (m != -INFINITY) L += stat[(i * kRowTile + row) * 2 + 1] * ex2_approx(m - M);
       }
-      const bool fin = w.whole();
+      const bool fin = w.whole();              // in a cluster: the unit is this CTA's alone
       const int slot = w.slot(cta);
       const int r = w.r_first + row;
       const size_t out_row = (size_t)(w.tok0 + r / p.group) * p.hq + w.h * p.group + r % p.group;
@@ -427,7 +451,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             y.z = T::pack(a[4] * inv, a[5] * inv); y.w = T::pack(a[6] * inv, a[7] * inv);
             *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.y) + out_row * D + x * 64 + d8) = y;
           } else {
-            float4* dst = reinterpret_cast<float4*>(p.row_part + ((size_t)slot * kRowTile + row) * D + x * 64 + d8);
+            float4* dst = reinterpret_cast<float4*>((SPLIT ? keep + (size_t)row * D : p.row_part + ((size_t)slot * kRowTile + row) * D) + x * 64 + d8);
             dst[0] = make_float4(a[0], a[1], a[2], a[3]);
             dst[1] = make_float4(a[4], a[5], a[6], a[7]);
           }
@@ -438,24 +462,76 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         if (fin) {
           if (p.lse) p.lse[out_row] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
         } else {
-          p.row_stat[((size_t)slot * kRowTile + row) * 2] = M;
-          p.row_stat[((size_t)slot * kRowTile + row) * 2 + 1] = L;
+          float* st = SPLIT ? keep_stat + row * 2 : p.row_stat + ((size_t)slot * kRowTile + row) * 2;
+          st[0] = M;
+          st[1] = L;
         }
       }
     }
+  }
+  if (SPLIT && p.n_split > 1) {
+    // ================================================================ join of the cluster's pieces, rank by rank
+    __syncwarp();
+    cluster_sync();
+    RowWalk<BLOCK, SPLIT> w(p, cta);
+    const int rank = cta % p.n_split;
+    const int per = (w.tiles + p.n_split - 1) / p.n_split;
+    const int pieces = w.rows > 0 && w.tiles > per ? (w.tiles + per - 1) / per : 0;     // 0: nothing to join
+    if (pieces > 0 && warp < kRowWarps) {
+      // rows in turn over the ranks' warps; a lane owns D / 32 dims
+      constexpr int V = D / 32;
+      for (int row = rank * kRowWarps + warp; row < w.rows; row += p.n_split * kRowWarps) {
+        float2 st[8];
+        float2 v[8][V / 2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int from = i < pieces ? i : 0;
+          st[i] = ld_cluster_f2(keep_stat + row * 2, from);
+#pragma unroll
+          for (int e = 0; e < V / 2; ++e) v[i][e] = ld_cluster_f2(keep + (size_t)row * D + lane * V + 2 * e, from);
+        }
+        float M = -INFINITY, L = 0.f, a[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) a[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < pieces) M = fmaxf(M, st[i].x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float f = i < pieces && st[i].x != -INFINITY ? ex2_approx(st[i].x - M) : 0.f;
+          L += st[i].y * f;
+#pragma unroll
+          for (int e = 0; e < V / 2; ++e) { a[2 * e] += v[i][e].x * f; a[2 * e + 1] += v[i][e].y * f; }
+        }
+        const float inv = L > 0.f ? 1.f / L : 0.f;
+        const int r = w.r_first + row;
+        const size_t out_row = (size_t)(w.tok0 + r / p.group) * p.hq + w.h * p.group + r % p.group;
+        uint32_t* y = static_cast<uint32_t*>(p.y) + out_row * (D / 2) + lane * (V / 2);
+#pragma unroll
+        for (int e = 0; e < V / 2; ++e) y[e] = T::pack(a[2 * e] * inv, a[2 * e + 1] * inv);
+        if (lane == 0 && p.lse) p.lse[out_row] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+      }
+    }
+    __syncwarp();
+    cluster_sync();                            // shared memory is read by the other ranks until here
   }
   __syncthreads();
   if (*s_abort && tid == 0) atomicExch(p.status, kStatusTimeout);
   // (beside a tile-kernel launch this grid may run next to it: it must not be complete before that one is, because the
   // joins that follow wait for this grid only)
-  if (!BLOCK) pdl_wait();
+  if (p.beside) pdl_wait();
 }
 
-// Joins the partial results of the units that were cut: a CTA per (unit, row), a thread per pair of dims; the parts
-// are added in the order of their keys.
+// Joins the partial results of the units that were cut: a CTA per (unit, row), in groups of one thread per pair of dims;
+// the parts go to the groups in turn, and everything is added in a fixed order.
+constexpr int kMergeThreads = 256;
 template <typename T, int D, bool BLOCK>
-__global__ void __launch_bounds__(D / 2) paged_rows_merge_kernel(const __grid_constant__ PagedProblem p) {
+__global__ void __launch_bounds__(kMergeThreads) paged_rows_merge_kernel(const __grid_constant__ PagedProblem p) {
+  constexpr int TPG = D / 2, GROUPS = kMergeThreads / TPG;
+  __shared__ float s_stat[GROUPS][2];
+  __shared__ float2 s_acc[GROUPS][TPG];
   pdl_wait();
+  pdl_launch_next();
   const int lane = threadIdx.x & 31, row = blockIdx.y;
   int first, count, step, rows, tok0, h, r;
   if (BLOCK) {
@@ -500,43 +576,84 @@ __global__ void __launch_bounds__(D / 2) paged_rows_merge_kernel(const __grid_co
     rows = mine; tok0 = (int)__ldg(p.cu_q + b); r = row;
   }
   if (count < 2 || row >= rows) return;   // written by the row kernel itself
-  const int rr = r % kRowTile;
-  auto slot_of = [&](int i) { return BLOCK ? first + i : i == 0 ? first + 1 : first + step * i; };
-  float M = -INFINITY;
-  for (int i = lane; i < count; i += 32) M = fmaxf(M, __ldcg(p.row_stat + ((size_t)slot_of(i) * kRowTile + rr) * 2));
+  const int rr = r % kRowTile, grp = threadIdx.x / TPG, d = threadIdx.x % TPG;
+  float M = -INFINITY, L = 0.f, a0 = 0.f, a1 = 0.f;
+  for (int i0 = grp; i0 < count; i0 += 4 * GROUPS) {
+    float2 st[4], v[4];
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-  float L = 0.f, a0 = 0.f, a1 = 0.f;
-#pragma unroll 4
-  for (int i = 0; i < count; ++i) {
-    const size_t s = (size_t)slot_of(i) * kRowTile + rr;
-    const float2 st = __ldcg(reinterpret_cast<const float2*>(p.row_stat) + s);
-    const float2 v = __ldcg(reinterpret_cast<const float2*>(p.row_part + s * D) + threadIdx.x);
-    const float f = st.x == -INFINITY ? 0.f : ex2_approx(st.x - M);
-    L += st.y * f;
+    for (int x = 0; x < 4; ++x) {
+      const int i = i0 + x * GROUPS;
+      st[x] = make_float2(-INFINITY, 0.f);
+      v[x] = make_float2(0.f, 0.f);
+      if (i < count) {
+        const size_t s = (size_t)(BLOCK ? first + i : i == 0 ? first + 1 : first + step * i) * kRowTile + rr;
+        st[x] = __ldcg(reinterpret_cast<const float2*>(p.row_stat) + s);
+        v[x] = __ldcg(reinterpret_cast<const float2*>(p.row_part + s * D) + d);
+      }
+    }
+    const float m = fmaxf(fmaxf(fmaxf(st[0].x, st[1].x), fmaxf(st[2].x, st[3].x)), M);
+    const float g = M == -INFINITY ? 0.f : ex2_approx(M - m);
+    L *= g; a0 *= g; a1 *= g;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float f = st[x].x == -INFINITY ? 0.f : ex2_approx(st[x].x - m);
+      L += st[x].y * f;
+      a0 += v[x].x * f;
+      a1 += v[x].y * f;
+    }
+    M = m;
+  }
+  if (d == 0) { s_stat[grp][0] = M; s_stat[grp][1] = L; }
+  s_acc[grp][d] = make_float2(a0, a1);
+  __syncthreads();
+  if (grp > 0) return;
+  M = -INFINITY; L = 0.f; a0 = 0.f; a1 = 0.f;
+#pragma unroll
+  for (int i = 0; i < GROUPS; ++i) M = fmaxf(M, s_stat[i][0]);
+#pragma unroll
+  for (int i = 0; i < GROUPS; ++i) {
+    const float f = s_stat[i][0] == -INFINITY ? 0.f : ex2_approx(s_stat[i][0] - M);
+    const float2 v = s_acc[i][d];
+    L += s_stat[i][1] * f;
     a0 += v.x * f;
     a1 += v.y * f;
   }
   const float inv = L > 0.f ? 1.f / L : 0.f;
   const size_t out_row = (size_t)(tok0 + r / p.group) * p.hq + h * p.group + r % p.group;
-  reinterpret_cast<uint32_t*>(p.y)[out_row * (D / 2) + threadIdx.x] = T::pack(a0 * inv, a1 * inv);
-  if (threadIdx.x == 0 && p.lse) p.lse[out_row] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+  reinterpret_cast<uint32_t*>(p.y)[out_row * (D / 2) + d] = T::pack(a0 * inv, a1 * inv);
+  if (d == 0 && p.lse) p.lse[out_row] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+}
+
+template <typename T, int D, bool BLOCK, bool SPLIT>
+static cudaError_t launch_rows_s(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int grid, cudaStream_t st) {
+  static PerDeviceFlag configured;
+  const size_t smem = RowCfg<D>::total;
+  const cudaError_t e = set_max_dynamic_smem(configured, reinterpret_cast<const void*>(paged_rows_kernel<T, D, BLOCK, SPLIT>), smem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kRowThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = p.n_split; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = SPLIT && p.n_split > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, paged_rows_kernel<T, D, BLOCK, SPLIT>, tk, tv, p);
 }
 
 template <typename T, int D, bool BLOCK>
-static cudaError_t launch_rows_t(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int grid,
-                                 bool dependent, cudaStream_t st) {
-  static PerDeviceFlag configured;
-  cudaError_t e = set_max_dynamic_smem(configured, reinterpret_cast<const void*>(paged_rows_kernel<T, D, BLOCK>), RowCfg<D>::total);
-  if (e != cudaSuccess) return e;
-  if (dependent) return launch_pdl(paged_rows_kernel<T, D, BLOCK>, dim3(grid), dim3(kRowThreads), RowCfg<D>::total, st, tk, tv, p);
-  paged_rows_kernel<T, D, BLOCK><<<grid, kRowThreads, RowCfg<D>::total, st>>>(tk, tv, p);
-  return cudaGetLastError();
+static cudaError_t launch_rows_t(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int grid, bool split,
+                                 cudaStream_t st) {
+  return split ? launch_rows_s<T, D, BLOCK, true>(p, tk, tv, grid, st) : launch_rows_s<T, D, BLOCK, false>(p, tk, tv, grid, st);
 }
 
 template <typename T, int D, bool BLOCK>
 static cudaError_t launch_merge_t(const PagedProblem& p, int units, int max_rows, cudaStream_t st) {
-  return launch_pdl(paged_rows_merge_kernel<T, D, BLOCK>, dim3(units, max_rows), dim3(D / 2), 0, st, p);
+  return launch_pdl(paged_rows_merge_kernel<T, D, BLOCK>, dim3(units, max_rows), dim3(kMergeThreads), 0, st, p);
 }
 
 #define TKPHI_BY_TYPE(call)                                                          \
@@ -546,8 +663,8 @@ static cudaError_t launch_merge_t(const PagedProblem& p, int units, int max_rows
                    : (block ? call(Fp16, 128, true) : call(Fp16, 128, false))))
 
 cudaError_t launch_paged_rows(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int d, bool bf16,
-                              bool block, int grid, bool dependent, cudaStream_t st) {
-#define ROWS(T, D, B) launch_rows_t<T, D, B>(p, tk, tv, grid, dependent, st)
+                              bool block, bool split, int grid, cudaStream_t st) {
+#define ROWS(T, D, B) launch_rows_t<T, D, B>(p, tk, tv, grid, split, st)
   return TKPHI_BY_TYPE(ROWS);
 #undef ROWS
 }

@@ -15,7 +15,7 @@
 namespace tkphi {
 
 constexpr int kScoreThreads = 256;
-constexpr int kScorePages = 128;           // pages of a scoring CTA: 8 warps x 4 steps x 4 pages (8 lanes each)
+constexpr int kScoreSteps = 4;             // page steps of a warp, all loads in flight at once
 
 template <typename T>
 __device__ __forceinline__ int dbl_hi_word(uint32_t w, bool upper) {       // scaled double of one half of w (low word 0)
@@ -39,81 +39,94 @@ __device__ __forceinline__ Candidates candidates_of(const PagedProblem& p, int t
   return c;
 }
 
+// Lanes of a page: 8 dims (16 bytes of each bound) per lane.  Pages of a CTA.
+template <int D>
+struct ScoreCfg {
+  static constexpr int LPP = D / 8;
+  static constexpr int PPS = 32 / LPP;                       // pages of a warp's step
+  static constexpr int PAGES = kScoreThreads / 32 * kScoreSteps * PPS;
+};
+
+// Bound: DRAM for single tokens, the 64-bit FMA rate (64 per clock and SM) for several query heads or tokens.  The
+// bounds of a page are converted once and serve all query heads of the group; per element and head a select by the
+// query's sign and one FMA remain.
 template <typename T, int D>
-__global__ void __launch_bounds__(kScoreThreads) paged_score_kernel(const __grid_constant__ PagedProblem p) {
-  constexpr int PIECES = D / 64;           // 16-byte pieces of a lane: piece sub + 8 i
-  __shared__ double s_q[kMaxGroup][D];
+__global__ void __launch_bounds__(kScoreThreads, 2) paged_score_kernel(const __grid_constant__ PagedProblem p) {
+  using C = ScoreCfg<D>;
+  __shared__ __align__(16) double s_q[kMaxGroup * D];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int unit = blockIdx.x, tok = unit / p.hkv, h = unit % p.hkv;
+  pdl_wait();
   pdl_launch_next();
+  const int unit = blockIdx.x, tok = unit / p.hkv, h = unit % p.hkv;
   const Candidates c = candidates_of(p, tok);
-  const int p0 = blockIdx.y * kScorePages;
+  const int p0 = blockIdx.y * C::PAGES;
   if (c.n <= p.topk || p0 >= c.n) return;              // all are taken, or none is left for this CTA
+  const int sub = lane % C::LPP;
+  const int j0 = p0 + warp * kScoreSteps * C::PPS + lane / C::LPP;
+  const int* table = p.table + (size_t)c.b * p.max_pages + c.first;
+  int phys[kScoreSteps];
+#pragma unroll
+  for (int s = 0; s < kScoreSteps; ++s) phys[s] = j0 + s * C::PPS < c.n ? __ldg(table + j0 + s * C::PPS) : 0;
   const double up = T::kBf16 ? __hiloint2double((1023 + 896) << 20, 0) : __hiloint2double((1023 + 1008) << 20, 0);
   const uint32_t* q = static_cast<const uint32_t*>(p.q) + ((size_t)tok * p.hq + h * p.group) * (D / 2);
   for (int i = tid; i < p.group * D / 2; i += kScoreThreads) {
     const uint32_t w = __ldg(q + i);
-    s_q[0][2 * i] = (double)T::lo(w) * up;
-    s_q[0][2 * i + 1] = (double)T::hi(w) * up;
+    s_q[2 * i] = (double)T::lo(w) * up;
+    s_q[2 * i + 1] = (double)T::hi(w) * up;
+  }
+  uint4 rl[kScoreSteps], rh[kScoreSteps];
+  bool ok[kScoreSteps];
+#pragma unroll
+  for (int s = 0; s < kScoreSteps; ++s) {
+    ok[s] = phys[s] >= 0 && phys[s] < p.n_pages;
+    if (!ok[s] && sub == 0) atomicExch(p.status, kStatusBadPage);
+    const uint4* src = static_cast<const uint4*>(p.bounds) + ((size_t)(ok[s] ? phys[s] : 0) * p.hkv + h) * (2 * D / 8) + sub;
+    rl[s] = __ldg(src);
+    rh[s] = __ldg(src + D / 8);
   }
   __syncthreads();
-  const int sub = lane & 7;
-  const uint4* bounds = static_cast<const uint4*>(p.bounds);
-  unsigned long long* keys = p.page_keys + (size_t)unit * p.key_stride;
-  uint4 lo[4][PIECES], hi[4][PIECES];
-  bool ok[4];
+  // high words of the scaled doubles (their low words are 0)
+  int lo[kScoreSteps][8], hi[kScoreSteps][8];
 #pragma unroll
-  for (int s = 0; s < 4; ++s) {
-    const int j = p0 + warp * 16 + s * 4 + (lane >> 3);
-    ok[s] = false;
-    if (j < c.n) {
-      const int phys = __ldg(p.table + (size_t)c.b * p.max_pages + c.first + j);
-      ok[s] = phys >= 0 && phys < p.n_pages;
-      if (!ok[s]) atomicExch(p.status, kStatusBadPage);
-      const uint4* src = bounds + ((size_t)(ok[s] ? phys : 0) * p.hkv + h) * (2 * D / 8) + sub;
+  for (int s = 0; s < kScoreSteps; ++s)
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) { lo[s][i] = __ldg(src + 8 * i); hi[s][i] = __ldg(src + D / 8 + 8 * i); }
-    } else {
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) lo[s][i] = hi[s][i] = make_uint4(0, 0, 0, 0);
+    for (int e = 0; e < 8; ++e) {
+      lo[s][e] = dbl_hi_word<T>(reinterpret_cast<const uint32_t*>(&rl[s])[e >> 1], e & 1);
+      hi[s][e] = dbl_hi_word<T>(reinterpret_cast<const uint32_t*>(&rh[s])[e >> 1], e & 1);
+      asm("" : "+r"(lo[s][e]), "+r"(hi[s][e]));           // kept, not converted again for every head
     }
-  }
-  double best[4];
-#pragma unroll
-  for (int s = 0; s < 4; ++s) best[s] = -INFINITY;
+  double best = -INFINITY;                   // of the page step that this lane ends up with
   for (int g = 0; g < p.group; ++g) {
-    double acc[4] = {0., 0., 0., 0.};
+    double acc[kScoreSteps] = {0., 0., 0., 0.};
+    const double2* qs = reinterpret_cast<const double2*>(s_q + g * D + sub * 8);
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const double2* qs = reinterpret_cast<const double2*>(&s_q[g][(sub + 8 * i) * 8]);
+    for (int e = 0; e < 4; ++e) {
+      const double2 qq = qs[e];
+      const bool n0 = __double2hiint(qq.x) < 0, n1 = __double2hiint(qq.y) < 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const double2 qq = qs[e];
-        const bool n0 = __double2hiint(qq.x) < 0, n1 = __double2hiint(qq.y) < 0;
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          const uint32_t wl = reinterpret_cast<const uint32_t*>(&lo[s][i])[e], wh = reinterpret_cast<const uint32_t*>(&hi[s][i])[e];
-          acc[s] = fma(qq.x, __hiloint2double(dbl_hi_word<T>(n0 ? wl : wh, false), 0), acc[s]);
-          acc[s] = fma(qq.y, __hiloint2double(dbl_hi_word<T>(n1 ? wl : wh, true), 0), acc[s]);
-        }
+      for (int s = 0; s < kScoreSteps; ++s) {
+        acc[s] = fma(qq.x, __hiloint2double(n0 ? lo[s][2 * e] : hi[s][2 * e], 0), acc[s]);
+        acc[s] = fma(qq.y, __hiloint2double(n1 ? lo[s][2 * e + 1] : hi[s][2 * e + 1], 0), acc[s]);
       }
     }
+    // four sums over the page's lanes: two are handed over, then one, so that a lane ends up with one of them
+    const bool b0 = lane & 1, b1 = lane & 2;
+    double u = b0 ? acc[2] : acc[0], v = b0 ? acc[3] : acc[1];
+    u += __shfl_xor_sync(0xffffffffu, b0 ? acc[0] : acc[2], 1);
+    v += __shfl_xor_sync(0xffffffffu, b0 ? acc[1] : acc[3], 1);
+    double w = b1 ? v : u;
+    w += __shfl_xor_sync(0xffffffffu, b1 ? u : v, 2);
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-#pragma unroll
-      for (int o = 1; o < 8; o <<= 1) acc[s] += __shfl_xor_sync(0xffffffffu, acc[s], o);
-      best[s] = fmax(best[s], acc[s]);
-    }
+    for (int o = 4; o < C::LPP; o <<= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
+    best = fmax(best, w);
   }
-  if (sub == 0) {
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const int j = p0 + warp * 16 + s * 4 + (lane >> 3);
-      if (j < c.n) {
-        // larger bound <=> larger key; -0 counts as 0
-        const unsigned long long u = (unsigned long long)__double_as_longlong(best[s] + 0.0);
-        keys[j] = !ok[s] ? 0ull : (u >> 63) ? ~u : (u | (1ull << 63));
-      }
+  if (sub < 4) {
+    const int s = (lane & 1) * 2 + ((lane >> 1) & 1), j = j0 + s * C::PPS;
+    const bool fine = s == 0 ? ok[0] : s == 1 ? ok[1] : s == 2 ? ok[2] : ok[3];
+    if (j < c.n) {
+      // larger bound <=> larger key; -0 counts as 0
+      const unsigned long long x = (unsigned long long)__double_as_longlong(best + 0.0);
+      p.page_keys[(size_t)unit * p.key_stride + j] = !fine ? 0ull : (x >> 63) ? ~x : (x | (1ull << 63));
     }
   }
 }
@@ -121,18 +134,21 @@ __global__ void __launch_bounds__(kScoreThreads) paged_score_kernel(const __grid
 __device__ __forceinline__ unsigned long long shr64(unsigned long long x, int s) { return s >= 64 ? 0ull : x >> s; }
 
 constexpr int kPageBins = 2048;
-constexpr int kHeldKeys = 8;               // keys a thread keeps in registers; with more it reads them again
 
-// Exact topk of n keys, one CTA per unit; thread t owns a contiguous run of keys, so that thread order is page order.
-template <int NT>
+// Exact topk of the unit's keys, one CTA per unit.  Thread t holds keys t, t + NT, ..: KPT of them in registers, any
+// further ones are read again in each pass.
+template <int NT, int KPT>
 __global__ void __launch_bounds__(NT) paged_select_kernel(const __grid_constant__ PagedProblem p) {
+  constexpr int NW = NT / 32;
   __shared__ int s_hist[kPageBins];
-  __shared__ unsigned long long s_min[NT / 32], s_max[NT / 32];
-  __shared__ int s_sum[NT / 32], s_sum2[NT / 32];
+  __shared__ unsigned long long s_min[NW], s_max[NW];
+  __shared__ int s_sum[NW];
   __shared__ int s_bin, s_need, s_count;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int unit = blockIdx.x, tok = unit / p.hkv;
   pdl_launch_next();
+  for (int i = tid; i < kPageBins; i += NT) s_hist[i] = 0;
+  pdl_wait();
   const Candidates c = candidates_of(p, tok);
   int* list = p.page_list + (size_t)unit * p.n_keep;
   int* out = p.page_out ? p.page_out + (size_t)unit * p.n_keep : nullptr;
@@ -140,36 +156,30 @@ __global__ void __launch_bounds__(NT) paged_select_kernel(const __grid_constant_
   const int taken = c.n < p.topk ? c.n : p.topk;        // of the candidates
   const int last0 = c.first + c.n;                      // first page of the tail
   const int n_list = c.first + taken + (c.seen - last0);
-  pdl_wait();
+  const bool search = c.n > p.topk && p.topk > 0;
+  const unsigned long long* keys = p.page_keys + (size_t)unit * p.key_stride;
+  unsigned long long held[KPT];
+  if (search) {
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) held[i] = i * NT + tid < c.n ? __ldcg(keys + i * NT + tid) : 0ull;
+  }
   // the pages that are always taken, and the padding
   for (int i = tid; i < p.n_keep; i += NT) {
-    const int page = i < c.first ? i : i < c.first + taken ? -2 : i < n_list ? last0 + (i - c.first - taken) : -1;
+    const int page = i < c.first ? i : i < c.first + taken ? (search ? -2 : i) : i < n_list ? last0 + (i - c.first - taken) : -1;
     if (page != -2) {
       list[i] = page < 0 ? -1 : __ldg(table + page);
       if (out) out[i] = page;
     }
   }
-  if (c.n <= p.topk) {
-    for (int i = tid; i < c.n; i += NT) {
-      list[c.first + i] = __ldg(table + c.first + i);
-      if (out) out[c.first + i] = c.first + i;
-    }
-    return;
-  }
-  if (p.topk == 0) return;
-  const unsigned long long* keys = p.page_keys + (size_t)unit * p.key_stride;
-  const int per = (c.n + NT - 1) / NT, i0 = tid * per < c.n ? tid * per : c.n, i1 = i0 + per < c.n ? i0 + per : c.n;
-  unsigned long long held[kHeldKeys];
-#pragma unroll
-  for (int i = 0; i < kHeldKeys; ++i) held[i] = i0 + i < i1 ? __ldcg(keys + i0 + i) : 0ull;
+  if (!search) return;
   auto each = [&](auto&& fn) {
 #pragma unroll
-    for (int i = 0; i < kHeldKeys; ++i)
-      if (i0 + i < i1) fn(i0 + i, held[i]);
-    for (int i = i0 + kHeldKeys; i < i1; ++i) fn(i, __ldcg(keys + i));
+    for (int i = 0; i < KPT; ++i)
+      if (i * NT + tid < c.n) fn(held[i]);
+    for (int i = KPT * NT + tid; i < c.n; i += NT) fn(__ldcg(keys + i));
   };
   unsigned long long mn = ~0ull, mx = 0ull;
-  each([&](int, unsigned long long k) { mn = k < mn ? k : mn; mx = k > mx ? k : mx; });
+  each([&](unsigned long long k) { mn = k < mn ? k : mn; mx = k > mx ? k : mx; });
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     const unsigned long long a = __shfl_xor_sync(0xffffffffu, mn, o), b = __shfl_xor_sync(0xffffffffu, mx, o);
@@ -179,16 +189,21 @@ __global__ void __launch_bounds__(NT) paged_select_kernel(const __grid_constant_
   if (lane == 0) { s_min[warp] = mn; s_max[warp] = mx; }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < NT / 32; ++i) { mn = s_min[i] < mn ? s_min[i] : mn; mx = s_max[i] > mx ? s_max[i] : mx; }
-  // the keys share all bits above `top`; of those that share `prefix` above it, `need` are still to be taken
+  for (int i = 0; i < NW; ++i) { mn = s_min[i] < mn ? s_min[i] : mn; mx = s_max[i] > mx ? s_max[i] : mx; }
+  // The keys share all bits above `top`; of those that share `prefix` above it, `need` are still to be taken.  A pass
+  // counts them by their next 11 bits.
   int top = mn == mx ? 0 : 64 - __clzll((long long)(mn ^ mx));
   unsigned long long prefix = shr64(mx, top);
   int need = p.topk, count = c.n;
+  bool clean = true;
   while (top > 0 && count > need) {
     const int width = top < 11 ? top : 11, shift = top - width, bins = 1 << width;
-    for (int i = tid; i < bins; i += NT) s_hist[i] = 0;
-    __syncthreads();
-    each([&](int, unsigned long long k) {
+    if (!clean) {
+      for (int i = tid; i < bins; i += NT) s_hist[i] = 0;
+      __syncthreads();
+    }
+    clean = false;
+    each([&](unsigned long long k) {
       if (shr64(k, top) == prefix) atomicAdd(&s_hist[(int)(k >> shift) & (bins - 1)], 1);
     });
     __syncthreads();
@@ -203,7 +218,12 @@ __global__ void __launch_bounds__(NT) paged_select_kernel(const __grid_constant_
     if (lane == 31) s_sum[warp] = incl;
     __syncthreads();
     int before = incl - mine;
-    for (int i = 0; i < warp; ++i) before += s_sum[i];
+    if (NW <= 8) {
+#pragma unroll
+      for (int i = 0; i < NW; ++i) before += i < warp ? s_sum[i] : 0;
+    } else {
+      before += __reduce_add_sync(0xffffffffu, lane < warp ? s_sum[lane] : 0);
+    }
     if (before < need && before + mine >= need) {
       for (int i = 0; i < run; ++i) {
         const int bin = bins - 1 - (tid * run + i), n = s_hist[bin];
@@ -216,52 +236,54 @@ __global__ void __launch_bounds__(NT) paged_select_kernel(const __grid_constant_
     count = s_count;
     prefix = (prefix << width) | (unsigned long long)s_bin;
     top = shift;
-    __syncthreads();
   }
-  // larger than the prefix: taken; equal: the first `need` in page order
-  int sure = 0, tie = 0;
-  each([&](int, unsigned long long k) {
+  // Keys above the prefix are taken, of those equal to it the first `need` in page order.  32 consecutive pages are one
+  // ballot of a warp; (taken, equal) counts of a row of NT pages, 16 bits each, are added up over the warps.
+  int sure0 = 0, tie0 = 0;                              // before this row
+  for (int r = 0; r * NT < c.n; ++r) {
+    const int j = r * NT + tid;
+    unsigned long long k = 0ull;
+    if (r < KPT) {
+#pragma unroll
+      for (int i = 0; i < KPT; ++i)
+        if (i == r) k = held[i];
+    } else if (j < c.n) {
+      k = __ldcg(keys + j);
+    }
     const unsigned long long x = shr64(k, top);
-    sure += x > prefix;
-    tie += x == prefix;
-  });
-  const int isure = warp_inclusive_scan(sure), itie = warp_inclusive_scan(tie);
-  if (lane == 31) { s_sum[warp] = isure; s_sum2[warp] = itie; }
-  __syncthreads();
-  int nsure = isure - sure, ntie = itie - tie;
-  for (int i = 0; i < warp; ++i) { nsure += s_sum[i]; ntie += s_sum2[i]; }
-  each([&](int j, unsigned long long k) {
-    const unsigned long long x = shr64(k, top);
-    const bool take = x > prefix || (x == prefix && ntie < need);
-    if (take) {
+    const bool sure = j < c.n && x > prefix, tie = j < c.n && x == prefix;
+    const unsigned ms = __ballot_sync(0xffffffffu, sure), mt = __ballot_sync(0xffffffffu, tie);
+    __syncthreads();
+    if (lane == 0) s_sum[warp] = __popc(ms) | (__popc(mt) << 16);
+    __syncthreads();
+    const int w = lane < NW ? s_sum[lane] : 0;
+    const int before = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0), all = __reduce_add_sync(0xffffffffu, w);
+    const unsigned below = (1u << lane) - 1;
+    const int nsure = sure0 + (before & 0xffff) + __popc(ms & below), ntie = tie0 + (before >> 16) + __popc(mt & below);
+    if (sure || (tie && ntie < need)) {
       const int at = c.first + nsure + (ntie < need ? ntie : need);
       list[at] = __ldg(table + c.first + j);
       if (out) out[at] = c.first + j;
     }
-    nsure += x > prefix;
-    ntie += x == prefix;
-  });
+    sure0 += all & 0xffff;
+    tie0 += all >> 16;
+  }
 }
 
 cudaError_t launch_paged_select(const PagedProblem& p, int d, bool bf16, int max_pages_seq, cudaStream_t st) {
   const int units = p.total_q * p.hkv;
   const int n = max_pages_seq - p.n_sink - p.n_tail;      // most candidates of a token
   if (n > p.topk && p.topk > 0) {
-    const dim3 grid(units, (n + kScorePages - 1) / kScorePages);
-    if (d == 64) {
-      if (bf16) paged_score_kernel<Bf16, 64><<<grid, kScoreThreads, 0, st>>>(p);
-      else paged_score_kernel<Fp16, 64><<<grid, kScoreThreads, 0, st>>>(p);
-    } else {
-      if (bf16) paged_score_kernel<Bf16, 128><<<grid, kScoreThreads, 0, st>>>(p);
-      else paged_score_kernel<Fp16, 128><<<grid, kScoreThreads, 0, st>>>(p);
-    }
-    const cudaError_t e = cudaGetLastError();
+    const int pages = d == 64 ? ScoreCfg<64>::PAGES : ScoreCfg<128>::PAGES;
+    const dim3 grid(units, (n + pages - 1) / pages), block(kScoreThreads);
+    cudaError_t e;
+    if (d == 64) e = bf16 ? launch_pdl(paged_score_kernel<Bf16, 64>, grid, block, 0, st, p) : launch_pdl(paged_score_kernel<Fp16, 64>, grid, block, 0, st, p);
+    else e = bf16 ? launch_pdl(paged_score_kernel<Bf16, 128>, grid, block, 0, st, p) : launch_pdl(paged_score_kernel<Fp16, 128>, grid, block, 0, st, p);
     if (e != cudaSuccess) return e;
-    if (n <= 256 * kHeldKeys) return launch_pdl(paged_select_kernel<256>, dim3(units), dim3(256), 0, st, p);
-    return launch_pdl(paged_select_kernel<1024>, dim3(units), dim3(1024), 0, st, p);
   }
-  paged_select_kernel<256><<<units, 256, 0, st>>>(p);
-  return cudaGetLastError();
+  if (n <= 1024) return launch_pdl(paged_select_kernel<256, 4>, dim3(units), dim3(256), 0, st, p);
+  if (n <= 4096) return launch_pdl(paged_select_kernel<512, 8>, dim3(units), dim3(512), 0, st, p);
+  return launch_pdl(paged_select_kernel<1024, 16>, dim3(units), dim3(1024), 0, st, p);
 }
 
 }  // namespace tkphi

@@ -678,8 +678,7 @@ static cudaError_t launch_tiles_t(const PagedProblem& p, const CUtensorMap& tk, 
   static PerDeviceFlag configured;
   const cudaError_t e = set_max_dynamic_smem(configured, reinterpret_cast<const void*>(paged_tiles_kernel<T, D>), TileCfg<D>::total);
   if (e != cudaSuccess) return e;
-  paged_tiles_kernel<T, D><<<grid, kTileThreads, TileCfg<D>::total, st>>>(tk, tv, p);
-  return cudaGetLastError();
+  return launch_pdl(paged_tiles_kernel<T, D>, dim3(grid), dim3(kTileThreads), TileCfg<D>::total, st, tk, tv, p);
 }
 
 cudaError_t launch_paged_tiles(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int d, bool bf16, int grid,
