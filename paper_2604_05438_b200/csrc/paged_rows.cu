@@ -190,12 +190,15 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     *s_abort = 0;
   }
   __syncthreads();
-  if (!p.beside) pdl_wait();
+  // Inputs of the call may be read once all work before the call is complete.  The block form follows the selection,
+  // whose first grid has waited for that: only the page lists remain to be waited for, by the producer.
+  if (!BLOCK && !p.beside) pdl_wait();
   pdl_launch_next();
 
   if (warp == kRowWarps) {
     // ================================================================ TMA producer
     RowWalk<BLOCK, SPLIT> w(p, cta);
+    if (BLOCK) pdl_wait();
     const int ps = 1 << p.page_shift;
     const int npg = ps < kRowKeys ? kRowKeys >> p.page_shift : 1;             // pages of a tile
     const int box_rows = ps < kRowKeys ? ps : kRowKeys;

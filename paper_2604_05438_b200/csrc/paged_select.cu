@@ -53,80 +53,98 @@ struct ScoreCfg {
 template <typename T, int D>
 __global__ void __launch_bounds__(kScoreThreads, 2) paged_score_kernel(const __grid_constant__ PagedProblem p) {
   using C = ScoreCfg<D>;
-  __shared__ __align__(16) double s_q[kMaxGroup * D];
+  __shared__ double2 s_q[kMaxGroup * D / 2];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait();
   pdl_launch_next();
   const int unit = blockIdx.x, tok = unit / p.hkv, h = unit % p.hkv;
   const Candidates c = candidates_of(p, tok);
-  const int p0 = blockIdx.y * C::PAGES;
-  if (c.n <= p.topk || p0 >= c.n) return;              // all are taken, or none is left for this CTA
-  const int sub = lane % C::LPP;
-  const int j0 = p0 + warp * kScoreSteps * C::PPS + lane / C::LPP;
+  if (c.n <= p.topk || (int)blockIdx.y * C::PAGES >= c.n) return;      // all are taken, or none is left for this CTA
+  const int sub = lane % C::LPP, stride = gridDim.y * C::PAGES;
   const int* table = p.table + (size_t)c.b * p.max_pages + c.first;
-  int phys[kScoreSteps];
+  const uint4* bounds = static_cast<const uint4*>(p.bounds) + (size_t)h * (2 * D / 8) + sub;
+  const size_t page_step = (size_t)p.hkv * (2 * D / 8);
+  int j0 = blockIdx.y * C::PAGES + warp * kScoreSteps * C::PPS + lane / C::LPP;        // this lane's page of step 0
+  // a round's bounds are loaded while the round before is computed, its page ids one round earlier still
+  int ids[kScoreSteps];
+  uint4 rl[kScoreSteps], rh[kScoreSteps];
+  unsigned fine = 0;                                       // steps of the loaded round with a valid page id
+  auto load_ids = [&](int j) {
 #pragma unroll
-  for (int s = 0; s < kScoreSteps; ++s) phys[s] = j0 + s * C::PPS < c.n ? __ldg(table + j0 + s * C::PPS) : 0;
+    for (int s = 0; s < kScoreSteps; ++s) ids[s] = j + s * C::PPS < c.n ? __ldg(table + j + s * C::PPS) : 0;
+  };
+  auto load_bounds = [&]() {
+    fine = 0;
+#pragma unroll
+    for (int s = 0; s < kScoreSteps; ++s) {
+      const bool ok = ids[s] >= 0 && ids[s] < p.n_pages;
+      if (!ok && sub == 0) atomicExch(p.status, kStatusBadPage);
+      fine |= (ok ? 1u : 0u) << s;
+      const uint4* src = bounds + (ok ? ids[s] : 0) * page_step;
+      rl[s] = __ldg(src);
+      rh[s] = __ldg(src + D / 8);
+    }
+  };
+  load_ids(j0);
   const double up = T::kBf16 ? __hiloint2double((1023 + 896) << 20, 0) : __hiloint2double((1023 + 1008) << 20, 0);
   const uint32_t* q = static_cast<const uint32_t*>(p.q) + ((size_t)tok * p.hq + h * p.group) * (D / 2);
   for (int i = tid; i < p.group * D / 2; i += kScoreThreads) {
     const uint32_t w = __ldg(q + i);
-    s_q[2 * i] = (double)T::lo(w) * up;
-    s_q[2 * i + 1] = (double)T::hi(w) * up;
+    // pair i of a head is read by lane (i / 4) of the page in its step i % 4: lanes beside each other, no bank twice
+    const int g = i / (D / 2), x = i % (D / 2);
+    s_q[(g * 4 + x % 4) * C::LPP + x / 4] = make_double2((double)T::lo(w) * up, (double)T::hi(w) * up);
   }
-  uint4 rl[kScoreSteps], rh[kScoreSteps];
-  bool ok[kScoreSteps];
-#pragma unroll
-  for (int s = 0; s < kScoreSteps; ++s) {
-    ok[s] = phys[s] >= 0 && phys[s] < p.n_pages;
-    if (!ok[s] && sub == 0) atomicExch(p.status, kStatusBadPage);
-    const uint4* src = static_cast<const uint4*>(p.bounds) + ((size_t)(ok[s] ? phys[s] : 0) * p.hkv + h) * (2 * D / 8) + sub;
-    rl[s] = __ldg(src);
-    rh[s] = __ldg(src + D / 8);
-  }
+  load_bounds();
+  load_ids(j0 + stride);
   __syncthreads();
-  // high words of the scaled doubles (their low words are 0)
-  int lo[kScoreSteps][8], hi[kScoreSteps][8];
+  for (int r0 = blockIdx.y * C::PAGES; r0 < c.n; r0 += stride, j0 += stride) {
+    // high words of the scaled doubles (their low words are 0)
+    int lo[kScoreSteps][8], hi[kScoreSteps][8];
 #pragma unroll
-  for (int s = 0; s < kScoreSteps; ++s)
+    for (int s = 0; s < kScoreSteps; ++s)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      lo[s][e] = dbl_hi_word<T>(reinterpret_cast<const uint32_t*>(&rl[s])[e >> 1], e & 1);
-      hi[s][e] = dbl_hi_word<T>(reinterpret_cast<const uint32_t*>(&rh[s])[e >> 1], e & 1);
-      asm("" : "+r"(lo[s][e]), "+r"(hi[s][e]));           // kept, not converted again for every head
-    }
-  double best = -INFINITY;                   // of the page step that this lane ends up with
-  for (int g = 0; g < p.group; ++g) {
-    double acc[kScoreSteps] = {0., 0., 0., 0.};
-    const double2* qs = reinterpret_cast<const double2*>(s_q + g * D + sub * 8);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const double2 qq = qs[e];
-      const bool n0 = __double2hiint(qq.x) < 0, n1 = __double2hiint(qq.y) < 0;
-#pragma unroll
-      for (int s = 0; s < kScoreSteps; ++s) {
-        acc[s] = fma(qq.x, __hiloint2double(n0 ? lo[s][2 * e] : hi[s][2 * e], 0), acc[s]);
-        acc[s] = fma(qq.y, __hiloint2double(n1 ? lo[s][2 * e + 1] : hi[s][2 * e + 1], 0), acc[s]);
+      for (int e = 0; e < 8; ++e) {
+        lo[s][e] = dbl_hi_word<T>(reinterpret_cast<const uint32_t*>(&rl[s])[e >> 1], e & 1);
+        hi[s][e] = dbl_hi_word<T>(reinterpret_cast<const uint32_t*>(&rh[s])[e >> 1], e & 1);
+        asm("" : "+r"(lo[s][e]), "+r"(hi[s][e]));          // kept, not converted again for every head
       }
+    const unsigned fine_now = fine;
+    if (r0 + stride < c.n) {
+      load_bounds();
+      load_ids(j0 + 2 * stride);
     }
-    // four sums over the page's lanes: two are handed over, then one, so that a lane ends up with one of them
-    const bool b0 = lane & 1, b1 = lane & 2;
-    double u = b0 ? acc[2] : acc[0], v = b0 ? acc[3] : acc[1];
-    u += __shfl_xor_sync(0xffffffffu, b0 ? acc[0] : acc[2], 1);
-    v += __shfl_xor_sync(0xffffffffu, b0 ? acc[1] : acc[3], 1);
-    double w = b1 ? v : u;
-    w += __shfl_xor_sync(0xffffffffu, b1 ? u : v, 2);
+    double best = -INFINITY;                   // of the page step that this lane ends up with
+    for (int g = 0; g < p.group; ++g) {
+      double acc[kScoreSteps] = {0., 0., 0., 0.};
+      const double2* qs = s_q + g * 4 * C::LPP + sub;
 #pragma unroll
-    for (int o = 4; o < C::LPP; o <<= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
-    best = fmax(best, w);
-  }
-  if (sub < 4) {
-    const int s = (lane & 1) * 2 + ((lane >> 1) & 1), j = j0 + s * C::PPS;
-    const bool fine = s == 0 ? ok[0] : s == 1 ? ok[1] : s == 2 ? ok[2] : ok[3];
-    if (j < c.n) {
-      // larger bound <=> larger key; -0 counts as 0
-      const unsigned long long x = (unsigned long long)__double_as_longlong(best + 0.0);
-      p.page_keys[(size_t)unit * p.key_stride + j] = !fine ? 0ull : (x >> 63) ? ~x : (x | (1ull << 63));
+      for (int e = 0; e < 4; ++e) {
+        const double2 qq = qs[e * C::LPP];
+        const bool n0 = __double2hiint(qq.x) < 0, n1 = __double2hiint(qq.y) < 0;
+#pragma unroll
+        for (int s = 0; s < kScoreSteps; ++s) {
+          acc[s] = fma(qq.x, __hiloint2double(n0 ? lo[s][2 * e] : hi[s][2 * e], 0), acc[s]);
+          acc[s] = fma(qq.y, __hiloint2double(n1 ? lo[s][2 * e + 1] : hi[s][2 * e + 1], 0), acc[s]);
+        }
+      }
+      // four sums over the page's lanes: two are handed over, then one, so that a lane ends up with one of them
+      const bool b0 = lane & 1, b1 = lane & 2;
+      double u = b0 ? acc[2] : acc[0], v = b0 ? acc[3] : acc[1];
+      u += __shfl_xor_sync(0xffffffffu, b0 ? acc[0] : acc[2], 1);
+      v += __shfl_xor_sync(0xffffffffu, b0 ? acc[1] : acc[3], 1);
+      double w = b1 ? v : u;
+      w += __shfl_xor_sync(0xffffffffu, b1 ? u : v, 2);
+#pragma unroll
+      for (int o = 4; o < C::LPP; o <<= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
+      best = fmax(best, w);
+    }
+    if (sub < 4) {
+      const int s = (lane & 1) * 2 + ((lane >> 1) & 1), j = j0 + s * C::PPS;
+      if (j < c.n) {
+        // larger bound <=> larger key; -0 counts as 0
+        const unsigned long long x = (unsigned long long)__double_as_longlong(best + 0.0);
+        p.page_keys[(size_t)unit * p.key_stride + j] = !(fine_now >> s & 1u) ? 0ull : (x >> 63) ? ~x : (x | (1ull << 63));
+      }
     }
   }
 }
@@ -142,14 +160,16 @@ __global__ void __launch_bounds__(NT) paged_select_kernel(const __grid_constant_
   constexpr int NW = NT / 32;
   __shared__ int s_hist[kPageBins];
   __shared__ unsigned long long s_min[NW], s_max[NW];
-  __shared__ int s_sum[NW];
+  __shared__ int s_sum[NW], s_cnt[KPT * NW];
   __shared__ int s_bin, s_need, s_count;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int unit = blockIdx.x, tok = unit / p.hkv;
   pdl_launch_next();
   for (int i = tid; i < kPageBins; i += NT) s_hist[i] = 0;
-  pdl_wait();
+  // (the call's inputs may be read before the wait: this grid starts when the scoring grid has begun, which had waited
+  // for everything before it)
   const Candidates c = candidates_of(p, tok);
+  pdl_wait();
   int* list = p.page_list + (size_t)unit * p.n_keep;
   int* out = p.page_out ? p.page_out + (size_t)unit * p.n_keep : nullptr;
   const int* table = p.table + (size_t)c.b * p.max_pages;
@@ -238,35 +258,42 @@ __global__ void __launch_bounds__(NT) paged_select_kernel(const __grid_constant_
     top = shift;
   }
   // Keys above the prefix are taken, of those equal to it the first `need` in page order.  32 consecutive pages are one
-  // ballot of a warp; (taken, equal) counts of a row of NT pages, 16 bits each, are added up over the warps.
-  int sure0 = 0, tie0 = 0;                              // before this row
-  for (int r = 0; r * NT < c.n; ++r) {
-    const int j = r * NT + tid;
-    unsigned long long k = 0ull;
-    if (r < KPT) {
+  // ballot of a warp; (taken, equal) counts of the ballots, 16 bits each, are scanned in page order.  KPT * NT pages at
+  // a time (at most 16384, so that no count overflows).
+  static_assert(KPT * NW <= NT && KPT * NT <= 16384, "one count per thread");
+  int sure0 = 0, tie0 = 0;                              // of the pages before
+  for (int base = 0; base < c.n; base += KPT * NT) {
+    unsigned ms[KPT], mt[KPT];
 #pragma unroll
-      for (int i = 0; i < KPT; ++i)
-        if (i == r) k = held[i];
-    } else if (j < c.n) {
-      k = __ldcg(keys + j);
+    for (int i = 0; i < KPT; ++i) {
+      const int j = base + i * NT + tid;
+      const unsigned long long x = shr64(base == 0 ? held[i] : j < c.n ? __ldcg(keys + j) : 0ull, top);
+      ms[i] = __ballot_sync(0xffffffffu, j < c.n && x > prefix);
+      mt[i] = __ballot_sync(0xffffffffu, j < c.n && x == prefix);
+      if (lane == 0) s_cnt[i * NW + warp] = __popc(ms[i]) | (__popc(mt[i]) << 16);
     }
-    const unsigned long long x = shr64(k, top);
-    const bool sure = j < c.n && x > prefix, tie = j < c.n && x == prefix;
-    const unsigned ms = __ballot_sync(0xffffffffu, sure), mt = __ballot_sync(0xffffffffu, tie);
     __syncthreads();
-    if (lane == 0) s_sum[warp] = __popc(ms) | (__popc(mt) << 16);
+    const int mine = tid < KPT * NW ? s_cnt[tid] : 0, incl = warp_inclusive_scan(mine);
+    if (lane == 31) s_sum[warp] = incl;
     __syncthreads();
-    const int w = lane < NW ? s_sum[lane] : 0;
-    const int before = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0), all = __reduce_add_sync(0xffffffffu, w);
+    const int sums = lane < NW ? s_sum[lane] : 0;
+    const int before = __reduce_add_sync(0xffffffffu, lane < warp ? sums : 0), all = __reduce_add_sync(0xffffffffu, sums);
+    if (tid < KPT * NW) s_cnt[tid] = before + incl - mine;
+    __syncthreads();
     const unsigned below = (1u << lane) - 1;
-    const int nsure = sure0 + (before & 0xffff) + __popc(ms & below), ntie = tie0 + (before >> 16) + __popc(mt & below);
-    if (sure || (tie && ntie < need)) {
-      const int at = c.first + nsure + (ntie < need ? ntie : need);
-      list[at] = __ldg(table + c.first + j);
-      if (out) out[at] = c.first + j;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+      const int at0 = s_cnt[i * NW + warp];
+      const int nsure = sure0 + (at0 & 0xffff) + __popc(ms[i] & below), ntie = tie0 + (at0 >> 16) + __popc(mt[i] & below);
+      if ((ms[i] >> lane & 1u) || ((mt[i] >> lane & 1u) && ntie < need)) {
+        const int at = c.first + nsure + (ntie < need ? ntie : need), page = c.first + base + i * NT + tid;
+        list[at] = __ldg(table + page);
+        if (out) out[at] = page;
+      }
     }
     sure0 += all & 0xffff;
     tie0 += all >> 16;
+    __syncthreads();
   }
 }
 
@@ -275,7 +302,9 @@ cudaError_t launch_paged_select(const PagedProblem& p, int d, bool bf16, int max
   const int n = max_pages_seq - p.n_sink - p.n_tail;      // most candidates of a token
   if (n > p.topk && p.topk > 0) {
     const int pages = d == 64 ? ScoreCfg<64>::PAGES : ScoreCfg<128>::PAGES;
-    const dim3 grid(units, (n + pages - 1) / pages), block(kScoreThreads);
+    // a unit's pages over enough CTAs for two per multiprocessor twice over, and no more: each converts the queries anew
+    const int want = (4 * sm_count_current_device() + units - 1) / units, most = (n + pages - 1) / pages;
+    const dim3 grid(units, want < most ? want : most), block(kScoreThreads);
     cudaError_t e;
     if (d == 64) e = bf16 ? launch_pdl(paged_score_kernel<Bf16, 64>, grid, block, 0, st, p) : launch_pdl(paged_score_kernel<Fp16, 64>, grid, block, 0, st, p);
     else e = bf16 ? launch_pdl(paged_score_kernel<Bf16, 128>, grid, block, 0, st, p) : launch_pdl(paged_score_kernel<Fp16, 128>, grid, block, 0, st, p);
