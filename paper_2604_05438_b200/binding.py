@@ -1,4 +1,5 @@
-"""ctypes binding of libtkphi.so: same names as the C entry points, marshalling only."""
+"""Binding of libtkphi.so: same names as the C entry points, marshalling only (ctypes; the paged calls, whose GPU time can
+be a few microseconds, through a CPython module)."""
 from __future__ import annotations
 
 import ctypes as C
@@ -245,6 +246,23 @@ class MlpMaps:
         return _MlpDesc(self.w_1.shape[1], self.w_s.shape[0], *[t.data_ptr() for t in ts])
 
 
+_native_module = None
+
+
+def _native():
+    """The CPython module of the paged calls (built in-tree beside libtkphi.so); raises if absent."""
+    global _native_module
+    if _native_module is None:
+        load_library()
+        try:
+            from . import _paged_binding
+        except ImportError as e:
+            raise RuntimeError("_paged_binding.so is missing or does not load: build it with "
+                               "`python -m paper_2604_05438_b200.build`") from e
+        _native_module = _paged_binding
+    return _native_module
+
+
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1}
 
 
@@ -282,17 +300,12 @@ class PagedKVCache:
         for t in (v, page_table, key_bounds, self.kv_lens_dev, self.cu_q_dev, self.status):
             assert t is None or t.device == dev, "the cache, its page table and its lengths must be on one device"
         self.total_q = int(self.cu_q[-1])
-        self._index = -1 if dev.type != "cuda" else torch.cuda.current_device() if dev.index is None else dev.index
-        self._q_shape = (self.total_q, n_q_heads, k.shape[3])
-        self._kv_shape = (self.total_q, k.shape[1], k.shape[3])
-        self._lse_shape = (self.total_q, n_q_heads)
-        self._dtype = k.dtype
         self._desc = _PagedDesc(len(self.kv_lens), n_q_heads, k.shape[1], k.shape[3], _DTYPES[k.dtype], k.shape[2],
                                 k.shape[0], page_table.shape[1], k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
                                 k.stride(2), page_table.data_ptr(), self.kv_lens.ctypes.data, self.kv_lens_dev.data_ptr(),
                                 self.cu_q.ctypes.data, self.cu_q_dev.data_ptr(),
                                 None if key_bounds is None else key_bounds.data_ptr(), self.status.data_ptr())
-        self._ref = C.byref(self._desc)
+        self._handle = _native().handle(C.addressof(self._desc), k.get_device())
 
     @property
     def batch(self) -> int:
@@ -304,24 +317,6 @@ class PagedKVCache:
     def device_status(self) -> int:
         """0, or the error that a call on this descriptor's status word left there (waits for the device)."""
         return int(self.status.item())
-
-    def _take(self, t: torch.Tensor, shape: tuple, contiguous: bool = True) -> int:
-        """Pointer of a tensor of the cache's type on the cache's device."""
-        if t.dtype is not self._dtype or t.shape != shape or t.get_device() != self._index:
-            raise ValueError(f"expected {self._dtype} {list(shape)} on {self.k.device}, got {t.dtype} {list(t.shape)} on {t.device}")
-        if not (t.is_contiguous() if contiguous else t.stride(2) == 1):
-            raise ValueError("tensor must be contiguous" if contiguous else "the last dim must be contiguous")
-        return t.data_ptr()
-
-    def _call(self, fn, args, stream) -> None:
-        """fn(*args, stream) with the cache's device current: launches go to the device that holds the data."""
-        if self._index == torch.cuda.current_device():
-            st = fn(*args, _stream_ptr(stream))
-        else:
-            with torch.cuda.device(self._index):
-                st = fn(*args, _stream_ptr(stream))
-        if st != 0:
-            _check(st)
 
 
 @dataclass
@@ -469,48 +464,20 @@ def paged_append(kv: PagedKVCache, k_new: torch.Tensor, v_new: torch.Tensor, rot
                  positions: Optional[torch.Tensor] = None, stream=None) -> None:
     """Rotates the new keys (and q into q_out) by their positions and writes keys and values into the cache's pages;
     key bounds of the touched pages follow.  k_new, v_new, q, q_out: [total_q, heads, head_dim], any token and head
-    strides."""
-    k0, k1, k2 = k_new.stride()
-    v0, v1, v2 = v_new.stride()
-    if k2 != 1 or v2 != 1:
-        raise ValueError("the last dim must be contiguous")
-    qp = op = inv = pos = None
-    q0 = q1 = o0 = o1 = rot = pairs = 0
-    if q is not None:
-        qp = kv._take(q, kv._q_shape, False)
-        q0, q1, _ = q.stride()
-    if q_out is not None:
-        op = kv._take(q_out, kv._q_shape, False)
-        o0, o1, _ = q_out.stride()
-    if rotary is not None:
-        if rotary.inv_freq.get_device() != kv._index:
-            raise ValueError(f"inv_freq must be on {kv.k.device}")
-        inv, rot, pairs = rotary.inv_freq.data_ptr(), 2 * rotary.inv_freq.shape[0], int(rotary.pairs)
-    if positions is not None:
-        if positions.dtype != torch.int64 or positions.shape != (kv.total_q,) or not positions.is_contiguous() or positions.get_device() != kv._index:
-            raise ValueError(f"positions must be contiguous int64 [{kv.total_q}] on {kv.k.device}")
-        pos = positions.data_ptr()
-    d = _AppendDesc(kv._take(k_new, kv._kv_shape, False), k0, k1, kv._take(v_new, kv._kv_shape, False), v0, v1, qp, q0, q1,
-                    op, o0, o1, inv, rot, pairs, pos)
-    kv._call(load_library().tkphi_paged_append, (kv._ref, C.byref(d)), stream)
-
-
-def _lse_ptr(kv: PagedKVCache, lse: Optional[torch.Tensor]) -> Optional[int]:
-    if lse is None:
-        return None
-    if lse.dtype is not torch.float32 or lse.shape != kv._lse_shape or not lse.is_contiguous() or lse.get_device() != kv._index:
-        raise ValueError(f"lse_out must be contiguous float32 {list(kv._lse_shape)} on {kv.k.device}")
-    return lse.data_ptr()
+    strides; positions: int64 [total_q] or None for the cache positions."""
+    inv, pairs = (None, False) if rotary is None else (rotary.inv_freq, rotary.pairs)
+    st = _native().append(kv._handle, k_new, v_new, inv, pairs, q, q_out, positions, stream)
+    if st:
+        _check(st)
 
 
 def paged_attention(kv: PagedKVCache, q: torch.Tensor, y_out: torch.Tensor, lse_out: Optional[torch.Tensor],
                     scale: Optional[float], flags: int, workspace: torch.Tensor, stream=None) -> None:
     """Attention of the step's new tokens over their sequences' whole caches; q, y_out [total_q, n_q_heads, head_dim],
     lse_out fp32 [total_q, n_q_heads] or None, scale None for 1/sqrt(head_dim), flags FLAG_NONE or FLAG_FULL_CONTEXT."""
-    kv._call(load_library().tkphi_paged_attention,
-             (kv._ref, kv._take(q, kv._q_shape), kv._take(y_out, kv._q_shape), _lse_ptr(kv, lse_out),
-              0.0 if scale is None else _positive(scale), flags, _ws_ptr(kv, workspace),
-              workspace.numel() * workspace.element_size()), stream)
+    st = _native().attention(kv._handle, q, y_out, lse_out, scale, flags, workspace, stream)
+    if st:
+        _check(st)
 
 
 def paged_block_attention(kv: PagedKVCache, selection: PageSelection, q: torch.Tensor, y_out: torch.Tensor,
@@ -518,29 +485,10 @@ def paged_block_attention(kv: PagedKVCache, selection: PageSelection, q: torch.T
                           workspace: torch.Tensor, stream=None) -> None:
     """Attention over the pages that ``selection`` takes for each new token and KV head; page_idx_out int32
     [total_q, n_kv_heads, selection.n_pages] or None gets them."""
-    idx = None
-    if page_idx_out is not None:
-        want = (kv.total_q, kv.k.shape[1], selection.n_pages)
-        if page_idx_out.dtype is not torch.int32 or page_idx_out.shape != want or not page_idx_out.is_contiguous() or page_idx_out.get_device() != kv._index:
-            raise ValueError(f"page_idx_out must be contiguous int32 {list(want)} on {kv.k.device}")
-        idx = page_idx_out.data_ptr()
-    sel = selection.desc()
-    kv._call(load_library().tkphi_paged_block_attention,
-             (kv._ref, C.byref(sel), kv._take(q, kv._q_shape), kv._take(y_out, kv._q_shape), _lse_ptr(kv, lse_out), idx,
-              0.0 if scale is None else _positive(scale), _ws_ptr(kv, workspace),
-              workspace.numel() * workspace.element_size()), stream)
-
-
-def _positive(scale: float) -> float:
-    if not scale > 0:
-        raise ValueError(f"scale must be positive, got {scale}")
-    return float(scale)
-
-
-def _ws_ptr(kv: PagedKVCache, workspace: torch.Tensor) -> int:
-    if workspace.get_device() != kv._index or not workspace.is_contiguous():
-        raise ValueError(f"workspace must be contiguous on {kv.k.device}")
-    return workspace.data_ptr()
+    st = _native().block_attention(kv._handle, selection.n_sink_pages, selection.n_tail_pages, selection.topk_pages, q,
+                                   y_out, lse_out, page_idx_out, scale, workspace, stream)
+    if st:
+        _check(st)
 
 
 def device_status(workspace: torch.Tensor, stream=None) -> int:

@@ -288,6 +288,7 @@ tkphi_status tkphi_paged_append(const tkphi_paged_desc* kv, const tkphi_append_d
   tkphi_status st = validate_paged(kv, &sh, true, false);
   if (st != TKPHI_OK) return st;
   if (!step) return fail(TKPHI_ERR_INVALID_ARG, "step descriptor is NULL");
+  if (sh.total_q == 0) return TKPHI_OK;
   if (!step->k_new || !step->v_new || !aligned16(step->k_new) || !aligned16(step->v_new))
     return fail(TKPHI_ERR_INVALID_ARG, "k_new or v_new is NULL or not 16-byte aligned");
   if ((step->q == nullptr) != (step->q_out == nullptr))
@@ -309,7 +310,6 @@ tkphi_status tkphi_paged_append(const tkphi_paged_desc* kv, const tkphi_append_d
   if (step->q && step->q == step->q_out &&
       (step->q_stride_token != step->o_stride_token || step->q_stride_head != step->o_stride_head))
     return fail(TKPHI_ERR_INVALID_ARG, "q_out is q with other strides");
-  if (sh.total_q == 0) return TKPHI_OK;
   int64_t items = 0;
   const int64_t span = std::max(kv->page_size, 64);          // positions of a CTA
   for (int b = 0; b < kv->batch; ++b) {
@@ -347,6 +347,7 @@ tkphi_status tkphi_paged_attention(const tkphi_paged_desc* kv, const void* q, vo
   PagedShape sh{};
   tkphi_status st = validate_paged(kv, &sh, true, (flags & TKPHI_FLAG_FULL_CONTEXT) != 0);
   if (st != TKPHI_OK) return st;
+  if (sh.total_q == 0) return TKPHI_OK;
   st = check_io(q, y_out, lse_out, scale);
   if (st != TKPHI_OK) return st;
   AttendPlan pl{};
@@ -354,7 +355,6 @@ tkphi_status tkphi_paged_attention(const tkphi_paged_desc* kv, const void* q, vo
   if (st != TKPHI_OK) return st;
   st = check_ws(workspace, workspace_bytes, pl.total);
   if (st != TKPHI_OK) return st;
-  if (sh.total_q == 0) return TKPHI_OK;
   CUtensorMap tk, tv;
   st = make_page_map(kv, kv->k, &tk);
   if (st != TKPHI_OK) return st;
@@ -403,6 +403,7 @@ tkphi_status tkphi_paged_block_attention(const tkphi_paged_desc* kv, const tkphi
   tkphi_status st = validate_paged(kv, &sh, true, false);
   if (st != TKPHI_OK) return st;
   if (!kv->key_bounds) return fail(TKPHI_ERR_INVALID_ARG, "key_bounds is NULL");
+  if (sh.total_q == 0) return TKPHI_OK;
   st = check_io(q, y_out, lse_out, scale);
   if (st != TKPHI_OK) return st;
   BlockPlan pl{};
@@ -411,7 +412,6 @@ tkphi_status tkphi_paged_block_attention(const tkphi_paged_desc* kv, const tkphi
   st = check_ws(workspace, workspace_bytes, pl.total);
   if (st != TKPHI_OK) return st;
   if (reinterpret_cast<uintptr_t>(page_idx_out) & 3u) return fail(TKPHI_ERR_INVALID_ARG, "page_idx_out must be 4-byte aligned");
-  if (sh.total_q == 0) return TKPHI_OK;
   CUtensorMap tk, tv;
   st = make_page_map(kv, kv->k, &tk);
   if (st != TKPHI_OK) return st;
