@@ -153,7 +153,7 @@ int choose_chunk(const tkphi_paged_desc* kv, const PagedShape& sh, int64_t longe
 // CTAs per unit of the row kernel's cluster form, or 0 for the line: units of at most `tiles` tiles.
 int split_rows(int64_t units, int64_t tiles, int n_sm) {
   int split = 1;
-  while (split < 8 && tiles > split && units * split * 2 <= 2 * n_sm) split *= 2;
+  while (split < 8 && tiles > 2 * split && units * split * 2 <= n_sm) split *= 2;
   return tiles <= 16 * split ? split : 0;
 }
 

@@ -10,8 +10,8 @@
 // tile); what carries the kernel is the TMA ring that keeps copies in flight:
 //   - one producer warp: a tile of 64 keys and their values is a handful of page boxes (lane = one box); page ids are
 //     read 32 at a time, one batch ahead;
-//   - four compute warps, each with 16 keys of the tile and a running softmax of its own, so that nothing is exchanged
-//     between warps until a unit ends; rows are rescaled only when a maximum moved.
+//   - compute warps, each with 16 keys of a tile and a running softmax of its own, so that nothing is exchanged between
+//     warps until a unit ends; rows are rescaled only when a maximum moved.
 // Probabilities enter the second product as hi + lo pairs of the element type (2^-16 relative for bf16): that costs
 // 16 extra matrix instructions per tile, which the kernel has time for, and leaves the output's own rounding as the
 // only one of its size.
@@ -23,8 +23,6 @@
 
 namespace tkphi {
 
-constexpr int kRowWarps = 4;
-constexpr int kRowThreads = (kRowWarps + 1) * 32;
 
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -38,16 +36,21 @@ __device__ __forceinline__ float2 ld_cluster_f2(const float* p, int rank) {
   return v;
 }
 
-template <int D>
+// The cluster form has few CTAs, where the time is latency: eight compute warps (four for the even, four for the odd
+// tiles) and one CTA per multiprocessor.  Otherwise four warps and two CTAs, so that one works while the other begins or
+// ends a unit (page-selected form, 236 tokens x 65 pages of 32: 307 us, with eight warps 383).
+template <int D, bool SPLIT>
 struct RowCfg {
+  static constexpr int WARPS = SPLIT ? 8 : 4;
+  static constexpr int THREADS = (WARPS + 1) * 32;
   static constexpr int HALVES = D / 64;
   static constexpr int HALF = kRowKeys * 128;               // bytes of one 64-dim half of a 64-key tile
   static constexpr int TILE = HALVES * HALF;                // keys or values of a tile
   static constexpr int STAGE = 2 * TILE;
-  static constexpr int NS = D == 128 ? 3 : 6;
-  static constexpr size_t red = (size_t)NS * STAGE;         // [4 warps][16 rows][64 dims] fp32
-  static constexpr size_t stat = red + kRowWarps * kRowTile * 64 * 4;   // [4][16][2]
-  static constexpr size_t bars = stat + kRowWarps * kRowTile * 2 * 4;
+  static constexpr int NS = (D == 128 ? 3 : 6) * (SPLIT ? 2 : 1);
+  static constexpr size_t red = (size_t)NS * STAGE;         // [warps][16 rows][64 dims] fp32
+  static constexpr size_t stat = red + WARPS * kRowTile * 64 * 4;   // [warps][16][2]
+  static constexpr size_t bars = stat + WARPS * kRowTile * 2 * 4;
   static constexpr size_t total = bars + (2 * NS) * 8 + 16;
   // cluster form: [16][D] piece of this CTA and [16][2] its statistics, over the ring's first tiles (a CTA has one
   // piece there, and writes it when its warps have read all of them)
@@ -168,10 +171,11 @@ struct RowWalk {
 };
 
 template <typename T, int D, bool BLOCK, bool SPLIT>
-__global__ void __launch_bounds__(kRowThreads, 2)
+__global__ void __launch_bounds__(RowCfg<D, SPLIT>::THREADS, SPLIT ? 1 : 2)
 paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                   const __grid_constant__ PagedProblem p) {
-  using C = RowCfg<D>;
+  using C = RowCfg<D, SPLIT>;
+  constexpr int kRowWarps = C::WARPS;
   constexpr int NS = C::NS;
   extern __shared__ __align__(1024) unsigned char smem[];
   float* red = reinterpret_cast<float*>(smem + C::red);
@@ -185,7 +189,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
   const int cta = blockIdx.x;
 
   if (tid == 0) {
-    for (int s = 0; s < NS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], kRowWarps); }
+    for (int s = 0; s < NS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 4); }
     mbar_fence_init();
     *s_abort = 0;
   }
@@ -294,6 +298,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       float mA = -INFINITY, mB = -INFINITY, lA = 0.f, lB = 0.f;
 
       for (int t = w.t0; t < w.t1; ++t, ++it) {
+        if (SPLIT && (it & 1) != warp >> 2) continue;
         const int stage = it % NS;
         if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&full[stage], (uint32_t)(it / NS) & 1u, s_abort));
         if (!ok) continue;                                // the barriers below are still met
@@ -301,7 +306,8 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         unsigned char* vs = ks + C::TILE;
         // position of this warp's first key (its 16 keys never straddle a page); in the block form only the last
         // page of a list can be partly visible, everything before it is
-        int key0 = t * kRowKeys + warp * 16;
+        const int kg = warp & 3;
+        int key0 = t * kRowKeys + kg * 16;
         if (BLOCK) {
           const int entry = key0 >> p.page_shift;
           if (entry < w.n_list - 1) key0 = 0 - 16;                          // all visible
@@ -314,7 +320,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
 #pragma unroll
           for (int n = 0; n < 2; ++n) { s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f; }
           {
-            const int row = warp * 16 + ((lane >> 4) << 3) + (lane & 7), sub = (lane >> 3) & 1;
+            const int row = kg * 16 + ((lane >> 4) << 3) + (lane & 7), sub = (lane >> 3) & 1;
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
               uint32_t bf[4];
@@ -337,7 +343,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             if (keep < 16) {
               constexpr int CPR = D / 8;                    // 16-byte pieces of a row
               for (int i = lane; i < (16 - keep) * CPR; i += 32) {
-                const int row = warp * 16 + keep + i / CPR, c = i % CPR;
+                const int row = kg * 16 + keep + i / CPR, c = i % CPR;
                 *reinterpret_cast<uint4*>(vs + (c >> 3) * C::HALF + swz128(row, c & 7)) = make_uint4(0, 0, 0, 0);
               }
               fence_proxy_async_smem();                     // before the slot's next copy
@@ -378,7 +384,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             pl[j] = T::pack(x - T::lo(ph[j]), y - T::hi(ph[j]));
           }
           {
-            const int row = warp * 16 + (((lane >> 3) & 1) << 3) + (lane & 7), sub = lane >> 4;
+            const int row = kg * 16 + (((lane >> 3) & 1) << 3) + (lane & 7), sub = lane >> 4;
 #pragma unroll
             for (int n = 0; n < D / 16; ++n) {
               uint32_t bf[4];
@@ -394,7 +400,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         if (lane == 0) mbar_arrive(&empty[stage]);
       }
 
-      // ---- the four warps' softmaxes joined; a thread ends up with 8 dims of one row
+      // ---- the warps' softmaxes joined; a thread ends up with PER of 64 dims of one row
 #pragma unroll
       for (int d = 1; d < 4; d <<= 1) {
         lA += __shfl_xor_sync(0xffffffffu, lA, d);
@@ -412,7 +418,8 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         MB = fmaxf(MB, stat[(i * kRowTile + rB) * 2]);
       }
       const float sA = mA == -INFINITY ? 0.f : ex2_approx(mA - MA), sB = mB == -INFINITY ? 0.f : ex2_approx(mB - MB);
-      const int row = tid >> 3, d8 = (tid & 7) * 8;
+      constexpr int PER = 32 / kRowWarps, TPR = 64 / PER;      // dims of a thread, threads of a row
+      const int row = tid / TPR, dp = tid % TPR * PER;
       float M = -INFINITY, L = 0.f;
 #pragma unroll
       for (int i = 0; i < kRowWarps; ++i) M = fmaxf(M, stat[(i * kRowTile + row) * 2]);
@@ -436,32 +443,31 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
           *reinterpret_cast<float2*>(mine + rB * 64 + pb) = make_float2(o[x * 8 + n][2] * sB, o[x * 8 + n][3] * sB);
         }
         named_barrier(1, kRowWarps * 32);
-        float a[8];
+        float a[PER];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) a[e] = 0.f;
+        for (int e = 0; e < PER; ++e) a[e] = 0.f;
 #pragma unroll
-        for (int i = 0; i < kRowWarps; ++i) {
-          const float4* src = reinterpret_cast<const float4*>(red + (i * kRowTile + row) * 64 + (((tid & 7) + row) & 7) * 8);
-          const float4 u = src[0], v = src[1];
-          a[0] += u.x; a[1] += u.y; a[2] += u.z; a[3] += u.w;
-          a[4] += v.x; a[5] += v.y; a[6] += v.z; a[7] += v.w;
-        }
+        for (int i = 0; i < kRowWarps; ++i)
+#pragma unroll
+          for (int e = 0; e < PER; e += 4) {
+            const float4 u = *reinterpret_cast<const float4*>(red + (i * kRowTile + row) * 64 + (((dp >> 3) + row) & 7) * 8 + (dp & 7) + e);
+            a[e] += u.x; a[e + 1] += u.y; a[e + 2] += u.z; a[e + 3] += u.w;
+          }
         if (row < w.rows) {
-          if (fin) {
-            const float inv = L > 0.f ? 1.f / L : 0.f;
-            uint4 y;
-            y.x = T::pack(a[0] * inv, a[1] * inv); y.y = T::pack(a[2] * inv, a[3] * inv);
-            y.z = T::pack(a[4] * inv, a[5] * inv); y.w = T::pack(a[6] * inv, a[7] * inv);
-            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.y) + out_row * D + x * 64 + d8) = y;
-          } else {
-            float4* dst = reinterpret_cast<float4*>((SPLIT ? keep + (size_t)row * D : p.row_part + ((size_t)slot * kRowTile + row) * D) + x * 64 + d8);
-            dst[0] = make_float4(a[0], a[1], a[2], a[3]);
-            dst[1] = make_float4(a[4], a[5], a[6], a[7]);
+          const float inv = L > 0.f ? 1.f / L : 0.f;
+          float* part = (SPLIT ? keep + (size_t)row * D : p.row_part + ((size_t)slot * kRowTile + row) * D) + x * 64 + dp;
+#pragma unroll
+          for (int e = 0; e < PER; e += 4) {
+            if (fin)
+              *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.y) + out_row * D + x * 64 + dp + e) =
+                  make_uint2(T::pack(a[e] * inv, a[e + 1] * inv), T::pack(a[e + 2] * inv, a[e + 3] * inv));
+            else
+              *reinterpret_cast<float4*>(part + e) = make_float4(a[e], a[e + 1], a[e + 2], a[e + 3]);
           }
         }
         named_barrier(1, kRowWarps * 32);
       }
-      if ((tid & 7) == 0 && row < w.rows) {
+      if (tid % TPR == 0 && row < w.rows) {
         if (fin) {
           if (p.lse) p.lse[out_row] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
         } else {
@@ -630,12 +636,12 @@ __global__ void __launch_bounds__(kMergeThreads) paged_rows_merge_kernel(const _
 template <typename T, int D, bool BLOCK, bool SPLIT>
 static cudaError_t launch_rows_s(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int grid, cudaStream_t st) {
   static PerDeviceFlag configured;
-  const size_t smem = RowCfg<D>::total;
+  const size_t smem = RowCfg<D, SPLIT>::total;
   const cudaError_t e = set_max_dynamic_smem(configured, reinterpret_cast<const void*>(paged_rows_kernel<T, D, BLOCK, SPLIT>), smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(kRowThreads);
+  cfg.blockDim = dim3(RowCfg<D, SPLIT>::THREADS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
