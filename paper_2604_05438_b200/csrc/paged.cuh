@@ -14,6 +14,7 @@ constexpr int kRowTile = 16;                // query rows (tokens x query heads 
 constexpr int kRowKeys = 64;                // keys of one tile of the row kernel
 constexpr int kTileRows = 256;              // query rows of a tile-kernel CTA: two 128-row MMA tiles
 constexpr int kTileKeys = 128;              // keys of one tile of the tile kernel
+constexpr int kMaxSelectPages = 131072;     // pages of a sequence of the page-selected form
 constexpr int kMaxGroup = 16;               // query heads per KV head of the paged calls
 
 // One step over a paged cache.  Sequence b brings cu_q[b+1] - cu_q[b] new tokens, the last ones of its
@@ -41,8 +42,12 @@ struct PagedProblem {
   // page selection
   int n_keep, n_sink, n_tail, topk;
   const void* bounds;              // [n_pages][hkv][2][d]
-  unsigned long long* page_keys;   // [units][key_stride] ordered bounds of the candidate pages
+  float* page_scores;              // [units][key_stride] 32-bit bounds of the candidate pages
+  unsigned long long* page_keys;   // [units][key_stride] their 64-bit bounds as ordered keys, where many are equal
   int key_stride;
+  uint4* page_mags;                // [units][mag_parts] per scoring CTA: largest sum of magnitudes behind a bound (bits), smallest
+                                   // and largest bound (ordered keys)
+  int mag_parts;
   int* page_list;                  // [units][n_keep] physical pages, -1 padded
   int* page_out;                   // [units][n_keep] logical pages, -1 padded, or null
   // tile kernel: sequences with more than rows_limit rows
@@ -143,6 +148,9 @@ __device__ __forceinline__ void named_barrier(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
+// Rows of a scoring tile: tokens of one sequence x the group padded to a power of two.
+__host__ __device__ inline int padded_group(int g) { return g <= 1 ? 1 : g <= 2 ? 2 : g <= 4 ? 4 : g <= 8 ? 8 : 16; }
+
 // ---------------------------------------------------------------- launches (host)
 struct AppendProblem {
   int batch, hq, hkv, group, d;
@@ -167,8 +175,10 @@ struct AppendProblem {
 cudaError_t launch_paged_append(const AppendProblem& p, bool bf16, cudaStream_t st);
 cudaError_t launch_paged_rows(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int d, bool bf16,
                               bool block, bool split, int grid, cudaStream_t st);
+int paged_score_parts(int row_tiles, int hkv, int n);        // scoring CTAs per row tile and KV head, for n candidates
+cudaError_t launch_paged_select(const PagedProblem& p, int d, bool bf16, int max_pages_seq, int row_tiles, cudaStream_t st);
 cudaError_t launch_paged_rows_merge(const PagedProblem& p, int d, bool bf16, bool block, int units, int max_rows, cudaStream_t st);
-cudaError_t launch_paged_select(const PagedProblem& p, int d, bool bf16, int max_pages_seq, cudaStream_t st);
+
 cudaError_t launch_paged_tiles(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int d, bool bf16, int grid,
                                cudaStream_t st);
 cudaError_t launch_paged_tiles_merge(const PagedProblem& p, int d, bool bf16, cudaStream_t st);

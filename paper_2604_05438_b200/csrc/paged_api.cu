@@ -205,9 +205,9 @@ tkphi_status plan_attend(const tkphi_paged_desc* kv, const PagedShape& sh, Atten
 }
 
 struct BlockPlan {
-  int n_split, n_keep, key_stride;
+  int n_split, n_keep, key_stride, row_tiles, mag_parts;
   bool cluster;                  // the CTAs of a unit are a cluster and join their pieces themselves
-  size_t keys, list, part, stat, total;
+  size_t scores, keys, mags, list, part, stat, total;
 };
 
 tkphi_status plan_block(const tkphi_paged_desc* kv, const PagedShape& sh, const tkphi_page_selection* sel, BlockPlan* pl) {
@@ -220,14 +220,24 @@ tkphi_status plan_block(const tkphi_paged_desc* kv, const PagedShape& sh, const 
   pl->n_keep = (int)keep;
   const int64_t units = (int64_t)sh.total_q * kv->n_kv_heads;
   const int64_t middle = sh.max_pages_seq - sel->n_sink_pages - sel->n_tail_pages;
-  pl->key_stride = (int)std::max<int64_t>(middle > sel->topk_pages ? middle : 0, 1);
+  if (sh.max_pages_seq > kMaxSelectPages)
+    return fail(TKPHI_ERR_UNSUPPORTED, "%lld pages in a sequence > %d", (long long)sh.max_pages_seq, kMaxSelectPages);
+  pl->key_stride = (int)((std::max<int64_t>(middle > sel->topk_pages ? middle : 0, 1) + 3) & ~(int64_t)3);
   const int64_t tiles = ((std::min<int64_t>(keep, std::max<int64_t>(sh.max_pages_seq, 1)) << sh.page_shift) + kRowKeys - 1) / kRowKeys;
   const int n_sm = sm_count_current_device();
   pl->n_split = split_rows(units, tiles, n_sm);
   pl->cluster = pl->n_split > 0;
   if (!pl->cluster) pl->n_split = (int)std::max<int64_t>(1, std::min<int64_t>((tiles + 1) / 2, units > 0 ? 2 * n_sm / units : 1));
   size_t o = 0;
+  // score row tiles: tokens of one sequence, 16 rows at a time
+  const int tpt = kRowTile / padded_group(sh.group);
+  int64_t row_tiles = 0;
+  for (int b = 0; b < kv->batch; ++b) row_tiles += (kv->cu_q_host[b + 1] - kv->cu_q_host[b] + tpt - 1) / tpt;
+  pl->row_tiles = (int)row_tiles;
+  pl->mag_parts = paged_score_parts(pl->row_tiles, kv->n_kv_heads, pl->key_stride);
+  pl->scores = o; o = align_up(o + sizeof(float) * units * pl->key_stride, 256);
   pl->keys = o; o = align_up(o + sizeof(unsigned long long) * units * pl->key_stride, 256);
+  pl->mags = o; o = align_up(o + 16 * units * pl->mag_parts, 256);
   pl->list = o; o = align_up(o + sizeof(int) * units * pl->n_keep, 256);
   const size_t parts = pl->n_split > 1 && !pl->cluster ? (size_t)units * pl->n_split : 0;
   pl->part = o; o = align_up(o + sizeof(float) * parts * kRowTile * kv->head_dim, 256);
@@ -421,7 +431,9 @@ tkphi_status tkphi_paged_block_attention(const tkphi_paged_desc* kv, const tkphi
   char* w = static_cast<char*>(workspace);
   p.n_split = pl.n_split; p.n_keep = pl.n_keep;
   p.n_sink = selection->n_sink_pages; p.n_tail = selection->n_tail_pages; p.topk = selection->topk_pages;
+  p.page_scores = reinterpret_cast<float*>(w + pl.scores);
   p.page_keys = reinterpret_cast<unsigned long long*>(w + pl.keys); p.key_stride = pl.key_stride;
+  p.page_mags = reinterpret_cast<uint4*>(w + pl.mags); p.mag_parts = pl.mag_parts;
   p.page_list = reinterpret_cast<int*>(w + pl.list);
   p.page_out = page_idx_out;
   p.row_part = reinterpret_cast<float*>(w + pl.part);
@@ -432,7 +444,7 @@ tkphi_status tkphi_paged_block_attention(const tkphi_paged_desc* kv, const tkphi
   cudaError_t e;
   {
     ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_SELECT);
-    e = launch_paged_select(p, kv->head_dim, bf16, (int)sh.max_pages_seq, cs);
+    e = launch_paged_select(p, kv->head_dim, bf16, (int)sh.max_pages_seq, pl.row_tiles, cs);
   }
   if (e != cudaSuccess) return cuda_fail(e, "page selection launch");
   {
