@@ -12,7 +12,7 @@ namespace tkphi {
 constexpr int kStatusBadPage = -1;          // a page-table entry outside [0, n_pages) was met
 constexpr int kRowTile = 16;                // query rows (tokens x query heads of a KV head) of a row-kernel unit
 constexpr int kRowKeys = 64;                // keys of one tile of the row kernel
-constexpr int kTileRows = 256;              // query rows of a tile-kernel CTA: two 128-row MMA tiles
+constexpr int kTileRows = 256;              // rows of a tile-kernel CTA: two 128-row MMA tiles
 constexpr int kTileKeys = 128;              // keys of one tile of the tile kernel
 constexpr int kMaxSelectPages = 131072;     // pages of a sequence of the page-selected form
 constexpr int kMaxGroup = 16;               // query heads per KV head of the paged calls
@@ -148,6 +148,8 @@ __device__ __forceinline__ void named_barrier(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
+// Query rows of an MMA tile: whole tokens, so that a tile of queries is one box of the tensor map.
+__host__ __device__ inline int tile_rows(int group) { return 128 / group * group; }
 // Rows of a scoring tile: tokens of one sequence x the group padded to a power of two.
 __host__ __device__ inline int padded_group(int g) { return g <= 1 ? 1 : g <= 2 ? 2 : g <= 4 ? 4 : g <= 8 ? 8 : 16; }
 
@@ -179,8 +181,8 @@ int paged_score_parts(int row_tiles, int hkv, int n);        // scoring CTAs per
 cudaError_t launch_paged_select(const PagedProblem& p, int d, bool bf16, int max_pages_seq, int row_tiles, cudaStream_t st);
 cudaError_t launch_paged_rows_merge(const PagedProblem& p, int d, bool bf16, bool block, int units, int max_rows, cudaStream_t st);
 
-cudaError_t launch_paged_tiles(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int d, bool bf16, int grid,
-                               cudaStream_t st);
+cudaError_t launch_paged_tiles(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tq, int d,
+                               bool bf16, int grid, cudaStream_t st);
 cudaError_t launch_paged_tiles_merge(const PagedProblem& p, int d, bool bf16, cudaStream_t st);
 
 }  // namespace tkphi

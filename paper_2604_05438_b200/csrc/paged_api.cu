@@ -109,6 +109,23 @@ tkphi_status make_page_map(const tkphi_paged_desc* kv, const void* base, CUtenso
   return TKPHI_OK;
 }
 
+// 4-D view [token][KV head][query head of the group][dim] of the step's queries; box = 64 dims x the group x the tokens of
+// an MMA tile of one KV head: a tile's rows as they lie in shared memory.
+tkphi_status make_query_map(const tkphi_paged_desc* kv, const PagedShape& sh, const void* q, CUtensorMap* tm) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return fail(TKPHI_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
+  const cuuint64_t row = (cuuint64_t)kv->head_dim * 2;
+  const cuuint64_t dims[4] = {(cuuint64_t)kv->head_dim, (cuuint64_t)sh.group, (cuuint64_t)kv->n_kv_heads, (cuuint64_t)sh.total_q};
+  const cuuint64_t st[3] = {row, row * sh.group, row * kv->n_q_heads};
+  const cuuint32_t box[4] = {64, (cuuint32_t)sh.group, 1, (cuuint32_t)(128 / sh.group)};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  const CUresult r = fn(tm, kv->dtype == TKPHI_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                        4, const_cast<void*>(q), dims, st, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(TKPHI_ERR_CUDA, "cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
+  return TKPHI_OK;
+}
+
 // What a call launches and where its pieces of the workspace lie; a function of the host lengths and the device's
 // multiprocessor count only, so that the size query and the call agree.
 struct AttendPlan {
@@ -137,7 +154,8 @@ int choose_chunk(const tkphi_paged_desc* kv, const PagedShape& sh, int64_t longe
     for (int b = 0; b < kv->batch; ++b) {
       const int64_t q = kv->cu_q_host[b + 1] - kv->cu_q_host[b], len = kv->kv_lens_host[b];
       if (q * sh.group <= kRowsLimit) continue;
-      const double rt = (double)((q * sh.group + kTileRows - 1) / kTileRows) * kv->n_kv_heads;
+      const int pair = 2 * tile_rows(sh.group);
+      const double rt = (double)((q * sh.group + pair - 1) / pair) * kv->n_kv_heads;
       const double seen = std::max<double>(1., ((double)len - 0.5 * (double)std::min(q, len)) / kTileKeys);   // of an average row tile
       ctas += rt * std::max(1., seen / (double)per + (seen > (double)per ? 0.5 : 0.));
       work += rt * seen;
@@ -183,13 +201,14 @@ tkphi_status plan_attend(const tkphi_paged_desc* kv, const PagedShape& sh, Atten
   pl->row_grid = pl->row_split ? units * pl->row_split : pl->row_ctas;
   if (pl->any_tiles) {
     pl->chunk = choose_chunk(kv, sh, longest, n_sm);
+    const int pair = 2 * tile_rows(sh.group);
     int64_t grid = 0;
     for (int b = 0; b < kv->batch; ++b) {
       const int64_t rows = (kv->cu_q_host[b + 1] - kv->cu_q_host[b]) * sh.group, len = kv->kv_lens_host[b];
       if (rows <= kRowsLimit) continue;
       const int64_t chunks = len > pl->chunk ? (len + pl->chunk - 1) / pl->chunk : 1;
       pl->max_chunks = (int)std::max<int64_t>(pl->max_chunks, chunks);
-      grid += (rows + kTileRows - 1) / kTileRows * chunks * kv->n_kv_heads;
+      grid += (rows + pair - 1) / pair * chunks * kv->n_kv_heads;
     }
     if (grid > INT_MAX / 2) return fail(TKPHI_ERR_UNSUPPORTED, "too many query rows for one call");
     pl->tile_grid = (int)grid;
@@ -387,8 +406,11 @@ tkphi_status tkphi_paged_attention(const tkphi_paged_desc* kv, const void* q, vo
   // tiles, rows (may start beside the tiles' last CTAs), then the joins
   cudaError_t e = cudaSuccess;
   if (pl.any_tiles) {
+    CUtensorMap tq;
+    st = make_query_map(kv, sh, q, &tq);
+    if (st != TKPHI_OK) return st;
     ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_TILES);
-    e = launch_paged_tiles(p, tk, tv, kv->head_dim, bf16, pl.tile_grid, cs);
+    e = launch_paged_tiles(p, tk, tv, tq, kv->head_dim, bf16, pl.tile_grid, cs);
   }
   if (e == cudaSuccess && pl.any_rows) {
     ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_ROWS);

@@ -117,7 +117,7 @@ struct TileCfg {
   static constexpr size_t ring = 2 * TILE;
   static constexpr size_t bars = ring + (size_t)NS * TILE;
   static constexpr size_t bar_bytes = 512;                   // barriers and four words
-  static_assert((NS + NV + 2 * NB + 6) * 8 + 16 <= bar_bytes, "barriers");
+  static_assert((NS + NV + 2 * NB + 6) * 8 + 8 + 11 * 4 <= bar_bytes, "barriers");
   static constexpr size_t total = bars + bar_bytes;
 };
 
@@ -132,13 +132,18 @@ __device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t* r) {
       "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
+// 32 bytes, a whole sector (dst 32-byte aligned).
+__device__ __forceinline__ void st_global_32(float* dst, const float* v) {
+  asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
+               "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+}
 // kind::f16 instruction descriptor with both operands of one 16-bit type (1: bf16, 0: f16)
 __host__ __device__ constexpr uint32_t umma_idesc_16(int bf16, int M, int N, int a_mn, int b_mn) {
   return (1u << 4) | ((uint32_t)bf16 << 7) | ((uint32_t)bf16 << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
          ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
-// CTAs of a sequence: KV heads x key chunks x row tiles.
+// CTAs of a sequence: KV heads x key chunks x row tiles (pairs of MMA tiles).
 struct TileSeq {
   int rows, len, chunks, row_tiles;
 };
@@ -149,15 +154,23 @@ __device__ __forceinline__ TileSeq tile_seq_of(const PagedProblem& p, int b) {
   s.len = paged_kv_len(p, b);
   s.rows = q > 0 ? q * p.group : 0;
   if (s.rows <= p.rows_limit) s.rows = 0;
-  s.row_tiles = (s.rows + kTileRows - 1) / kTileRows;
+  const int pair = 2 * tile_rows(p.group);
+  s.row_tiles = (s.rows + pair - 1) / pair;
   s.chunks = s.len > p.chunk ? (s.len + p.chunk - 1) / p.chunk : 1;
   return s;
 }
 
+// What a CTA works on.
+struct TileWork {
+  int seq;                                 // -1: nothing
+  int h, c0, row0, rows, len, q_len, tok0, chunks;
+  int n, tiles;                            // key tiles, row tiles
+};
+
 template <typename T, int D>
 __global__ void __launch_bounds__(kTileThreads, 1)
 paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
-                   const __grid_constant__ PagedProblem p) {
+                   const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ PagedProblem p) {
   using C = TileCfg<D>;
   constexpr int NS = C::NS, NV = C::NV;
   constexpr float kShift = T::kBf16 ? 0.f : 7.f;             // P = 2^kShift exp2(..)
@@ -177,7 +190,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   int* misc = reinterpret_cast<int*>(drained + 1);
   volatile int* s_abort = misc;
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(misc + 1);
-  int* s_find = misc + 2;                  // sequence, index within it
+  TileWork* s_work = reinterpret_cast<TileWork*>(misc + 2);
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int cta = blockIdx.x;
 
@@ -185,19 +198,33 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   pdl_launch_next();
   if (warp == 0) {
     int base = 0;
-    bool found = false;
-    for (int s = 0; s < p.batch && !found; s += 32) {
+    if (lane == 0) s_work->seq = -1;
+    for (int s = 0; s < p.batch; s += 32) {
       const TileSeq q = tile_seq_of(p, s + lane);
       const int w = q.row_tiles * q.chunks * p.hkv, incl = warp_inclusive_scan(w) + base;
-      const unsigned hit = __ballot_sync(0xffffffffu, incl > cta);
-      if (hit) {
-        const int l = __ffs(hit) - 1, first = __shfl_sync(0xffffffffu, incl - w, l);
-        if (lane == 0) { s_find[0] = s + l; s_find[1] = cta - first; }
-        found = true;
+      if (incl > cta && incl - w <= cta) {             // one lane
+        const int b = s + lane;
+        int i = cta - (incl - w);
+        TileWork k;
+        k.seq = b;
+        k.q_len = paged_q_len(p, b);
+        k.tok0 = (int)__ldg(p.cu_q + b);
+        k.row0 = (q.row_tiles - 1 - i % q.row_tiles) * 2 * tile_rows(p.group);       // the rows that see most first
+        i /= q.row_tiles;
+        k.c0 = (i % q.chunks) * p.chunk;
+        k.h = i / q.chunks;
+        k.rows = q.rows; k.len = q.len; k.chunks = q.chunks;
+        const int pair = 2 * tile_rows(p.group), rows = q.rows - k.row0 < pair ? q.rows - k.row0 : pair;
+        k.tiles = rows > pair / 2 ? 2 : 1;
+        // up to the last key that the last row sees; both row tiles take all of these (the first one may see less: masked)
+        int end = p.causal ? q.len - k.q_len + (k.row0 + rows - 1) / p.group + 1 : q.len;
+        if (end > k.c0 + p.chunk) end = k.c0 + p.chunk;
+        k.n = end > k.c0 ? (end - k.c0 + kTileKeys - 1) / kTileKeys : 0;
+        *s_work = k;
       }
       base = __shfl_sync(0xffffffffu, incl, 31);
+      if (base > cta) break;
     }
-    if (!found && lane == 0) s_find[0] = -1;
   } else if (warp == 1) {
     tmem_alloc(s_tmem, kTileTmemCols);
   } else if (tid == 64) {
@@ -206,7 +233,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     for (int i = 0; i < C::NB; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_ready[i], 4); }
     mbar_init(&o_full[0], 1); mbar_init(&o_full[1], 1);
     mbar_init(pv_done, 1);
-    mbar_init(q_ready, 256);
+    mbar_init(q_ready, 1);
     mbar_init(v_fixed, 1);
     mbar_init(drained, 1);
     mbar_fence_init();
@@ -216,27 +243,10 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = *s_tmem;
-  const int b = s_find[0];
-
-  int n = 0, tiles = 1;                    // key tiles, row tiles of this CTA
-  int h = 0, c0 = 0, row0 = 0, q_len = 0;
-  TileSeq sq{0, 0, 1, 0};
-  if (b >= 0) {
-    sq = tile_seq_of(p, b);
-    q_len = paged_q_len(p, b);
-    int i = s_find[1];
-    row0 = (sq.row_tiles - 1 - i % sq.row_tiles) * kTileRows;        // the rows that see most first
-    i /= sq.row_tiles;
-    c0 = (i % sq.chunks) * p.chunk;
-    h = i / sq.chunks;
-    const int rows = sq.rows - row0 < kTileRows ? sq.rows - row0 : kTileRows;
-    tiles = rows > 128 ? 2 : 1;
-    // up to the last key that the last row sees; both row tiles take all of these (the first one may see less: masked)
-    int end = p.causal ? sq.len - q_len + (row0 + rows - 1) / p.group + 1 : sq.len;
-    if (end > c0 + p.chunk) end = c0 + p.chunk;
-    n = end > c0 ? (end - c0 + kTileKeys - 1) / kTileKeys : 0;
-  }
-  const bool fix = n > 0 && c0 + n * kTileKeys > sq.len;              // the last tile reaches behind the sequence
+  const TileWork k = *s_work;
+  const int b = k.seq, n = b >= 0 ? k.n : 0, tiles = b >= 0 ? k.tiles : 1;
+  const int h = k.h, c0 = k.c0, row0 = k.row0, q_len = k.q_len, t_rows = tile_rows(p.group);
+  const bool fix = n > 0 && c0 + n * kTileKeys > k.len;              // the last tile reaches behind the sequence
   // Scores, P and products run through one sequence: number i = key tile * tiles + row tile, buffer i % NB.  Keys are
   // used `lead` tiles ahead of values: the ring holds K 0 .. K lead-1, V 0, K lead, V 1, ..
   const int lead = (C::NB + tiles - 1) / tiles;
@@ -244,29 +254,19 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   if (warp < 8) {
     // ================================================================ softmax: thread = row
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    const int t = warp >> 2, r = tid & 127, quad = warp & 3;
-    const int row = row0 + t * 128 + r;
+    const int t = warp >> 2, quad = warp & 3;
     const int nt = t < tiles ? n : 0;
-    const bool live = row < sq.rows;
-    const size_t tok0 = b >= 0 ? (size_t)__ldg(p.cu_q + b) : 0;
-    const size_t out_row = live ? (tok0 + row / p.group) * p.hq + (size_t)h * p.group + row % p.group : 0;
-    const size_t slot_row = (size_t)cta * kTileRows + t * 128 + r;
-    if (n > 0) {
-      // queries: the tile's 128 threads copy its rows, 16 bytes at a time (rows past the last are zeros)
-      constexpr int CPR = D / 8;
-      const uint4* q = static_cast<const uint4*>(p.q);
-#pragma unroll 4
-      for (int i = r; i < 128 * CPR; i += 128) {
-        const int rr = i / CPR, c = i % CPR, g = row0 + t * 128 + rr;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (g < sq.rows) v = __ldg(q + ((tok0 + g / p.group) * p.hq + (size_t)h * p.group + g % p.group) * CPR + c);
-        *reinterpret_cast<uint4*>(qs + t * C::TILE + (c >> 3) * C::BOX + swz128(rr, c & 7)) = v;
-      }
-      fence_proxy_async_smem();
-      mbar_arrive(q_ready);
-    }
-    // last visible key; rows without a query run along unmasked and are not stored
-    const int lim = !live ? INT_MAX : p.causal ? sq.len - q_len + row / p.group : sq.len - 1;
+    // The row's place: computed here and again at the end (the loop between has no registers to spare).
+    auto row_of = [&](int& row) {
+      const volatile TileWork* w = s_work;
+      const int r = tid & 127;
+      row = w->row0 + t * t_rows + r;
+      return w->seq >= 0 && r < t_rows && row < w->rows;
+    };
+    int row;
+    const bool live = row_of(row);
+    // last visible key; rows without a query (their tile rows hold anything) run along, have no say and are not stored
+    const int lim = !live ? INT_MAX : p.causal ? k.len - q_len + row / p.group : k.len - 1;
     const uint32_t o_addr = tmem_addr(tmem, quad * 32, C::O_COL + t * D);
     int buf = t;
     uint32_t phase = 0;
@@ -279,7 +279,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       const uint32_t s_addr = tmem_addr(tmem, quad * 32, buf * 128);
       const int key0 = c0 + j * kTileKeys;
       uint32_t w[64];
-      bool careful = j == 0 || __any_sync(0xffffffffu, key0 + kTileKeys - 1 > lim || m == -INFINITY);
+      bool careful = j == 0 || __any_sync(0xffffffffu, live && (key0 + kTileKeys - 1 > lim || m == -INFINITY));
       if (!careful) {
         const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), off2 = pack2(kShift - m, kShift - m);
         uint64_t sum2[2] = {0, 0};
@@ -317,7 +317,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         piece(v, 3);
         float a, d;
         unpack2(add2(sum2[0], sum2[1]), a, d);
-        careful = __any_sync(0xffffffffu, !(a + d < kSumLimit));
+        careful = __any_sync(0xffffffffu, live && !(a + d < kSumLimit));
         if (!careful) l += a + d;
       }
       if (careful) {
@@ -340,7 +340,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           for (int e = 2; e < 32; e += 2) mx[c] = fmaxf(mx[c], fmaxf(s[c][e], s[c][e + 1]));
         }
         const float cand = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
-        const bool grow = cand > m + kGrow;
+        const bool grow = live && cand > m + kGrow;
         if (__any_sync(0xffffffffu, grow)) {
           const float f = grow ? ex2_approx(m - cand) : 1.f;   // m = -inf: 0
           if (j > 0) {
@@ -393,7 +393,11 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     if (ok && nt > 0) ok = __all_sync(0xffffffffu, mbar_wait(&o_full[t], 0, s_abort));
     if (ok && b >= 0) {
       tc_fence_after_sync();
-      if (sq.chunks == 1) {
+      const volatile TileWork* w = s_work;
+      int row;
+      const bool live = row_of(row);
+      if (w->chunks == 1) {
+        const size_t out_row = live ? ((size_t)w->tok0 + row / p.group) * p.hq + (size_t)w->h * p.group + row % p.group : 0;
         const float inv = l > 0.f ? 1.f / l : 0.f;
         uint4* y = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.y) + out_row * D);
 #pragma unroll
@@ -415,17 +419,18 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         }
         if (live && p.lse) p.lse[out_row] = l > 0.f ? (m - kShift + log2f(l)) * 0.6931471805599453f : -INFINITY;
       } else {
+        const size_t slot_row = (size_t)cta * kTileRows + t * t_rows + (tid & 127);
         if (live) reinterpret_cast<float2*>(p.tile_stat)[slot_row] = make_float2(l > 0.f ? m - kShift : -INFINITY, l);
         if (nt > 0) {
-          float4* dst = reinterpret_cast<float4*>(p.tile_part + slot_row * D);
+          float* dst = p.tile_part + slot_row * D;
 #pragma unroll
           for (int c = 0; c < D / 32; ++c) {
             float o[32];
             tmem_ld_x32(o_addr + c * 32, o);
             tc_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (live) dst[c * 8 + e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+            for (int e = 0; e < 4; ++e)
+              if (live) st_global_32(dst + c * 32 + e * 8, &o[e * 8]);
           }
         }
       }
@@ -439,7 +444,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       const int copies = C::HALVES * boxes, half = lane / boxes, bx = lane % boxes;
       const int page_off = (bx * box_rows) >> p.page_shift, row_off = (bx * box_rows) & (ps - 1);
       const uint32_t dst_off = half * C::BOX + bx * box_rows * 128;
-      const int n_pages_seq = (sq.len + ps - 1) >> p.page_shift;
+      const int n_pages_seq = (k.len + ps - 1) >> p.page_shift;
       const int* list = p.table + (size_t)b * p.max_pages;
       const uint64_t pol = l2_policy_normal();
       // page ids of the keys' and of the values' tiles: 32 at a time, the next 32 fetched ahead
@@ -449,6 +454,12 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       id_next[0] = id_next[1] = batch0[0] + 32 + lane < n_pages_seq ? __ldg(list + batch0[0] + 32 + lane) : p.n_pages;
       int slot = 0, last_slot = 0;
       uint32_t phase = 0, last_phase = 0;
+      // the queries: tokens x the group's heads, 64 dims at a time (a second tile of other tokens is not used)
+      if (lane == 0) mbar_expect_tx(q_ready, (uint32_t)(tiles * C::HALVES * t_rows * 128));
+      __syncwarp();
+      if (lane < tiles * C::HALVES)
+        tma_load_4d(qs + (lane / C::HALVES) * C::TILE + (lane % C::HALVES) * C::BOX, &tmap_q, q_ready, (lane % C::HALVES) * 64, 0,
+                    h, k.tok0 + (row0 + (lane / C::HALVES) * t_rows) / p.group, pol);
       int issued = 0;
       uint32_t pending = 0, parity = 0;                       // slots with a copy issued, and its phase
       bool ok = true;
@@ -490,7 +501,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       if (ok && fix) {
         // Value rows of the last tile behind the end of the sequence.  (The slot's barrier is in the phase of this
         // copy until the wait returns, because nothing is loaded after it.)
-        const int keep = sq.len - (c0 + (n - 1) * kTileKeys);        // 1 .. 127
+        const int keep = k.len - (c0 + (n - 1) * kTileKeys);        // 1 .. 127
         ok = __all_sync(0xffffffffu, mbar_wait(&full[last_slot], last_phase, s_abort));
         if (ok) {
           constexpr int CPR = D / 8;
@@ -506,6 +517,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       }
       if (!ok) {
         // every copy that was issued must land before shared memory is released
+        for (uint32_t w = 0; w < kWaitPolls && !mbar_try_wait(q_ready, 0); ++w) __nanosleep(64);
         for (int s = 0; s < NS; ++s)
           for (uint32_t w = 0; (pending >> s & 1u) && w < kWaitPolls; ++w) {
             if (mbar_try_wait(&full[s], parity >> s & 1u)) break;
@@ -639,8 +651,8 @@ __global__ void __launch_bounds__(256) paged_tiles_merge_kernel(const __grid_con
     before += __reduce_add_sync(0xffffffffu, s + lane < b ? o.row_tiles * o.chunks * p.hkv : 0);
   }
   const int row = (tok - (int)__ldg(p.cu_q + b)) * p.group + head % p.group;
-  const int i = sq.row_tiles - 1 - row / kTileRows;
-  const size_t first = ((size_t)before + (size_t)(head / p.group) * sq.chunks * sq.row_tiles + i) * kTileRows + row % kTileRows;
+  const int pair = 2 * tile_rows(p.group), i = sq.row_tiles - 1 - row / pair;
+  const size_t first = ((size_t)before + (size_t)(head / p.group) * sq.chunks * sq.row_tiles + i) * kTileRows + row % pair;
   const size_t step = (size_t)sq.row_tiles * kTileRows;
   const float2* stat = reinterpret_cast<const float2*>(p.tile_stat);
   float M = -INFINITY;
@@ -674,17 +686,18 @@ __global__ void __launch_bounds__(256) paged_tiles_merge_kernel(const __grid_con
 }
 
 template <typename T, int D>
-static cudaError_t launch_tiles_t(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int grid, cudaStream_t st) {
+static cudaError_t launch_tiles_t(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tq, int grid,
+                                  cudaStream_t st) {
   static PerDeviceFlag configured;
   const cudaError_t e = set_max_dynamic_smem(configured, reinterpret_cast<const void*>(paged_tiles_kernel<T, D>), TileCfg<D>::total);
   if (e != cudaSuccess) return e;
-  return launch_pdl(paged_tiles_kernel<T, D>, dim3(grid), dim3(kTileThreads), TileCfg<D>::total, st, tk, tv, p);
+  return launch_pdl(paged_tiles_kernel<T, D>, dim3(grid), dim3(kTileThreads), TileCfg<D>::total, st, tk, tv, tq, p);
 }
 
-cudaError_t launch_paged_tiles(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, int d, bool bf16, int grid,
-                               cudaStream_t st) {
-  if (d == 64) return bf16 ? launch_tiles_t<Bf16, 64>(p, tk, tv, grid, st) : launch_tiles_t<Fp16, 64>(p, tk, tv, grid, st);
-  return bf16 ? launch_tiles_t<Bf16, 128>(p, tk, tv, grid, st) : launch_tiles_t<Fp16, 128>(p, tk, tv, grid, st);
+cudaError_t launch_paged_tiles(const PagedProblem& p, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tq, int d,
+                               bool bf16, int grid, cudaStream_t st) {
+  if (d == 64) return bf16 ? launch_tiles_t<Bf16, 64>(p, tk, tv, tq, grid, st) : launch_tiles_t<Fp16, 64>(p, tk, tv, tq, grid, st);
+  return bf16 ? launch_tiles_t<Bf16, 128>(p, tk, tv, tq, grid, st) : launch_tiles_t<Fp16, 128>(p, tk, tv, tq, grid, st);
 }
 
 cudaError_t launch_paged_tiles_merge(const PagedProblem& p, int d, bool bf16, cudaStream_t st) {
