@@ -370,7 +370,8 @@ typedef struct {
 } tkphi_page_selection;
 
 /* Bytes of workspace (256-byte aligned device memory, contents irrelevant) of the paged calls; selection may be NULL
- * for TKPHI_WS_PAGED_ATTENTION.  0 on invalid arguments.  Enough for all shorter kv_lens of the same cu_q, too. */
+ * for TKPHI_WS_PAGED_ATTENTION.  0 on invalid arguments.  The size goes by this step's cu_q and kv_lens (host copies): ask
+ * for every step, or for those that the workspace has to serve; a call that finds it too small is refused. */
 size_t tkphi_paged_workspace_bytes(const tkphi_paged_desc* kv, const tkphi_page_selection* selection, int which);
 
 /*

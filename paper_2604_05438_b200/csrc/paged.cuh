@@ -41,6 +41,7 @@ struct PagedProblem {
   float* row_stat;                 // [..][16][2] their maximum (log2 units) and sum
   // page selection
   int n_keep, n_sink, n_tail, topk;
+  int scored;                      // the selection follows a scoring grid
   const void* bounds;              // [n_pages][hkv][2][d]
   float* page_scores;              // [units][key_stride] 32-bit bounds of the candidate pages
   unsigned long long* page_keys;   // [units][key_stride] their 64-bit bounds as ordered keys, where many are equal

@@ -195,7 +195,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
   }
   __syncthreads();
   // Inputs of the call may be read once all work before the call is complete.  The block form follows the selection,
-  // whose first grid has waited for that: only the page lists remain to be waited for, by the producer.
+  // which begins only then: the page lists alone remain to be waited for, by the producer.
   if (!BLOCK && !p.beside) pdl_wait();
   pdl_launch_next();
 

@@ -318,11 +318,12 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) paged_select_kernel(con
   __shared__ unsigned long long s_min64, s_max64;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int unit = blockIdx.x, tok = unit / p.hkv, h = unit % p.hkv;
+  // Behind the scoring grid this one starts when all of that has begun, which had waited for everything before it: the
+  // call's inputs may be read before the wait, here and in the grid that follows.  As the call's first grid it waits.
+  if (!p.scored) pdl_wait();
   pdl_launch_next();
   for (int i = tid; i < kPageBins; i += NT) s_hist[i] = 0;
   if (tid == 0) { s_border = 0; s_sure = 0; s_mag = 0; s_min = ~0u; s_max = 0; s_min64 = ~0ull; s_max64 = 0ull; }
-  // (the call's inputs may be read before the wait: this grid starts when the scoring grid has begun, which had waited
-  // for everything before it)
   const int b = paged_seq_of(p, tok);
   const Candidates c = candidates_of(p, b, tok);
   const int* table = p.table + (size_t)b * p.max_pages;
@@ -514,8 +515,9 @@ static cudaError_t select_nt(const PagedProblem& p, int n, cudaStream_t st) {
 }
 
 template <typename T, int D>
-static cudaError_t select_t(const PagedProblem& p, int n, int row_tiles, cudaStream_t st) {
-  if (n > p.topk && p.topk > 0) {
+static cudaError_t select_t(PagedProblem p, int n, int row_tiles, cudaStream_t st) {
+  p.scored = n > p.topk && p.topk > 0;
+  if (p.scored) {
     const cudaError_t e = launch_pdl(paged_score_kernel<T, D>, dim3(row_tiles * p.hkv, p.mag_parts), dim3(kScoreThreads), 0, st, p);
     if (e != cudaSuccess) return e;
   }

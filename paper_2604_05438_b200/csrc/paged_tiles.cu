@@ -117,7 +117,7 @@ struct TileCfg {
   static constexpr size_t ring = 2 * TILE;
   static constexpr size_t bars = ring + (size_t)NS * TILE;
   static constexpr size_t bar_bytes = 512;                   // barriers and four words
-  static_assert((NS + NV + 2 * NB + 6) * 8 + 8 + 11 * 4 <= bar_bytes, "barriers");
+  static_assert((NS + NV + 3 * NB + 5) * 8 + 8 + 11 * 4 <= bar_bytes, "barriers");
   static constexpr size_t total = bars + bar_bytes;
 };
 
@@ -183,8 +183,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   uint64_t* s_full = v_free + NV;          // [NB] scores complete
   uint64_t* p_ready = s_full + C::NB;      // [NB] P stored
   uint64_t* o_full = p_ready + C::NB;      // [2]  last product of the row tile complete
-  uint64_t* pv_done = o_full + 2;          // [1]  (three score buffers) products whose completion no scores tell
-  uint64_t* q_ready = pv_done + 1;         // [1]
+  uint64_t* pv_done = o_full + 2;          // [NB] products whose completion no scores tell (more score buffers than row tiles)
+  uint64_t* q_ready = pv_done + C::NB;     // [1]
   uint64_t* v_fixed = q_ready + 1;         // [1]  tail rows of the last value tile zeroed
   uint64_t* drained = v_fixed + 1;         // [1]  after a wait that ran out: the MMAs issued so far are complete
   int* misc = reinterpret_cast<int*>(drained + 1);
@@ -232,7 +232,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     for (int s = 0; s < NV; ++s) mbar_init(&v_free[s], 1);
     for (int i = 0; i < C::NB; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_ready[i], 4); }
     mbar_init(&o_full[0], 1); mbar_init(&o_full[1], 1);
-    mbar_init(pv_done, 1);
+    for (int i = 0; i < C::NB; ++i) mbar_init(&pv_done[i], 1);
     mbar_init(q_ready, 1);
     mbar_init(v_fixed, 1);
     mbar_init(drained, 1);
@@ -344,13 +344,17 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         if (__any_sync(0xffffffffu, grow)) {
           const float f = grow ? ex2_approx(m - cand) : 1.f;   // m = -inf: 0
           if (j > 0) {
-            // The product before this one must be complete.  With two score buffers these scores were issued after it;
-            // with three, the next scores were (or, where there are none, it has a barrier of its own).
-            if (C::NB == 3) {
-              const bool next = tiles == 2 && 2 * j + t + 1 < 2 * n;
+            // The product before this one must be complete.  With as many score buffers as row tiles these scores were
+            // issued after it.  With three buffers and two row tiles the next scores were (or, where there are none, it
+            // has a barrier of its own); with one row tile every product tells its buffer's barrier.  (One barrier for all
+            // would not do: up to three products may be pending here, and two phases look alike.)
+            if (tiles == 1) {
+              ok = __all_sync(0xffffffffu, mbar_wait(&pv_done[(j - 1) % C::NB], (uint32_t)((j - 1) / C::NB) & 1u, s_abort));
+              tc_fence_after_sync();
+            } else if (C::NB == 3) {
               const int nb = buf + 1 == C::NB ? 0 : buf + 1;
-              ok = __all_sync(0xffffffffu, next ? mbar_wait(&s_full[nb], nb ? phase : phase ^ 1u, s_abort)
-                                                : mbar_wait(pv_done, tiles == 2 ? 0u : (uint32_t)(j - 1) & 1u, s_abort));
+              ok = __all_sync(0xffffffffu, 2 * j + t + 1 < 2 * n ? mbar_wait(&s_full[nb], nb ? phase : phase ^ 1u, s_abort)
+                                                                 : mbar_wait(&pv_done[0], 0, s_abort));
               tc_fence_after_sync();
             }
 #pragma unroll
@@ -605,7 +609,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             if (sj < nu) issue_scores(st, buf);
             if (t + 1 == T2) tc_commit(&v_free[j % NV]);
             if (j + 1 == nu) tc_commit(&o_full[t]);
-            if (NB == 3 && (T2 == 1 || (t == 1 && j + 2 == nu))) tc_commit(pv_done);
+            if (T2 == 1) tc_commit(&pv_done[buf]);
+            else if (NB == 3 && t == 1 && j + 2 == nu) tc_commit(&pv_done[0]);
           }
           __syncwarp();
           if (++st == T2) { st = 0; ++sj; }
