@@ -173,6 +173,7 @@ struct AppendProblem {
   const long long* positions;      // [total_q] or null: the cache position of each token
   void* bounds;
   int* status;
+  long long total_q;
   int items;                       // CTAs per KV head: spans of 64 positions (or a page of 128) of all sequences, at most
 };
 cudaError_t launch_paged_append(const AppendProblem& p, bool bf16, cudaStream_t st);

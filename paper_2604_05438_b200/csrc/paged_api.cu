@@ -363,6 +363,7 @@ tkphi_status tkphi_paged_append(const tkphi_paged_desc* kv, const tkphi_append_d
   p.bounds = kv->key_bounds;
   p.status = kv->status;
   p.items = (int)items;
+  p.total_q = sh.total_q;
   cudaStream_t cs = reinterpret_cast<cudaStream_t>(cuda_stream);
   ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_APPEND);
   const cudaError_t e = launch_paged_append(p, kv->dtype == TKPHI_DTYPE_BF16, cs);

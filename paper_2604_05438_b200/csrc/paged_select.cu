@@ -10,7 +10,7 @@
 // those below t - 2e out whatever the errors are.  Only the pages between are evaluated in 64 bits, where a sum of
 // products of 16-bit floats does not round unless their exponents span more than about 25 binades, so that the order does
 // not depend on how it is split.  (In 32 bits alone, neighbours among thousands of pages swap; 64 bits for all pages took
-// 132 us where this takes XX: 236 tokens over 27K of 32 / 8 heads of 64.)
+// 132 us where this takes 30: 236 tokens over 27K of 32 / 8 heads of 64.)
 #include <climits>
 
 #include "paged.cuh"

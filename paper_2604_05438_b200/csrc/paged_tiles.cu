@@ -2,10 +2,10 @@
 //
 //   S = Q K^T (fp32, tensor memory), P = exp2(scale_log2 S - m) (16 bits), O = O + P V (fp32, tensor memory)
 //
-// with the running maximum m and sum of each row; y = O / sum.  A CTA owns 256 query rows of one KV head (tokens x
-// query heads of the group, so that the group's heads share every key and value tile) as two MMA tiles of 128 rows, and
-// a range of keys.  While the softmax warps of one tile work on its scores, the tensor pipe runs the other tile's
-// products.  Per tile of 128 keys and 128 rows: 2 * 128 * 128 * head_dim FMAs of tensor work against 16384
+// with a reference m and the running sum of each row; y = O / sum.  A CTA owns 256 query rows of one KV head (tokens x
+// query heads of the group, so that the group's heads share every key and value tile) as two MMA tiles of up to 128 rows
+// (whole tokens), and a range of keys.  While the softmax warps of one tile work on its scores, the tensor pipe runs the
+// other tile's products.  Per tile of 128 keys and 128 rows: 2 * 128 * 128 * head_dim FMAs of tensor work against 16384
 // exponentials, at 16 per clock and SM as long as the tensor work at head_dim 128 and twice as long at 64.
 //   warps 0-3, 4-7  softmax of row tile 0, 1: thread = row = tensor-memory lane, so that a row's sum needs no exchange.
 //                   P is written over the scores it came from and read from there as the A operand.
@@ -13,20 +13,25 @@
 //                   maximum of the first tile, and later tiles go straight from the score to exp2(score - m) without
 //                   looking for theirs.  A tile whose row sum passes a limit (2^40; fp16: 61440, below which no term
 //                   can overflow the type) is redone with its maximum as the new reference and O rescaled; nothing of
-//                   a row is lost on the way, because m never exceeds a score the row has seen.  (One thread issues
-//                   the MMAs in order, so a complete S says that the product before it is complete, too.)
-//                   Part of the exponentials are computed on the FMA pipes (exp2_pair), which halves the time of a
-//                   tile where the 16 per clock of the special-function unit bound it.
-//   warp 8          issues the MMAs: P V of a row tile as soon as its P is stored, then the next S of the tile.
-//   warp 9          TMA producer: page boxes of keys and values into one ring, in the order of their use; in the end
-//                   it zeroes the value rows behind the sequence's end (they may hold NaN, and 0 * NaN would reach the
-//                   sums).
-// fp16: P is scaled by 2^7, because without it probabilities below 2^-24 of the maximum vanish, and a
-// long context is made of those; the sum carries the same factor.
-// Rounding P to 16 bits is the only rounding besides the output's: its relative error per term is that of one 16-bit
-// rounding and averages out over the terms.  The sum is of the unrounded values.
+//                   a row is lost on the way, because m never exceeds a score the row has seen.
+//                   At head_dim 64 a quarter of the exponentials are computed on the FMA pipes (exp2_pair).
+//   warp 8          issues the MMAs: P V of a row tile as soon as its P is stored, then the next S into the same buffer.
+//   warp 9          TMA producer: the queries, then page boxes of keys and values into one ring, in the order of their
+//                   use; in the end it zeroes the value rows behind the sequence's end (they may hold NaN, and 0 * NaN
+//                   would reach the sums).
+// fp16: P is scaled by 2^7, because without it probabilities below 2^-24 of the maximum vanish, and a long context is made
+// of those; the sum carries the same factor.  Rounding P to 16 bits is the only rounding besides the output's: per term it
+// is that of one 16-bit rounding, and it averages out over the terms.  The sum is of the unrounded values.
 // Keys are cut into chunks when there are too few row tiles to fill the SMs evenly; partial outputs are joined in key
 // order by a second, dependent kernel.
+// What it measured (24 / 8 heads of 128, 2048 tokens at the end of 32K; 32 / 8 heads of 64, 4096 at the end of 32K):
+//   first version 954 / 565 TFLOP/s: the issuing thread needed 75 cycles per MMA, see there
+//   convergent issue 1218 / 701; three score buffers at head_dim 64, a burst of MMAs per step, fewer commits 1203 / 868
+//   queries by TMA 1166 / 895 (a group of 3 fills 126 of the 128 rows; whole prompts 5% faster)
+// Bound now: at head_dim 128 the tensor pipe at the clock that the power limit leaves (the measured sustained library rate
+// is 1344 TFLOP/s); at 64 the softmax warps' issue and special-function rate.  A CTA's set-up and its output take about 12K
+// cycles, which shows where contexts are short (5K-8K prompts: 745 TFLOP/s).  Two issuing warps were slower (1005 / 631):
+// the row tiles then run in phase and wait together.
 #include <climits>
 
 #include "paged.cuh"
