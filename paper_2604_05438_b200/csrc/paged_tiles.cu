@@ -27,7 +27,7 @@
 // What it measured (24 / 8 heads of 128, 2048 tokens at the end of 32K; 32 / 8 heads of 64, 4096 at the end of 32K):
 //   first version 954 / 565 TFLOP/s: the issuing thread needed 75 cycles per MMA, see there
 //   convergent issue 1218 / 701; three score buffers at head_dim 64, a burst of MMAs per step, fewer commits 1203 / 868
-//   queries by TMA 1166 / 895 (a group of 3 fills 126 of the 128 rows; whole prompts 5% faster)
+//   queries by TMA, join in runs of rows 1190 / 896 (a group of 3 fills 126 of the 128 rows)
 // Bound now: at head_dim 128 the tensor pipe at the clock that the power limit leaves (the measured sustained library rate
 // is 1344 TFLOP/s); at 64 the softmax warps' issue and special-function rate.  A CTA's set-up and its output take about 12K
 // cycles, which shows where contexts are short (5K-8K prompts: 745 TFLOP/s).  Two issuing warps were slower (1005 / 631):
@@ -644,55 +644,85 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   if (*s_abort && tid == 0) atomicExch(p.status, kStatusTimeout);
 }
 
-// Joins the key chunks of a row in key order: a warp per (token, query head).
+// Joins the key chunks of a row in key order.  A row is a (token, query head); a warp takes eight in a row, so that the
+// look-up of their sequence is paid once (a warp per row spent its time on that: 44 us instead of 26 for 49K rows of three
+// chunks), and the chunks of a row are loaded four at a time.
+constexpr int kJoinRows = 8;
 template <typename T, int D>
 __global__ void __launch_bounds__(256) paged_tiles_merge_kernel(const __grid_constant__ PagedProblem p) {
+  constexpr int V = D / 32;                  // dims of a lane
   pdl_wait();
   pdl_launch_next();
   const int lane = threadIdx.x & 31;
-  const int idx = blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (idx >= p.total_q * p.hq) return;
-  const int tok = idx / p.hq, head = idx % p.hq, b = paged_seq_of(p, tok);
-  const TileSeq sq = tile_seq_of(p, b);
-  if (sq.rows == 0 || sq.chunks == 1) return;
-  int before = 0;
-  for (int s = 0; s < b; s += 32) {
-    const TileSeq o = tile_seq_of(p, s + lane);
-    before += __reduce_add_sync(0xffffffffu, s + lane < b ? o.row_tiles * o.chunks * p.hkv : 0);
-  }
-  const int row = (tok - (int)__ldg(p.cu_q + b)) * p.group + head % p.group;
-  const int pair = 2 * tile_rows(p.group), i = sq.row_tiles - 1 - row / pair;
-  const size_t first = ((size_t)before + (size_t)(head / p.group) * sq.chunks * sq.row_tiles + i) * kTileRows + row % pair;
-  const size_t step = (size_t)sq.row_tiles * kTileRows;
-  const float2* stat = reinterpret_cast<const float2*>(p.tile_stat);
-  float M = -INFINITY;
-  for (int c = lane; c < sq.chunks; c += 32) M = fmaxf(M, __ldcg(stat + first + c * step).x);
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-  constexpr int V = D / 32;                  // dims of a lane
-  float a[V], L = 0.f;
-#pragma unroll
-  for (int e = 0; e < V; ++e) a[e] = 0.f;
-#pragma unroll 4
-  for (int c = 0; c < sq.chunks; ++c) {
-    const size_t s = first + c * step;
-    const float2 st = __ldcg(stat + s);
-    if (st.x == -INFINITY) continue;         // (its partial output was not written)
-    const float f = ex2_approx(st.x - M);
-    L += st.y * f;
-    if (D == 128) {
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(p.tile_part + s * D) + lane);
-      a[0] += v.x * f; a[1] += v.y * f; a[V - 2] += v.z * f; a[V - 1] += v.w * f;
-    } else {
-      const float2 v = __ldcg(reinterpret_cast<const float2*>(p.tile_part + s * D) + lane);
-      a[0] += v.x * f; a[1] += v.y * f;
+  int idx = (blockIdx.x * 8 + (threadIdx.x >> 5)) * kJoinRows;
+  const int end = idx + kJoinRows < p.total_q * p.hq ? idx + kJoinRows : p.total_q * p.hq;
+  if (idx >= end) return;
+  int tok = idx / p.hq, head = idx % p.hq, kv_head = head / p.group, g = head % p.group, tok_end = 0, tok_0 = 0;
+  const int pair = 2 * tile_rows(p.group);
+  TileSeq sq{0, 0, 1, 0};
+  size_t before = 0;
+  for (; idx < end; ++idx) {
+    if (tok >= tok_end) {                    // another sequence
+      const int b = paged_seq_of(p, tok);
+      sq = tile_seq_of(p, b);
+      tok_0 = (int)__ldg(p.cu_q + b);
+      tok_end = (int)__ldg(p.cu_q + b + 1);
+      int n = 0;
+      for (int s = 0; s < b; s += 32) {
+        const TileSeq o = tile_seq_of(p, s + lane);
+        n += __reduce_add_sync(0xffffffffu, s + lane < b ? o.row_tiles * o.chunks * p.hkv : 0);
+      }
+      before = n;
     }
+    if (sq.rows > 0 && sq.chunks > 1) {
+      const int row = (tok - tok_0) * p.group + g, i = row / pair;
+      const size_t first = (before + (size_t)kv_head * sq.chunks * sq.row_tiles + (sq.row_tiles - 1 - i)) * kTileRows + (row - i * pair);
+      const size_t step = (size_t)sq.row_tiles * kTileRows;
+      float M = -INFINITY, L = 0.f, a[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) a[e] = 0.f;
+      for (int c = 0; c < sq.chunks; c += 4) {
+        float2 st[4];
+        float v[4][V];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          st[x] = make_float2(-INFINITY, 0.f);
+          if (c + x < sq.chunks) {
+            st[x] = __ldcg(reinterpret_cast<const float2*>(p.tile_stat) + first + (c + x) * step);
+            const float* src = p.tile_part + (first + (c + x) * step) * D + lane * V;
+            if (V == 4) {
+              const float4 w = __ldcg(reinterpret_cast<const float4*>(src));
+              v[x][0] = w.x; v[x][1] = w.y; v[x][V - 2] = w.z; v[x][V - 1] = w.w;
+            } else {
+              const float2 w = __ldcg(reinterpret_cast<const float2*>(src));
+              v[x][0] = w.x; v[x][1] = w.y;
+            }
+          }
+        }
+        const float m = fmaxf(fmaxf(fmaxf(st[0].x, st[1].x), fmaxf(st[2].x, st[3].x)), M);
+        const float keep = M == -INFINITY ? 0.f : ex2_approx(M - m);
+        L *= keep;
+#pragma unroll
+        for (int e = 0; e < V; ++e) a[e] *= keep;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          if (st[x].x == -INFINITY) continue;             // (nothing seen: its partial output was not written)
+          const float f = ex2_approx(st[x].x - m);
+          L += st[x].y * f;
+#pragma unroll
+          for (int e = 0; e < V; ++e) a[e] = fmaf(v[x][e], f, a[e]);
+        }
+        M = m;
+      }
+      const float inv = L > 0.f ? 1.f / L : 0.f;
+      uint32_t* y = static_cast<uint32_t*>(p.y) + (size_t)idx * (D / 2) + lane * (V / 2);
+      y[0] = T::pack(a[0] * inv, a[1] * inv);
+      if (V == 4) y[1] = T::pack(a[V - 2] * inv, a[V - 1] * inv);
+      if (lane == 0 && p.lse) p.lse[idx] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+    }
+    if (++g == p.group) { g = 0; ++kv_head; }
+    if (++head == p.hq) { head = 0; kv_head = 0; g = 0; ++tok; }
   }
-  const float inv = L > 0.f ? 1.f / L : 0.f;
-  uint32_t* y = static_cast<uint32_t*>(p.y) + (size_t)idx * (D / 2) + lane * (V / 2);
-  y[0] = T::pack(a[0] * inv, a[1] * inv);
-  if (D == 128) y[1] = T::pack(a[V - 2] * inv, a[V - 1] * inv);
-  if (lane == 0 && p.lse) p.lse[idx] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
 }
 
 template <typename T, int D>
@@ -711,7 +741,7 @@ cudaError_t launch_paged_tiles(const PagedProblem& p, const CUtensorMap& tk, con
 }
 
 cudaError_t launch_paged_tiles_merge(const PagedProblem& p, int d, bool bf16, cudaStream_t st) {
-  const dim3 grid((p.total_q * p.hq + 7) / 8), block(256);
+  const dim3 grid((p.total_q * p.hq + 8 * kJoinRows - 1) / (8 * kJoinRows)), block(256);
   if (d == 64)
     return bf16 ? launch_pdl(paged_tiles_merge_kernel<Bf16, 64>, grid, block, 0, st, p)
                 : launch_pdl(paged_tiles_merge_kernel<Fp16, 64>, grid, block, 0, st, p);
