@@ -312,6 +312,8 @@ tkphi_status tkphi_decode_step_mlp(const tkphi_kv_desc* kv, const tkphi_mlp_desc
  *    receive rows must belong to one sequence of the batch; pages that are only read may be shared.
  *  - status: a device int32 owned by the caller and set to 0 by it; the kernels store an error there (a bad page, or
  *    TKPHI_ERR_TIMEOUT) and never clear it.  Required.
+ *  - A workspace serves one call at a time: calls that may overlap (other streams, captured graphs that are replayed side
+ *    by side) need workspaces of their own.
  *  - Slots at or behind a sequence's length may hold anything, NaN included: nothing read from them reaches a result.
  *  - key_bounds (optional; needed by tkphi_paged_block_attention): [n_pages][n_kv_heads][2][head_dim] in the cache's
  *    type, the element-wise minimum and maximum of each page's keys.
@@ -335,7 +337,7 @@ typedef struct {
 
 /* New tokens of one step.  Element (token row t, head h, dim c) of k_new is at t*stride_token + h*stride_head + c, and
  * so on; all pointers 16-byte aligned, all strides multiples of 8 elements (a fused projection's slices work as they
- * are).  q and q_out (both or neither): the step's queries, rotated into q_out, which may be q itself (same strides)
+ * are), none of them overlapping the cache.  q and q_out (both or neither): the step's queries, rotated into q_out, which may be q itself (same strides)
  * and otherwise must not overlap it. */
 typedef struct {
   const void* k_new; int64_t k_stride_token, k_stride_head;  /* [total_q][n_kv_heads][head_dim] */

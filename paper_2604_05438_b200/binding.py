@@ -281,8 +281,10 @@ class PagedKVCache:
                  cu_q_dev: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
         dev = k.device
         self.k, self.v, self.page_table, self.key_bounds, self.n_q_heads = k, v, page_table, key_bounds, n_q_heads
-        self.kv_lens = np.ascontiguousarray(kv_lens, dtype=np.int64)
-        self.cu_q = np.ascontiguousarray(cu_q, dtype=np.int64)
+        # the descriptor points to these copies, and calls are checked against them: they do not change any more
+        self.kv_lens, self.cu_q = np.array(kv_lens, dtype=np.int64), np.array(cu_q, dtype=np.int64)
+        self.kv_lens.setflags(write=False)
+        self.cu_q.setflags(write=False)
         assert k.dtype in _DTYPES and v.dtype == k.dtype and k.dim() == 4 and v.shape == k.shape
         assert k.stride() == v.stride() and k.stride(3) == 1
         assert self.kv_lens.ndim == 1 and self.cu_q.shape == (len(self.kv_lens) + 1,)
@@ -291,11 +293,11 @@ class PagedKVCache:
         if key_bounds is not None:
             assert key_bounds.dtype == k.dtype and key_bounds.is_contiguous()
             assert key_bounds.shape == (k.shape[0], k.shape[1], 2, k.shape[3])
-        self.kv_lens_dev = torch.from_numpy(self.kv_lens).to(dev) if kv_lens_dev is None else kv_lens_dev
-        self.cu_q_dev = torch.from_numpy(self.cu_q).to(dev) if cu_q_dev is None else cu_q_dev
+        self.kv_lens_dev = torch.tensor(self.kv_lens, device=dev) if kv_lens_dev is None else kv_lens_dev
+        self.cu_q_dev = torch.tensor(self.cu_q, device=dev) if cu_q_dev is None else cu_q_dev
         self.status = torch.zeros(1, dtype=torch.int32, device=dev) if status is None else status
-        assert self.kv_lens_dev.dtype == torch.int64 and self.kv_lens_dev.shape == self.kv_lens.shape
-        assert self.cu_q_dev.dtype == torch.int64 and self.cu_q_dev.shape == self.cu_q.shape
+        for t, a in ((self.kv_lens_dev, self.kv_lens), (self.cu_q_dev, self.cu_q)):
+            assert t.dtype == torch.int64 and t.shape == a.shape and t.is_contiguous()
         assert self.status.dtype == torch.int32 and self.status.numel() == 1
         for t in (v, page_table, key_bounds, self.kv_lens_dev, self.cu_q_dev, self.status):
             assert t is None or t.device == dev, "the cache, its page table and its lengths must be on one device"

@@ -77,6 +77,9 @@ tkphi_status validate_paged(const tkphi_paged_desc* kv, PagedShape* sh, bool nee
       return fail(TKPHI_ERR_INVALID_ARG, "k or v is NULL or not 16-byte aligned");
     if (!kv->page_table || !kv->kv_lens_dev || !kv->cu_q_dev || !kv->status)
       return fail(TKPHI_ERR_INVALID_ARG, "page_table, kv_lens_dev, cu_q_dev or status is NULL");
+    if ((reinterpret_cast<uintptr_t>(kv->page_table) | reinterpret_cast<uintptr_t>(kv->status)) & 3u ||
+        (reinterpret_cast<uintptr_t>(kv->kv_lens_dev) | reinterpret_cast<uintptr_t>(kv->cu_q_dev)) & 7u)
+      return fail(TKPHI_ERR_INVALID_ARG, "page_table, kv_lens_dev, cu_q_dev or status is not aligned to its type");
     if (kv->key_bounds && !aligned16(kv->key_bounds))
       return fail(TKPHI_ERR_INVALID_ARG, "key_bounds must be 16-byte aligned");
     const int64_t st[3] = {kv->stride_page, kv->stride_head, kv->stride_token};
@@ -327,6 +330,7 @@ tkphi_status tkphi_paged_append(const tkphi_paged_desc* kv, const tkphi_append_d
     return fail(TKPHI_ERR_UNSUPPORTED, "rot_dim must be a multiple of 16 in [0, head_dim], got %d", step->rot_dim);
   if (step->rot_dim > 0 && (!step->inv_freq || (reinterpret_cast<uintptr_t>(step->inv_freq) & 3u)))
     return fail(TKPHI_ERR_INVALID_ARG, "inv_freq is NULL or not 4-byte aligned");
+  if (reinterpret_cast<uintptr_t>(step->positions) & 7u) return fail(TKPHI_ERR_INVALID_ARG, "positions must be 8-byte aligned");
   if (step->pairs != 0 && step->pairs != 1) return fail(TKPHI_ERR_INVALID_ARG, "pairs must be 0 or 1, got %d", step->pairs);
   const int64_t strides[8] = {step->k_stride_token, step->k_stride_head, step->v_stride_token, step->v_stride_head,
                               step->q ? step->q_stride_token : 0, step->q ? step->q_stride_head : 0,

@@ -108,6 +108,51 @@ def test_block_attention_long_list_of_pages():
     U.check_attention("bf16", 64, y, lse, *want, n_keys=783 * 16)
 
 
+def _check_selected(s, dtype, sink, tail, topk):
+    y, lse, idx = U.gpu_block_attention(s, sink, tail, topk)
+    *want, pages = PO.block_attention(U.f64(s.q), U.f64(s.k), U.f64(s.v), s.table, s.kv_lens, s.cu_q,
+                                      np.nan_to_num(U.f64(s.bounds)), sink, tail, topk)
+    assert (idx == pages).all()
+    U.check_attention(dtype, s.q.shape[2], y, lse, *want, n_keys=(sink + tail + topk) * s.k.shape[2])
+
+
+@pytest.mark.parametrize("pages,topk", [(1500, 700), (1500, 20), (700, 650), (5000, 1000), (5000, 3)])
+def test_block_attention_hundreds_of_equal_bounds(pages, topk):
+    # more pages tie at the threshold than are ranked directly; a few are above and below
+    s = U.make_step(4, 1, 64, 16, "bf16", [(2, 16 * pages + 5)], seed=12, with_bounds=True)
+    s.bounds[:, :, 0], s.bounds[:, :, 1] = -1.0, 1.0
+    for p in (pages // 2, pages // 3):
+        s.bounds[s.table[0, p], :, 1] = 1.5
+    for p in (4, 5, 6):
+        s.bounds[s.table[0, p], :, 1] = 0.5
+    _check_selected(s, "bf16", 1, 2, topk)
+
+
+@pytest.mark.parametrize("topk", [30, 600])
+def test_block_attention_bounds_that_32_bits_do_not_tell_apart(topk):
+    # pages whose bounds differ by one unit of a small element beside large ones: their order is in the last bits
+    s = U.make_step(2, 1, 128, 16, "bf16", [(1, 16 * 1200 + 9)], seed=13, with_bounds=True)
+    g = torch.Generator().manual_seed(14)
+    s.bounds[:, :, 0], s.bounds[:, :, 1] = -1.0, 8.0
+    n = int(s.table.max()) + 1
+    s.bounds[:n, :, 1, 64:] = (2.0 ** -12 * (1 + torch.randint(0, 64, (n, 1, 64), generator=g) / 128)).bfloat16()
+    _check_selected(s, "bf16", 2, 1, topk)
+
+
+def test_block_attention_scores_too_large_for_32_bits():
+    s = U.make_step(2, 1, 64, 16, "bf16", [(1, 16 * 100 + 9)], seed=15, with_bounds=True)
+    s.bounds *= 2.0 ** 100
+    s.q *= 2.0 ** 30
+    s.k *= 2.0 ** -30
+    _check_selected(s, "bf16", 1, 1, 9)
+
+
+@pytest.mark.parametrize("pages,topk", [(9000, 20), (42000, 50)])
+def test_block_attention_over_very_many_pages(pages, topk):
+    s = U.make_step(2, 1, 64, 16, "fp16", [(1, 16 * pages + 3)], seed=16, with_bounds=True)
+    _check_selected(s, "fp16", 1, 2, topk)
+
+
 # ---------------------------------------------------------------------------------------------- append
 def _append_inputs(s, seed, packed):
     g = torch.Generator().manual_seed(seed)

@@ -62,6 +62,7 @@ ALL = (_attend, _block, _append)
     (dict(k=0), -1), (dict(v=0x2008), -1), (dict(table=0), -1), (dict(kv_dev=0), -1), (dict(cu_dev=0), -1), (dict(status=0), -1),
     (dict(strides=(2048, 1024, 60)), -1), (dict(strides=(2048, 1024, 56)), -1), (dict(strides=(2048, 1024, -64)), -1),
     (dict(strides=(2048, 960, 64)), -1), (dict(strides=(2000, 1024, 64)), -1), (dict(strides=(0, 1024, 64)), -1),
+    (dict(table=0x3002), -1), (dict(kv_dev=0x4004), -1), (dict(cu_dev=0x5004), -1), (dict(status=0x7001), -1),
     (dict(bounds=0x6008), -1), (dict(cu=[0, 2, 1]), -1), (dict(cu=[1, 2, 3]), -1), (dict(kv=[-1, 64]), -1),
     (dict(kv=[100, 513]), -1), (dict(kv=[100, 2]), -1), (dict(kv=[1 << 40, 64]), -1), (dict(cu=[0, 1 << 40, 1 << 41]), -1),
 ])
@@ -105,7 +106,7 @@ def test_bad_arguments_of_append(lib):
     d = Desc()
     assert lib.tkphi_paged_append(d.ref, None, None) == -1
     for bad in (dict(k_new=0), dict(v_new=0x20008), dict(q=0), dict(q_out=0), dict(q=0x30008), dict(q_out=0x40004),
-                dict(inv_freq=0), dict(inv_freq=0x50002), dict(pairs=2), dict(k_stride_token=60), dict(v_stride_head=-64),
+                dict(inv_freq=0), dict(inv_freq=0x50002), dict(pairs=2), dict(positions=0x60004), dict(k_stride_token=60), dict(v_stride_head=-64),
                 dict(o_stride_head=0), dict(o_stride_token=448), dict(q_out=0x30000, o_stride_token=520)):
         assert _append(lib, d, **bad) == -1, bad
     for rot in (8, 24, 80, -16):
@@ -146,6 +147,16 @@ def test_workspace_sizes(lib):
     assert _attend(lib, d, ws_bytes=n - 1) == -3 and b"needed" in lib.tkphi_last_error()
     n = size(d, T.WS_PAGED_BLOCK_ATTENTION, (1, 1, 4))
     assert _block(lib, d, ws_bytes=n - 1) == -3
+
+
+def test_the_binding_keeps_its_own_lengths():
+    k = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+    lens, cu = np.array([20]), np.array([0, 1])
+    kv = T.PagedKVCache(k, k.clone(), torch.zeros(1, 4, dtype=torch.int32), lens, cu, 4)
+    lens[0], cu[1] = 10 ** 9, 10 ** 6
+    assert kv.kv_lens[0] == 20 and kv.total_q == 1
+    with pytest.raises(ValueError):
+        kv.cu_q[1] = 5
 
 
 def test_the_binding_refuses_tensors_of_another_device_type_or_shape(lib):
