@@ -42,6 +42,7 @@ struct PagedProblem {
   // page selection
   int n_keep, n_sink, n_tail, topk;
   int scored;                      // the selection follows a scoring grid
+  int held;                        // scores that the selecting CTAs have shared memory for (a multiple of 4)
   const void* bounds;              // [n_pages][hkv][2][d]
   float* page_scores;              // [units][key_stride] 32-bit bounds of the candidate pages
   unsigned long long* page_keys;   // [units][key_stride] their 64-bit bounds as ordered keys, where many are equal

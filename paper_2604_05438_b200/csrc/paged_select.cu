@@ -300,7 +300,10 @@ __device__ __forceinline__ unsigned long long exact_bound(const PagedProblem& p,
   return (x >> 63) ? ~x : (x | (1ull << 63));
 }
 
-constexpr int kHeldScores = 40960;         // scores that a selecting CTA keeps in shared memory
+// Scores that a selecting CTA keeps in shared memory at most.  What a launch gets goes by its longest sequence; every CTA of
+// it goes by what the launch got (its own token may see fewer pages: a shorter sequence, a replay with other lengths).
+constexpr int kHeldScores = 40960;
+static int held_scores(int n) { return n < 1 ? 4 : n < kHeldScores ? (n + 3) & ~3 : kHeldScores; }
 
 // Exact topk of the unit's pages, one CTA per unit, scores in shared memory (in global memory where there are more).
 // Loops are left rolled: the kernel is short enough for instruction fetches to count.
@@ -336,7 +339,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) paged_select_kernel(con
   __syncthreads();
   pdl_wait();
   const float* scores = p.page_scores + (size_t)unit * p.key_stride;       // (16-byte aligned: the stride is a multiple of 4)
-  const bool in_smem = c.n <= kHeldScores;
+  const bool in_smem = c.n <= p.held;
   uint32_t top_key = 0;                                 // the largest of this thread's keys
   // four scores as keys; those behind the last page as 0, which no score gives
   auto four = [&](const float4& v, int i) {
@@ -506,12 +509,12 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) paged_select_kernel(con
 }
 
 template <typename T, int D, int NT>
-static cudaError_t select_nt(const PagedProblem& p, int n, cudaStream_t st) {
+static cudaError_t select_nt(PagedProblem p, int n, cudaStream_t st) {
   static PerDeviceFlag configured;
   const cudaError_t e = set_max_dynamic_smem(configured, reinterpret_cast<const void*>(paged_select_kernel<T, D, NT>), kHeldScores * 4);
   if (e != cudaSuccess) return e;
-  const size_t held = n > kHeldScores ? 4 : n > 0 ? ((size_t)n + 3) & ~(size_t)3 : 4;
-  return launch_pdl(paged_select_kernel<T, D, NT>, dim3(p.total_q * p.hkv), dim3(NT), held * 4, st, p);
+  p.held = held_scores(n);
+  return launch_pdl(paged_select_kernel<T, D, NT>, dim3(p.total_q * p.hkv), dim3(NT), (size_t)p.held * 4, st, p);
 }
 
 template <typename T, int D>
