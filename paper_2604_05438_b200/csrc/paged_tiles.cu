@@ -63,12 +63,13 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 // exp2 of two values on the FMA and integer pipes: x = n + f with n the nearest integer, |f| <= 1/2, 2^f by the
 // Chebyshev interpolation polynomial of degree 5 (relative error below 2^-22: the terms of the series beyond it,
 // (ln 2 / 2)^6 / 6! = 2.4e-6, shrink by 2^5 when the six nodes are Chebyshev's), n added to the exponent field.
-// Below -126 the result is 2^-126.
+// Below -126 the result is 2^-126.  Above 127, where n would run into the sign, it is 2^127, which fails a row sum's limit
+// (2^40 or less), so that the tile is redone with its maximum as the reference.
 __device__ __forceinline__ uint64_t exp2_pair(uint64_t x2) {
   constexpr float c0 = 1.000000075e+00f, c1 = 6.931471880e-01f, c2 = 2.402210749e-01f, c3 = 5.550357114e-02f, c4 = 9.676031918e-03f, c5 = 1.339086336e-03f;
   float x, y;
   unpack2(x2, x, y);
-  x2 = pack2(fmaxf(x, -126.f), fmaxf(y, -126.f));
+  x2 = pack2(fminf(fmaxf(x, -126.f), 127.f), fminf(fmaxf(y, -126.f), 127.f));
   const uint64_t magic = pack2(12582912.f, 12582912.f), minus = pack2(-1.f, -1.f);      // 1.5 * 2^23: the sum's low bits are n
   const uint64_t t = add2(x2, magic);
   const uint64_t n = add2(t, pack2(-12582912.f, -12582912.f));

@@ -53,3 +53,67 @@ def test_a_selection_captured_for_very_many_pages_is_replayed_for_fewer():
         want, pages = _want_selected(short, 1, 2, 50)
         assert (idx.cpu().numpy() == pages).all()
         U.check_attention("bf16", 64, U.f64(y), U.f64(lse), *want, n_keys=53 * 16)
+
+
+# ---------------------------------------------------------------------------------------------- range of the scores
+def _one_high_key(d, dtype, high, at, q_len, kv_len, group=1):
+    """A sequence per entry of `high`: all keys score about 0 but the one at position at[i], which scores high[i] (scale 1)."""
+    s = U.make_step(group, 1, d, 32, dtype, [(q_len, kv_len)] * len(high), seed=110)
+    s.q = (0.25 * s.q.float()).to(s.q.dtype)
+    s.q[:, :, 0] = 16.0
+    s.k[:, :, :, 0] = torch.where(s.k[:, :, :, 0].isnan(), s.k[:, :, :, 0], 0.0)
+    for b, (x, t) in enumerate(zip(high, at)):
+        s.k[s.table[b, t // 32], 0, t % 32] = 0.0
+        s.k[s.table[b, t // 32], 0, t % 32, 0] = x / 16
+    return s
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("gap", [80, 92, 150, 200, 300, 500])
+def test_one_key_far_above_the_first_tile_at_every_offset_of_a_tile(d, dtype, gap):
+    s = _one_high_key(d, dtype, [gap] * 128, [128 + o for o in range(128)], 17, 530)
+    y, lse = U.gpu_attention(s, scale=1.0)
+    want = PO.attention(U.f64(s.q), U.f64(s.k), U.f64(s.v), s.table, s.kv_lens, s.cu_q, True, 1.0)
+    U.check_attention(dtype, d, y, lse, *want, n_keys=530)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_scores_of_a_wide_random_spread(d, dtype):
+    s = U.make_step(8, 2, d, 32, dtype, [(40, 2100), (3, 900)], seed=111, key_scale=8.0)
+    s.q = (12 * s.q.float()).to(s.q.dtype)
+    y, lse = U.gpu_attention(s)
+    want = PO.attention(U.f64(s.q), U.f64(s.k), U.f64(s.v), s.table, s.kv_lens, s.cu_q)
+    U.check_attention(dtype, d, y, lse, *want, n_keys=2100)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype,low", [("bf16", -118.0), ("fp16", -28.0)])
+def test_the_exponential_over_its_range(d, dtype, low):
+    # a sequence per exponent x: the keys of the first tile score 0, one behind it x (in powers of two), and only that one has
+    # a value in dim 0, so that y[0] = 2^x / (sum): down to the smallest x whose power the products' type holds.  fp16: scaled
+    # by 2^7 there (x >= -21 is a normal number)
+    x = torch.linspace(low, 126.0, 245).bfloat16().double().tolist()
+    at = [128 + (37 * i) % 128 for i in range(len(x))]
+    s = U.make_step(1, 1, d, 32, dtype, [(17, 300)] * len(x), seed=112)
+    for t in (s.q, s.k, s.v):
+        t[~t.isnan()] = 0.0
+    s.q[:, :, 0] = 1.0
+    for b in range(len(x)):
+        s.k[s.table[b, at[b] // 32], 0, at[b] % 32, 0] = x[b]
+        s.v[s.table[b, :9], :, :, 1] = 1.0
+        s.v[s.table[b, at[b] // 32], 0, at[b] % 32, :2] = torch.tensor([1.0, 0.0]).to(s.v.dtype)
+    y, lse = U.gpu_attention(s, scale=float(np.log(2.0)))
+    want, want_lse, A, C = PO.attention(U.f64(s.q), U.f64(s.k), U.f64(s.v), s.table, s.kv_lens, s.cu_q, True, float(np.log(2.0)))
+    # fp16: a product below 2^-14 is off by up to 2^-25, 2^-32 of the reference key's weight, so 300 keys by 300 2^-32
+    more = 300 * 2.0 ** -32 if dtype == "fp16" else 0.0
+    U.check_attention(dtype, d, y - np.clip(y - want, -more, more), lse, want, want_lse, A, C, n_keys=300)
+    # relative where check_attention is absolute: two roundings to 16 bits, the score's error (one product: 2^-23 of it
+    # twice), the polynomial's and the sum's
+    u = torch.finfo(U.DT[dtype]).eps / 2
+    X = np.repeat(np.abs(np.array(x)), 17)
+    tol = (2 * u + X * 2.0 ** -22 + 2.0 ** -20 + 300 * 2.0 ** -24) * want[:, 0, 0]
+    if dtype == "fp16":
+        tol = tol + 2.0 ** -25 + more
+    assert (np.abs(y[:, 0, 0] - want[:, 0, 0]) <= tol).all()
