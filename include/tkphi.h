@@ -381,7 +381,8 @@ size_t tkphi_paged_workspace_bytes(const tkphi_paged_desc* kv, const tkphi_page_
  * token's own position included), all new tokens of all sequences in one call, whatever mix of lengths.
  *   q     [total_q][n_q_heads][head_dim], y_out likewise, both in the cache's type, contiguous, 16-byte aligned.
  *   lse   fp32 [total_q][n_q_heads] or NULL: log of the softmax denominator, log sum exp(scale q.k), with which
- *         results over disjoint sets of keys can be joined.  A token that sees nothing gets y = 0, lse = -inf.
+ *         results over disjoint sets of keys can be joined.  A token that sees nothing (no keys, or none whose score
+ *         is above -inf) gets y = 0, lse = -inf; one with a score that is no number or +inf gets NaN in both.
  *   scale 0 for 1/sqrt(head_dim), else finite and positive.
  *   flags TKPHI_FLAG_FULL_CONTEXT or 0.
  */

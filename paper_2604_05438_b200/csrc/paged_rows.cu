@@ -418,7 +418,8 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         MA = fmaxf(MA, stat[(i * kRowTile + rA) * 2]);
         MB = fmaxf(MB, stat[(i * kRowTile + rB) * 2]);
       }
-      const float sA = mA == -INFINITY ? 0.f : ex2_approx(mA - MA), sB = mB == -INFINITY ? 0.f : ex2_approx(mB - MB);
+      // (a warp that has seen nothing has the sum 0; one that has seen no numbers alone has no maximum, but no 0 either)
+      const float sA = lA == 0.f ? 0.f : ex2_approx(mA - MA), sB = lB == 0.f ? 0.f : ex2_approx(mB - MB);
       constexpr int PER = 32 / kRowWarps, TPR = 64 / PER;      // dims of a thread, threads of a row
       const int row = tid / TPR, dp = tid % TPR * PER;
       float M = -INFINITY, L = 0.f;
@@ -426,8 +427,8 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       for (int i = 0; i < kRowWarps; ++i) M = fmaxf(M, stat[(i * kRowTile + row) * 2]);
 #pragma unroll
       for (int i = 0; i < kRowWarps; ++i) {
-        const float m = stat[(i * kRowTile + row) * 2];
-        if (m != -INFINITY) L += stat[(i * kRowTile + row) * 2 + 1] * ex2_approx(m - M);
+        const float l = stat[(i * kRowTile + row) * 2 + 1];
+        if (l != 0.f) L += l * ex2_approx(stat[(i * kRowTile + row) * 2] - M);
       }
       const bool fin = w.whole();              // in a cluster: the unit is this CTA's alone
       const int slot = w.slot(cta);
@@ -455,7 +456,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             a[e] += u.x; a[e + 1] += u.y; a[e + 2] += u.z; a[e + 3] += u.w;
           }
         if (row < w.rows) {
-          const float inv = L > 0.f ? 1.f / L : 0.f;
+          const float inv = L != 0.f ? 1.f / L : 0.f;
           float* part = (SPLIT ? keep + (size_t)row * D : p.row_part + ((size_t)slot * kRowTile + row) * D) + x * 64 + dp;
 #pragma unroll
           for (int e = 0; e < PER; e += 4) {
@@ -470,7 +471,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       }
       if (tid % TPR == 0 && row < w.rows) {
         if (fin) {
-          if (p.lse) p.lse[out_row] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+          if (p.lse) p.lse[out_row] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
         } else {
           float* st = SPLIT ? keep_stat + row * 2 : p.row_stat + ((size_t)slot * kRowTile + row) * 2;
           st[0] = M;
@@ -508,18 +509,18 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
           if (i < pieces) M = fmaxf(M, st[i].x);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float f = i < pieces && st[i].x != -INFINITY ? ex2_approx(st[i].x - M) : 0.f;
+          const float f = i < pieces && st[i].y != 0.f ? ex2_approx(st[i].x - M) : 0.f;
           L += st[i].y * f;
 #pragma unroll
           for (int e = 0; e < V / 2; ++e) { a[2 * e] += v[i][e].x * f; a[2 * e + 1] += v[i][e].y * f; }
         }
-        const float inv = L > 0.f ? 1.f / L : 0.f;
+        const float inv = L != 0.f ? 1.f / L : 0.f;
         const int r = w.r_first + row;
         const size_t out_row = (size_t)(w.tok0 + r / p.group) * p.hq + w.h * p.group + r % p.group;
         uint32_t* y = static_cast<uint32_t*>(p.y) + out_row * (D / 2) + lane * (V / 2);
 #pragma unroll
         for (int e = 0; e < V / 2; ++e) y[e] = T::pack(a[2 * e] * inv, a[2 * e + 1] * inv);
-        if (lane == 0 && p.lse) p.lse[out_row] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+        if (lane == 0 && p.lse) p.lse[out_row] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
       }
     }
     __syncwarp();
@@ -606,7 +607,7 @@ __global__ void __launch_bounds__(kMergeThreads) paged_rows_merge_kernel(const _
     L *= g; a0 *= g; a1 *= g;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      const float f = st[x].x == -INFINITY ? 0.f : ex2_approx(st[x].x - m);
+      const float f = st[x].y == 0.f ? 0.f : ex2_approx(st[x].x - m);
       L += st[x].y * f;
       a0 += v[x].x * f;
       a1 += v[x].y * f;
@@ -622,16 +623,16 @@ __global__ void __launch_bounds__(kMergeThreads) paged_rows_merge_kernel(const _
   for (int i = 0; i < GROUPS; ++i) M = fmaxf(M, s_stat[i][0]);
 #pragma unroll
   for (int i = 0; i < GROUPS; ++i) {
-    const float f = s_stat[i][0] == -INFINITY ? 0.f : ex2_approx(s_stat[i][0] - M);
+    const float f = s_stat[i][1] == 0.f ? 0.f : ex2_approx(s_stat[i][0] - M);
     const float2 v = s_acc[i][d];
     L += s_stat[i][1] * f;
     a0 += v.x * f;
     a1 += v.y * f;
   }
-  const float inv = L > 0.f ? 1.f / L : 0.f;
+  const float inv = L != 0.f ? 1.f / L : 0.f;
   const size_t out_row = (size_t)(tok0 + r / p.group) * p.hq + h * p.group + r % p.group;
   reinterpret_cast<uint32_t*>(p.y)[out_row * (D / 2) + d] = T::pack(a0 * inv, a1 * inv);
-  if (d == 0 && p.lse) p.lse[out_row] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+  if (d == 0 && p.lse) p.lse[out_row] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
 }
 
 template <typename T, int D, bool BLOCK, bool SPLIT>

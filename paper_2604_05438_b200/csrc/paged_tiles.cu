@@ -64,12 +64,18 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 // Chebyshev interpolation polynomial of degree 5 (relative error below 2^-22: the terms of the series beyond it,
 // (ln 2 / 2)^6 / 6! = 2.4e-6, shrink by 2^5 when the six nodes are Chebyshev's), n added to the exponent field.
 // Below -126 the result is 2^-126.  Above 127, where n would run into the sign, it is 2^127, which fails a row sum's limit
-// (2^40 or less), so that the tile is redone with its maximum as the reference.
+// (2^40 or less), so that the tile is redone with its maximum as the reference.  What is no number stays none until the
+// integer addition, which makes a number near 2^128 of it: that fails the limit as well, and the redone sum is none.
+__device__ __forceinline__ float exp2_range(float x) {
+  float r;
+  asm("max.NaN.f32 %0, %1, 0fC2FC0000;\n\tmin.NaN.f32 %0, %0, 0f42FE0000;" : "=f"(r) : "f"(x));      // [-126, 127]
+  return r;
+}
 __device__ __forceinline__ uint64_t exp2_pair(uint64_t x2) {
   constexpr float c0 = 1.000000075e+00f, c1 = 6.931471880e-01f, c2 = 2.402210749e-01f, c3 = 5.550357114e-02f, c4 = 9.676031918e-03f, c5 = 1.339086336e-03f;
   float x, y;
   unpack2(x2, x, y);
-  x2 = pack2(fminf(fmaxf(x, -126.f), 127.f), fminf(fmaxf(y, -126.f), 127.f));
+  x2 = pack2(exp2_range(x), exp2_range(y));
   const uint64_t magic = pack2(12582912.f, 12582912.f), minus = pack2(-1.f, -1.f);      // 1.5 * 2^23: the sum's low bits are n
   const uint64_t t = add2(x2, magic);
   const uint64_t n = add2(t, pack2(-12582912.f, -12582912.f));
@@ -408,7 +414,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       const bool live = row_of(row);
       if (w->chunks == 1) {
         const size_t out_row = live ? ((size_t)w->tok0 + row / p.group) * p.hq + (size_t)w->h * p.group + row % p.group : 0;
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const float inv = l != 0.f ? 1.f / l : 0.f;          // (a sum that is no number: so are y and lse)
         uint4* y = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.y) + out_row * D);
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
@@ -420,17 +426,17 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             uint4 v = make_uint4(0, 0, 0, 0);
-            if (l > 0.f) {
+            if (l != 0.f) {
               v.x = T::pack(o[8 * e] * inv, o[8 * e + 1] * inv); v.y = T::pack(o[8 * e + 2] * inv, o[8 * e + 3] * inv);
               v.z = T::pack(o[8 * e + 4] * inv, o[8 * e + 5] * inv); v.w = T::pack(o[8 * e + 6] * inv, o[8 * e + 7] * inv);
             }
             if (live) y[c * 4 + e] = v;
           }
         }
-        if (live && p.lse) p.lse[out_row] = l > 0.f ? (m - kShift + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        if (live && p.lse) p.lse[out_row] = l != 0.f ? (m - kShift + log2f(l)) * 0.6931471805599453f : -INFINITY;
       } else {
         const size_t slot_row = (size_t)cta * kTileRows + t * t_rows + (tid & 127);
-        if (live) reinterpret_cast<float2*>(p.tile_stat)[slot_row] = make_float2(l > 0.f ? m - kShift : -INFINITY, l);
+        if (live) reinterpret_cast<float2*>(p.tile_stat)[slot_row] = make_float2(l != 0.f ? m - kShift : -INFINITY, l);
         if (nt > 0) {
           float* dst = p.tile_part + slot_row * D;
 #pragma unroll
@@ -707,7 +713,7 @@ __global__ void __launch_bounds__(256) paged_tiles_merge_kernel(const __grid_con
         for (int e = 0; e < V; ++e) a[e] *= keep;
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          if (st[x].x == -INFINITY) continue;             // (nothing seen: its partial output was not written)
+          if (st[x].y == 0.f) continue;                   // (nothing seen: its partial output was not written)
           const float f = ex2_approx(st[x].x - m);
           L += st[x].y * f;
 #pragma unroll
@@ -715,11 +721,11 @@ __global__ void __launch_bounds__(256) paged_tiles_merge_kernel(const __grid_con
         }
         M = m;
       }
-      const float inv = L > 0.f ? 1.f / L : 0.f;
+      const float inv = L != 0.f ? 1.f / L : 0.f;
       uint32_t* y = static_cast<uint32_t*>(p.y) + (size_t)idx * (D / 2) + lane * (V / 2);
       y[0] = T::pack(a[0] * inv, a[1] * inv);
       if (V == 4) y[1] = T::pack(a[V - 2] * inv, a[V - 1] * inv);
-      if (lane == 0 && p.lse) p.lse[idx] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+      if (lane == 0 && p.lse) p.lse[idx] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
     }
     if (++g == p.group) { g = 0; ++kv_head; }
     if (++head == p.hq) { head = 0; kv_head = 0; g = 0; ++tok; }

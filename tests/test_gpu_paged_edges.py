@@ -117,3 +117,79 @@ def test_the_exponential_over_its_range(d, dtype, low):
     if dtype == "fp16":
         tol = tol + 2.0 ** -25 + more
     assert (np.abs(y[:, 0, 0] - want[:, 0, 0]) <= tol).all()
+
+
+# ---------------------------------------------------------------------------------------------- values that are no numbers
+def _check_rows(dtype, d, y, lse, want, n_keys):
+    """Rows whose sum is no number: y and lse are NaN.  The others as ever (C without the keys whose score is -inf)."""
+    w, want_lse, A, C = (x.reshape(-1, *x.shape[2:]) for x in want)
+    y, lse = y.reshape(w.shape), lse.reshape(want_lse.shape)
+    none = np.isnan(want_lse)
+    np.testing.assert_array_equal(np.isnan(lse), none)
+    assert np.isnan(y[none]).all()
+    C = np.where(np.isfinite(C), C, 60.0)
+    U.check_attention(dtype, d, y[~none], lse[~none], w[~none], want_lse[~none], A[~none], C[~none], n_keys)
+    return none
+
+
+# steps that reach every form: clusters, the line with its join, many rows with and without cuts over the keys
+WAYS = [([(1, 500)] * 4, 4, 2), ([(1, 20011)], 4, 1), ([(3, 1500), (1, 900), (2, 65)], 4, 2), ([(45, 7001)], 4, 1),
+        ([(60, 700), (33, 33), (1, 300)], 6, 2), ([(300, 300)], 3, 1)]
+
+
+def _step_of(way, d, dtype, seed):
+    lens, hq, hkv = WAYS[way]
+    return U.make_step(hq, hkv, d, 32, dtype, lens, seed=seed, with_bounds=True)
+
+
+def _attend_both(s):
+    y, lse = U.gpu_attention(s)
+    with np.errstate(all="ignore"):
+        return y, lse, PO.attention(U.f64(s.q), U.f64(s.k), U.f64(s.v), s.table, s.kv_lens, s.cu_q)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("way", range(len(WAYS)))
+def test_a_query_that_is_no_number_makes_its_row_none(way, d, dtype):
+    s = _step_of(way, d, dtype, 120)
+    T, hq = s.q.shape[:2]
+    s.q[T // 2, hq - 1, 3] = float("nan")
+    none = _check_rows(dtype, d, *_attend_both(s), int(s.kv_lens.max()))
+    assert none.sum() == 1
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("what", ["nan", "inf"])
+@pytest.mark.parametrize("way", range(len(WAYS)))
+def test_a_key_that_is_no_number_makes_the_rows_that_see_it_none(way, what, d, dtype):
+    # (an infinite one: rows whose score is -inf are without it; +inf is no number in the softmax)
+    s = _step_of(way, d, dtype, 121)
+    n = int(s.kv_lens[0])
+    for t in {n // 3, n - 1, min(n - 1, 136)}:
+        s.k[s.table[0, t // 32], 0, t % 32, 5] = float(what)
+    none = _check_rows(dtype, d, *_attend_both(s), int(s.kv_lens.max()))
+    assert what == "inf" or none.any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("o", [0, 1, 2, 7, 64, 120])
+def test_one_key_that_is_no_number_at_any_offset_of_a_tile(o, d, dtype):
+    s = U.make_step(4, 1, d, 32, dtype, [(20, 600), (40, 300)], seed=124)
+    s.k[s.table[0, (256 + o) // 32], 0, (256 + o) % 32, 9] = float("nan")
+    none = _check_rows(dtype, d, *_attend_both(s), 600)
+    assert none.sum() == 80
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens", [[(1, 20011), (1, 300)], [(1, 4000), (1, 300)], [(45, 7001), (20, 300)]])
+def test_pieces_of_a_row_whose_keys_are_all_no_numbers(lens, d, dtype):
+    # whole warps, tiles and chunks without a single number
+    s = U.make_step(4, 1, d, 32, dtype, lens, seed=122)
+    for p in range(64, 96):
+        s.k[s.table[0, p]] = float("nan")
+    none = _check_rows(dtype, d, *_attend_both(s), int(s.kv_lens.max()))
+    assert none.any() and not none.all()
