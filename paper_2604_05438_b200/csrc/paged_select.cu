@@ -206,9 +206,11 @@ constexpr int kBorder = 512;               // pages between in and out that are 
 // `count` equal to it `need`.
 template <typename K>
 struct Threshold { K prefix; int top, need, count; };
+constexpr int kAllBits = 64;               // passes of any search that is to know every bit
 
 // Whole CTA; the keys that matter are in [mn, mx], smaller ones are passed over.  each(fn) calls fn(key) for this thread's
-// keys.  Stops after `passes`, when at most `enough` keys equal the prefix, or exactly as many as are needed.  s_hist:
+// keys.  Stops after `passes`, when at most `enough` keys equal the prefix, exactly as many as are needed, or when all bits
+// of the keys are known (kAllBits passes at most).  s_hist:
 // kPageBins zeros on entry and on return.
 template <typename K, int NT, typename Each>
 __device__ __forceinline__ Threshold<K> find_threshold(Each each, K mn, K mx, int need, int count, int enough, int passes,
@@ -400,9 +402,9 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) paged_select_kernel(con
           if (max(max(k.x, k.y), max(k.z, k.w)) >= floor_key) { fn(k.x); fn(k.y); fn(k.z); fn(k.w); }
         }
       },
-      floor_key, s_max, p.topk, c.n, NW, 4, s_hist, s_sum, s_out);
+      floor_key, s_max, p.topk, c.n, NW, kAllBits, s_hist, s_sum, s_out);
   // (the k-th largest score lies in [prefix, prefix + 1) << top: both ends widen the range)
-  const uint32_t k0 = t.top >= 32 ? 0u : t.prefix << t.top, k1 = t.top == 0 ? t.prefix : k0 | ((1u << t.top) - 1u);
+  const uint32_t k0 = t.top >= 32 ? 0u : t.prefix << t.top, k1 = t.top >= 32 ? ~0u : k0 | ((1u << t.top) - 1u);
   const float e2 = 2.f * kBoundError * 1.01f * mag + 1e-30f;
   float low = ordered_value(k0 > floor_key ? k0 : floor_key) - e2, high = ordered_value(k1 < s_max ? k1 : s_max) + e2;
   if (!(low >= -INFINITY)) low = -INFINITY;             // (ends of the range that are no numbers)
@@ -446,7 +448,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) paged_select_kernel(con
     }
     __syncthreads();
     const Threshold<unsigned long long> t64 = find_threshold<unsigned long long, NT>(
-        [&](auto&& fn) { for (int j = tid; j < c.n; j += NT) fn(__ldcg(exact + j)); }, s_min64, s_max64, p.topk, c.n, 0, 6,
+        [&](auto&& fn) { for (int j = tid; j < c.n; j += NT) fn(__ldcg(exact + j)); }, s_min64, s_max64, p.topk, c.n, 0, kAllBits,
         s_hist, s_sum, s_out);
     // keys above the prefix, and the first t64.need of those equal to it: counted over the words by one warp
     for (int j0 = warp * 32; j0 < c.n; j0 += NT) {

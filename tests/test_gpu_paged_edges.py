@@ -193,3 +193,23 @@ def test_pieces_of_a_row_whose_keys_are_all_no_numbers(lens, d, dtype):
         s.k[s.table[0, p]] = float("nan")
     none = _check_rows(dtype, d, *_attend_both(s), int(s.kv_lens.max()))
     assert none.any() and not none.all()
+
+
+# ---------------------------------------------------------------------------------------------- page bounds at their edges
+@pytest.mark.parametrize("pages,topk", [(700, 300), (700, 20), (1020, 600), (2500, 900)])
+def test_bounds_that_differ_in_the_last_of_64_bits(pages, topk):
+    # more than 512 pages too close for 32 bits, of both signs: 1 + k 2^-50, the larger ones behind the smaller ones
+    s = U.make_step(2, 1, 64, 16, "bf16", [(1, 16 * pages + 9)], seed=140, with_bounds=True)
+    s.q[:] = 0.0
+    s.q[:, :, 0], s.q[:, :, 1] = 1.0, 2.0 ** -25
+    s.bounds[:] = 0.0
+    s.bounds[:, :, 1, 0] = 1.0
+    g = torch.Generator().manual_seed(141)
+    for p in range(pages + 1):
+        s.bounds[s.table[0, p], :, 1, 1] = (1 + int(torch.randint(0, 1 + 254 * p // pages, (1,), generator=g))) * 2.0 ** -25
+    for p in (5, 77, 300):
+        s.bounds[s.table[0, p], :, :, 0] = -1.0
+    y, lse, idx = U.gpu_block_attention(s, 1, 1, topk)
+    want, got = _want_selected(s, 1, 1, topk)
+    assert (idx == got).all()
+    U.check_attention("bf16", 64, y, lse, *want, n_keys=(topk + 2) * 16)
