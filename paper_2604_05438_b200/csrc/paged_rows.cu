@@ -14,7 +14,10 @@
 //     warps until a unit ends; rows are rescaled only when a maximum moved.
 // Probabilities enter the second product as hi + lo pairs of the element type (2^-16 relative for bf16): that costs
 // 16 extra matrix instructions per tile, which the kernel has time for, and leaves the output's own rounding as the
-// only one of its size.
+// only one of its size.  fp16 has few exponents: there the probabilities are scaled by 2^14 (the largest is then 2^14, since
+// m is the maximum), so that a pair holds them to 2^-22 relative down to 2^-17 of the largest and to 2^-39 of the largest
+// below that; the sum carries the same factor, and the maximum that is handed on has it taken off.  (Without it terms below
+// 2^-25 of the largest vanished from y but stayed in the sum.)
 // Work is dealt out in one of two ways.  Long caches: the tiles of all units form one line, cut into as many equal pieces
 // as there are resident CTAs; a unit that is cut leaves partial results, joined in a fixed order by a second, dependent
 // kernel.  Short ones and short page lists: a unit is cut into up to eight pieces, the CTAs of one cluster, which join
@@ -178,6 +181,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
   using C = RowCfg<D, SPLIT>;
   constexpr int kRowWarps = C::WARPS;
   constexpr int NS = C::NS;
+  constexpr float kShift = T::kBf16 ? 0.f : 14.f;           // p = 2^kShift exp2(..)
   extern __shared__ __align__(1024) unsigned char smem[];
   float* red = reinterpret_cast<float*>(smem + C::red);
   float* stat = reinterpret_cast<float*>(smem + C::stat);
@@ -367,13 +371,13 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             mA = nA; mB = nB;
           }
           // a row that has seen nothing yet: every term exp2(-inf - 0) = 0
-          const float uA = mA == -INFINITY ? 0.f : mA, uB = mB == -INFINITY ? 0.f : mB;
+          const float uA = kShift - (mA == -INFINITY ? 0.f : mA), uB = kShift - (mB == -INFINITY ? 0.f : mB);
 #pragma unroll
           for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              s[n][e] = ex2_approx(fmaf(s[n][e], p.scale_log2, -uA));
-              s[n][2 + e] = ex2_approx(fmaf(s[n][2 + e], p.scale_log2, -uB));
+              s[n][e] = ex2_approx(fmaf(s[n][e], p.scale_log2, uA));
+              s[n][2 + e] = ex2_approx(fmaf(s[n][2 + e], p.scale_log2, uB));
               lA += s[n][e];
               lB += s[n][2 + e];
             }
@@ -402,6 +406,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       }
 
       // ---- the warps' softmaxes joined; a thread ends up with PER of 64 dims of one row
+      mA -= kShift; mB -= kShift;
 #pragma unroll
       for (int d = 1; d < 4; d <<= 1) {
         lA += __shfl_xor_sync(0xffffffffu, lA, d);

@@ -213,3 +213,32 @@ def test_bounds_that_differ_in_the_last_of_64_bits(pages, topk):
     want, got = _want_selected(s, 1, 1, topk)
     assert (idx == got).all()
     U.check_attention("bf16", 64, y, lse, *want, n_keys=(topk + 2) * 16)
+
+
+# ---------------------------------------------------------------------------------------------- small probabilities
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens", [[(1, 500)], [(1, 20000)], [(4, 300)], [(30, 300)]])
+def test_many_keys_far_below_a_few(lens, d, dtype):
+    # one key in 16 has e^18 = 2^26 times the weight of each other one, and value 0: y is made of the others alone
+    s = U.make_step(4, 1, d, 32, dtype, lens * 3, seed=130)
+    s.q[:] = 0.0
+    s.q[:, :, 0] = 8.0
+    s.k[~s.k.isnan()] = 0.0
+    s.k[:, :, ::16, 0] = torch.where(s.k[:, :, ::16, 0].isnan(), s.k[:, :, ::16, 0], 2.25)
+    s.v = torch.where(s.v.isnan(), s.v, 16384.0 + 4096.0 * s.v.float().clamp(-3, 3)).to(s.v.dtype)
+    s.v[:, :, ::16] = torch.where(s.v[:, :, ::16].isnan(), s.v[:, :, ::16], 0.0)
+    y, lse = U.gpu_attention(s, scale=1.0)
+    want, want_lse, A, C = PO.attention(U.f64(s.q), U.f64(s.k), U.f64(s.v), s.table, s.kv_lens, s.cu_q, True, 1.0)
+    n = int(s.kv_lens.max())
+    # Many rows of fp16: a probability is rounded once as 2^7 p, here 2^-19, by up to 2^-25 absolute.  That is 2^-32 of the
+    # weight of one of the keys on top, for 15 keys of values up to 28672 per key on top.  (In range of the type otherwise.)
+    more = 15 * 2.0 ** -32 * 28672 if dtype == "fp16" and lens[0][0] == 30 else 0.0
+    y = y - np.clip(y - want, -more, more)
+    U.check_attention(dtype, d, y, lse, want, want_lse, A, C, n_keys=n)
+    # That tolerance counts two roundings to 16 bits; with few rows the probabilities are pairs: the output's alone, and
+    # the error of an exponent's argument of 26 (2^-22 of it), of exp2 (2^-21), of a pair (2^-16) and of the sums.
+    if lens[0][0] < 30:
+        u = torch.finfo(U.DT[dtype]).eps / 2
+        tol = (u + 26 * 2.0 ** -22 + 2.0 ** -20 + 2.0 ** -16 + 2 * n * 2.0 ** -24) * np.abs(want)
+        assert (np.abs(y - want) <= tol).all(), float((np.abs(y - want) / tol).max())
