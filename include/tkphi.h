@@ -393,7 +393,7 @@ tkphi_status tkphi_paged_attention(const tkphi_paged_desc* kv, const void* q, vo
  * Attention over selected pages.  For every new token and KV head the middle pages are ordered by the largest score
  * that a key within their bounds could have with one of the group's query heads,
  *   bound = max over the group of sum_c max(q_c lo_c, q_c hi_c)
- * (evaluated in 64 bits; equal bounds go to the lower page), and attention runs exactly over the rows of the selected
+ * (evaluated in 64 bits, 0 * inf as 0, heads whose sum is no number left out; equal bounds go to the lower page), and attention runs exactly over the rows of the selected
  * pages up to the token's position.  At most 131,072 pages per sequence.  A token that sees no more than n_sink_pages + n_tail_pages + topk_pages pages
  * gets plain attention.
  *   page_idx_out  int32 [total_q][n_kv_heads][n_sink_pages + n_tail_pages + topk_pages] or NULL: the selected pages

@@ -9,7 +9,9 @@
 // magnitudes, which bounds their error; with the k-th largest of them, t, and an error of e, pages above t + 2e are in and
 // those below t - 2e out whatever the errors are.  Only the pages between are evaluated in 64 bits, where a sum of
 // products of 16-bit floats does not round unless their exponents span more than about 25 binades, so that the order does
-// not depend on how it is split.  (In 32 bits alone, neighbours among thousands of pages swap; 64 bits for all pages took
+// not depend on how it is split.  Where a bound is infinite (an fp16 key that overflowed), or the sums are too large for
+// 32 bits, the magnitudes are not finite or very large, and all pages are evaluated in 64 bits: there a term whose query
+// element is 0 counts 0, and a query head whose sum is no number has no say.  (In 32 bits alone, neighbours among thousands of pages swap; 64 bits for all pages took
 // 132 us where this takes 30: 236 tokens over 27K of 32 / 8 heads of 64.)
 #include <climits>
 
@@ -36,6 +38,13 @@ __device__ __forceinline__ Candidates candidates_of(const PagedProblem& p, int b
   const int n = c.seen - p.n_tail - c.first;
   c.n = n > 0 ? n : 0;
   return c;
+}
+
+// The larger one; NaN if either is (as the positive NaN).
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
 }
 
 // Bounds of all candidate pages.  A tile of the matrix instruction is 16 query rows x 8 pages; a lane reads 16 bytes of
@@ -157,12 +166,12 @@ __global__ void __launch_bounds__(kScoreThreads, 2) paged_score_kernel(const __g
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           v[e] = fmaxf(v[e], __shfl_xor_sync(0xffffffffu, v[e], o));
-          m[e] = fmaxf(m[e], __shfl_xor_sync(0xffffffffu, m[e], o));
+          m[e] = max_nan(m[e], __shfl_xor_sync(0xffffffffu, m[e], o));
         }
       }
       if (gp == 16) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) { v[e] = fmaxf(v[e], v[2 + e]); m[e] = fmaxf(m[e], m[2 + e]); }
+        for (int e = 0; e < 2; ++e) { v[e] = fmaxf(v[e], v[2 + e]); m[e] = max_nan(m[e], m[2 + e]); }
       }
       // a page with a bad id comes last (its lanes hold page r, its results are in lanes of every row)
       const unsigned bad = __ballot_sync(0xffffffffu, !ok[s]);
@@ -172,23 +181,23 @@ __global__ void __launch_bounds__(kScoreThreads, 2) paged_score_kernel(const __g
         if (bad >> (4 * (2 * kq + e)) & 1u) v[e] = v[2 + e] = -INFINITY;
         if (writes && j + e < nA) {
           keysA[j + e] = v[e];
-          magA = fmaxf(magA, m[e]); minA = fminf(minA, v[e]); maxA = fmaxf(maxA, v[e]);
+          magA = max_nan(magA, m[e]); minA = fminf(minA, v[e]); maxA = fmaxf(maxA, v[e]);
         }
         if (writes && j + e < nB) {
           keysB[j + e] = v[2 + e];
-          magB = fmaxf(magB, m[2 + e]); minB = fminf(minB, v[2 + e]); maxB = fmaxf(maxB, v[2 + e]);
+          magB = max_nan(magB, m[2 + e]); minB = fminf(minB, v[2 + e]); maxB = fmaxf(maxB, v[2 + e]);
         }
       }
     }
   }
-  // each token's largest magnitude and range of scores here (non-negative floats order like their bits)
+  // each token's largest magnitude and range of scores here (non-negative floats order like their bits, NaN last)
   auto note = [&](int t, float mag, float lo, float hi) {
     atomicMax(&s_mag[t], __float_as_int(mag));
     atomicMin(&s_min[t], (int)(ordered_key(lo + 0.f) ^ 0x80000000u));
     atomicMax(&s_max[t], (int)(ordered_key(hi + 0.f) ^ 0x80000000u));
   };
-  if (writes && nA > 0 && minA <= maxA) note(tA, magA, minA, maxA);
-  if (writes && nB > 0 && minB <= maxB) note(tB, magB, minB, maxB);
+  if (writes && nA > 0) note(tA, magA, minA, maxA);
+  if (writes && nB > 0) note(tB, magB, minB, maxB);
   __syncthreads();
   if (tid < n_tok)
     p.page_mags[((size_t)(tok0 + tid) * p.hkv + h) * gridDim.y + blockIdx.y] =
@@ -289,7 +298,7 @@ __device__ __forceinline__ unsigned long long exact_bound(const PagedProblem& p,
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const double x = to_double<T>(w[g][i], e);
-          acc[g] = fma(x, to_double<T>(x < 0. ? wl[i] : wh[i], e), acc[g]);
+          if (x != 0.) acc[g] = fma(x, to_double<T>(x < 0. ? wl[i] : wh[i], e), acc[g]);      // 0 * inf would be NaN
         }
     }
 #pragma unroll
@@ -384,59 +393,62 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) paged_select_kernel(con
     return in_smem ? *reinterpret_cast<const uint4*>(s_held + i) : four(__ldcg(reinterpret_cast<const float4*>(scores + i)), i);
   };
   const float mag = __uint_as_float(s_mag);
-  // ---- A key that topk of the threads' largest keys reach is a lower end of the search: nearly all keys are below it,
-  // and are neither counted nor spread the bins.
-  uint32_t floor_key = s_min;
-  if (p.topk <= NT / 2 && c.n > 8 * NT) {
-    const Threshold<uint32_t> t = find_threshold<uint32_t, NT>([&](auto&& fn) { fn(top_key); }, s_min, s_max, p.topk, NT, 0, 1,
-                                                               s_hist, s_sum, s_out);
-    const uint32_t k = t.top >= 32 ? 0u : t.prefix << t.top;
-    floor_key = k > s_min ? k : s_min;
-  }
-  // ---- the threshold up to a few keys: those are ranked in 64 bits, like the ones too close to it to tell
-  const Threshold<uint32_t> t = find_threshold<uint32_t, NT>(
-      [&](auto&& fn) {
-#pragma unroll 2
-        for (int i = tid * 4; i < c.n; i += NT * 4) {
-          const uint4 k = keys_of(i);
-          if (max(max(k.x, k.y), max(k.z, k.w)) >= floor_key) { fn(k.x); fn(k.y); fn(k.z); fn(k.w); }
-        }
-      },
-      floor_key, s_max, p.topk, c.n, NW, kAllBits, s_hist, s_sum, s_out);
-  // (the k-th largest score lies in [prefix, prefix + 1) << top: both ends widen the range)
-  const uint32_t k0 = t.top >= 32 ? 0u : t.prefix << t.top, k1 = t.top >= 32 ? ~0u : k0 | ((1u << t.top) - 1u);
-  const float e2 = 2.f * kBoundError * 1.01f * mag + 1e-30f;
-  float low = ordered_value(k0 > floor_key ? k0 : floor_key) - e2, high = ordered_value(k1 < s_max ? k1 : s_max) + e2;
-  if (!(low >= -INFINITY)) low = -INFINITY;             // (ends of the range that are no numbers)
-  if (!(high <= INFINITY)) high = INFINITY;
-  const uint32_t kl = ordered_key(low), kh = ordered_key(high);
-  // ---- in, out, or between: eight lanes of four pages make a word of the bit map
-  int above = 0;
-  for (int i0 = warp * 128; i0 < c.n; i0 += NT * 4) {
-    const int i = i0 + lane * 4;
-    const uint4 k = i < c.n ? keys_of(i) : make_uint4(0, 0, 0, 0);
-    const unsigned in = (k.x > kh ? 1u : 0u) | (k.y > kh ? 2u : 0u) | (k.z > kh ? 4u : 0u) | (k.w > kh ? 8u : 0u);
-    const unsigned word = __reduce_or_sync(0xffu << (lane & 24), in << (4 * (lane & 7)));
-    if ((lane & 7) == 0 && i < c.n) s_bits[i >> 5] = word;
-    above += __popc(in);
-    if (max(max(k.x, k.y), max(k.z, k.w)) >= kl) {
-      const uint32_t kk[4] = {k.x, k.y, k.z, k.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (kk[e] <= kh && kk[e] >= kl) {
-          const int at = atomicAdd(&s_border, 1);
-          if (at < kBorder) { s_page[at] = i + e; s_phys[at] = __ldg(table + c.first + i + e); }
-        }
+  const bool wide = !(mag < 1e37f);                     // no numbers, or sums that 32 bits may not hold
+  if (!wide) {
+    // ---- A key that topk of the threads' largest keys reach is a lower end of the search: nearly all keys are below it,
+    // and are neither counted nor spread the bins.
+    uint32_t floor_key = s_min;
+    if (p.topk <= NT / 2 && c.n > 8 * NT) {
+      const Threshold<uint32_t> t = find_threshold<uint32_t, NT>([&](auto&& fn) { fn(top_key); }, s_min, s_max, p.topk, NT, 0, 1,
+                                                                 s_hist, s_sum, s_out);
+      const uint32_t k = t.top >= 32 ? 0u : t.prefix << t.top;
+      floor_key = k > s_min ? k : s_min;
     }
-    __syncwarp();
+    // ---- the threshold up to a few keys: those are ranked in 64 bits, like the ones too close to it to tell
+    const Threshold<uint32_t> t = find_threshold<uint32_t, NT>(
+        [&](auto&& fn) {
+  #pragma unroll 2
+          for (int i = tid * 4; i < c.n; i += NT * 4) {
+            const uint4 k = keys_of(i);
+            if (max(max(k.x, k.y), max(k.z, k.w)) >= floor_key) { fn(k.x); fn(k.y); fn(k.z); fn(k.w); }
+          }
+        },
+        floor_key, s_max, p.topk, c.n, NW, kAllBits, s_hist, s_sum, s_out);
+    // (the k-th largest score lies in [prefix, prefix + 1) << top: both ends widen the range)
+    const uint32_t k0 = t.top >= 32 ? 0u : t.prefix << t.top, k1 = t.top >= 32 ? ~0u : k0 | ((1u << t.top) - 1u);
+    const float e2 = 2.f * kBoundError * 1.01f * mag + 1e-30f;
+    float low = ordered_value(k0 > floor_key ? k0 : floor_key) - e2, high = ordered_value(k1 < s_max ? k1 : s_max) + e2;
+    if (!(low >= -INFINITY)) low = -INFINITY;             // (ends of the range that are no numbers)
+    if (!(high <= INFINITY)) high = INFINITY;
+    const uint32_t kl = ordered_key(low), kh = ordered_key(high);
+    // ---- in, out, or between: eight lanes of four pages make a word of the bit map
+    int above = 0;
+    for (int i0 = warp * 128; i0 < c.n; i0 += NT * 4) {
+      const int i = i0 + lane * 4;
+      const uint4 k = i < c.n ? keys_of(i) : make_uint4(0, 0, 0, 0);
+      const unsigned in = (k.x > kh ? 1u : 0u) | (k.y > kh ? 2u : 0u) | (k.z > kh ? 4u : 0u) | (k.w > kh ? 8u : 0u);
+      const unsigned word = __reduce_or_sync(0xffu << (lane & 24), in << (4 * (lane & 7)));
+      if ((lane & 7) == 0 && i < c.n) s_bits[i >> 5] = word;
+      above += __popc(in);
+      if (max(max(k.x, k.y), max(k.z, k.w)) >= kl) {
+        const uint32_t kk[4] = {k.x, k.y, k.z, k.w};
+  #pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (kk[e] <= kh && kk[e] >= kl) {
+            const int at = atomicAdd(&s_border, 1);
+            if (at < kBorder) { s_page[at] = i + e; s_phys[at] = __ldg(table + c.first + i + e); }
+          }
+      }
+      __syncwarp();
+    }
+    above = __reduce_add_sync(0xffffffffu, above);
+    if (lane == 0 && above) atomicAdd(&s_sure, above);
+    __syncthreads();
   }
-  above = __reduce_add_sync(0xffffffffu, above);
-  if (lane == 0 && above) atomicAdd(&s_sure, above);
-  __syncthreads();
   const int border = s_border, need = p.topk - s_sure;
   const uint32_t* q = static_cast<const uint32_t*>(p.q) + ((size_t)tok * p.hq + h * p.group) * (D / 2);
-  // many equal bounds, or sums that 32 bits may not hold: the whole list in 64 bits
-  if (border > kBorder || !(mag < 1e37f)) {
+  // many equal bounds, or nothing known from 32 bits: the whole list in 64 bits
+  if (wide || border > kBorder) {
     unsigned long long* exact = p.page_keys + (size_t)unit * p.key_stride;
     for (int j = warp; j < c.n; j += NW) {
       const unsigned long long k = exact_bound<T, D>(p, q, __ldg(table + c.first + j), h);

@@ -242,3 +242,55 @@ def test_many_keys_far_below_a_few(lens, d, dtype):
         u = torch.finfo(U.DT[dtype]).eps / 2
         tol = (u + 26 * 2.0 ** -22 + 2.0 ** -20 + 2.0 ** -16 + 2 * n * 2.0 ** -24) * np.abs(want)
         assert (np.abs(y - want) <= tol).all(), float((np.abs(y - want) / tol).max())
+
+
+# ---------------------------------------------------------------------------------------------- infinite bounds
+@pytest.mark.parametrize("pages,topk", [(60, 7), (700, 30), (1500, 20), (5000, 600)])
+@pytest.mark.parametrize("share", [0.02, 0.6, 1.0])
+@pytest.mark.parametrize("counts", [False, True])
+def test_infinite_bounds(pages, topk, share, counts):
+    # one infinite element in some pages: which side of it counts goes by the query's sign.  Without `counts` it is always the
+    # one that does not, so that every bound is finite
+    s = U.make_step(1, 1, 64, 16, "fp16", [(1, 16 * pages + 9)], seed=142, with_bounds=True)
+    g = torch.Generator().manual_seed(143)
+    for p in range(pages + 1):
+        if float(torch.rand(1, generator=g)) < share:
+            c, side = int(torch.randint(0, 64, (1,), generator=g)), p % 2
+            if not counts:
+                side = 0 if float(s.q[0, 0, c]) > 0 else 1
+            s.bounds[s.table[0, p], 0, side, c] = float("inf") if side else -float("inf")
+    s.q[:, :, 11] = 0.0
+    s.bounds[:, :, :, 11] = s.bounds[:, :, :, 11].nan_to_num(0.0, 0.0, 0.0)
+    y, lse, idx = U.gpu_block_attention(s, 1, 2, topk)
+    *want, got = PO.block_attention(U.f64(s.q), U.f64(s.k), U.f64(s.v), s.table, s.kv_lens, s.cu_q,
+                                    np.nan_to_num(U.f64(s.bounds), nan=0.0, posinf=np.inf, neginf=-np.inf), 1, 2, topk)
+    assert (idx == got).all()
+    U.check_attention("fp16", 64, y, lse, *want, n_keys=(topk + 3) * 16)
+
+
+def test_an_infinite_bound_beside_a_zero_of_the_query():
+    # 0 * inf counts as 0: a page with an infinite key element that the query does not look at is no better than without
+    s = U.make_step(1, 1, 64, 16, "fp16", [(1, 16 * 300 + 9)], seed=144, with_bounds=True)
+    s.q[:, :, 11] = 0.0
+    plain = U.Step(s.k, s.v, s.table, s.kv_lens, s.cu_q, s.hq, s.q, s.bounds.clone())
+    plain.bounds[:, :, :, 11] = 0.0
+    s.bounds[:, :, 0, 11], s.bounds[:, :, 1, 11] = -1.0, float("inf")
+    _, _, idx = U.gpu_block_attention(s, 1, 2, 20)
+    assert (idx == _want_selected(plain, 1, 2, 20)[1]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+def test_selection_for_a_query_that_is_no_number(what, dtype):
+    # whatever it selects, its page list is whole, its output is no number, and the tokens beside it are as ever
+    s = U.make_step(8, 2, 64, 16, dtype, [(5, 16 * 700), (1, 900)], seed=145, with_bounds=True)
+    s.q[2, :, 3] = what
+    y, lse, idx = U.gpu_block_attention(s, 1, 1, 9)
+    with np.errstate(all="ignore"):
+        (want, want_lse, A, C), pages = _want_selected(s, 1, 1, 9)
+    rest = [0, 1, 3, 4, 5]
+    assert (idx[rest] == pages[rest]).all()
+    U.check_attention(dtype, 64, y[rest], lse[rest], want[rest], want_lse[rest], A[rest], C[rest], n_keys=11 * 16)
+    assert (np.diff(idx[2], axis=-1) > 0).all() and (idx[2] >= 0).all() and (idx[2] < 700).all()
+    if what != what:
+        assert np.isnan(y[2]).all() and np.isnan(lse[2]).all()
