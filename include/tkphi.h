@@ -314,7 +314,8 @@ tkphi_status tkphi_decode_step_mlp(const tkphi_kv_desc* kv, const tkphi_mlp_desc
  *    TKPHI_ERR_TIMEOUT) and never clear it.  Required.
  *  - A workspace serves one call at a time: calls that may overlap (other streams, captured graphs that are replayed side
  *    by side) need workspaces of their own.
- *  - Slots at or behind a sequence's length may hold anything, NaN included: nothing read from them reaches a result.
+ *  - Slots at or behind a sequence's length may hold anything, NaN included: nothing read from them reaches a result.  Nor
+ *    does an infinity or NaN in the keys or values of a later new token reach the tokens before it.
  *  - key_bounds (optional; needed by tkphi_paged_block_attention): [n_pages][n_kv_heads][2][head_dim] in the cache's
  *    type, the element-wise minimum and maximum of each page's keys.
  */

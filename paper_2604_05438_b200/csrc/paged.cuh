@@ -61,6 +61,7 @@ struct PagedProblem {
 // ---------------------------------------------------------------- 16-bit element types
 struct Bf16 {
   static constexpr bool kBf16 = true;
+  static constexpr uint32_t kExp = 0x7f807f80u, kExpUnit = 0x00800080u;      // exponent fields of a pair and their lowest bits
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -81,6 +82,7 @@ struct Bf16 {
 };
 struct Fp16 {
   static constexpr bool kBf16 = false;
+  static constexpr uint32_t kExp = 0x7c007c00u, kExpUnit = 0x04000400u;
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -99,6 +101,20 @@ struct Fp16 {
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   }
 };
+
+// The sign bits of the pair's elements that are infinite or no number (an exponent of ones carries into the sign bit).
+template <typename T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & T::kExp) + T::kExpUnit) & 0x80008000u; }
+template <typename T>
+__device__ __forceinline__ uint32_t not_finite(const uint4& v) {
+  return not_finite<T>(v.x) | not_finite<T>(v.y) | not_finite<T>(v.z) | not_finite<T>(v.w);
+}
+// The pair with those elements 0.
+template <typename T>
+__device__ __forceinline__ uint32_t finite_part(uint32_t w) {
+  const uint32_t bad = not_finite<T>(w) >> 15;               // 1 in the element's lowest bit
+  return w & ~(bad * 0xffffu);
+}
 
 // ---------------------------------------------------------------- sequences
 __device__ __forceinline__ int paged_kv_len(const PagedProblem& p, int b) {

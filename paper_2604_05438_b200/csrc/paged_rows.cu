@@ -295,7 +295,8 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       int limA = -1, limB = -1;
       if (rA < w.rows) limA = BLOCK ? w.pos0 : p.causal ? w.pos0 + (w.r_first + rA) / p.group : w.len - 1;
       if (rB < w.rows) limB = BLOCK ? w.pos0 : p.causal ? w.pos0 + (w.r_first + rB) / p.group : w.len - 1;
-      // keys up to lim_all are visible to every row of the unit
+      // keys up to lim_all are visible to every row of the unit, keys behind lim_last (computed for every tile: there is no
+      // register left for it) to none
       const int lim_all = BLOCK ? w.pos0 : p.causal ? w.pos0 + w.r_first / p.group : w.len - 1;
       float o[D / 8][4];
 #pragma unroll
@@ -319,8 +320,9 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
           else if (entry == w.n_list - 1) key0 = ((w.pos0 >> p.page_shift) << p.page_shift) + (key0 & (ps - 1));
           else key0 = w.len;                                                // past the list
         }
-        const bool skip = key0 > (BLOCK ? w.pos0 : p.causal ? w.pos0 + (w.r_first + w.rows - 1) / p.group : w.len - 1);
-        if (!skip) {
+        const int lim_last = BLOCK ? w.pos0 : p.causal ? w.pos0 + (w.r_first + w.rows - 1) / p.group : w.len - 1;
+        if (key0 <= lim_last) {
+          bool odd_values = false;                          // a value that is not finite and that not every row sees
           float s[2][4];
 #pragma unroll
           for (int n = 0; n < 2; ++n) { s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f; }
@@ -343,16 +345,23 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
                 if (key > limA) s[n][e] = -INFINITY;
                 if (key > limB) s[n][2 + e] = -INFINITY;
               }
-            // rows of the tile at or behind the sequence's end may hold anything: they must not reach the product
-            const int keep = w.len - key0;                  // >= 1 here
+            // Values that no row sees may be anything (behind the sequence's end they may be left-overs): 0 times them must
+            // not reach the product.  Those that some rows see are looked through.
+            constexpr int CPR = D / 8;                      // 16-byte pieces of a row
+            const int keep = lim_last + 1 - key0;           // >= 1 here
             if (keep < 16) {
-              constexpr int CPR = D / 8;                    // 16-byte pieces of a row
               for (int i = lane; i < (16 - keep) * CPR; i += 32) {
                 const int row = kg * 16 + keep + i / CPR, c = i % CPR;
                 *reinterpret_cast<uint4*>(vs + (c >> 3) * C::HALF + swz128(row, c & 7)) = make_uint4(0, 0, 0, 0);
               }
               fence_proxy_async_smem();                     // before the slot's next copy
               __syncwarp();
+            }
+            if (!BLOCK && lim_all < lim_last) {
+              uint32_t bad = 0;
+              for (int i = lane; i < 16 * CPR; i += 32)
+                bad |= not_finite<T>(*reinterpret_cast<const uint4*>(vs + ((i % CPR) >> 3) * C::HALF + swz128(kg * 16 + i / CPR, i % CPR & 7)));
+              odd_values = __any_sync(0xffffffffu, bad != 0);
             }
           }
           float tA = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
@@ -387,6 +396,28 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             const float x = s[j >> 1][(j & 1) * 2], y = s[j >> 1][(j & 1) * 2 + 1];
             ph[j] = T::pack(x, y);
             pl[j] = T::pack(x - T::lo(ph[j]), y - T::hi(ph[j]));
+          }
+          if (!BLOCK && odd_values) {
+            // added to the rows that see them, and taken out of the product, where 0 times them would reach the others
+#pragma unroll 1
+            for (int k = 0; k < 16; ++k) {
+              const bool a = key0 + k <= limA, b = key0 + k <= limB;
+#pragma unroll
+              for (int n = 0; n < D / 8; ++n) {
+                const uint32_t x = *reinterpret_cast<const uint32_t*>(vs + (n >> 3) * C::HALF + swz128(kg * 16 + k, n & 7) + cc * 2);
+                const uint32_t f = not_finite<T>(x);
+                if (f & 0x8000u) { o[n][0] += a ? T::lo(x) : 0.f; o[n][2] += b ? T::lo(x) : 0.f; }
+                if (f >> 31) { o[n][1] += a ? T::hi(x) : 0.f; o[n][3] += b ? T::hi(x) : 0.f; }
+              }
+            }
+            __syncwarp();
+            for (int i = lane; i < 16 * (D / 2); i += 32) {
+              const int d2 = i % (D / 2);
+              uint32_t* x = reinterpret_cast<uint32_t*>(vs + (d2 >> 5) * C::HALF + swz128(kg * 16 + i / (D / 2), (d2 >> 2) & 7) + (d2 & 3) * 4);
+              *x = finite_part<T>(*x);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
           }
           {
             const int row = kg * 16 + (((lane >> 3) & 1) << 3) + (lane & 7), sub = lane >> 4;

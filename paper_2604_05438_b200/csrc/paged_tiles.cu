@@ -16,9 +16,11 @@
 //                   a row is lost on the way, because m never exceeds a score the row has seen.
 //                   At head_dim 64 a quarter of the exponentials are computed on the FMA pipes (exp2_pair).
 //   warp 8          issues the MMAs: P V of a row tile as soon as its P is stored, then the next S into the same buffer.
-//   warp 9          TMA producer: the queries, then page boxes of keys and values into one ring, in the order of their
-//                   use; in the end it zeroes the value rows behind the sequence's end (they may hold NaN, and 0 * NaN
-//                   would reach the sums).
+//   warp 9          TMA producer: the queries, then page boxes of keys and values into one ring, in the order of their use.
+//   warps 10, 11    look through the value tiles that not every row of the CTA sees whole (three at most), because 0 times an
+//                   infinity or NaN would reach the rows that do not see it: value rows that no row sees are zeroed (behind
+//                   the sequence's end they may hold anything), other elements that are not finite are zeroed and noted with
+//                   the first key that has one in their dim, and added at the end to the rows that see that key.
 // fp16: P is scaled by 2^7, because without it probabilities below 2^-24 of the maximum vanish, and a long context is made
 // of those; the sum carries the same factor.  Rounding P to 16 bits is the only rounding besides the output's: per term it
 // is that of one 16-bit rounding, and it averages out over the terms.  The sum is of the unrounded values.
@@ -129,9 +131,11 @@ struct TileCfg {
   static constexpr size_t ring = 2 * TILE;
   static constexpr size_t bars = ring + (size_t)NS * TILE;
   static constexpr size_t bar_bytes = 512;                   // barriers and four words
-  static_assert((NS + NV + 3 * NB + 5) * 8 + 8 + 11 * 4 <= bar_bytes, "barriers");
-  static constexpr size_t total = bars + bar_bytes;
+  static_assert((NS + NV + 3 * NB + 4 + 2 * 3) * 8 + 12 + 11 * 4 <= bar_bytes, "barriers");
+  static constexpr size_t odd = bars + bar_bytes;            // [3][D] per dim the first key whose value is inf, -inf, NaN
+  static constexpr size_t total = odd + 3 * D * sizeof(int);
 };
+constexpr int kMostMixed = 3;                // value tiles that some rows of a CTA see in part: 255 tokens touch three
 
 __device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t* r) {
   asm volatile(
@@ -197,12 +201,15 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   uint64_t* o_full = p_ready + C::NB;      // [2]  last product of the row tile complete
   uint64_t* pv_done = o_full + 2;          // [NB] products whose completion no scores tell (more score buffers than row tiles)
   uint64_t* q_ready = pv_done + C::NB;     // [1]
-  uint64_t* v_fixed = q_ready + 1;         // [1]  tail rows of the last value tile zeroed
-  uint64_t* drained = v_fixed + 1;         // [1]  after a wait that ran out: the MMAs issued so far are complete
+  uint64_t* v_issued = q_ready + 1;        // [3]  copy of a mixed value tile issued
+  uint64_t* v_fixed = v_issued + kMostMixed;   // [3]  that tile looked through
+  uint64_t* drained = v_fixed + kMostMixed;    // [1]  after a wait that ran out: the MMAs issued so far are complete
   int* misc = reinterpret_cast<int*>(drained + 1);
   volatile int* s_abort = misc;
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(misc + 1);
-  TileWork* s_work = reinterpret_cast<TileWork*>(misc + 2);
+  volatile int* s_odd = misc + 2;
+  TileWork* s_work = reinterpret_cast<TileWork*>(misc + 3);
+  int* odd_key = reinterpret_cast<int*>(smem + C::odd);
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int cta = blockIdx.x;
 
@@ -246,10 +253,13 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     mbar_init(&o_full[0], 1); mbar_init(&o_full[1], 1);
     for (int i = 0; i < C::NB; ++i) mbar_init(&pv_done[i], 1);
     mbar_init(q_ready, 1);
-    mbar_init(v_fixed, 1);
+    for (int i = 0; i < kMostMixed; ++i) { mbar_init(&v_issued[i], 1); mbar_init(&v_fixed[i], 2); }
     mbar_init(drained, 1);
     mbar_fence_init();
     *s_abort = 0;
+    *s_odd = 0;
+  } else if (warp >= 8) {
+    for (int i = tid - 256; i < 3 * D; i += 128) odd_key[i] = INT_MAX;
   }
   tc_fence_before_sync();
   __syncthreads();
@@ -258,7 +268,11 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   const TileWork k = *s_work;
   const int b = k.seq, n = b >= 0 ? k.n : 0, tiles = b >= 0 ? k.tiles : 1;
   const int h = k.h, c0 = k.c0, row0 = k.row0, q_len = k.q_len, t_rows = tile_rows(p.group);
-  const bool fix = n > 0 && c0 + n * kTileKeys > k.len;              // the last tile reaches behind the sequence
+  // Keys up to vis0 are visible to every row of the CTA, from vis1 on to none.  Value tiles from `mixed` on are neither.
+  const int pair_rows = k.rows - row0 < 2 * t_rows ? k.rows - row0 : 2 * t_rows;
+  const int vis0 = p.causal ? k.len - q_len + row0 / p.group + 1 : k.len;
+  const int vis1 = p.causal ? k.len - q_len + (row0 + pair_rows - 1) / p.group + 1 : k.len;
+  const int mixed = vis0 <= c0 ? 0 : (vis0 - c0) / kTileKeys < n ? (vis0 - c0) / kTileKeys : n;
   // Scores, P and products run through one sequence: number i = key tile * tiles + row tile, buffer i % NB.  Keys are
   // used `lead` tiles ahead of values: the ring holds K 0 .. K lead-1, V 0, K lead, V 1, ..
   const int lead = (C::NB + tiles - 1) / tiles;
@@ -407,6 +421,18 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       if (buf >= C::NB) { buf -= C::NB; phase ^= 1u; }
     }
     if (ok && nt > 0) ok = __all_sync(0xffffffffu, mbar_wait(&o_full[t], 0, s_abort));
+    for (int i = 0; i < nt - mixed && ok; ++i) ok = __all_sync(0xffffffffu, mbar_wait(&v_fixed[i], 0, s_abort));
+    // the values that are not finite, of the keys that this row sees
+    const bool odd = nt > 0 && *s_odd;
+    auto add_odd = [&](float (&o)[32], int c) {
+      const int* first = odd_key + c * 32;
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        if (first[e] <= lim) o[e] += INFINITY;
+        if (first[D + e] <= lim) o[e] -= INFINITY;
+        if (first[2 * D + e] <= lim) o[e] = __int_as_float(0x7fffffff);
+      }
+    };
     if (ok && b >= 0) {
       tc_fence_after_sync();
       const volatile TileWork* w = s_work;
@@ -422,6 +448,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           if (nt > 0) {                        // warp-uniform
             tmem_ld_x32(o_addr + c * 32, o);
             tc_wait_ld();
+            if (odd) add_odd(o, c);
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -444,6 +471,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             float o[32];
             tmem_ld_x32(o_addr + c * 32, o);
             tc_wait_ld();
+            if (odd) add_odd(o, c);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               if (live) st_global_32(dst + c * 32 + e * 8, &o[e * 8]);
@@ -468,8 +496,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       batch0[0] = batch0[1] = (c0 >> p.page_shift) & ~31;
       id[0] = id[1] = batch0[0] + lane < n_pages_seq ? __ldg(list + batch0[0] + lane) : p.n_pages;
       id_next[0] = id_next[1] = batch0[0] + 32 + lane < n_pages_seq ? __ldg(list + batch0[0] + 32 + lane) : p.n_pages;
-      int slot = 0, last_slot = 0;
-      uint32_t phase = 0, last_phase = 0;
+      int slot = 0;
+      uint32_t phase = 0;
       // the queries: tokens x the group's heads, 64 dims at a time (a second tile of other tokens is not used)
       if (lane == 0) mbar_expect_tx(q_ready, (uint32_t)(tiles * C::HALVES * t_rows * 128));
       __syncwarp();
@@ -506,30 +534,12 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                       page, pol);
         pending |= 1u << slot;
         parity = (parity & ~(1u << slot)) | (phase << slot);
-        last_slot = slot;
-        last_phase = phase;
+        if (x && j >= mixed && lane == 0) mbar_arrive(&v_issued[j - mixed]);
         if (++slot == NS) { slot = 0; phase ^= 1u; }
       };
       for (int jk = 0, jv = 0; jv < n && ok;) {
         if (jk < n && jk < jv + lead) load(0, jk++);
         else load(1, jv++);
-      }
-      if (ok && fix) {
-        // Value rows of the last tile behind the end of the sequence.  (The slot's barrier is in the phase of this
-        // copy until the wait returns, because nothing is loaded after it.)
-        const int keep = k.len - (c0 + (n - 1) * kTileKeys);        // 1 .. 127
-        ok = __all_sync(0xffffffffu, mbar_wait(&full[last_slot], last_phase, s_abort));
-        if (ok) {
-          constexpr int CPR = D / 8;
-          unsigned char* v = ring + (size_t)last_slot * C::TILE;
-          for (int x = lane; x < (kTileKeys - keep) * CPR; x += 32) {
-            const int row = keep + x / CPR, c = x % CPR;
-            *reinterpret_cast<uint4*>(v + (c >> 3) * C::BOX + swz128(row, c & 7)) = make_uint4(0, 0, 0, 0);
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(v_fixed);
-        }
       }
       if (!ok) {
         // every copy that was issued must land before shared memory is released
@@ -551,6 +561,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       constexpr uint32_t idesc_o = umma_idesc_16(T::kBf16, 128, D, 0, 1);
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), base = __shfl_sync(0xffffffffu, smem_u32(smem), 0);
       const int nu = __shfl_sync(0xffffffffu, n, 0), T2 = __shfl_sync(0xffffffffu, tiles, 0), L = __shfl_sync(0xffffffffu, lead, 0);
+      const int mixed_u = __shfl_sync(0xffffffffu, mixed, 0);
       const uint64_t q_desc = umma_smem_desc(base + (uint32_t)C::q, 16, 1024);
       const uint64_t k_desc = umma_smem_desc(base + (uint32_t)C::ring, 16, 1024);
       const uint64_t v_desc = umma_smem_desc(base + (uint32_t)C::ring, C::BOX, 1024);   // MN-major: 64-dim blocks BOX bytes apart
@@ -583,7 +594,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       auto wait_values = [&](int j) {
         advance(v_next, v_phase, j == 0 ? (L < nu ? L : nu) : j + L <= nu ? 2 : 1);
         wait_on(&full[v_next], v_phase);
-        if (fix && j + 1 == nu) wait_on(v_fixed, 0);
+        if (j >= mixed_u) wait_on(&v_fixed[j - mixed_u], 0);
       };
       wait_on(q_ready, 0);
       int sj = 0, st = 0;                                       // next scores to issue
@@ -638,6 +649,45 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           for (uint32_t w = 0; w < kWaitPolls && !mbar_try_wait(drained, 0); ++w) __nanosleep(64);
         }
         __syncwarp();
+      }
+    } else if (warp > kWarpTma) {
+      // ================================================================ values that not every row sees
+      constexpr int CPR = D / 8;                                // 16-byte pieces of a row
+      bool ok = true;
+      for (int j = mixed; j < n && ok; ++j) {
+        // V j is number min(j + lead, n) + j of the ring.  Its slot's barrier is waited for only once the copy is issued: from
+        // then on it is in the phase of this copy until the tile has been used, which needs this warp.
+        ok = __all_sync(0xffffffffu, mbar_wait(&v_issued[j - mixed], 0, s_abort));
+        const int number = (j + lead < n ? j + lead : n) + j, slot = number % NS;
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&full[slot], (uint32_t)(number / NS) & 1u, s_abort));
+        if (!ok) break;
+        unsigned char* v = ring + (size_t)slot * C::TILE;
+        const int key0 = c0 + j * kTileKeys;
+        const int seen = vis1 - key0 < kTileKeys ? vis1 - key0 : kTileKeys, from = vis0 > key0 ? vis0 - key0 : 0;
+#pragma unroll 2
+        for (int x = from * CPR + tid - (kWarpTma + 1) * 32; x < kTileKeys * CPR; x += 64) {
+          const int row = x / CPR, c = x % CPR;
+          uint4* at = reinterpret_cast<uint4*>(v + (c >> 3) * C::BOX + swz128(row, c & 7));
+          uint4 w = *at;
+          if (row < seen && not_finite<T>(w)) {
+            uint32_t* ws = reinterpret_cast<uint32_t*>(&w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              uint32_t& word = ws[e >> 1];
+              const float f = e & 1 ? T::hi(word) : T::lo(word);
+              if (fabsf(f) < INFINITY) continue;
+              atomicMin(&odd_key[(f != f ? 2 : f < 0.f ? 1 : 0) * D + c * 8 + e], key0 + row);
+              word &= e & 1 ? 0xffffu : 0xffff0000u;
+            }
+            *s_odd = 1;
+            *at = w;
+          } else if (row >= seen) {
+            *at = make_uint4(0, 0, 0, 0);
+          }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&v_fixed[j - mixed]);
       }
     }
   }

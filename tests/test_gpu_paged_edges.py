@@ -294,3 +294,46 @@ def test_selection_for_a_query_that_is_no_number(what, dtype):
     assert (np.diff(idx[2], axis=-1) > 0).all() and (idx[2] >= 0).all() and (idx[2] < 700).all()
     if what != what:
         assert np.isnan(y[2]).all() and np.isnan(lse[2]).all()
+
+
+# ---------------------------------------------------------------------------------------------- values that some rows do not see
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv,lens", [(8, 2, [(4, 300), (2, 77), (3, 3)]), (16, 2, [(2, 500)]), (2, 2, [(16, 40), (9, 200)]),
+                                         (8, 2, [(70, 500), (130, 130), (4, 200)]), (3, 1, [(300, 301)]), (1, 1, [(256, 400), (33, 1000)]),
+                                         (16, 1, [(50, 333)]), (4, 1, [(45, 7001)])])
+def test_values_that_are_no_numbers_stay_out_of_the_rows_that_do_not_see_them(hq, hkv, lens, d, dtype, what):
+    s = U.make_step(hq, hkv, d, 32, dtype, lens, seed=123, with_bounds=True)
+    for b, (m, n) in enumerate(lens):
+        for t, c in ((n - 1, 7), (n - (m + 1) // 2, 60), (n - m + 1, 0)):         # keys of new tokens
+            s.v[s.table[b, t // 32], :, t % 32, c:c + 2] = what
+    for form in ("all", "selected"):
+        if form == "all":
+            y, lse, (want, want_lse, A, C) = _attend_both(s)
+        else:
+            y, lse, idx = U.gpu_block_attention(s, 1, 1, 5)
+            with np.errstate(all="ignore"):
+                (want, want_lse, A, C), pages = _want_selected(s, 1, 1, 5)
+            assert (idx == pages).all()
+        out = ~np.isfinite(want)
+        assert out.any() and not out.all()
+        np.testing.assert_array_equal(~np.isfinite(y), out)
+        y, want, A = (np.where(out, 0.0, x) for x in (y, want, A))
+        U.check_attention(dtype, d, y, lse, want, want_lse, A, C, n_keys=int(s.kv_lens.max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_infinite_and_missing_values_of_one_dim_add_up(d, dtype):
+    # per token: inf alone stays inf (many rows), inf and -inf or NaN give NaN, in the dims that have them and from the first
+    # token on that sees them
+    s = U.make_step(2, 1, d, 16, dtype, [(200, 450)], seed=125)
+    for t, c, x in ((300, 1, "inf"), (310, 2, "-inf"), (320, 2, "inf"), (330, 3, "nan"), (260, 3, "inf"), (449, 4, "inf"), (260, 40, "-inf")):
+        s.v[s.table[0, t // 16], 0, t % 16, c] = float(x)
+    y, lse, (want, want_lse, A, C) = _attend_both(s)
+    np.testing.assert_array_equal(np.isnan(y), np.isnan(want))
+    np.testing.assert_array_equal(np.isinf(y) * np.sign(np.nan_to_num(y)), np.isinf(want) * np.sign(np.nan_to_num(want)))
+    out = ~np.isfinite(want)
+    y, want, A = (np.where(out, 0.0, x) for x in (y, want, A))
+    U.check_attention(dtype, d, y, lse, want, want_lse, A, C, n_keys=450)
