@@ -269,10 +269,11 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   const int b = k.seq, n = b >= 0 ? k.n : 0, tiles = b >= 0 ? k.tiles : 1;
   const int h = k.h, c0 = k.c0, row0 = k.row0, q_len = k.q_len, t_rows = tile_rows(p.group);
   // Keys up to vis0 are visible to every row of the CTA, from vis1 on to none.  Value tiles from `mixed` on are neither.
+  // (A CTA without work, as in a replay with shorter lengths, has n = 0 and nothing else in k that means anything.)
   const int pair_rows = k.rows - row0 < 2 * t_rows ? k.rows - row0 : 2 * t_rows;
   const int vis0 = p.causal ? k.len - q_len + row0 / p.group + 1 : k.len;
   const int vis1 = p.causal ? k.len - q_len + (row0 + pair_rows - 1) / p.group + 1 : k.len;
-  const int mixed = vis0 <= c0 ? 0 : (vis0 - c0) / kTileKeys < n ? (vis0 - c0) / kTileKeys : n;
+  const int mixed = n == 0 || vis0 <= c0 ? 0 : (vis0 - c0) / kTileKeys < n ? (vis0 - c0) / kTileKeys : n;
   // Scores, P and products run through one sequence: number i = key tile * tiles + row tile, buffer i % NB.  Keys are
   // used `lead` tiles ahead of values: the ring holds K 0 .. K lead-1, V 0, K lead, V 1, ..
   const int lead = (C::NB + tiles - 1) / tiles;

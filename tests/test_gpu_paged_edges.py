@@ -337,3 +337,34 @@ def test_infinite_and_missing_values_of_one_dim_add_up(d, dtype):
     out = ~np.isfinite(want)
     y, want, A = (np.where(out, 0.0, x) for x in (y, want, A))
     U.check_attention(dtype, d, y, lse, want, want_lse, A, C, n_keys=450)
+
+
+# ---------------------------------------------------------------------------------------------- thread blocks without work
+@pytest.mark.parametrize("d", [64, 128])
+def test_replays_with_shorter_lengths_between_other_calls(d):
+    # the graph's grid is that of the captured lengths: with shorter ones some thread blocks have nothing to do, and their
+    # shared memory holds what other calls left there
+    import paper_2604_05438_b200 as T
+    dev = torch.device("cuda:0")
+    lens, short = [(40, 900), (90, 9000), (7, 64)], [(40, 41), (90, 95), (7, 60)]
+    s = U.make_step(8, 2, d, 16, "bf16", lens, seed=160)
+    kv, q = U.to_device(s), s.q.to(dev)
+    y, lse = torch.empty_like(q), torch.empty(q.shape[:2], device=dev)
+    ws = torch.empty(T.paged_workspace_bytes(kv, T.WS_PAGED_ATTENTION), dtype=torch.uint8, device=dev)
+    T.paged_attention(kv, q, y, lse, None, 0, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        T.paged_attention(kv, q, y, lse, None, 0, ws)
+    others = [U.make_step(8, 2, dd, 32, "bf16", [(300, 5000), (64, 700)], seed=161) for dd in (64, 128)]
+    others = [(U.to_device(o), o.q.to(dev), torch.empty_like(o.q, device=dev), torch.empty(1 << 28, dtype=torch.uint8, device=dev)) for o in others]
+    kv.kv_lens_dev.copy_(torch.tensor([n for _, n in short]))
+    step = U.Step(s.k, s.v, s.table, np.array([n for _, n in short], np.int64), s.cu_q, 8, s.q)
+    want = PO.attention(U.f64(s.q), U.f64(s.k), U.f64(s.v), step.table, step.kv_lens, s.cu_q)
+    for i in range(12):
+        o = others[i % 2]
+        T.paged_attention(o[0], o[1], o[2], None, None, i % 2 * T.FLAG_FULL_CONTEXT, o[3])
+        y.fill_(7)
+        graph.replay()
+        assert kv.device_status() == 0
+        U.check_attention("bf16", d, U.f64(y), U.f64(lse), *want, n_keys=95)
