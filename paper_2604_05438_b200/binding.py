@@ -274,6 +274,10 @@ class PagedKVCache:
     kv_lens: int64 host [batch], cache lengths with this step's new tokens; cu_q: int64 host [batch+1], the new tokens'
     rows; device copies are kept alongside.  key_bounds: [n_pages, n_kv_heads, 2, head_dim] or None.  status: device
     int32 word in which the kernels leave errors (made here, zero, unless given); ``device_status()`` reads it.
+
+    What is made here may be used on any stream: a call on another stream than the one that was current here waits for it
+    there, and its memory is not handed out again before that call is complete.  The caller's own tensors are the caller's to
+    order and keep, here and in the calls.  With kv_lens_dev and cu_q_dev given nothing is copied and nothing waited for.
     """
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, kv_lens, cu_q, n_q_heads: int,
@@ -293,9 +297,19 @@ class PagedKVCache:
         if key_bounds is not None:
             assert key_bounds.dtype == k.dtype and key_bounds.is_contiguous()
             assert key_bounds.shape == (k.shape[0], k.shape[1], 2, k.shape[3])
-        self.kv_lens_dev = torch.tensor(self.kv_lens, device=dev) if kv_lens_dev is None else kv_lens_dev
-        self.cu_q_dev = torch.tensor(self.cu_q, device=dev) if cu_q_dev is None else cu_q_dev
-        self.status = torch.zeros(1, dtype=torch.int32, device=dev) if status is None else status
+        made = ()
+        if kv_lens_dev is None or cu_q_dev is None:
+            # lengths, cu_q and status in one copy, which is complete when it returns
+            made = (torch.from_numpy(np.concatenate([self.kv_lens, self.cu_q, [0]])).to(dev),)
+            lens, cu, word = made[0].split([len(self.kv_lens), len(self.cu_q), 1])
+            kv_lens_dev = lens if kv_lens_dev is None else kv_lens_dev
+            cu_q_dev = cu if cu_q_dev is None else cu_q_dev
+            status = word.view(torch.int32)[:1] if status is None else status
+            pending = False
+        elif status is None:
+            status = torch.zeros(1, dtype=torch.int32, device=dev)
+            made, pending = (status,), True
+        self.kv_lens_dev, self.cu_q_dev, self.status = kv_lens_dev, cu_q_dev, status
         for t, a in ((self.kv_lens_dev, self.kv_lens), (self.cu_q_dev, self.cu_q)):
             assert t.dtype == torch.int64 and t.shape == a.shape and t.is_contiguous()
         assert self.status.dtype == torch.int32 and self.status.numel() == 1
@@ -307,7 +321,7 @@ class PagedKVCache:
                                 k.stride(2), page_table.data_ptr(), self.kv_lens.ctypes.data, self.kv_lens_dev.data_ptr(),
                                 self.cu_q.ctypes.data, self.cu_q_dev.data_ptr(),
                                 None if key_bounds is None else key_bounds.data_ptr(), self.status.data_ptr())
-        self._handle = _native().handle(C.addressof(self._desc), k.get_device())
+        self._handle = _native().handle(C.addressof(self._desc), k.get_device(), made, bool(made) and pending)
 
     @property
     def batch(self) -> int:

@@ -2,39 +2,68 @@
 // Single-token calls are shorter on the GPU than the same checks written in Python (5 us of 8 for an append), which is
 // why these calls do not go through ctypes as the others do.  Marshalling only.
 #include <torch/csrc/autograd/python_variable.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
 #include <cstring>
+#include <memory>
+#include <vector>
 
 #include "../../include/tkphi.h"
 
 namespace {
 
-// What a PagedKVCache object stands for: the C descriptor and the shapes that a call's tensors must have.
+// What a PagedKVCache object stands for: the C descriptor and the shapes that a call's tensors must have; and the tensors
+// that the object made itself (lengths, status), which a call on another stream than theirs has to wait for and to mark as
+// used there, because the caller does not know them.
 struct Handle {
   tkphi_paged_desc desc;
   at::ScalarType type;
   int device;
   int64_t total_q;
+  std::vector<at::Tensor> made;
+  cudaStream_t made_on = nullptr;
+  cudaEvent_t ready = nullptr;             // behind their making, where that is not complete yet
+  ~Handle() {
+    if (ready) cudaEventDestroy(ready);
+  }
 };
 const char* kCapsule = "paged cache";
 
 Handle* handle_of(PyObject* o) { return static_cast<Handle*>(PyCapsule_GetPointer(o, kCapsule)); }
 void free_handle(PyObject* o) { delete handle_of(o); }
 
-// handle(address of the ctypes descriptor, device index)
+// handle(address of the ctypes descriptor, device index, tuple of the tensors made, whether their making may be pending)
 PyObject* make_handle(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 2) { PyErr_SetString(PyExc_TypeError, "handle(descriptor, device)"); return nullptr; }
+  if (n != 4 || !PyTuple_Check(args[2])) { PyErr_SetString(PyExc_TypeError, "handle(descriptor, device, tensors, pending)"); return nullptr; }
   const void* src = PyLong_AsVoidPtr(args[0]);
   const long dev = PyLong_AsLong(args[1]);
+  const int pending = PyObject_IsTrue(args[3]);
   if (PyErr_Occurred()) return nullptr;
-  Handle* h = new Handle;
-  std::memcpy(&h->desc, src, sizeof(h->desc));
-  h->type = h->desc.dtype == TKPHI_DTYPE_BF16 ? at::kBFloat16 : at::kHalf;
-  h->device = (int)dev;
-  h->total_q = h->desc.cu_q_host[h->desc.batch];
-  return PyCapsule_New(h, kCapsule, free_handle);
+  try {
+    std::unique_ptr<Handle> h(new Handle);
+    std::memcpy(&h->desc, src, sizeof(h->desc));
+    h->type = h->desc.dtype == TKPHI_DTYPE_BF16 ? at::kBFloat16 : at::kHalf;
+    h->device = (int)dev;
+    h->total_q = h->desc.cu_q_host[h->desc.batch];
+    if (dev >= 0) {
+      const c10::cuda::CUDAGuard guard((c10::DeviceIndex)dev);
+      for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(args[2]); ++i) h->made.push_back(THPVariable_Unpack(PyTuple_GET_ITEM(args[2], i)));
+      h->made_on = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream();
+      cudaStreamCaptureStatus captured = cudaStreamCaptureStatusNone;
+      // (made within a capture, the tensors belong to its graph, whose calls are ordered by it)
+      if (pending && cudaStreamIsCapturing(h->made_on, &captured) == cudaSuccess && captured == cudaStreamCaptureStatusNone)
+        if (cudaEventCreateWithFlags(&h->ready, cudaEventDisableTiming) != cudaSuccess || cudaEventRecord(h->ready, h->made_on) != cudaSuccess) {
+          PyErr_SetString(PyExc_RuntimeError, "no event for the cache's stream");
+          return nullptr;
+        }
+    }
+    return PyCapsule_New(h.release(), kCapsule, free_handle);
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
 }
 
 struct Refused {};
@@ -85,12 +114,27 @@ float take_scale(PyObject* o) {
 
 // The stream argument (None: the current one of the cache's device).
 void* take_stream(const Handle* h, PyObject* o) {
-  if (o == Py_None) return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)h->device).stream();
-  PyObject* raw = PyObject_GetAttrString(o, "cuda_stream");
-  if (!raw) throw Refused{};
-  void* s = PyLong_AsVoidPtr(raw);
-  Py_DECREF(raw);
-  if (PyErr_Occurred()) throw Refused{};
+  cudaStream_t s = nullptr;
+  if (o == Py_None) {
+    s = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)h->device).stream();
+  } else {
+    PyObject* raw = PyObject_GetAttrString(o, "cuda_stream");
+    if (!raw) throw Refused{};
+    s = static_cast<cudaStream_t>(PyLong_AsVoidPtr(raw));
+    Py_DECREF(raw);
+    if (PyErr_Occurred()) throw Refused{};
+  }
+  if (s != h->made_on && !h->made.empty()) {
+    cudaStreamCaptureStatus captured = cudaStreamCaptureStatusNone;
+    // (a captured call cannot wait for what was enqueued before the capture; the capture itself begins behind it)
+    if (h->ready && cudaStreamIsCapturing(s, &captured) == cudaSuccess && captured == cudaStreamCaptureStatusNone &&
+        cudaStreamWaitEvent(s, h->ready, 0) != cudaSuccess) {
+      PyErr_SetString(PyExc_RuntimeError, "the call's stream cannot wait for the cache's");
+      throw Refused{};
+    }
+    const c10::cuda::CUDAStream used = c10::cuda::getStreamFromExternal(s, (c10::DeviceIndex)h->device);
+    for (const at::Tensor& t : h->made) c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), used);
+  }
   return s;
 }
 

@@ -368,3 +368,76 @@ def test_replays_with_shorter_lengths_between_other_calls(d):
         graph.replay()
         assert kv.device_status() == 0
         U.check_attention("bf16", d, U.f64(y), U.f64(lse), *want, n_keys=95)
+# ---------------------------------------------------------------------------------------------- streams
+def _one_call(s, kv, stream):
+    import paper_2604_05438_b200 as T
+    q = s.q.cuda()
+    out = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda:0")
+    ws = torch.empty(T.paged_workspace_bytes(kv, T.WS_PAGED_ATTENTION), dtype=torch.uint8, device="cuda:0")
+    torch.cuda.current_stream().synchronize()
+    T.paged_attention(kv, q, *out, None, 0, ws, stream=stream)
+    return out + (q, ws)
+
+
+def test_a_call_on_another_stream_waits_for_the_status_word_that_the_cache_made():
+    import paper_2604_05438_b200 as T
+    s = U.make_step(4, 2, 64, 16, "bf16", [(1, 100)], seed=150)
+    s.table[0, 2] = -1                                      # a page that is reported
+    k, v, table = s.k.cuda(), s.v.cuda(), torch.from_numpy(s.table).cuda()
+    lens, cu, q = torch.tensor(s.kv_lens).cuda(), torch.tensor(s.cu_q).cuda(), s.q.cuda()
+    y, lse, ws = torch.empty_like(q), torch.empty(1, 4, device="cuda:0"), torch.empty(1 << 24, dtype=torch.uint8, device="cuda:0")
+    side, maker = torch.cuda.Stream(), torch.cuda.Stream()
+    # (a first call loads the kernels, which may wait for the device)
+    T.paged_attention(T.PagedKVCache(k, v, table, s.kv_lens, s.cu_q, 4), q, y, lse, None, 0, ws)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(maker):
+        torch.cuda._sleep(100_000_000)                      # the zero of the status word comes behind this
+        kv = T.PagedKVCache(k, v, table, s.kv_lens, s.cu_q, 4, kv_lens_dev=lens, cu_q_dev=cu)
+    T.paged_attention(kv, q, y, lse, None, 0, ws, stream=side)
+    torch.cuda.synchronize()
+    assert kv.device_status() == -1
+
+
+@pytest.mark.parametrize("given", [False, True])
+def test_memory_that_the_cache_made_is_kept_until_a_call_on_another_stream_is_complete(given):
+    import paper_2604_05438_b200 as T
+    s = U.make_step(4, 2, 64, 16, "bf16", [(1, 100)], seed=151)
+    k, v, table = s.k.cuda(), s.v.cuda(), torch.from_numpy(s.table).cuda()
+    more = dict(kv_lens_dev=torch.tensor(s.kv_lens).cuda(), cu_q_dev=torch.tensor(s.cu_q).cuda()) if given else {}
+    side = torch.cuda.Stream()
+    for use in ("argument", "current"):
+        kv = T.PagedKVCache(k, v, table, s.kv_lens, s.cu_q, 4, **more)
+        made = {t.untyped_storage().data_ptr() for t in ([kv.status] if given else [kv.status, kv.kv_lens_dev, kv.cu_q_dev])}
+        size = max(t.untyped_storage().nbytes() for t in (kv.status, kv.kv_lens_dev, kv.cu_q_dev))
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)
+        if use == "argument":
+            keep = _one_call(s, kv, side)
+        else:
+            with torch.cuda.stream(side):
+                q = s.q.cuda(non_blocking=True)
+                ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda:0")
+                keep = torch.empty_like(q), q, ws
+                T.paged_attention(kv, q, keep[0], None, None, 0, ws)
+        busy = not side.query()
+        del kv
+        fresh = [torch.empty(size, dtype=torch.uint8, device="cuda:0") for _ in range(8)]
+        taken = {t.data_ptr() for t in fresh} & made
+        torch.cuda.synchronize()
+        assert busy and not taken, use
+        del keep, fresh
+
+
+def test_the_same_results_on_another_stream_than_the_cache_was_made_on():
+    import paper_2604_05438_b200 as T
+    s = U.make_step(4, 2, 64, 16, "bf16", [(1, 100), (40, 90)], seed=152)
+    want, want_lse = U.gpu_attention(s)
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        kv = U.to_device(s)
+        y, lse, *keep = _one_call(s, kv, side)
+        del kv
+        junk = [torch.full((4096,), 255, dtype=torch.uint8, device="cuda:0") for _ in range(4)]
+        torch.cuda.synchronize()
+        np.testing.assert_array_equal(U.f64(y), want)
+        np.testing.assert_array_equal(U.f64(lse), want_lse)
