@@ -331,7 +331,9 @@ class PagedKVCache:
         return self._desc
 
     def device_status(self) -> int:
-        """0, or the error that a call on this descriptor's status word left there (waits for the device)."""
+        """0, or the error that a call on this descriptor's status word left there (waits for all streams of the device)."""
+        if self.status.is_cuda:
+            torch.cuda.synchronize(self.status.device)
         return int(self.status.item())
 
 

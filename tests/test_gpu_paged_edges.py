@@ -441,3 +441,18 @@ def test_the_same_results_on_another_stream_than_the_cache_was_made_on():
         torch.cuda.synchronize()
         np.testing.assert_array_equal(U.f64(y), want)
         np.testing.assert_array_equal(U.f64(lse), want_lse)
+
+
+def test_device_status_waits_for_calls_on_every_stream():
+    import paper_2604_05438_b200 as T
+    s = U.make_step(4, 2, 64, 16, "bf16", [(1, 100)], seed=153)
+    s.table[0, 2] = -1
+    kv, q = U.to_device(s), s.q.cuda()
+    y, ws = torch.empty_like(q), torch.empty(1 << 24, dtype=torch.uint8, device="cuda:0")
+    T.paged_attention(U.to_device(s), q, y, None, None, 0, ws)         # (loads the kernels)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+    T.paged_attention(kv, q, y, None, None, 0, ws, stream=side)
+    assert kv.device_status() == -1
