@@ -153,10 +153,16 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _stream_ptr(stream) -> Optional[int]:
+def _stream_ptr(stream, kv: Optional["KVCache"] = None) -> Optional[int]:
+    """The stream's handle; what kv made itself is marked as used there."""
     if stream is None:      # (the raw handle: building a Stream object for it takes longer than a kernel launch)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
-    return stream.cuda_stream or None
+        raw = torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    else:
+        raw = stream.cuda_stream
+    if kv is not None and kv._made and raw != kv._made_on:
+        for t in kv._made:
+            t.record_stream(torch.cuda.current_stream() if stream is None else stream)
+    return raw or None
 
 
 @dataclass
@@ -165,7 +171,8 @@ class KVCache:
 
     k, v: bf16 device tensors addressed as [head, row, dim] through the strides
     (any layout whose innermost dim is contiguous).  cu_seqlens: int64 host array
-    [batch+1]; a device copy is kept alongside.
+    [batch+1]; a device copy is kept alongside (its memory is not handed out again
+    before calls on other streams that read it are complete).
     """
     k: torch.Tensor
     v: torch.Tensor
@@ -180,13 +187,17 @@ class KVCache:
 
     def __post_init__(self):
         self.cu_seqlens = np.ascontiguousarray(self.cu_seqlens, dtype=np.int64)
+        self._made = []                            # device tensors that the caller does not know
         if self.cu_seqlens_dev is None:
             self.cu_seqlens_dev = torch.from_numpy(self.cu_seqlens).to(self.k.device)
+            self._made.append(self.cu_seqlens_dev)
         if self.n_tail_seq is not None:
             self.n_tail_seq = np.ascontiguousarray(self.n_tail_seq, dtype=np.int32)
             assert self.n_tail_seq.shape == (len(self.cu_seqlens) - 1,)
             if self.n_tail_seq_dev is None:
                 self.n_tail_seq_dev = torch.from_numpy(self.n_tail_seq).to(self.k.device)
+                self._made.append(self.n_tail_seq_dev)
+        self._made_on = torch._C._cuda_getCurrentRawStream(self.k.get_device()) if self.k.is_cuda else None
 
     @property
     def batch(self) -> int:
@@ -383,7 +394,7 @@ def build_summaries(kv: KVCache, phi: PhiMaps, S: torch.Tensor, u: torch.Tensor,
     d, ph = kv.desc(), phi.desc()
     _check(lib.tkphi_build_summaries(C.byref(d), C.byref(ph), S.data_ptr(), u.data_ptr(),
                                      workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                     _stream_ptr(stream)))
+                                     _stream_ptr(stream, kv)))
 
 
 def build_summaries_static(kv: KVCache, phi: PhiMaps, S: torch.Tensor, u: torch.Tensor, stream=None) -> None:
@@ -392,7 +403,7 @@ def build_summaries_static(kv: KVCache, phi: PhiMaps, S: torch.Tensor, u: torch.
     scratch raise TkphiError (status -3).  Calls that overlap on the GPU race."""
     lib = load_library()
     d, ph = kv.desc(), phi.desc()
-    st = lib.tkphi_build_summaries_static(C.byref(d), C.byref(ph), S.data_ptr(), u.data_ptr(), _stream_ptr(stream))
+    st = lib.tkphi_build_summaries_static(C.byref(d), C.byref(ph), S.data_ptr(), u.data_ptr(), _stream_ptr(stream, kv))
     if st != 0:
         raise TkphiError(st, lib.tkphi_static_last_error().decode())
 
@@ -418,7 +429,7 @@ def mlp_key_features(kv: KVCache, mlp_k: MlpMaps, phi_k_cache: torch.Tensor, wor
     lib = load_library()
     d, m = kv.desc(), mlp_k.desc()
     _check(lib.tkphi_mlp_key_features(C.byref(d), C.byref(m), phi_k_cache.data_ptr(), workspace.data_ptr(),
-                                      workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+                                      workspace.numel() * workspace.element_size(), _stream_ptr(stream, kv)))
 
 
 def build_summaries_cached(kv: KVCache, phi_k_cache: torch.Tensor, S: torch.Tensor, u: torch.Tensor,
@@ -427,7 +438,7 @@ def build_summaries_cached(kv: KVCache, phi_k_cache: torch.Tensor, S: torch.Tens
     d = kv.desc()
     _check(lib.tkphi_build_summaries_cached(C.byref(d), phi_k_cache.data_ptr(), S.data_ptr(), u.data_ptr(),
                                             workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                            _stream_ptr(stream)))
+                                            _stream_ptr(stream, kv)))
 
 
 def decode_step_mlp(kv: KVCache, mlp_q: MlpMaps, phi_k_cache: Optional[torch.Tensor], q: torch.Tensor, topk_host,
@@ -440,7 +451,7 @@ def decode_step_mlp(kv: KVCache, mlp_q: MlpMaps, phi_k_cache: Optional[torch.Ten
     _check(lib.tkphi_decode_step_mlp(C.byref(d), C.byref(m), _ptr(phi_k_cache), q.data_ptr(), th.ctypes.data,
                                      topk_dev.data_ptr(), int(topk_max), S.data_ptr(), u.data_ptr(), _ptr(idx_out),
                                      y_out.data_ptr(), _ptr(dbg_out), int(flags), workspace.data_ptr(),
-                                     workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+                                     workspace.numel() * workspace.element_size(), _stream_ptr(stream, kv)))
 
 
 def topk_decode(kv: KVCache, q: torch.Tensor, topk_host, topk_dev: torch.Tensor, topk_max: int,
@@ -451,7 +462,7 @@ def topk_decode(kv: KVCache, q: torch.Tensor, topk_host, topk_dev: torch.Tensor,
     th = _topk_host(topk_host)
     _check(lib.tkphi_topk_decode(C.byref(d), q.data_ptr(), th.ctypes.data, topk_dev.data_ptr(), int(topk_max),
                                  _ptr(idx_out), y_out.data_ptr(), workspace.data_ptr(),
-                                 workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+                                 workspace.numel() * workspace.element_size(), _stream_ptr(stream, kv)))
 
 
 def decode_step(kv: KVCache, phi: PhiMaps, q: torch.Tensor, topk_host, topk_dev: torch.Tensor,
@@ -464,7 +475,7 @@ def decode_step(kv: KVCache, phi: PhiMaps, q: torch.Tensor, topk_host, topk_dev:
     _check(lib.tkphi_decode_step(C.byref(d), C.byref(ph), q.data_ptr(), th.ctypes.data, topk_dev.data_ptr(),
                                  int(topk_max), S.data_ptr(), u.data_ptr(), _ptr(idx_out), y_out.data_ptr(),
                                  _ptr(dbg_out), int(flags), workspace.data_ptr(),
-                                 workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+                                 workspace.numel() * workspace.element_size(), _stream_ptr(stream, kv)))
 
 
 def paged_workspace_bytes(kv: PagedKVCache, which: int, selection: Optional[PageSelection] = None) -> int:

@@ -456,3 +456,33 @@ def test_device_status_waits_for_calls_on_every_stream():
         torch.cuda._sleep(100_000_000)
     T.paged_attention(kv, q, y, None, None, 0, ws, stream=side)
     assert kv.device_status() == -1
+
+
+@pytest.mark.parametrize("use", ["argument", "current"])
+def test_memory_that_a_contiguous_cache_made_is_kept_for_other_streams_too(use):
+    import paper_2604_05438_b200 as T
+    dev = torch.device("cuda:0")
+    k = torch.randn(2, 300, 64, device=dev).bfloat16()
+    q, y = torch.randn(1, 4, 64, device=dev).bfloat16(), torch.empty(1, 4, 64, device=dev)
+    topk = np.array([20], np.int32)
+    topk_dev, side = torch.from_numpy(topk).to(dev), torch.cuda.Stream()
+    kv = T.KVCache(k, k, np.array([0, 300]), 4, 64, 4, 16, n_tail_seq=[12])
+    ws = torch.empty(T.workspace_bytes(kv, topk, 20, T.WS_TOPK_DECODE), dtype=torch.uint8, device=dev)
+    T.topk_decode(kv, q, topk, topk_dev, 20, None, y, ws)              # (loads the kernels)
+    torch.cuda.synchronize()
+    want = y.clone()
+    made = {kv.cu_seqlens_dev.untyped_storage().data_ptr(), kv.n_tail_seq_dev.untyped_storage().data_ptr()}
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+    if use == "argument":
+        T.topk_decode(kv, q, topk, topk_dev, 20, None, y, ws, stream=side)
+    else:
+        with torch.cuda.stream(side):
+            T.topk_decode(kv, q, topk, topk_dev, 20, None, y, ws)
+    busy = not side.query()
+    del kv
+    fresh = [torch.empty(16, dtype=torch.uint8, device=dev) for _ in range(8)]
+    taken = {t.data_ptr() for t in fresh} & made
+    torch.cuda.synchronize()
+    assert busy and not taken
+    assert torch.equal(y, want)
