@@ -7,6 +7,7 @@
 #include <c10/cuda/CUDAStream.h>
 
 #include <cstring>
+#include <limits>
 #include <memory>
 #include <vector>
 
@@ -108,8 +109,16 @@ float take_scale(PyObject* o) {
   if (o == Py_None) return 0.f;
   const double s = PyFloat_AsDouble(o);
   if (PyErr_Occurred()) throw Refused{};
-  if (!(s > 0)) refuse("scale", "must be positive");
+  // (in 32 bits, as the library takes it: there 0 stands for 1 / sqrt(head_dim))
+  if (!((float)s > 0.f && (float)s <= std::numeric_limits<float>::max())) refuse("scale", "must be positive and finite in 32 bits");
   return (float)s;
+}
+
+uint32_t take_flags(PyObject* o) {
+  const unsigned long f = PyLong_AsUnsignedLong(o);
+  if (PyErr_Occurred()) throw Refused{};
+  if (f > 0xffffffffu) refuse("flags", "has unknown bits");
+  return (uint32_t)f;
 }
 
 // The stream argument (None: the current one of the cache's device).
@@ -179,15 +188,14 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // attention(handle, q, y_out, lse_out, scale, flags, workspace, stream)
 PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return run(a, n, 8, [&](const Handle* h) {
+    const float scale = take_scale(a[4]);
+    const uint32_t flags = take_flags(a[5]);
     const void* q = take_heads(h, a[1], "q", h->desc.n_q_heads, true);
     void* y = take_heads(h, a[2], "y_out", h->desc.n_q_heads, true);
     float* lse = take_lse(h, a[3]);
-    const float scale = take_scale(a[4]);
-    const unsigned long flags = PyLong_AsUnsignedLong(a[5]);
-    if (PyErr_Occurred()) throw Refused{};
     size_t bytes = 0;
     void* ws = take_workspace(h, a[6], &bytes);
-    return tkphi_paged_attention(&h->desc, q, y, lse, scale, (uint32_t)flags, ws, bytes, take_stream(h, a[7]));
+    return tkphi_paged_attention(&h->desc, q, y, lse, scale, flags, ws, bytes, take_stream(h, a[7]));
   });
 }
 
@@ -202,13 +210,13 @@ PyObject* block_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
       v[i] = (int32_t)x;
     }
     const tkphi_page_selection sel{v[0], v[1], v[2]};
+    const float scale = take_scale(a[8]);
     const void* q = take_heads(h, a[4], "q", h->desc.n_q_heads, true);
     void* y = take_heads(h, a[5], "y_out", h->desc.n_q_heads, true);
     float* lse = take_lse(h, a[6]);
     int32_t* idx = nullptr;
     if (a[7] != Py_None)
       idx = static_cast<int32_t*>(take(h, a[7], "page_idx_out", at::kInt, {h->total_q, h->desc.n_kv_heads, (int64_t)v[0] + v[1] + v[2]}, true));
-    const float scale = take_scale(a[8]);
     size_t bytes = 0;
     void* ws = take_workspace(h, a[9], &bytes);
     return tkphi_paged_block_attention(&h->desc, &sel, q, y, lse, idx, scale, ws, bytes, take_stream(h, a[10]));
