@@ -303,7 +303,7 @@ tkphi_status tkphi_decode_step_mlp(const tkphi_kv_desc* kv, const tkphi_mlp_desc
  * Requirements: 1 <= batch <= 1024; head_dim 64 or 128; n_q_heads a multiple of n_kv_heads, at most 16 query heads per
  * KV head; page_size 16, 32, 64 or 128; k, v (and key_bounds) 16-byte aligned; strides multiples of 8 elements that
  * give every element memory of its own (in any order of page, head and slot); cu_q[0] = 0, non-decreasing;
- * 0 <= q_len <= kv_len <= max_pages * page_size (TKPHI_FLAG_FULL_CONTEXT lifts q_len <= kv_len), kv_len < 2^31 - 1024.
+ * 0 <= q_len <= kv_len <= max_pages * page_size (TKPHI_FLAG_FULL_CONTEXT lifts q_len <= kv_len), kv_len <= 2^30.
  * Host and device copies as in the general rules, with one addition for captured graphs: the launches are sized by
  * the host copy of kv_lens, and a replayed graph may find other device lengths as long as each is at most the captured
  * host value and still at least q_len; cu_q must be the captured one.

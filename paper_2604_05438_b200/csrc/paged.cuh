@@ -15,6 +15,7 @@ constexpr int kRowKeys = 64;                // keys of one tile of the row kerne
 constexpr int kTileRows = 256;              // rows of a tile-kernel CTA: two 128-row MMA tiles
 constexpr int kTileKeys = 128;              // keys of one tile of the tile kernel
 constexpr int kMaxSelectPages = 131072;     // pages of a sequence of the page-selected form
+constexpr int kMaxKvLen = 1 << 30;          // cache rows of a sequence: a length and a chunk of it add up within 31 bits
 constexpr int kMaxGroup = 16;               // query heads per KV head of the paged calls
 
 // One step over a paged cache.  Sequence b brings cu_q[b+1] - cu_q[b] new tokens, the last ones of its

@@ -55,7 +55,7 @@ tkphi_status validate_paged(const tkphi_paged_desc* kv, PagedShape* sh, bool nee
   if (!kv->kv_lens_host || !kv->cu_q_host) return fail(TKPHI_ERR_INVALID_ARG, "kv_lens_host or cu_q_host is NULL");
   const int64_t* cu = kv->cu_q_host;
   if (cu[0] != 0) return fail(TKPHI_ERR_INVALID_ARG, "cu_q[0] must be 0");
-  const int64_t room = std::min<int64_t>((int64_t)kv->max_pages * kv->page_size, (int64_t)INT_MAX - 1024);
+  const int64_t room = std::min<int64_t>((int64_t)kv->max_pages * kv->page_size, kMaxKvLen);
   sh->max_kv = 0; sh->max_q = 0;
   for (int b = 0; b < kv->batch; ++b) {
     // no overflow: both checked against small bounds before they are subtracted

@@ -47,3 +47,16 @@ def test_selections_out_of_range(kv):
     for bad in ((1 << 25, 1, 1), (1, -2, 1), (1, 1, 1 << 62)):
         with pytest.raises(ValueError, match="selection"):
             T.paged_block_attention(kv, T.PageSelection(*bad), Q, Q.clone(), None, None, None, WS)
+
+
+def test_the_longest_sequence():
+    # 2^30 rows: beyond it a length and a chunk of it no longer add up within 31 bits on the device (a table may repeat pages,
+    # so that such a cache need not be large)
+    import test_paged_host as H
+    lib = T.load_library()
+    for d, page in ((64, 16), (128, 128)):
+        for rows, status in ((1 << 30, -3), ((1 << 30) + 1, -1), ((1 << 31) - 1025, -1)):
+            desc = H.Desc(lens=((1, rows), (500, rows)), d=d, ps=page, strides=(2 * page * d, page * d, d), max_pages=(1 << 31) // page)
+            assert H._attend(lib, desc, ws=0) == status, (rows, lib.tkphi_last_error())
+            if status == -1:
+                assert H._append(lib, desc, rot_dim=d, inv_freq=0) == -1 and b"kv_lens" in lib.tkphi_last_error()
