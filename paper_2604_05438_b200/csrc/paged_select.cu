@@ -544,10 +544,10 @@ static cudaError_t select_t(PagedProblem p, int n, int row_tiles, cudaStream_t s
 }
 
 int paged_score_parts(int row_tiles, int hkv, int n) {
-  // A row tile's pages over enough CTAs for two per multiprocessor, and no more: each builds its fragments anew.  Four
-  // where the row tiles alone are one to three per multiprocessor, so that lengths that differ even out (32 sequences of
-  // 8K-64K: 90.5 us a call against 93.0; with more row tiles it costs: 236 tokens, 217 against 214).
-  const int n_sm = sm_count_current_device(), have = row_tiles * hkv, ctas = (have >= n_sm && have < 3 * n_sm ? 4 : 2) * n_sm;
+  // A row tile's pages over enough CTAs for two per multiprocessor, and no more: each builds its fragments anew.  (Four per
+  // multiprocessor, one token of 16 to 96 sequences of 16K or 4K-30K each: a call is up to 2.5% shorter at head_dim 128 and up
+  // to 7% longer at 64, at either where the row tiles alone are three per multiprocessor.)
+  const int have = row_tiles * hkv, ctas = 2 * sm_count_current_device();
   const int want = (ctas + have - 1) / (have > 0 ? have : 1);
   const int most = (n + kScorePages - 1) / kScorePages;
   return want < most ? want : most > 0 ? most : 1;
