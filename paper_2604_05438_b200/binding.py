@@ -261,7 +261,7 @@ _native_module = None
 
 
 def _native():
-    """The CPython module of the paged calls (built in-tree beside libtkphi.so); raises if absent."""
+    """The CPython module of the paged calls (built in-tree beside libtkphi.so); raises if absent or built for another torch."""
     global _native_module
     if _native_module is None:
         load_library()
@@ -270,6 +270,9 @@ def _native():
         except ImportError as e:
             raise RuntimeError("_paged_binding.so is missing or does not load: build it with "
                                "`python -m paper_2604_05438_b200.build`") from e
+        if _paged_binding.torch_version != torch.__version__:
+            raise RuntimeError(f"_paged_binding.so was built for torch {_paged_binding.torch_version}, this is "
+                               f"{torch.__version__}: build it again with `python -m paper_2604_05438_b200.build`")
         _native_module = _paged_binding
     return _native_module
 

@@ -223,14 +223,23 @@ PyObject* block_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// (a fast call has another signature than the table's)
+PyCFunction fast(PyObject* (*f)(PyObject*, PyObject* const*, Py_ssize_t)) {
+  return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f));
+}
+
 PyMethodDef methods[] = {
-    {"handle", reinterpret_cast<PyCFunction>(make_handle), METH_FASTCALL, nullptr},
-    {"append", reinterpret_cast<PyCFunction>(append), METH_FASTCALL, nullptr},
-    {"attention", reinterpret_cast<PyCFunction>(attention), METH_FASTCALL, nullptr},
-    {"block_attention", reinterpret_cast<PyCFunction>(block_attention), METH_FASTCALL, nullptr},
+    {"handle", fast(make_handle), METH_FASTCALL, nullptr},
+    {"append", fast(append), METH_FASTCALL, nullptr},
+    {"attention", fast(attention), METH_FASTCALL, nullptr},
+    {"block_attention", fast(block_attention), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_paged_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__paged_binding(void) { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__paged_binding(void) {
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "torch_version", TKPHI_TORCH_VERSION) < 0) { Py_DECREF(m); return nullptr; }
+  return m;
+}
