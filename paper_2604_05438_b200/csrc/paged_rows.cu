@@ -371,22 +371,24 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             tA = fmaxf(tA, __shfl_xor_sync(0xffffffffu, tA, d));
             tB = fmaxf(tB, __shfl_xor_sync(0xffffffffu, tB, d));
           }
-          const float nA = fmaxf(mA, tA * p.scale_log2), nB = fmaxf(mB, tB * p.scale_log2);
+          // (maxima are kept as scores, before the scale: the largest score less the maximum is then exactly 0, where
+          // scale * score - scaled maximum in one FMA would leave the rounding of the maximum, beyond 2^30 a factor of 2^64)
+          const float nA = fmaxf(mA, tA), nB = fmaxf(mB, tB);
           if (__any_sync(0xffffffffu, nA > mA || nB > mB)) {
-            const float fA = nA > mA ? ex2_approx(mA - nA) : 1.f, fB = nB > mB ? ex2_approx(mB - nB) : 1.f;
+            const float fA = nA > mA ? ex2_approx((mA - nA) * p.scale_log2) : 1.f, fB = nB > mB ? ex2_approx((mB - nB) * p.scale_log2) : 1.f;
             lA *= fA; lB *= fB;
 #pragma unroll
             for (int n = 0; n < D / 8; ++n) { o[n][0] *= fA; o[n][1] *= fA; o[n][2] *= fB; o[n][3] *= fB; }
             mA = nA; mB = nB;
           }
           // a row that has seen nothing yet: every term exp2(-inf - 0) = 0
-          const float uA = kShift - (mA == -INFINITY ? 0.f : mA), uB = kShift - (mB == -INFINITY ? 0.f : mB);
+          const float uA = mA == -INFINITY ? 0.f : mA, uB = mB == -INFINITY ? 0.f : mB;
 #pragma unroll
           for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              s[n][e] = ex2_approx(fmaf(s[n][e], p.scale_log2, uA));
-              s[n][2 + e] = ex2_approx(fmaf(s[n][2 + e], p.scale_log2, uB));
+              s[n][e] = ex2_approx(fmaf(s[n][e] - uA, p.scale_log2, kShift));
+              s[n][2 + e] = ex2_approx(fmaf(s[n][2 + e] - uB, p.scale_log2, kShift));
               lA += s[n][e];
               lB += s[n][2 + e];
             }
@@ -437,7 +439,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       }
 
       // ---- the warps' softmaxes joined; a thread ends up with PER of 64 dims of one row
-      mA -= kShift; mB -= kShift;
+      mA = mA * p.scale_log2 - kShift; mB = mB * p.scale_log2 - kShift;
 #pragma unroll
       for (int d = 1; d < 4; d <<= 1) {
         lA += __shfl_xor_sync(0xffffffffu, lA, d);

@@ -43,6 +43,10 @@ namespace tkphi {
 constexpr int kTileThreads = 384;
 constexpr int kWarpMma = 8, kWarpTma = 9;
 constexpr uint32_t kTileTmemCols = 512;      // S / P buffers of 128 columns, then the two outputs
+// References in log2 units (and the -inf of a row that has seen nothing) beyond which every tile is done carefully: scale *
+// score - scaled reference in one FMA carries the rounding of the reference, 2^-2 here, which beyond 2^31 would push the
+// largest term out of range.  Carefully, the reference is taken off before the scale.
+constexpr float kFarReference = 4194304.f;
 constexpr float kGrow = 1.f;                 // log2: how far a tile's maximum passes the reference before it replaces it
 
 // Two fp32 values as one operand of the packed FMA instructions.
@@ -297,7 +301,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     const uint32_t o_addr = tmem_addr(tmem, quad * 32, C::O_COL + t * D);
     int buf = t;
     uint32_t phase = 0;
-    float m = -INFINITY, l = 0.f;
+    float m = -INFINITY, l = 0.f;                              // the reference (a score, before the scale) and the sum
     bool ok = true;
     for (int j = 0; j < nt; ++j) {
       ok = __all_sync(0xffffffffu, mbar_wait(&s_full[buf], phase, s_abort));
@@ -306,9 +310,10 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       const uint32_t s_addr = tmem_addr(tmem, quad * 32, buf * 128);
       const int key0 = c0 + j * kTileKeys;
       uint32_t w[64];
-      bool careful = j == 0 || __any_sync(0xffffffffu, live && (key0 + kTileKeys - 1 > lim || m == -INFINITY));
+      bool careful = j == 0 || __any_sync(0xffffffffu, live && (key0 + kTileKeys - 1 > lim || !(fabsf(m * p.scale_log2) < kFarReference)));
       if (!careful) {
-        const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), off2 = pack2(kShift - m, kShift - m);
+        const float off = fmaf(-m, p.scale_log2, kShift);
+        const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), off2 = pack2(off, off);
         uint64_t sum2[2] = {0, 0};
         float u[32], v[32];
         // pairs of a 32-column piece: the first kEmulated on the FMA pipes, spread between the others
@@ -366,10 +371,10 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 #pragma unroll
           for (int e = 2; e < 32; e += 2) mx[c] = fmaxf(mx[c], fmaxf(s[c][e], s[c][e + 1]));
         }
-        const float cand = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
-        const bool grow = live && cand > m + kGrow;
+        const float cand = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        const bool grow = live && (cand - m) * p.scale_log2 > kGrow;
         if (__any_sync(0xffffffffu, grow)) {
-          const float f = grow ? ex2_approx(m - cand) : 1.f;   // m = -inf: 0
+          const float f = grow ? ex2_approx((m - cand) * p.scale_log2) : 1.f;   // m = -inf: 0
           if (j > 0) {
             // The product before this one must be complete.  With as many score buffers as row tiles these scores were
             // issued after it.  With three buffers and two row tiles the next scores were (or, where there are none, it
@@ -398,18 +403,22 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           l *= f;
           if (grow) m = cand;
         }
-        const float off = kShift - (m == -INFINITY ? 0.f : m);
+        const float ref = m == -INFINITY ? 0.f : m, off = fmaf(-ref, p.scale_log2, kShift);
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        auto terms = [&](auto arg) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+          for (int c = 0; c < 4; ++c)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float a = ex2_approx(fmaf(s[c][2 * e], p.scale_log2, off));
-            const float d = ex2_approx(fmaf(s[c][2 * e + 1], p.scale_log2, off));
-            sum[(c & 1) * 2] += a;
-            sum[(c & 1) * 2 + 1] += d;
-            w[c * 16 + e] = T::pack(a, d);
-          }
+            for (int e = 0; e < 16; ++e) {
+              const float a = ex2_approx(arg(s[c][2 * e])), d = ex2_approx(arg(s[c][2 * e + 1]));
+              sum[(c & 1) * 2] += a;
+              sum[(c & 1) * 2 + 1] += d;
+              w[c * 16 + e] = T::pack(a, d);
+            }
+        };
+        // far: the difference before the scale, exactly 0 for the score that is the reference, whatever its size
+        if (__any_sync(0xffffffffu, live && fabsf(off) >= kFarReference)) terms([&](float x) { return fmaf(x - ref, p.scale_log2, kShift); });
+        else terms([&](float x) { return fmaf(x, p.scale_log2, off); });
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       }
       tmem_st_x32(s_addr, w);
@@ -461,10 +470,10 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             if (live) y[c * 4 + e] = v;
           }
         }
-        if (live && p.lse) p.lse[out_row] = l != 0.f ? (m - kShift + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        if (live && p.lse) p.lse[out_row] = l != 0.f ? (m * p.scale_log2 - kShift + log2f(l)) * 0.6931471805599453f : -INFINITY;
       } else {
         const size_t slot_row = (size_t)cta * kTileRows + t * t_rows + (tid & 127);
-        if (live) reinterpret_cast<float2*>(p.tile_stat)[slot_row] = make_float2(l != 0.f ? m - kShift : -INFINITY, l);
+        if (live) reinterpret_cast<float2*>(p.tile_stat)[slot_row] = make_float2(l != 0.f ? m * p.scale_log2 - kShift : -INFINITY, l);
         if (nt > 0) {
           float* dst = p.tile_part + slot_row * D;
 #pragma unroll

@@ -119,6 +119,37 @@ def test_the_exponential_over_its_range(d, dtype, low):
     assert (np.abs(y[:, 0, 0] - want[:, 0, 0]) <= tol).all()
 
 
+@pytest.mark.parametrize("dtype,high", [("fp16", 2.0 ** 15), ("bf16", 2.0 ** 15), ("bf16", 2.0 ** 24)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("q_len,n", [(1, 900), (3, 1200), (1, 20000), (30, 700), (60, 7001)])
+def test_scores_of_very_large_size(q_len, n, d, dtype, high):
+    # exact products up to 2^30 (2^48), no two of them closer than 2^15: the largest key takes all
+    s = U.make_step(2, 1, d, 32, dtype, [(q_len, n)], seed=113)
+    g = torch.Generator().manual_seed(114)
+    s.q[:] = 0.0
+    s.q[:, :, 0] = high
+    s.k[~s.k.isnan()] = 0.0
+    unit = 128.0 if dtype == "fp16" else high / 256                    # 256 different keys, the largest one from each of them on
+    best, at = -1, []
+    for t in range(n):
+        x = int(torch.randint(0, 4 + 252 * t // n, (1,), generator=g))
+        while x == best:                                               # (one key is the largest of those before it)
+            x = int(torch.randint(0, 4 + 252 * t // n, (1,), generator=g))
+        if x > best:
+            best, top = x, t
+        at.append(top)
+        s.k[s.table[0, t // 32], 0, t % 32, 0] = x * unit
+    y, lse = U.gpu_attention(s, scale=1.0)
+    v, k = U.f64(s.v), U.f64(s.k)
+    u = torch.finfo(U.DT[dtype]).eps / 2
+    for i in range(q_len):
+        t = at[n - q_len + i]
+        row = v[s.table[0, t // 32], 0, t % 32]
+        assert (np.abs(y[i] - row) <= 2 * u * np.abs(row) + 2.0 ** -24).all(), i      # (the weight 1 and the output rounded)
+        want = high * k[s.table[0, t // 32], 0, t % 32, 0]
+        assert (np.abs(lse[i] - want) <= 2.0 ** -21 * want).all()      # product by log2 e, the sum's logarithm, and back
+
+
 # ---------------------------------------------------------------------------------------------- values that are no numbers
 def _check_rows(dtype, d, y, lse, want, n_keys):
     """Rows whose sum is no number: y and lse are NaN.  The others as ever (C without the keys whose score is -inf)."""
