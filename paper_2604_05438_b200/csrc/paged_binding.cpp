@@ -169,6 +169,8 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return run(a, n, 9, [&](const Handle* h) {
     tkphi_append_desc d{};
     const int64_t hkv = h->desc.n_kv_heads, hq = h->desc.n_q_heads;
+    d.pairs = PyObject_IsTrue(a[4]);
+    if (d.pairs < 0) throw Refused{};                  // (something without a truth value)
     d.k_new = take_heads(h, a[1], "k_new", hkv, false, &d.k_stride_token, &d.k_stride_head);
     d.v_new = take_heads(h, a[2], "v_new", hkv, false, &d.v_stride_token, &d.v_stride_head);
     if (a[3] != Py_None) {
@@ -177,7 +179,6 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
       d.inv_freq = static_cast<const float*>(take(h, a[3], "inv_freq", at::kFloat, {half}, true));
       d.rot_dim = half > 1 << 20 ? -1 : (int32_t)(2 * half);
     }
-    d.pairs = PyObject_IsTrue(a[4]);
     if (a[5] != Py_None) d.q = take_heads(h, a[5], "q", hq, false, &d.q_stride_token, &d.q_stride_head);
     if (a[6] != Py_None) d.q_out = take_heads(h, a[6], "q_out", hq, false, &d.o_stride_token, &d.o_stride_head);
     if (a[7] != Py_None) d.positions = static_cast<const int64_t*>(take(h, a[7], "positions", at::kLong, {h->total_q}, true));

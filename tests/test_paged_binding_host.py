@@ -60,3 +60,10 @@ def test_the_longest_sequence():
             assert H._attend(lib, desc, ws=0) == status, (rows, lib.tkphi_last_error())
             if status == -1:
                 assert H._append(lib, desc, rot_dim=d, inv_freq=0) == -1 and b"kv_lens" in lib.tkphi_last_error()
+
+
+def test_pairs_without_a_truth_value(kv):
+    import numpy as np
+    k = torch.zeros(1, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="truth value"):
+        T.paged_append(kv, k, k, T.RotaryMap(torch.zeros(8), np.array([True, False])))
