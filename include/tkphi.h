@@ -380,6 +380,10 @@ size_t tkphi_paged_workspace_bytes(const tkphi_paged_desc* kv, const tkphi_page_
 /*
  * Attention of the new tokens over their sequences' caches: y = softmax(scale q.k) v over the visible keys (the
  * token's own position included), all new tokens of all sequences in one call, whatever mix of lengths.
+ * Scores, sums and products are accumulated in fp32.  A sequence whose new tokens have at most 16 query heads of one KV
+ * head together (q_len * n_q_heads / n_kv_heads <= 16) has its probabilities multiplied as pairs of 16-bit numbers; with
+ * more of them they are rounded to 16 bits once, fp16 ones by up to 2^-32 of the largest where they are below 2^-21 of it.
+ * So a token's result differs in its last bits with the number of tokens that come with it.
  *   q     [total_q][n_q_heads][head_dim], y_out likewise, both in the cache's type, contiguous, 16-byte aligned.
  *   lse   fp32 [total_q][n_q_heads] or NULL: log of the softmax denominator, log sum exp(scale q.k), with which
  *         results over disjoint sets of keys can be joined.  A token that sees nothing (no keys, or none whose score
@@ -408,7 +412,8 @@ tkphi_status tkphi_paged_block_attention(const tkphi_paged_desc* kv, const tkphi
 /*
  * Reads the device status word that the kernels of the last call using this
  * workspace set (0 = fine; TKPHI_ERR_TIMEOUT if a bounded wait ran out).  Waits
- * for the stream.  *status_out is a host int.
+ * for the stream.  *status_out is a host int.  (The workspaces of the paged calls
+ * hold no such word: theirs is tkphi_paged_desc.status.)
  */
 tkphi_status tkphi_device_status(const void* workspace, void* cuda_stream, int32_t* status_out);
 

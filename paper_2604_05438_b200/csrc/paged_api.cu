@@ -140,7 +140,7 @@ struct AttendPlan {
   size_t row_part, row_stat, tile_part, tile_stat, total;
 };
 
-// Sequences with at most this many rows per KV head go to the row kernel.
+// Sequences with at most this many rows per KV head go to the row kernel: one tile of its matrix instruction.
 constexpr int kRowsLimit = 16;
 
 // Keys per CTA of the tile kernel: the whole context if the row tiles alone fill the SMs evenly, otherwise a part of it.

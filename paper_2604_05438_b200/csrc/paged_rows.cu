@@ -1,5 +1,6 @@
-// Attention of few query rows over a paged cache: decoding (one token per sequence), a few drafted tokens, and the
-// page-selected form, where every token of a KV head reads a page list of its own.
+// Attention of few query rows over a paged cache: sequences with at most 16 rows (tokens x query heads of a KV head: one
+// token of a group of 16, four of a group of 4), and the page-selected form, where every token of a KV head reads a page list
+// of its own.
 //
 //   y = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale * q.k_t - m),  lse = m + log sum_t p_t   over the visible keys t
 //

@@ -12,8 +12,8 @@
 //                   The reference m of a row need not be its maximum, it only has to keep P in range: it is the
 //                   maximum of the first tile, and later tiles go straight from the score to exp2(score - m) without
 //                   looking for theirs.  A tile whose row sum passes a limit (2^40; fp16: 61440, below which no term
-//                   can overflow the type) is redone with its maximum as the new reference and O rescaled; nothing of
-//                   a row is lost on the way, because m never exceeds a score the row has seen.
+//                   can overflow the type) or is no number is redone with its maximum as the new reference and O
+//                   rescaled.  Both ways of computing exp2 let a term that is out of range fail that limit.
 //                   At head_dim 64 a quarter of the exponentials are computed on the FMA pipes (exp2_pair).
 //   warp 8          issues the MMAs: P V of a row tile as soon as its P is stored, then the next S into the same buffer.
 //   warp 9          TMA producer: the queries, then page boxes of keys and values into one ring, in the order of their use.
@@ -21,19 +21,23 @@
 //                   infinity or NaN would reach the rows that do not see it: value rows that no row sees are zeroed (behind
 //                   the sequence's end they may hold anything), other elements that are not finite are zeroed and noted with
 //                   the first key that has one in their dim, and added at the end to the rows that see that key.
-// fp16: P is scaled by 2^7, because without it probabilities below 2^-24 of the maximum vanish, and a long context is made
-// of those; the sum carries the same factor.  Rounding P to 16 bits is the only rounding besides the output's: per term it
-// is that of one 16-bit rounding, and it averages out over the terms.  The sum is of the unrounded values.
+// Rounding P to 16 bits (the kernel for few rows does not) is the only rounding besides the output's: per term it is that of
+// one 16-bit rounding, and it averages out over the terms; bf16 outputs are off by 0.0022 (norm, against 0.0017 from their
+// own rounding alone).  The sum is of the unrounded values.  fp16: P is scaled by 2^7 and the sum with it, because without it
+// probabilities below 2^-24 of the maximum vanish, and a long context is made of those; with it they have all their bits down
+// to 2^-21 of the reference and are off by 2^-32 of it below that.
 // Keys are cut into chunks when there are too few row tiles to fill the SMs evenly; partial outputs are joined in key
 // order by a second, dependent kernel.
 // What it measured (24 / 8 heads of 128, 2048 tokens at the end of 32K; 32 / 8 heads of 64, 4096 at the end of 32K):
 //   first version 954 / 565 TFLOP/s: the issuing thread needed 75 cycles per MMA, see there
 //   convergent issue 1218 / 701; three score buffers at head_dim 64, a burst of MMAs per step, fewer commits 1203 / 868
 //   queries by TMA, join in runs of rows 1190 / 896 (a group of 3 fills 126 of the 128 rows)
-// Bound now: at head_dim 128 the tensor pipe at the clock that the power limit leaves (the measured sustained library rate
-// is 1344 TFLOP/s); at 64 the softmax warps' issue and special-function rate.  A CTA's set-up and its output take about 12K
-// cycles, which shows where contexts are short (5K-8K prompts: 745 TFLOP/s).  Two issuing warps were slower (1005 / 631):
-// the row tiles then run in phase and wait together.
+//   exponentials cut at both ends, values that not every row sees looked through, far references 1176 / 865-884
+// Bound now: at head_dim 128 the chain of a row tile (scores, softmax, product) where the other row tile does not cover it
+// (tensor pipe active 59%), under the power limit (the sustained library rate is 1344 TFLOP/s); at 64 the softmax warps'
+// issue and special-function rate.  A CTA's set-up and its output take about 12K cycles, which shows where contexts are short
+// (5K-8K prompts: 700-735 TFLOP/s).  Two issuing warps were slower (1005 / 631): the row tiles then run in phase and wait
+// together.
 #include <climits>
 
 #include "paged.cuh"
@@ -98,9 +102,9 @@ __device__ __forceinline__ uint64_t exp2_pair(uint64_t x2) {
                __int_as_float(__float_as_int(b) + (__float_as_int(tb) << 23)));
 }
 // Which of the 16 pairs of a 32-column piece go through exp2_pair: a quarter at head_dim 64, where the special-function
-// unit is the bound (4096 x 32K tokens, 32 / 8 heads: 1322 us with none, 1250 with an eighth, 1187 with a quarter, 1230
-// with three eighths, 1375 with a half); none at 128, where the tensor pipe is (2048 x 32K, 24 / 8 heads: 664 us with none
-// or a quarter, 714 with a half).
+// unit is the bound (4096 x 32K tokens, 32 / 8 heads, fp16: 1320 us with none, 1237 with an eighth, 1192 with a quarter, 1256
+// with three eighths, 1430 with a half); none at 128, where it is not (2048 x 32K, 24 / 8 heads: 664 us with none or a
+// quarter, 714 with a half).
 template <int D>
 __device__ __forceinline__ constexpr bool emulated(int e) { return D == 64 && e % 4 == 0; }
 __device__ __forceinline__ bool elect_one() {
