@@ -385,6 +385,7 @@ size_t tkphi_paged_workspace_bytes(const tkphi_paged_desc* kv, const tkphi_page_
  * more of them they are rounded to 16 bits once, fp16 ones by up to 2^-32 of the largest where they are below 2^-21 of it.
  * So a token's result differs in its last bits with the number of tokens that come with it.
  *   q     [total_q][n_q_heads][head_dim], y_out likewise, both in the cache's type, contiguous, 16-byte aligned.
+ *         y_out may be q itself; otherwise they must not overlap.
  *   lse   fp32 [total_q][n_q_heads] or NULL: log of the softmax denominator, log sum exp(scale q.k), with which
  *         results over disjoint sets of keys can be joined.  A token that sees nothing (no keys, or none whose score
  *         is above -inf) gets y = 0, lse = -inf; one with a score that is no number or +inf gets NaN in both.

@@ -517,3 +517,64 @@ def test_memory_that_a_contiguous_cache_made_is_kept_for_other_streams_too(use):
     torch.cuda.synchronize()
     assert busy and not taken
     assert torch.equal(y, want)
+
+
+def test_two_captured_steps_replayed_side_by_side():
+    # each with outputs, status word and workspaces of its own
+    import paper_2604_05438_b200 as T
+    dev = torch.device("cuda:0")
+    jobs = []
+    for i, lens in enumerate(([(1, 3000), (50, 700), (1, 9)], [(90, 2000), (1, 20000), (3, 400)])):
+        s = U.make_step(8, 2, 64, 32, "bf16", lens, seed=170 + i, with_bounds=True)
+        kv, q, sel = U.to_device(s), s.q.to(dev), T.PageSelection(1, 2, 4)
+        out = torch.zeros_like(q), torch.zeros(q.shape[:2], device=dev), torch.zeros_like(q)
+        idx = torch.zeros(q.shape[0], 2, sel.n_pages, dtype=torch.int32, device=dev)
+        wa = torch.empty(T.paged_workspace_bytes(kv, T.WS_PAGED_ATTENTION), dtype=torch.uint8, device=dev)
+        wb = torch.empty(T.paged_workspace_bytes(kv, T.WS_PAGED_BLOCK_ATTENTION, sel), dtype=torch.uint8, device=dev)
+
+        def run(kv=kv, q=q, sel=sel, out=out, idx=idx, wa=wa, wb=wb):
+            T.paged_attention(kv, q, out[0], out[1], None, 0, wa)
+            T.paged_block_attention(kv, sel, q, out[2], None, idx, None, wb)
+        run()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in out + (idx,)]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run()
+        jobs.append((graph, out + (idx,), want, kv, run))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(6):
+        for job in jobs:
+            for t in job[1]:
+                t.fill_(7)
+        torch.cuda.synchronize()
+        for st, job in zip(streams, jobs):
+            with torch.cuda.stream(st):
+                for _ in range(3):
+                    job[0].replay()
+        torch.cuda.synchronize()
+        for _, got, want, kv, _ in jobs:
+            assert kv.device_status() == 0
+            for a, b in zip(got, want):
+                assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("way", range(len(WAYS)))
+def test_outputs_in_the_place_of_the_queries(way, d):
+    import paper_2604_05438_b200 as T
+    s = _step_of(way, d, "bf16", 180)
+    kv, sel = U.to_device(s), T.PageSelection(1, 1, 5)
+    ws = [torch.empty(T.paged_workspace_bytes(kv, w, sel), dtype=torch.uint8, device="cuda:0") for w in (T.WS_PAGED_ATTENTION, T.WS_PAGED_BLOCK_ATTENTION)]
+    q = s.q.cuda()
+    apart = torch.empty_like(q), torch.empty_like(q)
+    T.paged_attention(kv, q, apart[0], None, None, 0, ws[0])
+    T.paged_block_attention(kv, sel, q, apart[1], None, None, None, ws[1])
+    for _ in range(3):
+        a, b = q.clone(), q.clone()
+        T.paged_attention(kv, a, a, None, None, 0, ws[0])
+        T.paged_block_attention(kv, sel, b, b, None, None, None, ws[1])
+        torch.cuda.synchronize()
+        assert torch.equal(a, apart[0]) and torch.equal(b, apart[1])
+
