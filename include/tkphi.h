@@ -410,6 +410,76 @@ tkphi_status tkphi_paged_block_attention(const tkphi_paged_desc* kv, const tkphi
                                          const void* q, void* y_out, float* lse_out, int32_t* page_idx_out, float scale,
                                          void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/* Norms of the new tokens' heads, each head on its own: x -> x * weight / sqrt(mean(x^2) + eps), before the rotation.  Weights
+ * are fp32 device arrays, 16-byte aligned, [heads][head_dim] with a stride between heads (a multiple of 4 elements, at least
+ * head_dim, or 0: one [head_dim] for all).  A NULL side is not normed.  The sum of squares is taken in 32 bits: elements
+ * beyond 2^60 overflow it. */
+typedef struct {
+  const float* q_weight; int64_t q_stride_head;
+  const float* k_weight; int64_t k_stride_head;
+  float eps;                      /* finite, not negative */
+} tkphi_norm_desc;
+
+/* tkphi_paged_append with norms: norm, rotation and rounding in one pass, in 32 bits, rounded once. */
+tkphi_status tkphi_paged_append_norm(const tkphi_paged_desc* kv, const tkphi_append_desc* step, const tkphi_norm_desc* norm,
+                                     void* cuda_stream);
+
+/*
+ * ---------------------------------------------------------------------------------------------
+ * A paged cache in 8 bits: half the bytes of the same cache in 16.
+ *
+ * Every row x (one token of one KV head, keys and values each) is held as head_dim e4m3 codes c and one scale byte e,
+ * x_i ~ c_i * 2^(e - 127), where e is the smallest in [1, 254] with max |x_i| <= 448 * 2^(e - 127) and the codes are the
+ * nearest (ties to even): a value is off by 2^-4 of itself at most, or by 2^(e - 137) if that is more.  A row with an
+ * element that is infinite or no number is held as NaN: codes 0x7f, e = 255.  Rows written by others may have any codes and
+ * any e (0 stands for 2^-127, 255 for NaN).
+ *
+ * step is a tkphi_paged_desc with these differences: k and v are the codes, their strides in bytes, multiples of 16; dtype
+ * is the type of everything else (q, y, new tokens, key_bounds, rows read back).  key_bounds are the element-wise minimum
+ * and maximum of what the pages' keys stand for.  k_scales, v_scales: device uint8 [n_pages][n_kv_heads][page_size],
+ * 16-byte aligned.  All that is said of the paged calls above (host and device lengths, captured graphs, page table,
+ * status, workspaces, slots that hold no row) is true of these.
+ */
+typedef struct {
+  tkphi_paged_desc step;
+  uint8_t* k_scales;
+  uint8_t* v_scales;
+} tkphi_coded_desc;
+
+/* tkphi_paged_append into an 8-bit cache, with norms (or NULL): the rows are rounded once, from 32 bits to their codes. */
+tkphi_status tkphi_coded_append(const tkphi_coded_desc* kv, const tkphi_append_desc* step, const tkphi_norm_desc* norm,
+                                 void* cuda_stream);
+
+/* Rows to read back: output row cu_rows[b] + i gets position first[b] + i of sequence b.  cu_rows as cu_q: [batch+1], from
+ * 0, non-decreasing, below 2^31; first: [batch], >= 0, host and device or both NULL (0 for all); first[b] + the sequence's
+ * number of rows is at most kv_lens[b].  Element (row, head, dim) of k_out is at row*k_stride_row + head*k_stride_head +
+ * dim, in dtype; 16-byte aligned, strides multiples of 8 elements that give every element memory of its own.  k_out or
+ * v_out may be NULL; they must not overlap each other or the cache. */
+typedef struct {
+  const int64_t* cu_rows_host; const int64_t* cu_rows_dev;
+  const int64_t* first_host;   const int64_t* first_dev;
+  void* k_out; int64_t k_stride_row, k_stride_head;
+  void* v_out; int64_t v_stride_row, v_stride_head;
+} tkphi_read_desc;
+
+/*
+ * What rows of an 8-bit cache stand for, as 16-bit rows (rounded once: exact in bf16; in fp16 infinite beyond 65504).
+ * Written to a head-major or token-major array this is a cache as tkphi_build_summaries and the decode calls take it.
+ * kv's cu_q plays no part.  Rows of positions at or behind a sequence's device length, or on a bad page, are left as they
+ * were.  No workspace.
+ */
+tkphi_status tkphi_coded_read(const tkphi_coded_desc* kv, const tkphi_read_desc* rows, void* cuda_stream);
+
+/* As tkphi_paged_workspace_bytes, tkphi_paged_attention and tkphi_paged_block_attention, over an 8-bit cache: the codes and
+ * scales enter the products exactly, everything else is rounded as there.  (With bf16 queries and at most 16 rows per KV
+ * head the probabilities are rounded to fp16 once.  fp16 with more rows: values beyond 65504 count as infinite.) */
+size_t tkphi_coded_workspace_bytes(const tkphi_coded_desc* kv, const tkphi_page_selection* selection, int which);
+tkphi_status tkphi_coded_attention(const tkphi_coded_desc* kv, const void* q, void* y_out, float* lse_out, float scale,
+                                    uint32_t flags, void* workspace, size_t workspace_bytes, void* cuda_stream);
+tkphi_status tkphi_coded_block_attention(const tkphi_coded_desc* kv, const tkphi_page_selection* selection,
+                                          const void* q, void* y_out, float* lse_out, int32_t* page_idx_out, float scale,
+                                          void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /*
  * Reads the device status word that the kernels of the last call using this
  * workspace set (0 = fine; TKPHI_ERR_TIMEOUT if a bounded wait ran out).  Waits
@@ -453,7 +523,8 @@ enum {
   TKPHI_KERNEL_PAGED_SELECT = 8,    /* page bounds and selection */
   TKPHI_KERNEL_PAGED_ROWS = 9,      /* attention of few query rows over a paged cache, and its join */
   TKPHI_KERNEL_PAGED_TILES = 10,    /* attention of many query rows over a paged cache, and its join */
-  TKPHI_KERNEL_KINDS = 11
+  TKPHI_KERNEL_PAGED_READ = 11,     /* rows of an 8-bit paged cache read back */
+  TKPHI_KERNEL_KINDS = 12
 };
 void tkphi_kernel_timing_enable(int32_t on);
 tkphi_status tkphi_kernel_timing_read(float* ms_out, int32_t* count_out);

@@ -26,10 +26,12 @@ EXPORTED_SYMBOLS = (
     "tkphi_selftest_timeout",
     "tkphi_mlp_key_features", "tkphi_build_summaries_cached", "tkphi_decode_step_mlp",
     "tkphi_paged_workspace_bytes", "tkphi_paged_append", "tkphi_paged_attention", "tkphi_paged_block_attention",
+    "tkphi_paged_append_norm", "tkphi_coded_append", "tkphi_coded_read", "tkphi_coded_workspace_bytes",
+    "tkphi_coded_attention", "tkphi_coded_block_attention",
 )
 STATIC_SCRATCH_BYTES = 8 << 20
 KERNEL_KINDS = ("score", "select", "exact_residual", "build", "memset", "cached_z", "mlp", "paged_append", "paged_select",
-                "paged_rows", "paged_tiles")
+                "paged_rows", "paged_tiles", "paged_read")
 ERR_TIMEOUT = -5
 
 
@@ -65,6 +67,21 @@ class _PagedDesc(C.Structure):
                 ("stride_token", C.c_int64), ("page_table", C.c_void_p), ("kv_lens_host", C.c_void_p),
                 ("kv_lens_dev", C.c_void_p), ("cu_q_host", C.c_void_p), ("cu_q_dev", C.c_void_p),
                 ("key_bounds", C.c_void_p), ("status", C.c_void_p)]
+
+
+class _CodedDesc(C.Structure):
+    _fields_ = [("step", _PagedDesc), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p)]
+
+
+class _NormDesc(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("q_stride_head", C.c_int64), ("k_weight", C.c_void_p), ("k_stride_head", C.c_int64),
+                ("eps", C.c_float)]
+
+
+class _ReadDesc(C.Structure):
+    _fields_ = [("cu_rows_host", C.c_void_p), ("cu_rows_dev", C.c_void_p), ("first_host", C.c_void_p), ("first_dev", C.c_void_p),
+                ("k_out", C.c_void_p), ("k_stride_row", C.c_int64), ("k_stride_head", C.c_int64),
+                ("v_out", C.c_void_p), ("v_stride_row", C.c_int64), ("v_stride_head", C.c_int64)]
 
 
 class _AppendDesc(C.Structure):
@@ -132,6 +149,20 @@ def load_library():
     lib.tkphi_paged_block_attention.restype = C.c_int
     lib.tkphi_paged_block_attention.argtypes = [C.POINTER(_PagedDesc), C.POINTER(_PageSelection), C.c_void_p, C.c_void_p,
                                                 C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.tkphi_paged_append_norm.restype = C.c_int
+    lib.tkphi_paged_append_norm.argtypes = [C.POINTER(_PagedDesc), C.POINTER(_AppendDesc), C.POINTER(_NormDesc), C.c_void_p]
+    lib.tkphi_coded_append.restype = C.c_int
+    lib.tkphi_coded_append.argtypes = [C.POINTER(_CodedDesc), C.POINTER(_AppendDesc), C.POINTER(_NormDesc), C.c_void_p]
+    lib.tkphi_coded_read.restype = C.c_int
+    lib.tkphi_coded_read.argtypes = [C.POINTER(_CodedDesc), C.POINTER(_ReadDesc), C.c_void_p]
+    lib.tkphi_coded_workspace_bytes.restype = C.c_size_t
+    lib.tkphi_coded_workspace_bytes.argtypes = [C.POINTER(_CodedDesc), C.POINTER(_PageSelection), C.c_int]
+    lib.tkphi_coded_attention.restype = C.c_int
+    lib.tkphi_coded_attention.argtypes = [C.POINTER(_CodedDesc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
+                                           C.c_uint32, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.tkphi_coded_block_attention.restype = C.c_int
+    lib.tkphi_coded_block_attention.argtypes = [C.POINTER(_CodedDesc), C.POINTER(_PageSelection), C.c_void_p, C.c_void_p,
+                                                 C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_size_t, C.c_void_p]
     lib.tkphi_device_status.restype = C.c_int
     lib.tkphi_device_status.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(C.c_int32)]
     lib.tkphi_kernel_timing_enable.restype = None
@@ -297,19 +328,24 @@ class PagedKVCache:
     def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, kv_lens, cu_q, n_q_heads: int,
                  key_bounds: Optional[torch.Tensor] = None, kv_lens_dev: Optional[torch.Tensor] = None,
                  cu_q_dev: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+        assert k.dtype in _DTYPES
+        self.dtype = k.dtype
+        self._set(k, v, page_table, kv_lens, cu_q, n_q_heads, key_bounds, kv_lens_dev, cu_q_dev, status)
+
+    def _set(self, k, v, page_table, kv_lens, cu_q, n_q_heads, key_bounds, kv_lens_dev, cu_q_dev, status):
         dev = k.device
         self.k, self.v, self.page_table, self.key_bounds, self.n_q_heads = k, v, page_table, key_bounds, n_q_heads
         # the descriptor points to these copies, and calls are checked against them: they do not change any more
         self.kv_lens, self.cu_q = np.array(kv_lens, dtype=np.int64), np.array(cu_q, dtype=np.int64)
         self.kv_lens.setflags(write=False)
         self.cu_q.setflags(write=False)
-        assert k.dtype in _DTYPES and v.dtype == k.dtype and k.dim() == 4 and v.shape == k.shape
+        assert v.dtype == k.dtype and k.dim() == 4 and v.shape == k.shape
         assert k.stride() == v.stride() and k.stride(3) == 1
         assert self.kv_lens.ndim == 1 and self.cu_q.shape == (len(self.kv_lens) + 1,)
         assert page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.is_contiguous()
         assert page_table.shape[0] == len(self.kv_lens)
         if key_bounds is not None:
-            assert key_bounds.dtype == k.dtype and key_bounds.is_contiguous()
+            assert key_bounds.dtype == self.dtype and key_bounds.is_contiguous()
             assert key_bounds.shape == (k.shape[0], k.shape[1], 2, k.shape[3])
         made = ()
         if kv_lens_dev is None or cu_q_dev is None:
@@ -330,18 +366,24 @@ class PagedKVCache:
         for t in (v, page_table, key_bounds, self.kv_lens_dev, self.cu_q_dev, self.status):
             assert t is None or t.device == dev, "the cache, its page table and its lengths must be on one device"
         self.total_q = int(self.cu_q[-1])
-        self._desc = _PagedDesc(len(self.kv_lens), n_q_heads, k.shape[1], k.shape[3], _DTYPES[k.dtype], k.shape[2],
-                                k.shape[0], page_table.shape[1], k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
-                                k.stride(2), page_table.data_ptr(), self.kv_lens.ctypes.data, self.kv_lens_dev.data_ptr(),
-                                self.cu_q.ctypes.data, self.cu_q_dev.data_ptr(),
-                                None if key_bounds is None else key_bounds.data_ptr(), self.status.data_ptr())
-        self._handle = _native().handle(C.addressof(self._desc), k.get_device(), made, bool(made) and pending)
+        step = _PagedDesc(len(self.kv_lens), n_q_heads, k.shape[1], k.shape[3], _DTYPES[self.dtype], k.shape[2],
+                          k.shape[0], page_table.shape[1], k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
+                          k.stride(2), page_table.data_ptr(), self.kv_lens.ctypes.data, self.kv_lens_dev.data_ptr(),
+                          self.cu_q.ctypes.data, self.cu_q_dev.data_ptr(),
+                          None if key_bounds is None else key_bounds.data_ptr(), self.status.data_ptr())
+        self._desc = self._descriptor(step)
+        self._handle = _native().handle(C.addressof(self._desc), k.get_device(), made, bool(made) and pending, self.held8)
+
+    held8 = False            # the cache is in 8 bits
+
+    def _descriptor(self, step: _PagedDesc):
+        return step
 
     @property
     def batch(self) -> int:
         return len(self.kv_lens)
 
-    def desc(self) -> _PagedDesc:
+    def desc(self):
         return self._desc
 
     def device_status(self) -> int:
@@ -349,6 +391,77 @@ class PagedKVCache:
         if self.status.is_cuda:
             torch.cuda.synchronize(self.status.device)
         return int(self.status.item())
+
+
+class PagedKVCache8(PagedKVCache):
+    """One step of a batch of sequences over a paged K/V cache in 8 bits: the paged calls take it as they take a PagedKVCache.
+
+    k, v: float8_e4m3fn codes, addressed [page, head, slot, dim] as there; k_scales, v_scales: float8_e8m0fnu
+    [n_pages, n_kv_heads, page_size], a power of two for each row (0 for codes and 0 for scales is an empty cache).  dtype:
+    bfloat16 or float16, the type of queries, outputs, new tokens, key_bounds and rows read back.  Everything else as there.
+    """
+
+    held8 = True
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor, page_table: torch.Tensor,
+                 kv_lens, cu_q, n_q_heads: int, dtype: torch.dtype, key_bounds: Optional[torch.Tensor] = None,
+                 kv_lens_dev: Optional[torch.Tensor] = None, cu_q_dev: Optional[torch.Tensor] = None,
+                 status: Optional[torch.Tensor] = None):
+        assert k.dtype == torch.float8_e4m3fn and dtype in _DTYPES
+        for t in (k_scales, v_scales):
+            assert t.dtype == torch.float8_e8m0fnu and t.is_contiguous() and t.shape == k.shape[:3]
+            assert t.device == k.device, "the cache, its page table and its lengths must be on one device"
+        self.dtype, self.k_scales, self.v_scales = dtype, k_scales, v_scales
+        self._set(k, v, page_table, kv_lens, cu_q, n_q_heads, key_bounds, kv_lens_dev, cu_q_dev, status)
+
+    def _descriptor(self, step: _PagedDesc):
+        return _CodedDesc(step, self.k_scales.data_ptr(), self.v_scales.data_ptr())
+
+
+class CacheRows:
+    """Rows of an 8-bit cache that paged_read takes: output row cu_rows[b] + i gets position first[b] + i of sequence b (first
+    None: 0).  Device copies are made here (one copy, which is complete when it returns) unless given."""
+
+    def __init__(self, cu_rows, first=None, device=None, cu_rows_dev: Optional[torch.Tensor] = None,
+                 first_dev: Optional[torch.Tensor] = None):
+        self.cu_rows = np.array(cu_rows, dtype=np.int64)
+        self.first = None if first is None else np.array(first, dtype=np.int64)
+        assert self.cu_rows.ndim == 1 and len(self.cu_rows) > 1
+        assert self.first is None or self.first.shape == (len(self.cu_rows) - 1,)
+        assert first_dev is None or first is not None, "first_dev is a device copy of first"
+        made = ()
+        if cu_rows_dev is None or (first is not None and first_dev is None):
+            both = self.cu_rows if first is None else np.concatenate([self.cu_rows, self.first])
+            made = (torch.from_numpy(both).to(device),)
+            parts = made[0].split([len(self.cu_rows), len(both) - len(self.cu_rows)])
+            cu_rows_dev = parts[0] if cu_rows_dev is None else cu_rows_dev
+            first_dev = parts[1] if first is not None and first_dev is None else first_dev
+        for t, a in ((cu_rows_dev, self.cu_rows), (first_dev, self.first)):
+            assert t is None or (t.dtype == torch.int64 and t.shape == a.shape and t.is_contiguous() and t.device == cu_rows_dev.device)
+        self.cu_rows_dev, self.first_dev = cu_rows_dev, first_dev
+        for a in (self.cu_rows, self.first):
+            if a is not None:
+                a.setflags(write=False)
+        self._desc = _ReadDesc(self.cu_rows.ctypes.data, cu_rows_dev.data_ptr(), None if first is None else self.first.ctypes.data,
+                               None if first is None else first_dev.data_ptr())
+        self._handle = _native().rows(C.addressof(self._desc), cu_rows_dev.get_device(), len(self.cu_rows) - 1, int(self.cu_rows[-1]), made)
+
+    @property
+    def total(self) -> int:
+        return int(self.cu_rows[-1])
+
+
+@dataclass
+class HeadNorms:
+    """Root-mean-square norms of the new tokens' heads before the rotation: x * weight / sqrt(mean(x^2) + eps), each head on
+    its own.  Weights: fp32 device [head_dim] (for all heads) or [heads, head_dim]; a None side is not normed."""
+    q_weight: Optional[torch.Tensor]
+    k_weight: Optional[torch.Tensor]
+    eps: float = 1e-6
+
+    def __post_init__(self):
+        for w in (self.q_weight, self.k_weight):
+            assert w is None or (w.dtype == torch.float32 and w.dim() in (1, 2) and w.is_contiguous())
 
 
 @dataclass
@@ -484,8 +597,9 @@ def decode_step(kv: KVCache, phi: PhiMaps, q: torch.Tensor, topk_host, topk_dev:
 def paged_workspace_bytes(kv: PagedKVCache, which: int, selection: Optional[PageSelection] = None) -> int:
     lib = load_library()
     sel = None if selection is None else C.byref(selection.desc())
+    ask = lib.tkphi_coded_workspace_bytes if kv.held8 else lib.tkphi_paged_workspace_bytes
     with torch.cuda.device(kv.k.device):          # the plan goes by the device's multiprocessors
-        n = lib.tkphi_paged_workspace_bytes(C.byref(kv.desc()), sel, which)
+        n = ask(C.byref(kv.desc()), sel, which)
     if n == 0:
         raise TkphiError(-1, lib.tkphi_last_error().decode())
     return int(n)
@@ -493,19 +607,32 @@ def paged_workspace_bytes(kv: PagedKVCache, which: int, selection: Optional[Page
 
 def paged_append(kv: PagedKVCache, k_new: torch.Tensor, v_new: torch.Tensor, rotary: Optional[RotaryMap] = None,
                  q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
-                 positions: Optional[torch.Tensor] = None, stream=None) -> None:
-    """Rotates the new keys (and q into q_out) by their positions and writes keys and values into the cache's pages;
-    key bounds of the touched pages follow.  k_new, v_new, q, q_out: [total_q, heads, head_dim], any token and head
-    strides; positions: int64 [total_q] or None for the cache positions."""
+                 positions: Optional[torch.Tensor] = None, stream=None, norms: Optional[HeadNorms] = None) -> None:
+    """Rotates the new keys (and q into q_out) by their positions and writes keys and values into the cache's pages, rounded to
+    8 bits where kv is a PagedKVCache8; key bounds of the touched pages follow.  norms: the heads' norms before the rotation.
+    k_new, v_new, q, q_out: [total_q, heads, head_dim], any token and head strides; positions: int64 [total_q] or None for
+    the cache positions."""
     inv, pairs = (None, False) if rotary is None else (rotary.inv_freq, rotary.pairs)
-    st = _native().append(kv._handle, k_new, v_new, inv, pairs, q, q_out, positions, stream)
+    if norms is None:
+        st = _native().append(kv._handle, k_new, v_new, inv, pairs, q, q_out, positions, stream)
+    else:
+        st = _native().append_norm(kv._handle, k_new, v_new, inv, pairs, q, q_out, positions, norms.q_weight, norms.k_weight,
+                                   norms.eps, stream)
+    if st:
+        _check(st)
+
+
+def paged_read(kv: PagedKVCache8, rows: CacheRows, k_out: Optional[torch.Tensor], v_out: Optional[torch.Tensor], stream=None) -> None:
+    """What rows of an 8-bit cache stand for, as 16-bit rows: k_out, v_out [rows.total, n_kv_heads, head_dim] of kv's dtype, any
+    row and head strides (a [head, row, dim] array is passed as its transpose(0, 1)), either may be None."""
+    st = _native().read(kv._handle, rows._handle, k_out, v_out, stream)
     if st:
         _check(st)
 
 
 def paged_attention(kv: PagedKVCache, q: torch.Tensor, y_out: torch.Tensor, lse_out: Optional[torch.Tensor],
                     scale: Optional[float], flags: int, workspace: torch.Tensor, stream=None) -> None:
-    """Attention of the step's new tokens over their sequences' whole caches; q, y_out [total_q, n_q_heads, head_dim],
+    """Attention of the step's new tokens over their sequences' whole caches (of 16 or of 8 bits); q, y_out [total_q, n_q_heads, head_dim],
     lse_out fp32 [total_q, n_q_heads] or None, scale None for 1/sqrt(head_dim), flags FLAG_NONE or FLAG_FULL_CONTEXT."""
     st = _native().attention(kv._handle, q, y_out, lse_out, scale, flags, workspace, stream)
     if st:

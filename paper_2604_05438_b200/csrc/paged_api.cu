@@ -1,5 +1,6 @@
 // Entry points of the paged cache: argument validation, workspace layout, launches.
 #include "host.cuh"
+#include "held8.cuh"
 #include "paged.cuh"
 
 #include <algorithm>
@@ -32,7 +33,8 @@ bool disjoint(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2, int64_
   return true;
 }
 
-tkphi_status validate_paged(const tkphi_paged_desc* kv, PagedShape* sh, bool need_data, bool full_context) {
+// held: the cache is in 8 bits, its strides are bytes.
+tkphi_status validate_paged(const tkphi_paged_desc* kv, PagedShape* sh, bool need_data, bool full_context, bool held = false) {
   if (!kv) return fail(TKPHI_ERR_INVALID_ARG, "kv descriptor is NULL");
   if (kv->batch < 1 || kv->batch > kMaxBatch)
     return fail(TKPHI_ERR_INVALID_ARG, "batch must be in [1, %d], got %d", kMaxBatch, kv->batch);
@@ -83,9 +85,10 @@ tkphi_status validate_paged(const tkphi_paged_desc* kv, PagedShape* sh, bool nee
     if (kv->key_bounds && !aligned16(kv->key_bounds))
       return fail(TKPHI_ERR_INVALID_ARG, "key_bounds must be 16-byte aligned");
     const int64_t st[3] = {kv->stride_page, kv->stride_head, kv->stride_token};
+    const int unit = held ? 16 : 8;                  // elements in 16 bytes
     for (int64_t s : st)
-      if (s < 0 || s % 8 != 0 || s >= (1ll << 38))
-        return fail(TKPHI_ERR_INVALID_ARG, "cache strides must be non-negative multiples of 8 elements below 2^38, got %lld", (long long)s);
+      if (s < 0 || s % unit != 0 || s >= (1ll << 38))
+        return fail(TKPHI_ERR_INVALID_ARG, "cache strides must be non-negative multiples of %d elements below 2^38, got %lld", unit, (long long)s);
     if (!disjoint(kv->n_pages, kv->stride_page, kv->n_kv_heads, kv->stride_head, kv->page_size, kv->stride_token, kv->head_dim))
       return fail(TKPHI_ERR_INVALID_ARG, "the cache strides (page %lld, head %lld, token %lld) let elements share memory",
                   (long long)st[0], (long long)st[1], (long long)st[2]);
@@ -108,6 +111,24 @@ tkphi_status make_page_map(const tkphi_paged_desc* kv, const void* base, CUtenso
   const CUresult r = fn(tm, kv->dtype == TKPHI_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
                         4, const_cast<void*>(base), dims, st, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(TKPHI_ERR_CUDA, "cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
+  return TKPHI_OK;
+}
+
+// 4-D view [page][head][slot][dim] of an 8-bit cache's codes; box = all dims x a page's slots of one head, swizzled by its width.
+tkphi_status make_code_map(const tkphi_paged_desc* kv, const void* base, CUtensorMap* tm) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return fail(TKPHI_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
+  const cuuint64_t d = (cuuint64_t)kv->head_dim;
+  const cuuint64_t dims[4] = {d, (cuuint64_t)kv->page_size, (cuuint64_t)kv->n_kv_heads, (cuuint64_t)kv->n_pages};
+  // (a dim of one index: any legal stride will do, the caller's may be 0)
+  const cuuint64_t st[3] = {(cuuint64_t)kv->stride_token, kv->n_kv_heads > 1 ? (cuuint64_t)kv->stride_head : d,
+                            kv->n_pages > 1 ? (cuuint64_t)kv->stride_page : d};
+  const cuuint32_t box[4] = {(cuuint32_t)d, (cuuint32_t)kv->page_size, 1, 1};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  const CUresult r = fn(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), dims, st, box, estr,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(TKPHI_ERR_CUDA, "cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
   return TKPHI_OK;
 }
@@ -172,26 +193,27 @@ int choose_chunk(const tkphi_paged_desc* kv, const PagedShape& sh, int64_t longe
 }
 
 // CTAs per unit of the row kernel's cluster form, or 0 for the line: units of at most `tiles` tiles.
-int split_rows(int64_t units, int64_t tiles, int n_sm) {
+int split_rows(int64_t units, int64_t tiles, int n_sm, int most_tiles = 16) {
   int split = 1;
   while (split < 8 && tiles > 2 * split && units * split * 2 <= n_sm) split *= 2;
-  return tiles <= 16 * split ? split : 0;
+  return tiles <= most_tiles * split ? split : 0;
 }
 
-tkphi_status plan_attend(const tkphi_paged_desc* kv, const PagedShape& sh, AttendPlan* pl) {
+tkphi_status plan_attend(const tkphi_paged_desc* kv, const PagedShape& sh, AttendPlan* pl, bool held = false) {
   const int n_sm = sm_count_current_device();
+  const int row_keys = held ? kHeldKeys : kRowKeys, row_ctas = held ? paged8_row_ctas(kv->head_dim) : 2;
   *pl = AttendPlan{};
   int64_t longest_row = 0, longest = 0;
   for (int b = 0; b < kv->batch; ++b) {
     const int64_t q = kv->cu_q_host[b + 1] - kv->cu_q_host[b];
     if (q == 0) continue;
     const int64_t rows = q * sh.group, len = kv->kv_lens_host[b];
-    if (rows > kRowsLimit) {
+    if (rows > kRowsLimit && !held) {
       pl->any_tiles = true;
       longest = std::max<int64_t>(longest, len > 0 ? (len + kTileKeys - 1) / kTileKeys : 1);
       continue;
     }
-    const int64_t tiles = len > 0 ? (len + kRowKeys - 1) / kRowKeys : 1;
+    const int64_t tiles = len > 0 ? (len + row_keys - 1) / row_keys : 1;
     pl->any_rows = true;
     pl->max_rows = (int)std::max<int64_t>(pl->max_rows, rows);
     pl->row_tiles += tiles * kv->n_kv_heads * ((rows + kRowTile - 1) / kRowTile);
@@ -200,7 +222,8 @@ tkphi_status plan_attend(const tkphi_paged_desc* kv, const PagedShape& sh, Atten
   if (pl->row_tiles > INT_MAX / 2) return fail(TKPHI_ERR_UNSUPPORTED, "too many key tiles for one call");
   const int units = kv->batch * kv->n_kv_heads;
   pl->row_split = split_rows(units, longest_row, n_sm);
-  pl->row_ctas = pl->row_split ? 0 : (int)std::min<int64_t>(2 * n_sm, pl->row_tiles);
+  if (held && pl->max_rows > kRowsLimit) pl->row_split = 0;
+  pl->row_ctas = pl->row_split ? 0 : (int)std::min<int64_t>(row_ctas * n_sm, pl->row_tiles);
   pl->row_grid = pl->row_split ? units * pl->row_split : pl->row_ctas;
   if (pl->any_tiles) {
     pl->chunk = choose_chunk(kv, sh, longest, n_sm);
@@ -232,7 +255,9 @@ struct BlockPlan {
   size_t scores, keys, mags, list, part, stat, total;
 };
 
-tkphi_status plan_block(const tkphi_paged_desc* kv, const PagedShape& sh, const tkphi_page_selection* sel, BlockPlan* pl) {
+tkphi_status plan_block(const tkphi_paged_desc* kv, const PagedShape& sh, const tkphi_page_selection* sel, BlockPlan* pl,
+                        bool held = false) {
+  const int row_keys = held ? kHeldKeys : kRowKeys, row_ctas = held ? paged8_row_ctas(kv->head_dim) : 2;
   if (!sel) return fail(TKPHI_ERR_INVALID_ARG, "selection is NULL");
   if (sel->n_sink_pages < 0 || sel->n_tail_pages < 1 || sel->topk_pages < 0)
     return fail(TKPHI_ERR_INVALID_ARG, "n_sink_pages (%d) and topk_pages (%d) must be >= 0, n_tail_pages (%d) >= 1",
@@ -245,11 +270,11 @@ tkphi_status plan_block(const tkphi_paged_desc* kv, const PagedShape& sh, const 
   if (sh.max_pages_seq > kMaxSelectPages)
     return fail(TKPHI_ERR_UNSUPPORTED, "%lld pages in a sequence > %d", (long long)sh.max_pages_seq, kMaxSelectPages);
   pl->key_stride = (int)((std::max<int64_t>(middle > sel->topk_pages ? middle : 0, 1) + 3) & ~(int64_t)3);
-  const int64_t tiles = ((std::min<int64_t>(keep, std::max<int64_t>(sh.max_pages_seq, 1)) << sh.page_shift) + kRowKeys - 1) / kRowKeys;
+  const int64_t tiles = ((std::min<int64_t>(keep, std::max<int64_t>(sh.max_pages_seq, 1)) << sh.page_shift) + row_keys - 1) / row_keys;
   const int n_sm = sm_count_current_device();
   pl->n_split = split_rows(units, tiles, n_sm);
   pl->cluster = pl->n_split > 0;
-  if (!pl->cluster) pl->n_split = (int)std::max<int64_t>(1, std::min<int64_t>((tiles + 1) / 2, units > 0 ? 2 * n_sm / units : 1));
+  if (!pl->cluster) pl->n_split = (int)std::max<int64_t>(1, std::min<int64_t>((tiles + 1) / 2, units > 0 ? row_ctas * n_sm / units : 1));
   size_t o = 0;
   // score row tiles: tokens of one sequence, 16 rows at a time
   const int tpt = kRowTile / padded_group(sh.group);
@@ -292,34 +317,14 @@ tkphi_status check_io(const void* q, const void* y, const float* lse, float scal
   return TKPHI_OK;
 }
 
-}  // namespace
-
-extern "C" {
-
-size_t tkphi_paged_workspace_bytes(const tkphi_paged_desc* kv, const tkphi_page_selection* selection, int which) {
-  clear_error();
+// Checks a step's tensors and fills the append kernels' problem; p->total_q 0: nothing to do.
+tkphi_status append_problem(const tkphi_paged_desc* kv, const tkphi_append_desc* step, bool held, AppendProblem* out) {
   PagedShape sh{};
-  if (which == TKPHI_WS_PAGED_ATTENTION) {
-    AttendPlan pl{};
-    // the size does not depend on the mask, so that the looser rule of the lengths is enough
-    if (validate_paged(kv, &sh, false, true) != TKPHI_OK || plan_attend(kv, sh, &pl) != TKPHI_OK) return 0;
-    return pl.total;
-  }
-  if (which == TKPHI_WS_PAGED_BLOCK_ATTENTION) {
-    BlockPlan pl{};
-    if (validate_paged(kv, &sh, false, false) != TKPHI_OK || plan_block(kv, sh, selection, &pl) != TKPHI_OK) return 0;
-    return pl.total;
-  }
-  fail(TKPHI_ERR_INVALID_ARG, "unknown workspace kind %d", which);
-  return 0;
-}
-
-tkphi_status tkphi_paged_append(const tkphi_paged_desc* kv, const tkphi_append_desc* step, void* cuda_stream) {
-  clear_error();
-  PagedShape sh{};
-  tkphi_status st = validate_paged(kv, &sh, true, false);
+  tkphi_status st = validate_paged(kv, &sh, true, false, held);
   if (st != TKPHI_OK) return st;
   if (!step) return fail(TKPHI_ERR_INVALID_ARG, "step descriptor is NULL");
+  AppendProblem& p = *out;
+  p = AppendProblem{};
   if (sh.total_q == 0) return TKPHI_OK;
   if (!step->k_new || !step->v_new || !aligned16(step->k_new) || !aligned16(step->v_new))
     return fail(TKPHI_ERR_INVALID_ARG, "k_new or v_new is NULL or not 16-byte aligned");
@@ -349,7 +354,6 @@ tkphi_status tkphi_paged_append(const tkphi_paged_desc* kv, const tkphi_append_d
     const int64_t q = kv->cu_q_host[b + 1] - kv->cu_q_host[b];
     if (q > 0) items += ((q + span - 2) / span) + 1;
   }
-  AppendProblem p{};
   p.batch = kv->batch; p.hq = kv->n_q_heads; p.hkv = kv->n_kv_heads; p.group = sh.group; p.d = kv->head_dim;
   p.page_shift = sh.page_shift; p.n_pages = kv->n_pages; p.max_pages = kv->max_pages;
   p.table = kv->page_table;
@@ -368,36 +372,92 @@ tkphi_status tkphi_paged_append(const tkphi_paged_desc* kv, const tkphi_append_d
   p.status = kv->status;
   p.items = (int)items;
   p.total_q = sh.total_q;
+  return TKPHI_OK;
+}
+
+tkphi_status check_scales(const tkphi_coded_desc* kv) {
+  if (!kv) return fail(TKPHI_ERR_INVALID_ARG, "kv descriptor is NULL");
+  if (!kv->k_scales || !kv->v_scales || !aligned16(kv->k_scales) || !aligned16(kv->v_scales))
+    return fail(TKPHI_ERR_INVALID_ARG, "k_scales or v_scales is NULL or not 16-byte aligned");
+  return TKPHI_OK;
+}
+
+tkphi_status check_norm(const float* w, int64_t stride, int head_dim, const char* what) {
+  if (!w) return TKPHI_OK;
+  if (!aligned16(w)) return fail(TKPHI_ERR_INVALID_ARG, "%s must be 16-byte aligned", what);
+  if (stride != 0 && (stride < head_dim || stride % 4 != 0 || stride >= (1ll << 38)))
+    return fail(TKPHI_ERR_INVALID_ARG, "the head stride of %s must be 0 or a multiple of 4 from head_dim to 2^38, got %lld", what, (long long)stride);
+  return TKPHI_OK;
+}
+
+// The append calls with norms or to an 8-bit cache.
+tkphi_status write_rows(const tkphi_paged_desc* kv, const tkphi_append_desc* step, const tkphi_norm_desc* norm, const HeldCache& held,
+                        void* cuda_stream) {
+  WriteProblem p{};
+  tkphi_status st = append_problem(kv, step, held.k_scales != nullptr, &p.a);
+  if (st != TKPHI_OK) return st;
+  if (norm) {
+    if (!std::isfinite(norm->eps) || norm->eps < 0.f) return fail(TKPHI_ERR_INVALID_ARG, "eps must be finite and not negative");
+    st = check_norm(norm->q_weight, norm->q_stride_head, kv->head_dim, "q_weight");
+    if (st == TKPHI_OK) st = check_norm(norm->k_weight, norm->k_stride_head, kv->head_dim, "k_weight");
+    if (st != TKPHI_OK) return st;
+    p.q_weight = norm->q_weight; p.q_weight_head = norm->q_stride_head;
+    p.k_weight = norm->k_weight; p.k_weight_head = norm->k_stride_head;
+    p.eps = norm->eps;
+  }
+  if (p.a.total_q == 0) return TKPHI_OK;
+  p.held = held;
   cudaStream_t cs = reinterpret_cast<cudaStream_t>(cuda_stream);
   ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_APPEND);
-  const cudaError_t e = launch_paged_append(p, kv->dtype == TKPHI_DTYPE_BF16, cs);
+  const cudaError_t e = launch_paged_write(p, kv->dtype == TKPHI_DTYPE_BF16, cs);
   return e == cudaSuccess ? TKPHI_OK : cuda_fail(e, "paged append launch");
 }
 
-tkphi_status tkphi_paged_attention(const tkphi_paged_desc* kv, const void* q, void* y_out, float* lse_out, float scale,
-                                   uint32_t flags, void* workspace, size_t workspace_bytes, void* cuda_stream) {
-  clear_error();
+tkphi_status make_cache_map(const tkphi_paged_desc* kv, const void* base, const HeldCache* held, CUtensorMap* tm) {
+  return held ? make_code_map(kv, base, tm) : make_page_map(kv, base, tm);
+}
+
+size_t workspace_bytes_of(const tkphi_paged_desc* kv, const tkphi_page_selection* selection, int which, bool held) {
+  PagedShape sh{};
+  if (which == TKPHI_WS_PAGED_ATTENTION) {
+    AttendPlan pl{};
+    // the size does not depend on the mask, so that the looser rule of the lengths is enough
+    if (validate_paged(kv, &sh, false, true) != TKPHI_OK || plan_attend(kv, sh, &pl, held) != TKPHI_OK) return 0;
+    return pl.total;
+  }
+  if (which == TKPHI_WS_PAGED_BLOCK_ATTENTION) {
+    BlockPlan pl{};
+    if (validate_paged(kv, &sh, false, false) != TKPHI_OK || plan_block(kv, sh, selection, &pl, held) != TKPHI_OK) return 0;
+    return pl.total;
+  }
+  fail(TKPHI_ERR_INVALID_ARG, "unknown workspace kind %d", which);
+  return 0;
+}
+
+// held: the scales of an 8-bit cache, or null.
+tkphi_status attend(const tkphi_paged_desc* kv, const HeldCache* held, const void* q, void* y_out, float* lse_out, float scale,
+                    uint32_t flags, void* workspace, size_t workspace_bytes, void* cuda_stream) {
   if (flags & ~(uint32_t)TKPHI_FLAG_FULL_CONTEXT) return fail(TKPHI_ERR_INVALID_ARG, "unknown flag bits 0x%x", flags);
   PagedShape sh{};
-  tkphi_status st = validate_paged(kv, &sh, true, (flags & TKPHI_FLAG_FULL_CONTEXT) != 0);
+  tkphi_status st = validate_paged(kv, &sh, true, (flags & TKPHI_FLAG_FULL_CONTEXT) != 0, held != nullptr);
   if (st != TKPHI_OK) return st;
   if (sh.total_q == 0) return TKPHI_OK;
   st = check_io(q, y_out, lse_out, scale);
   if (st != TKPHI_OK) return st;
   AttendPlan pl{};
-  st = plan_attend(kv, sh, &pl);
+  st = plan_attend(kv, sh, &pl, held != nullptr);
   if (st != TKPHI_OK) return st;
   st = check_ws(workspace, workspace_bytes, pl.total);
   if (st != TKPHI_OK) return st;
   CUtensorMap tk, tv;
-  st = make_page_map(kv, kv->k, &tk);
+  st = make_cache_map(kv, kv->k, held, &tk);
   if (st != TKPHI_OK) return st;
-  st = make_page_map(kv, kv->v, &tv);
+  st = make_cache_map(kv, kv->v, held, &tv);
   if (st != TKPHI_OK) return st;
   PagedProblem p = problem_of(kv, sh, q, y_out, lse_out, scale);
   p.causal = (flags & TKPHI_FLAG_FULL_CONTEXT) ? 0 : 1;
   char* w = static_cast<char*>(workspace);
-  p.rows_limit = kRowsLimit;
+  p.rows_limit = held ? INT_MAX : kRowsLimit;
   p.row_ctas = pl.row_ctas;
   p.n_split = pl.row_split;
   p.beside = pl.any_tiles ? 1 : 0;
@@ -419,7 +479,8 @@ tkphi_status tkphi_paged_attention(const tkphi_paged_desc* kv, const void* q, vo
   }
   if (e == cudaSuccess && pl.any_rows) {
     ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_ROWS);
-    e = launch_paged_rows(p, tk, tv, kv->head_dim, bf16, false, pl.row_split > 0, pl.row_grid, cs);
+    e = held ? launch_paged8_rows(p, *held, tk, tv, kv->head_dim, bf16, false, pl.row_split > 0, pl.row_grid, cs)
+             : launch_paged_rows(p, tk, tv, kv->head_dim, bf16, false, pl.row_split > 0, pl.row_grid, cs);
   }
   if (e == cudaSuccess && pl.max_chunks > 1) {
     ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_TILES);
@@ -427,32 +488,31 @@ tkphi_status tkphi_paged_attention(const tkphi_paged_desc* kv, const void* q, vo
   }
   if (e == cudaSuccess && pl.any_rows && !pl.row_split) {
     ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_ROWS);
-    e = launch_paged_rows_merge(p, kv->head_dim, bf16, false, kv->batch * kv->n_kv_heads, pl.max_rows, cs);
+    e = (held ? launch_paged8_rows_merge : launch_paged_rows_merge)(p, kv->head_dim, bf16, false, kv->batch * kv->n_kv_heads, pl.max_rows, cs);
   }
   return e == cudaSuccess ? TKPHI_OK : cuda_fail(e, "paged attention launch");
 }
 
-tkphi_status tkphi_paged_block_attention(const tkphi_paged_desc* kv, const tkphi_page_selection* selection,
-                                         const void* q, void* y_out, float* lse_out, int32_t* page_idx_out, float scale,
-                                         void* workspace, size_t workspace_bytes, void* cuda_stream) {
-  clear_error();
+tkphi_status block_attend(const tkphi_paged_desc* kv, const HeldCache* held, const tkphi_page_selection* selection, const void* q,
+                          void* y_out, float* lse_out, int32_t* page_idx_out, float scale, void* workspace,
+                          size_t workspace_bytes, void* cuda_stream) {
   PagedShape sh{};
-  tkphi_status st = validate_paged(kv, &sh, true, false);
+  tkphi_status st = validate_paged(kv, &sh, true, false, held != nullptr);
   if (st != TKPHI_OK) return st;
   if (!kv->key_bounds) return fail(TKPHI_ERR_INVALID_ARG, "key_bounds is NULL");
   if (sh.total_q == 0) return TKPHI_OK;
   st = check_io(q, y_out, lse_out, scale);
   if (st != TKPHI_OK) return st;
   BlockPlan pl{};
-  st = plan_block(kv, sh, selection, &pl);
+  st = plan_block(kv, sh, selection, &pl, held != nullptr);
   if (st != TKPHI_OK) return st;
   st = check_ws(workspace, workspace_bytes, pl.total);
   if (st != TKPHI_OK) return st;
   if (reinterpret_cast<uintptr_t>(page_idx_out) & 3u) return fail(TKPHI_ERR_INVALID_ARG, "page_idx_out must be 4-byte aligned");
   CUtensorMap tk, tv;
-  st = make_page_map(kv, kv->k, &tk);
+  st = make_cache_map(kv, kv->k, held, &tk);
   if (st != TKPHI_OK) return st;
-  st = make_page_map(kv, kv->v, &tv);
+  st = make_cache_map(kv, kv->v, held, &tv);
   if (st != TKPHI_OK) return st;
   PagedProblem p = problem_of(kv, sh, q, y_out, lse_out, scale);
   char* w = static_cast<char*>(workspace);
@@ -476,11 +536,143 @@ tkphi_status tkphi_paged_block_attention(const tkphi_paged_desc* kv, const tkphi
   if (e != cudaSuccess) return cuda_fail(e, "page selection launch");
   {
     ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_ROWS);
-    e = launch_paged_rows(p, tk, tv, kv->head_dim, bf16, true, pl.cluster, units * pl.n_split, cs);
-    if (e == cudaSuccess && pl.n_split > 1 && !pl.cluster) e = launch_paged_rows_merge(p, kv->head_dim, bf16, true, units, sh.group, cs);
+    e = held ? launch_paged8_rows(p, *held, tk, tv, kv->head_dim, bf16, true, pl.cluster, units * pl.n_split, cs)
+             : launch_paged_rows(p, tk, tv, kv->head_dim, bf16, true, pl.cluster, units * pl.n_split, cs);
+    if (e == cudaSuccess && pl.n_split > 1 && !pl.cluster)
+      e = (held ? launch_paged8_rows_merge : launch_paged_rows_merge)(p, kv->head_dim, bf16, true, units, sh.group, cs);
   }
   if (e != cudaSuccess) return cuda_fail(e, "paged block attention launch");
   return TKPHI_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t tkphi_paged_workspace_bytes(const tkphi_paged_desc* kv, const tkphi_page_selection* selection, int which) {
+  clear_error();
+  return workspace_bytes_of(kv, selection, which, false);
+}
+
+tkphi_status tkphi_paged_append(const tkphi_paged_desc* kv, const tkphi_append_desc* step, void* cuda_stream) {
+  clear_error();
+  AppendProblem p{};
+  const tkphi_status st = append_problem(kv, step, false, &p);
+  if (st != TKPHI_OK || p.total_q == 0) return st;
+  cudaStream_t cs = reinterpret_cast<cudaStream_t>(cuda_stream);
+  ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_APPEND);
+  const cudaError_t e = launch_paged_append(p, kv->dtype == TKPHI_DTYPE_BF16, cs);
+  return e == cudaSuccess ? TKPHI_OK : cuda_fail(e, "paged append launch");
+}
+
+tkphi_status tkphi_paged_append_norm(const tkphi_paged_desc* kv, const tkphi_append_desc* step, const tkphi_norm_desc* norm,
+                                     void* cuda_stream) {
+  clear_error();
+  if (!norm) return fail(TKPHI_ERR_INVALID_ARG, "norm descriptor is NULL");
+  return write_rows(kv, step, norm, HeldCache{}, cuda_stream);
+}
+
+tkphi_status tkphi_coded_append(const tkphi_coded_desc* kv, const tkphi_append_desc* step, const tkphi_norm_desc* norm,
+                                 void* cuda_stream) {
+  clear_error();
+  const tkphi_status st = check_scales(kv);
+  if (st != TKPHI_OK) return st;
+  return write_rows(&kv->step, step, norm, HeldCache{kv->k_scales, kv->v_scales}, cuda_stream);
+}
+
+tkphi_status tkphi_coded_read(const tkphi_coded_desc* kv, const tkphi_read_desc* rows, void* cuda_stream) {
+  clear_error();
+  tkphi_status st = check_scales(kv);
+  if (st != TKPHI_OK) return st;
+  PagedShape sh{};
+  st = validate_paged(&kv->step, &sh, true, true, true);
+  if (st != TKPHI_OK) return st;
+  if (!rows) return fail(TKPHI_ERR_INVALID_ARG, "rows descriptor is NULL");
+  const tkphi_paged_desc& d = kv->step;
+  if (!rows->cu_rows_host || !rows->cu_rows_dev || reinterpret_cast<uintptr_t>(rows->cu_rows_dev) & 7u)
+    return fail(TKPHI_ERR_INVALID_ARG, "cu_rows_host or cu_rows_dev is NULL or not aligned to its type");
+  if ((rows->first_host == nullptr) != (rows->first_dev == nullptr) || reinterpret_cast<uintptr_t>(rows->first_dev) & 7u)
+    return fail(TKPHI_ERR_INVALID_ARG, "first_host and first_dev must both be NULL or both be given, 8-byte aligned");
+  const int64_t* cu = rows->cu_rows_host;
+  if (cu[0] != 0) return fail(TKPHI_ERR_INVALID_ARG, "cu_rows[0] must be 0");
+  int64_t max_kv = 0;
+  for (int b = 0; b < d.batch; ++b) {
+    if (cu[b + 1] < cu[b] || cu[b + 1] > (int64_t)INT_MAX)
+      return fail(TKPHI_ERR_INVALID_ARG, "cu_rows must be non-decreasing and below 2^31 (sequence %d)", b);
+    const int64_t n = cu[b + 1] - cu[b], from = rows->first_host ? rows->first_host[b] : 0, len = d.kv_lens_host[b];
+    if (from < 0 || from > len || n > len - from)
+      return fail(TKPHI_ERR_INVALID_ARG, "sequence %d: rows %lld .. %lld of a cache of %lld", b, (long long)from, (long long)(from + n), (long long)len);
+    max_kv = std::max(max_kv, len);
+  }
+  if (!rows->k_out && !rows->v_out) return fail(TKPHI_ERR_INVALID_ARG, "k_out and v_out are both NULL");
+  if (!aligned16(rows->k_out) || !aligned16(rows->v_out)) return fail(TKPHI_ERR_INVALID_ARG, "k_out and v_out must be 16-byte aligned");
+  const int64_t total = cu[d.batch];
+  for (int i = 0; i < 2; ++i) {
+    if (!(i ? rows->v_out : rows->k_out)) continue;
+    const int64_t row = i ? rows->v_stride_row : rows->k_stride_row, head = i ? rows->v_stride_head : rows->k_stride_head;
+    for (int64_t s : {row, head})
+      if (s < 0 || s % 8 != 0 || s >= (1ll << 38))
+        return fail(TKPHI_ERR_INVALID_ARG, "output strides must be non-negative multiples of 8 elements below 2^38, got %lld", (long long)s);
+    if (!disjoint(total, row, d.n_kv_heads, head, 1, 0, d.head_dim))
+      return fail(TKPHI_ERR_INVALID_ARG, "the strides of %s let elements share memory", i ? "v_out" : "k_out");
+  }
+  if (total == 0) return TKPHI_OK;
+  ReadProblem p{};
+  p.batch = d.batch; p.hkv = d.n_kv_heads; p.d = d.head_dim;
+  p.page_shift = sh.page_shift; p.n_pages = d.n_pages; p.max_pages = d.max_pages;
+  p.table = d.page_table;
+  p.kv_lens = reinterpret_cast<const long long*>(d.kv_lens_dev);
+  p.max_kv = max_kv;
+  p.k = static_cast<const uint8_t*>(d.k); p.v = static_cast<const uint8_t*>(d.v);
+  p.stride_page = d.stride_page; p.stride_head = d.stride_head; p.stride_token = d.stride_token;
+  p.held = HeldCache{kv->k_scales, kv->v_scales};
+  p.cu_rows = reinterpret_cast<const long long*>(rows->cu_rows_dev);
+  p.first = reinterpret_cast<const long long*>(rows->first_dev);
+  p.k_out = rows->k_out; p.k_row = rows->k_stride_row; p.k_head = rows->k_stride_head;
+  p.v_out = rows->v_out; p.v_row = rows->v_stride_row; p.v_head = rows->v_stride_head;
+  p.total_rows = total;
+  p.status = d.status;
+  cudaStream_t cs = reinterpret_cast<cudaStream_t>(cuda_stream);
+  ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_READ);
+  const cudaError_t e = launch_paged_read(p, d.dtype == TKPHI_DTYPE_BF16, cs);
+  return e == cudaSuccess ? TKPHI_OK : cuda_fail(e, "paged read launch");
+}
+
+tkphi_status tkphi_paged_attention(const tkphi_paged_desc* kv, const void* q, void* y_out, float* lse_out, float scale,
+                                   uint32_t flags, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  clear_error();
+  return attend(kv, nullptr, q, y_out, lse_out, scale, flags, workspace, workspace_bytes, cuda_stream);
+}
+
+tkphi_status tkphi_paged_block_attention(const tkphi_paged_desc* kv, const tkphi_page_selection* selection,
+                                         const void* q, void* y_out, float* lse_out, int32_t* page_idx_out, float scale,
+                                         void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  clear_error();
+  return block_attend(kv, nullptr, selection, q, y_out, lse_out, page_idx_out, scale, workspace, workspace_bytes, cuda_stream);
+}
+
+size_t tkphi_coded_workspace_bytes(const tkphi_coded_desc* kv, const tkphi_page_selection* selection, int which) {
+  clear_error();
+  return workspace_bytes_of(kv ? &kv->step : nullptr, selection, which, true);
+}
+
+tkphi_status tkphi_coded_attention(const tkphi_coded_desc* kv, const void* q, void* y_out, float* lse_out, float scale,
+                                    uint32_t flags, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  clear_error();
+  const tkphi_status st = check_scales(kv);
+  if (st != TKPHI_OK) return st;
+  const HeldCache held{kv->k_scales, kv->v_scales};
+  return attend(&kv->step, &held, q, y_out, lse_out, scale, flags, workspace, workspace_bytes, cuda_stream);
+}
+
+tkphi_status tkphi_coded_block_attention(const tkphi_coded_desc* kv, const tkphi_page_selection* selection,
+                                          const void* q, void* y_out, float* lse_out, int32_t* page_idx_out, float scale,
+                                          void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  clear_error();
+  const tkphi_status st = check_scales(kv);
+  if (st != TKPHI_OK) return st;
+  const HeldCache held{kv->k_scales, kv->v_scales};
+  return block_attend(&kv->step, &held, selection, q, y_out, lse_out, page_idx_out, scale, workspace, workspace_bytes, cuda_stream);
 }
 
 }  // extern "C"

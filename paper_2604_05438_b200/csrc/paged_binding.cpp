@@ -20,6 +20,8 @@ namespace {
 // used there, because the caller does not know them.
 struct Handle {
   tkphi_paged_desc desc;
+  bool held = false;                       // the cache is in 8 bits: desc is eight.step
+  tkphi_coded_desc eight{};
   at::ScalarType type;
   int device;
   int64_t total_q;
@@ -35,16 +37,59 @@ const char* kCapsule = "paged cache";
 Handle* handle_of(PyObject* o) { return static_cast<Handle*>(PyCapsule_GetPointer(o, kCapsule)); }
 void free_handle(PyObject* o) { delete handle_of(o); }
 
-// handle(address of the ctypes descriptor, device index, tuple of the tensors made, whether their making may be pending)
-PyObject* make_handle(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 4 || !PyTuple_Check(args[2])) { PyErr_SetString(PyExc_TypeError, "handle(descriptor, device, tensors, pending)"); return nullptr; }
+// What a CacheRows object stands for: the C descriptor without outputs, and the tensors that the object made (complete by then).
+struct Rows {
+  tkphi_read_desc desc;
+  int device;
+  int64_t batch, total;
+  std::vector<at::Tensor> made;
+  cudaStream_t made_on = nullptr;
+};
+const char* kRowsCapsule = "cache rows";
+Rows* rows_of(PyObject* o) { return static_cast<Rows*>(PyCapsule_GetPointer(o, kRowsCapsule)); }
+void free_rows(PyObject* o) { delete rows_of(o); }
+
+// rows(address of the ctypes descriptor, device index, sequences, rows, tuple of the tensors made)
+PyObject* make_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 5 || !PyTuple_Check(args[4])) { PyErr_SetString(PyExc_TypeError, "rows(descriptor, device, batch, total, tensors)"); return nullptr; }
   const void* src = PyLong_AsVoidPtr(args[0]);
   const long dev = PyLong_AsLong(args[1]);
-  const int pending = PyObject_IsTrue(args[3]);
+  const long long batch = PyLong_AsLongLong(args[2]), total = PyLong_AsLongLong(args[3]);
+  if (PyErr_Occurred()) return nullptr;
+  try {
+    std::unique_ptr<Rows> r(new Rows);
+    std::memcpy(&r->desc, src, sizeof(r->desc));
+    r->device = (int)dev;
+    r->batch = batch;
+    r->total = total;
+    if (dev >= 0) {
+      for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(args[4]); ++i) r->made.push_back(THPVariable_Unpack(PyTuple_GET_ITEM(args[4], i)));
+      r->made_on = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream();
+    }
+    return PyCapsule_New(r.release(), kRowsCapsule, free_rows);
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
+// handle(address of the ctypes descriptor, device index, tuple of the tensors made, whether their making may be pending,
+// whether it is that of an 8-bit cache)
+PyObject* make_handle(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 5 || !PyTuple_Check(args[2])) { PyErr_SetString(PyExc_TypeError, "handle(descriptor, device, tensors, pending, held)"); return nullptr; }
+  const void* src = PyLong_AsVoidPtr(args[0]);
+  const long dev = PyLong_AsLong(args[1]);
+  const int pending = PyObject_IsTrue(args[3]), held = PyObject_IsTrue(args[4]);
   if (PyErr_Occurred()) return nullptr;
   try {
     std::unique_ptr<Handle> h(new Handle);
-    std::memcpy(&h->desc, src, sizeof(h->desc));
+    h->held = held != 0;
+    if (h->held) {
+      std::memcpy(&h->eight, src, sizeof(h->eight));
+      h->desc = h->eight.step;
+    } else {
+      std::memcpy(&h->desc, src, sizeof(h->desc));
+    }
     h->type = h->desc.dtype == TKPHI_DTYPE_BF16 ? at::kBFloat16 : at::kHalf;
     h->device = (int)dev;
     h->total_q = h->desc.cu_q_host[h->desc.batch];
@@ -164,25 +209,80 @@ PyObject* run(PyObject* const* args, Py_ssize_t n, Py_ssize_t want, F body) {
   }
 }
 
+// The tensors of an append: a[1] k_new, v_new, inv_freq, pairs, q, q_out, positions.
+tkphi_append_desc take_step(const Handle* h, PyObject* const* a) {
+  tkphi_append_desc d{};
+  const int64_t hkv = h->desc.n_kv_heads, hq = h->desc.n_q_heads;
+  d.pairs = PyObject_IsTrue(a[4]);
+  if (d.pairs < 0) throw Refused{};                    // (something without a truth value)
+  d.k_new = take_heads(h, a[1], "k_new", hkv, false, &d.k_stride_token, &d.k_stride_head);
+  d.v_new = take_heads(h, a[2], "v_new", hkv, false, &d.v_stride_token, &d.v_stride_head);
+  if (a[3] != Py_None) {
+    if (!THPVariable_Check(a[3])) refuse("inv_freq", "must be a tensor");
+    const int64_t half = THPVariable_Unpack(a[3]).numel();
+    d.inv_freq = static_cast<const float*>(take(h, a[3], "inv_freq", at::kFloat, {half}, true));
+    d.rot_dim = half > 1 << 20 ? -1 : (int32_t)(2 * half);
+  }
+  if (a[5] != Py_None) d.q = take_heads(h, a[5], "q", hq, false, &d.q_stride_token, &d.q_stride_head);
+  if (a[6] != Py_None) d.q_out = take_heads(h, a[6], "q_out", hq, false, &d.o_stride_token, &d.o_stride_head);
+  if (a[7] != Py_None) d.positions = static_cast<const int64_t*>(take(h, a[7], "positions", at::kLong, {h->total_q}, true));
+  return d;
+}
+
 // append(handle, k_new, v_new, inv_freq, pairs, q, q_out, positions, stream)
 PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return run(a, n, 9, [&](const Handle* h) {
-    tkphi_append_desc d{};
-    const int64_t hkv = h->desc.n_kv_heads, hq = h->desc.n_q_heads;
-    d.pairs = PyObject_IsTrue(a[4]);
-    if (d.pairs < 0) throw Refused{};                  // (something without a truth value)
-    d.k_new = take_heads(h, a[1], "k_new", hkv, false, &d.k_stride_token, &d.k_stride_head);
-    d.v_new = take_heads(h, a[2], "v_new", hkv, false, &d.v_stride_token, &d.v_stride_head);
-    if (a[3] != Py_None) {
-      if (!THPVariable_Check(a[3])) refuse("inv_freq", "must be a tensor");
-      const int64_t half = THPVariable_Unpack(a[3]).numel();
-      d.inv_freq = static_cast<const float*>(take(h, a[3], "inv_freq", at::kFloat, {half}, true));
-      d.rot_dim = half > 1 << 20 ? -1 : (int32_t)(2 * half);
+    const tkphi_append_desc d = take_step(h, a);
+    void* stream = take_stream(h, a[8]);
+    return h->held ? tkphi_coded_append(&h->eight, &d, nullptr, stream) : tkphi_paged_append(&h->desc, &d, stream);
+  });
+}
+
+// Norm weights [head_dim] or [heads, head_dim].
+const float* take_weight(const Handle* h, PyObject* o, const char* what, int64_t heads, int64_t* stride) {
+  if (o == Py_None) return nullptr;
+  if (!THPVariable_Check(o)) refuse(what, "must be a tensor");
+  const int64_t d = h->desc.head_dim;
+  if (THPVariable_Unpack(o).dim() == 1) return static_cast<const float*>(take(h, o, what, at::kFloat, {d}, true));
+  *stride = d;
+  return static_cast<const float*>(take(h, o, what, at::kFloat, {heads, d}, true));
+}
+
+// append_norm(handle, k_new, v_new, inv_freq, pairs, q, q_out, positions, q_weight, k_weight, eps, stream)
+PyObject* append_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(a, n, 12, [&](const Handle* h) {
+    const tkphi_append_desc d = take_step(h, a);
+    tkphi_norm_desc w{};
+    w.q_weight = take_weight(h, a[8], "q_weight", h->desc.n_q_heads, &w.q_stride_head);
+    w.k_weight = take_weight(h, a[9], "k_weight", h->desc.n_kv_heads, &w.k_stride_head);
+    const double eps = PyFloat_AsDouble(a[10]);
+    if (PyErr_Occurred()) throw Refused{};
+    w.eps = (float)eps;
+    if (!(w.eps >= 0.f && w.eps <= std::numeric_limits<float>::max())) refuse("eps", "must not be negative, and finite in 32 bits");
+    void* stream = take_stream(h, a[11]);
+    return h->held ? tkphi_coded_append(&h->eight, &d, &w, stream) : tkphi_paged_append_norm(&h->desc, &d, &w, stream);
+  });
+}
+
+// read(handle, rows, k_out, v_out, stream)
+PyObject* read_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(a, n, 5, [&](const Handle* h) {
+    const Rows* r = rows_of(a[1]);
+    if (!r) throw Refused{};
+    if (!h->held) refuse("kv", "is not a cache in 8 bits");
+    if (r->batch != h->desc.batch) refuse("rows", "are of another number of sequences");
+    if (r->device != h->device) refuse("rows", "are not on the cache's device");
+    tkphi_read_desc d = r->desc;
+    const int64_t hkv = h->desc.n_kv_heads, dim = h->desc.head_dim;
+    if (a[2] != Py_None) d.k_out = take(h, a[2], "k_out", h->type, {r->total, hkv, dim}, false, &d.k_stride_row, &d.k_stride_head);
+    if (a[3] != Py_None) d.v_out = take(h, a[3], "v_out", h->type, {r->total, hkv, dim}, false, &d.v_stride_row, &d.v_stride_head);
+    if (r->total == 0 && (a[2] != Py_None || a[3] != Py_None)) return (tkphi_status)TKPHI_OK;   // (an empty tensor has no address)
+    cudaStream_t s = static_cast<cudaStream_t>(take_stream(h, a[4]));
+    if (s != r->made_on && !r->made.empty()) {
+      const c10::cuda::CUDAStream used = c10::cuda::getStreamFromExternal(s, (c10::DeviceIndex)h->device);
+      for (const at::Tensor& t : r->made) c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), used);
     }
-    if (a[5] != Py_None) d.q = take_heads(h, a[5], "q", hq, false, &d.q_stride_token, &d.q_stride_head);
-    if (a[6] != Py_None) d.q_out = take_heads(h, a[6], "q_out", hq, false, &d.o_stride_token, &d.o_stride_head);
-    if (a[7] != Py_None) d.positions = static_cast<const int64_t*>(take(h, a[7], "positions", at::kLong, {h->total_q}, true));
-    return tkphi_paged_append(&h->desc, &d, take_stream(h, a[8]));
+    return tkphi_coded_read(&h->eight, &d, s);
   });
 }
 
@@ -196,7 +296,9 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     float* lse = take_lse(h, a[3]);
     size_t bytes = 0;
     void* ws = take_workspace(h, a[6], &bytes);
-    return tkphi_paged_attention(&h->desc, q, y, lse, scale, flags, ws, bytes, take_stream(h, a[7]));
+    void* stream = take_stream(h, a[7]);
+    return h->held ? tkphi_coded_attention(&h->eight, q, y, lse, scale, flags, ws, bytes, stream)
+                   : tkphi_paged_attention(&h->desc, q, y, lse, scale, flags, ws, bytes, stream);
   });
 }
 
@@ -220,7 +322,9 @@ PyObject* block_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
       idx = static_cast<int32_t*>(take(h, a[7], "page_idx_out", at::kInt, {h->total_q, h->desc.n_kv_heads, (int64_t)v[0] + v[1] + v[2]}, true));
     size_t bytes = 0;
     void* ws = take_workspace(h, a[9], &bytes);
-    return tkphi_paged_block_attention(&h->desc, &sel, q, y, lse, idx, scale, ws, bytes, take_stream(h, a[10]));
+    void* stream = take_stream(h, a[10]);
+    return h->held ? tkphi_coded_block_attention(&h->eight, &sel, q, y, lse, idx, scale, ws, bytes, stream)
+                   : tkphi_paged_block_attention(&h->desc, &sel, q, y, lse, idx, scale, ws, bytes, stream);
   });
 }
 
@@ -231,7 +335,10 @@ PyCFunction fast(PyObject* (*f)(PyObject*, PyObject* const*, Py_ssize_t)) {
 
 PyMethodDef methods[] = {
     {"handle", fast(make_handle), METH_FASTCALL, nullptr},
+    {"rows", fast(make_rows), METH_FASTCALL, nullptr},
     {"append", fast(append), METH_FASTCALL, nullptr},
+    {"append_norm", fast(append_norm), METH_FASTCALL, nullptr},
+    {"read", fast(read_rows), METH_FASTCALL, nullptr},
     {"attention", fast(attention), METH_FASTCALL, nullptr},
     {"block_attention", fast(block_attention), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};

@@ -1,0 +1,326 @@
+// New tokens into a paged cache, with head norms on the way, into pages of 16 or of 8 bits.
+//
+// For token i of sequence b (cache position t = kv_len - q_len + i, angle position x = positions[i] or t), each key and
+// query head h on its own:
+//   norm      u = h * w / sqrt(mean(h^2) + eps), where the side has weights (otherwise u = h)
+//   rotation  pair (a, c) of u -> (a cos w - c sin w, c cos w + a sin w), w = x * inv_freq[pair]
+// in 32 bits.  A 16-bit cache takes keys rounded once and values as they are; an 8-bit one takes both as codes and a power
+// of two per row (held8.cuh), rounded once from the 32-bit numbers.  Queries are rounded once to the element type.  Key
+// bounds of the touched pages are recomputed from what the pages hold, those of earlier calls read back.
+//
+// Bound: memory.  As in the append without norms, a CTA takes 64 positions (a page of 128) of one KV head, 8 lanes per row
+// at head_dim 128 (4 at 64), a lane owning the two 8-element pieces whose elements are each other's partners in the
+// rotation.  A row's sum of squares and its largest magnitude are two or three shuffles between its lanes; all lanes of a
+// warp take part in them, with zeros where they have no row.
+#include "held8.cuh"
+
+namespace tkphi {
+
+template <typename T>
+__device__ __forceinline__ void unpack_piece(const uint4& v, float* x) {
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(&v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[2 * i] = T::lo(w[i]); x[2 * i + 1] = T::hi(w[i]); }
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack_piece(const float* x) {
+  return make_uint4(T::pack(x[0], x[1]), T::pack(x[2], x[3]), T::pack(x[4], x[5]), T::pack(x[6], x[7]));
+}
+// x: the lane's two pieces of 8 dims.
+__device__ __forceinline__ void rotate16(float (&x)[16], const float (&cs)[8], const float (&sn)[8], bool pairs) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    // partners: neighbours, pair i of the 16, or the same place in the two pieces
+    const float a = pairs ? x[2 * i] : x[i], c = pairs ? x[2 * i + 1] : x[8 + i];
+    const float u = a * cs[i] - c * sn[i], w = c * cs[i] + a * sn[i];
+    if (pairs) { x[2 * i] = u; x[2 * i + 1] = w; } else { x[i] = u; x[8 + i] = w; }
+  }
+}
+template <int LPR>
+__device__ __forceinline__ void norm16(float (&x)[16], const float* weight, int c0, int c1, float eps) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s = fmaf(x[i], x[i], s);
+#pragma unroll
+  for (int o = 1; o < LPR; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  const float r = rsqrtf(fmaf(s, 1.f / (16 * LPR), eps));
+  float w[16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float4 v = __ldg(reinterpret_cast<const float4*>(weight + 8 * (i < 2 ? c0 : c1)) + (i & 1));
+    w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = x[i] * r * w[i];
+}
+// Scale byte of the row that LPR lanes hold.
+template <int LPR>
+__device__ __forceinline__ uint32_t row_byte(const float (&x)[16]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+#pragma unroll
+  for (int o = 1; o < LPR; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+  return held_byte(m);
+}
+__device__ __forceinline__ uint4 row_codes(const float (&x)[16], uint32_t e) {
+  if (e == 255u) return make_uint4(0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu);
+  const float r = held_inverse(e);
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = pack_codes(x[4 * i] * r, x[4 * i + 1] * r, x[4 * i + 2] * r, x[4 * i + 3] * r);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// An item is one KV head of 64 aligned cache positions (128 where the page is that long): whole pages, so that their
+// bounds need no other CTA.
+template <typename T, int D, int NT, bool HELD>
+__global__ void __launch_bounds__(NT, NT == 128 ? 4 : 2) paged_write_kernel(const __grid_constant__ WriteProblem wp) {
+  constexpr int LPR = D / 16;                  // lanes of a row
+  constexpr int RPW = 32 / LPR;                // rows of a warp
+  constexpr int RPP = NT / LPR;                // rows of one pass of the CTA
+  constexpr size_t es = 2;
+  const AppendProblem& p = wp.a;
+  __shared__ long long s_find[4];              // sequence, its first token row, cache length, first new position
+  __shared__ int s_item;
+  __shared__ uint4 s_red[128 / RPW][2][2 * LPR];     // a warp's rows: their minimum and maximum
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int h = blockIdx.y, span_shift = p.page_shift > 6 ? p.page_shift : 6;
+  pdl_wait();
+  pdl_launch_next();
+
+  // ---- which positions: a sequence holds (q_len + span - 2) / span + 1 items, enough for every start inside one
+  if (warp == 0) {
+    const int item = blockIdx.x, span = 1 << span_shift;
+    int base = 0;
+    if (lane == 0) s_find[0] = -1;
+    for (int s = 0; s < p.batch; s += 32) {
+      int n = 0;
+      long long t0 = 0, m = 0, len = 0;
+      if (s + lane < p.batch) {
+        t0 = __ldg(p.cu_q + s + lane);
+        m = __ldg(p.cu_q + s + lane + 1) - t0;
+        len = __ldg(p.kv_lens + s + lane);
+        n = m > 0 ? (int)((m + span - 2) >> span_shift) + 1 : 0;
+      }
+      const int incl = warp_inclusive_scan(n) + base;
+      if (incl > item && incl - n <= item) {           // one lane
+        s_find[0] = s + lane; s_find[1] = t0;
+        s_find[2] = len < p.max_kv ? len : p.max_kv;
+        s_find[3] = s_find[2] - m;
+        s_item = item - (incl - n);
+      }
+      base = __shfl_sync(0xffffffffu, incl, 31);
+      if (base > item) break;
+    }
+  }
+  __syncthreads();
+  const int b = (int)s_find[0];
+  const long long tok0 = s_find[1], len = s_find[2], begin = s_find[3];
+  if (b < 0 || begin < 0) return;
+  const long long t0 = ((begin >> span_shift) + s_item) << span_shift;       // first position of the item
+  if (t0 >= len) return;
+  const int lo = begin > t0 ? (int)(begin - t0) : 0;                         // new rows: lo .. hi-1 of the item
+  const int hi = len - t0 < (1ll << span_shift) ? (int)(len - t0) : 1 << span_shift;
+  const int ps = 1 << p.page_shift, first = p.bounds ? lo & ~(ps - 1) : lo;  // with bounds: every row of the touched pages
+  const int* table = p.table + (size_t)b * p.max_pages + (t0 >> p.page_shift);
+
+  const int l = lane % LPR;
+  // the lane's two pieces: partners of each other in the rotated part, otherwise neighbours
+  int c0 = 2 * l, c1 = 2 * l + 1;
+  const int turned = p.rot / 16;                          // lanes whose pieces are rotated
+  const bool rotate = l < turned;
+  if (rotate && !p.pairs) { c0 = l; c1 = l + turned; }
+  double turn[8];
+  if (rotate) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) turn[i] = (double)__ldg(p.inv_freq + 8 * l + i) * 0.15915494309189533577;
+  }
+  const float* kw = wp.k_weight ? wp.k_weight + h * wp.k_weight_head : nullptr;
+  for (int r0 = 0; r0 < hi; r0 += RPP) {
+    const int row = r0 + tid / LPR;
+    const bool in = row >= first && row < hi, fresh = in && row >= lo;
+    uint4 a = make_uint4(0, 0, 0, 0), c = a;              // the held key, as 16-bit pieces, for the bounds
+    int phys = 0;
+    bool ok = false;
+    if (in) {
+      // a page id outside the cache: its rows are dropped, the queries of its tokens are written all the same
+      phys = __ldg(table + (row >> p.page_shift));
+      ok = phys >= 0 && phys < p.n_pages;
+      if (!ok && l == 0) atomicExch(p.status, kStatusBadPage);
+      phys = ok ? phys : 0;
+    }
+    const size_t at = (size_t)phys * p.stride_page + (size_t)h * p.stride_head + (size_t)(row & (ps - 1)) * p.stride_token;
+    const size_t scale_at = ((size_t)phys * p.hkv + h) * ps + (row & (ps - 1));
+    if (__any_sync(0xffffffffu, fresh)) {
+      const long long t = t0 + row, tok = fresh ? tok0 + (t - begin) : tok0;
+      const uint4* ks = reinterpret_cast<const uint4*>(static_cast<const char*>(p.k_new) + ((size_t)tok * p.k_new_token + (size_t)h * p.k_new_head) * es);
+      const uint4* vs = reinterpret_cast<const uint4*>(static_cast<const char*>(p.v_new) + ((size_t)tok * p.v_new_token + (size_t)h * p.v_new_head) * es);
+      uint4 ka = a, kc = a, v0 = a, v1 = a;
+      float cs[8], sn[8];
+      if (fresh) {
+        ka = __ldg(ks + c0);
+        kc = __ldg(ks + c1);
+        v0 = __ldg(vs + 2 * l);
+        v1 = __ldg(vs + 2 * l + 1);
+        if (rotate) {
+          const double x = (double)(p.positions ? __ldg(p.positions + tok) : t);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const double w = x * turn[i];
+            sincospif(2.f * (float)(w - rint(w)), &sn[i], &cs[i]);
+          }
+        }
+      }
+      float x[16];
+      unpack_piece<T>(ka, x);
+      unpack_piece<T>(kc, x + 8);
+      if (kw) norm16<LPR>(x, kw, c0, c1, wp.eps);
+      if (fresh && rotate) rotate16(x, cs, sn, p.pairs);
+      if (HELD) {
+        const uint32_t ke = row_byte<LPR>(x);
+        const uint4 kcode = row_codes(x, ke);
+        float y[16];
+        unpack_piece<T>(v0, y);
+        unpack_piece<T>(v1, y + 8);
+        const uint32_t ve = row_byte<LPR>(y);
+        if (ok && fresh) {
+          uint2* kd = reinterpret_cast<uint2*>(static_cast<char*>(p.k) + at);
+          kd[c0] = make_uint2(kcode.x, kcode.y);
+          kd[c1] = make_uint2(kcode.z, kcode.w);
+          reinterpret_cast<uint4*>(static_cast<char*>(p.v) + at)[l] = row_codes(y, ve);
+          if (l == 0) {
+            wp.held.k_scales[scale_at] = (uint8_t)ke;
+            wp.held.v_scales[scale_at] = (uint8_t)ve;
+          }
+        }
+        if (p.bounds && fresh) {
+          const float s = held_scale(ke);
+          const uint2 w0 = held_values<T>(kcode.x, s), w1 = held_values<T>(kcode.y, s);
+          const uint2 w2 = held_values<T>(kcode.z, s), w3 = held_values<T>(kcode.w, s);
+          a = make_uint4(w0.x, w0.y, w1.x, w1.y);
+          c = make_uint4(w2.x, w2.y, w3.x, w3.y);
+        }
+      } else if (fresh) {
+        a = pack_piece<T>(x);
+        c = pack_piece<T>(x + 8);
+        if (ok) {
+          uint4* kd = reinterpret_cast<uint4*>(static_cast<char*>(p.k) + at * es);
+          uint4* vd = reinterpret_cast<uint4*>(static_cast<char*>(p.v) + at * es);
+          kd[c0] = a;
+          kd[c1] = c;
+          vd[2 * l] = v0;
+          vd[2 * l + 1] = v1;
+        }
+      }
+      if (p.q) {
+        const char* qs = static_cast<const char*>(p.q) + ((size_t)tok * p.q_token + (size_t)h * p.group * p.q_head) * es;
+        char* qd = static_cast<char*>(p.q_out) + ((size_t)tok * p.q_out_token + (size_t)h * p.group * p.q_out_head) * es;
+        // four heads at a time, all loads before the stores (plain loads: q_out may be q itself)
+        for (int g = 0; g < p.group; g += 4) {
+          uint4 u[4], w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            u[i] = w[i] = make_uint4(0, 0, 0, 0);
+            if (g + i < p.group && fresh) {
+              const uint4* s = reinterpret_cast<const uint4*>(qs + (size_t)(g + i) * p.q_head * es);
+              u[i] = s[c0];
+              w[i] = s[c1];
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (g + i < p.group) {
+              float z[16];
+              unpack_piece<T>(u[i], z);
+              unpack_piece<T>(w[i], z + 8);
+              if (wp.q_weight) norm16<LPR>(z, wp.q_weight + (h * p.group + g + i) * wp.q_weight_head, c0, c1, wp.eps);
+              if (fresh) {
+                if (rotate) rotate16(z, cs, sn, p.pairs);
+                uint4* o = reinterpret_cast<uint4*>(qd + (size_t)(g + i) * p.q_out_head * es);
+                o[c0] = pack_piece<T>(z);
+                o[c1] = pack_piece<T>(z + 8);
+              }
+            }
+        }
+      }
+    }
+    if (in && !fresh) {                                   // a row of an earlier call
+      if (HELD) {
+        const uint2* kd = reinterpret_cast<const uint2*>(static_cast<const char*>(p.k) + at);
+        const uint2 k0 = kd[c0], k1 = kd[c1];
+        const float s = held_scale(wp.held.k_scales[scale_at]);
+        const uint2 w0 = held_values<T>(k0.x, s), w1 = held_values<T>(k0.y, s);
+        const uint2 w2 = held_values<T>(k1.x, s), w3 = held_values<T>(k1.y, s);
+        a = make_uint4(w0.x, w0.y, w1.x, w1.y);
+        c = make_uint4(w2.x, w2.y, w3.x, w3.y);
+      } else {
+        const uint4* kd = reinterpret_cast<const uint4*>(static_cast<const char*>(p.k) + at * es);
+        a = kd[c0];
+        c = kd[c1];
+      }
+    }
+    if (p.bounds) {
+      // over the warp's rows (all of one page); lanes without a row take their partner's
+      uint4 n0 = a, n1 = c, x0 = a, x1 = c;
+      uint32_t* w[4] = {reinterpret_cast<uint32_t*>(&n0), reinterpret_cast<uint32_t*>(&n1), reinterpret_cast<uint32_t*>(&x0),
+                        reinterpret_cast<uint32_t*>(&x1)};
+      bool any = in;
+#pragma unroll
+      for (int o = LPR; o < 32; o <<= 1) {
+        const bool theirs = __shfl_xor_sync(0xffffffffu, (int)any, o) != 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t x = __shfl_xor_sync(0xffffffffu, w[j][i], o);
+            if (theirs) w[j][i] = !any ? x : j < 2 ? T::min2(w[j][i], x) : T::max2(w[j][i], x);
+          }
+        any = any || theirs;
+      }
+      if (lane < LPR) {
+        const int grp = (r0 + warp * RPW) / RPW;
+        s_red[grp][0][c0] = n0; s_red[grp][0][c1] = n1;
+        s_red[grp][1][c0] = x0; s_red[grp][1][c1] = x1;
+      }
+    }
+  }
+  if (!p.bounds) return;
+  __syncthreads();
+  // ---- the touched pages' bounds: over their groups of rows (those that hold a row)
+  for (int i = tid; i < 4 * LPR * ((hi - first + ps - 1) >> p.page_shift); i += NT) {
+    const int c = i % (2 * LPR), side = i / (2 * LPR) % 2, page = (first >> p.page_shift) + i / (4 * LPR);
+    const int g0 = (page << p.page_shift) / RPW, rows_end = ((page + 1) << p.page_shift) < hi ? (page + 1) << p.page_shift : hi;
+    const int g1 = (rows_end + RPW - 1) / RPW;
+    uint4 r = s_red[g0][side][c];
+    uint32_t* rr = reinterpret_cast<uint32_t*>(&r);
+    for (int g = g0 + 1; g < g1; ++g) {
+      const uint4 x = s_red[g][side][c];
+      const uint32_t* xx = reinterpret_cast<const uint32_t*>(&x);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) rr[e] = side == 0 ? T::min2(rr[e], xx[e]) : T::max2(rr[e], xx[e]);
+    }
+    const int phys = __ldg(table + page);
+    if (phys >= 0 && phys < p.n_pages)
+      reinterpret_cast<uint4*>(static_cast<char*>(p.bounds) + (((size_t)phys * p.hkv + h) * 2 + side) * D * es)[c] = r;
+  }
+}
+
+// 256 threads per CTA where items hold few new rows (decoding: a single pass, all latency), 128 otherwise.
+template <typename T, int D, bool HELD>
+static cudaError_t launch_write_t(const WriteProblem& p, cudaStream_t st) {
+  const dim3 grid(p.a.items, p.a.hkv);
+  return p.a.total_q <= 16ll * p.a.items ? launch_pdl(paged_write_kernel<T, D, 256, HELD>, grid, dim3(256), 0, st, p)
+                                         : launch_pdl(paged_write_kernel<T, D, 128, HELD>, grid, dim3(128), 0, st, p);
+}
+template <typename T, int D>
+static cudaError_t launch_write_d(const WriteProblem& p, cudaStream_t st) {
+  return p.held.k_scales ? launch_write_t<T, D, true>(p, st) : launch_write_t<T, D, false>(p, st);
+}
+
+cudaError_t launch_paged_write(const WriteProblem& p, bool bf16, cudaStream_t st) {
+  if (p.a.d == 64) return bf16 ? launch_write_d<Bf16, 64>(p, st) : launch_write_d<Fp16, 64>(p, st);
+  return bf16 ? launch_write_d<Bf16, 128>(p, st) : launch_write_d<Fp16, 128>(p, st);
+}
+
+}  // namespace tkphi
