@@ -78,6 +78,16 @@ struct ReadProblem {
 };
 cudaError_t launch_paged_read(const ReadProblem& p, bool bf16, cudaStream_t st);
 
+constexpr int kExpandRows = 128;             // rows of an expanded page
+struct ExpandProblem {
+  const uint8_t* k; const uint8_t* v;
+  long long stride_page, stride_head, stride_token;    // bytes
+  HeldCache held;
+  void* k_out; void* v_out;                  // [pages][hkv][128][d]
+  int* table; int max_pages;                 // [batch][max_pages] written for the sequences with many rows
+};
+cudaError_t launch_paged_expand(const PagedProblem& p, const ExpandProblem& x, int d, bool bf16, int pages, cudaStream_t st);
+
 constexpr int kHeldKeys = 128;               // keys of one tile of the row kernel
 int paged8_row_ctas(int d);                  // its CTAs per multiprocessor where units are dealt out as a line
 cudaError_t launch_paged8_rows(const PagedProblem& p, const HeldCache& held, const CUtensorMap& tk, const CUtensorMap& tv, int d,

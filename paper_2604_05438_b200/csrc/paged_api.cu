@@ -159,16 +159,28 @@ struct AttendPlan {
   bool any_rows, any_tiles;
   int chunk, max_chunks, tile_grid;
   size_t row_part, row_stat, tile_part, tile_stat, total;
+  // 8-bit cache: the caches of the tile kernel's sequences are first written as 16-bit pages of 128 rows.  (A tile kernel that
+  // reads codes and converts its tiles itself was built and measured: 1.06x to 1.26x faster up to 192 rows, 0.74x with 2048
+  // tokens, because every 256 rows convert the cache again and the conversion's shared-memory traffic comes on top of the
+  // products'.)
+  int expand_pages, expand_max;  // of all sequences, of the longest
+  size_t expand_k, expand_v, expand_table;
 };
 
-// Sequences with at most this many rows per KV head go to the row kernel: one tile of its matrix instruction.
+// Sequences with at most this many rows per KV head go to the row kernel.  Over a 16-bit cache: one tile of its matrix instruction.
 constexpr int kRowsLimit = 16;
+// Over an 8-bit cache: four.  The row kernel then reads such a sequence's cache once per tile, the other way writes it as 16-bit
+// pages first and reads those with the tile kernel.  One sequence of 128K rows, 24 / 8 heads of 128: 67 us with 16 rows, 205
+// with 64, 298 with 96, 391 with 128 against 328 to 332; eight of them 1505 us with 64, 2252 with 96 against 2000; 32 / 8 heads
+// of 64, eight of 128K: 1146 with 64 against 1106, eight of 32K: 315 against 300, of 4K: 61 against 66, 109 with 128 against 70.
+constexpr int kHeldRowsLimit = 64;
+constexpr int rows_limit(bool held) { return held ? kHeldRowsLimit : kRowsLimit; }
 
 // Keys per CTA of the tile kernel: the whole context if the row tiles alone fill the SMs evenly, otherwise a part of it.
 // The estimate of a choice, in key tiles of one CTA: the larger of the waves' sum and the balanced share plus half of
 // the longest CTA; a CTA costs about four tiles of set-up and, if its output is partial, a thirtieth of a tile of the
 // device's time for writing and joining it.
-int choose_chunk(const tkphi_paged_desc* kv, const PagedShape& sh, int64_t longest, int n_sm) {
+int choose_chunk(const tkphi_paged_desc* kv, const PagedShape& sh, int64_t longest, int n_sm, int limit) {
   int best = 0;
   double best_cost = 0;
   for (int parts = 1; parts <= 64; ++parts) {
@@ -177,7 +189,7 @@ int choose_chunk(const tkphi_paged_desc* kv, const PagedShape& sh, int64_t longe
     double ctas = 0, work = 0;
     for (int b = 0; b < kv->batch; ++b) {
       const int64_t q = kv->cu_q_host[b + 1] - kv->cu_q_host[b], len = kv->kv_lens_host[b];
-      if (q * sh.group <= kRowsLimit) continue;
+      if (q * sh.group <= limit) continue;
       const int pair = 2 * tile_rows(sh.group);
       const double rt = (double)((q * sh.group + pair - 1) / pair) * kv->n_kv_heads;
       const double seen = std::max<double>(1., ((double)len - 0.5 * (double)std::min(q, len)) / kTileKeys);   // of an average row tile
@@ -208,7 +220,7 @@ tkphi_status plan_attend(const tkphi_paged_desc* kv, const PagedShape& sh, Atten
     const int64_t q = kv->cu_q_host[b + 1] - kv->cu_q_host[b];
     if (q == 0) continue;
     const int64_t rows = q * sh.group, len = kv->kv_lens_host[b];
-    if (rows > kRowsLimit && !held) {
+    if (rows > rows_limit(held)) {
       pl->any_tiles = true;
       longest = std::max<int64_t>(longest, len > 0 ? (len + kTileKeys - 1) / kTileKeys : 1);
       continue;
@@ -221,17 +233,16 @@ tkphi_status plan_attend(const tkphi_paged_desc* kv, const PagedShape& sh, Atten
   }
   if (pl->row_tiles > INT_MAX / 2) return fail(TKPHI_ERR_UNSUPPORTED, "too many key tiles for one call");
   const int units = kv->batch * kv->n_kv_heads;
-  pl->row_split = split_rows(units, longest_row, n_sm);
-  if (held && pl->max_rows > kRowsLimit) pl->row_split = 0;
+  pl->row_split = pl->max_rows <= kRowTile ? split_rows(units, longest_row, n_sm) : 0;     // (a cluster has one row tile)
   pl->row_ctas = pl->row_split ? 0 : (int)std::min<int64_t>(row_ctas * n_sm, pl->row_tiles);
   pl->row_grid = pl->row_split ? units * pl->row_split : pl->row_ctas;
   if (pl->any_tiles) {
-    pl->chunk = choose_chunk(kv, sh, longest, n_sm);
+    pl->chunk = choose_chunk(kv, sh, longest, n_sm, rows_limit(held));
     const int pair = 2 * tile_rows(sh.group);
     int64_t grid = 0;
     for (int b = 0; b < kv->batch; ++b) {
       const int64_t rows = (kv->cu_q_host[b + 1] - kv->cu_q_host[b]) * sh.group, len = kv->kv_lens_host[b];
-      if (rows <= kRowsLimit) continue;
+      if (rows <= rows_limit(held)) continue;
       const int64_t chunks = len > pl->chunk ? (len + pl->chunk - 1) / pl->chunk : 1;
       pl->max_chunks = (int)std::max<int64_t>(pl->max_chunks, chunks);
       grid += (rows + pair - 1) / pair * chunks * kv->n_kv_heads;
@@ -239,7 +250,25 @@ tkphi_status plan_attend(const tkphi_paged_desc* kv, const PagedShape& sh, Atten
     if (grid > INT_MAX / 2) return fail(TKPHI_ERR_UNSUPPORTED, "too many query rows for one call");
     pl->tile_grid = (int)grid;
   }
+  if (held && pl->any_tiles) {
+    int64_t pages = 0, most = 0;
+    for (int b = 0; b < kv->batch; ++b) {
+      if ((kv->cu_q_host[b + 1] - kv->cu_q_host[b]) * sh.group <= rows_limit(held)) continue;
+      const int64_t n = (kv->kv_lens_host[b] + kExpandRows - 1) / kExpandRows;
+      pages += n;
+      most = std::max(most, n);
+    }
+    if (pages > (1 << 30)) return fail(TKPHI_ERR_UNSUPPORTED, "too many cache rows of sequences with many query rows for one call");
+    pl->expand_pages = (int)std::max<int64_t>(pages, 1);     // (nothing but empty sequences: a page that is not written)
+    pl->expand_max = (int)std::max<int64_t>(most, 1);
+  }
   size_t o = 0;
+  if (pl->expand_pages) {
+    const size_t cache = (size_t)pl->expand_pages * kv->n_kv_heads * kExpandRows * kv->head_dim * 2;
+    pl->expand_k = o; o = align_up(o + cache, 256);
+    pl->expand_v = o; o = align_up(o + cache, 256);
+    pl->expand_table = o; o = align_up(o + sizeof(int) * (size_t)kv->batch * pl->expand_max, 256);
+  }
   pl->row_part = o; o = align_up(o + sizeof(float) * 2 * pl->row_ctas * kRowTile * kv->head_dim, 256);
   pl->row_stat = o; o = align_up(o + sizeof(float) * 2 * pl->row_ctas * kRowTile * 2, 256);
   const size_t parts = pl->max_chunks > 1 ? (size_t)pl->tile_grid * kTileRows : 0;
@@ -457,7 +486,7 @@ tkphi_status attend(const tkphi_paged_desc* kv, const HeldCache* held, const voi
   PagedProblem p = problem_of(kv, sh, q, y_out, lse_out, scale);
   p.causal = (flags & TKPHI_FLAG_FULL_CONTEXT) ? 0 : 1;
   char* w = static_cast<char*>(workspace);
-  p.rows_limit = held ? INT_MAX : kRowsLimit;
+  p.rows_limit = rows_limit(held != nullptr);
   p.row_ctas = pl.row_ctas;
   p.n_split = pl.row_split;
   p.beside = pl.any_tiles ? 1 : 0;
@@ -471,11 +500,26 @@ tkphi_status attend(const tkphi_paged_desc* kv, const HeldCache* held, const voi
   // tiles, rows (may start beside the tiles' last CTAs), then the joins
   cudaError_t e = cudaSuccess;
   if (pl.any_tiles) {
-    CUtensorMap tq;
+    CUtensorMap tq, xk, xv;
     st = make_query_map(kv, sh, q, &tq);
     if (st != TKPHI_OK) return st;
+    PagedProblem t = p;
+    if (pl.expand_pages) {
+      const ExpandProblem x{static_cast<const uint8_t*>(kv->k), static_cast<const uint8_t*>(kv->v), kv->stride_page, kv->stride_head,
+                            kv->stride_token, *held, w + pl.expand_k, w + pl.expand_v, reinterpret_cast<int*>(w + pl.expand_table), pl.expand_max};
+      tkphi_paged_desc d = *kv;
+      d.page_size = kExpandRows; d.n_pages = pl.expand_pages; d.max_pages = pl.expand_max;
+      d.stride_token = kv->head_dim; d.stride_head = d.stride_token * kExpandRows; d.stride_page = d.stride_head * kv->n_kv_heads;
+      st = make_page_map(&d, x.k_out, &xk);
+      if (st != TKPHI_OK) return st;
+      st = make_page_map(&d, x.v_out, &xv);
+      if (st != TKPHI_OK) return st;
+      t.page_shift = 7; t.n_pages = d.n_pages; t.max_pages = d.max_pages; t.table = x.table;
+      ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_READ);
+      e = launch_paged_expand(p, x, kv->head_dim, bf16, pl.expand_pages, cs);
+    }
     ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_TILES);
-    e = launch_paged_tiles(p, tk, tv, tq, kv->head_dim, bf16, pl.tile_grid, cs);
+    if (e == cudaSuccess) e = launch_paged_tiles(t, held ? xk : tk, held ? xv : tv, tq, kv->head_dim, bf16, pl.tile_grid, cs);
   }
   if (e == cudaSuccess && pl.any_rows) {
     ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_ROWS);

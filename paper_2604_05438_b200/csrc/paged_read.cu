@@ -80,4 +80,78 @@ cudaError_t launch_paged_read(const ReadProblem& p, bool bf16, cudaStream_t st) 
   return bf16 ? launch_pdl(paged_read_kernel<Bf16, 128>, grid, block, 0, st, p) : launch_pdl(paged_read_kernel<Fp16, 128>, grid, block, 0, st, p);
 }
 
+// ---------------------------------------------------------------- for attention of many rows
+// The caches of the sequences with many rows as 16-bit pages of 128 rows in the workspace, [page][head][slot][dim], one
+// sequence's pages behind another's, and a page table of them; codes times powers of two, so nothing is lost.  A CTA takes
+// a page of one KV head.  Rows at or behind a sequence's length and on bad pages become 0.
+template <typename T, int D>
+__global__ void __launch_bounds__(kReadThreads) paged_expand_kernel(const __grid_constant__ PagedProblem p, const __grid_constant__ ExpandProblem x) {
+  constexpr int LPR = D / 16, RPP = kReadThreads / LPR, PASSES = kExpandRows / RPP;
+  __shared__ int s_seq, s_page;
+  const int tid = threadIdx.x, lane = tid & 31, h = blockIdx.y;
+  pdl_wait();
+  pdl_launch_next();
+  if (tid < 32) {
+    int base = 0;
+    if (lane == 0) s_seq = -1;
+    for (int s = 0; s < p.batch; s += 32) {
+      int n = 0;
+      if (s + lane < p.batch && (long long)paged_q_len(p, s + lane) * p.group > p.rows_limit) n = (paged_kv_len(p, s + lane) + kExpandRows - 1) / kExpandRows;
+      const int incl = warp_inclusive_scan(n) + base;
+      if (incl > (int)blockIdx.x && incl - n <= (int)blockIdx.x) {           // one lane
+        s_seq = s + lane;
+        s_page = blockIdx.x - (incl - n);
+      }
+      base = __shfl_sync(0xffffffffu, incl, 31);
+      if (base > (int)blockIdx.x) break;
+    }
+  }
+  __syncthreads();
+  const int b = s_seq;
+  if (b < 0) return;                           // (a replay with shorter lengths)
+  const int l = tid % LPR, ps = 1 << p.page_shift, len = paged_kv_len(p, b);
+  if (h == 0 && tid == 0) x.table[(size_t)b * x.max_pages + s_page] = blockIdx.x;
+  uint4 kw[PASSES], vw[PASSES];
+  uint32_t ke[PASSES], ve[PASSES];
+#pragma unroll
+  for (int i = 0; i < PASSES; ++i) {
+    kw[i] = vw[i] = make_uint4(0, 0, 0, 0);
+    ke[i] = ve[i] = 0;
+    const int pos = s_page * kExpandRows + i * RPP + tid / LPR;
+    if (pos >= len) continue;
+    const int page = __ldg(p.table + (size_t)b * p.max_pages + (pos >> p.page_shift));
+    if (page < 0 || page >= p.n_pages) {
+      if (l == 0) atomicExch(p.status, kStatusBadPage);
+      continue;
+    }
+    const int slot = pos & (ps - 1);
+    const size_t at = (size_t)page * x.stride_page + (size_t)h * x.stride_head + (size_t)slot * x.stride_token;
+    const size_t scale_at = ((size_t)page * p.hkv + h) * ps + slot;
+    kw[i] = __ldg(reinterpret_cast<const uint4*>(x.k + at) + l);
+    vw[i] = __ldg(reinterpret_cast<const uint4*>(x.v + at) + l);
+    ke[i] = __ldg(x.held.k_scales + scale_at);
+    ve[i] = __ldg(x.held.v_scales + scale_at);
+  }
+  const size_t out = ((size_t)blockIdx.x * p.hkv + h) * kExpandRows;
+#pragma unroll
+  for (int i = 0; i < PASSES; ++i) {
+    auto put = [&](void* to, const uint4& w, uint32_t e) {
+      const float s = held_scale(e);
+      const uint2 a = held_values<T>(w.x, s), c = held_values<T>(w.y, s), d = held_values<T>(w.z, s), f = held_values<T>(w.w, s);
+      uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(to) + (out + i * RPP + tid / LPR) * D + l * 16);
+      o[0] = make_uint4(a.x, a.y, c.x, c.y);
+      o[1] = make_uint4(d.x, d.y, f.x, f.y);
+    };
+    put(x.k_out, kw[i], ke[i]);
+    put(x.v_out, vw[i], ve[i]);
+  }
+}
+
+cudaError_t launch_paged_expand(const PagedProblem& p, const ExpandProblem& x, int d, bool bf16, int pages, cudaStream_t st) {
+  const dim3 grid(pages, p.hkv), block(kReadThreads);
+  if (d == 64)
+    return bf16 ? launch_pdl(paged_expand_kernel<Bf16, 64>, grid, block, 0, st, p, x) : launch_pdl(paged_expand_kernel<Fp16, 64>, grid, block, 0, st, p, x);
+  return bf16 ? launch_pdl(paged_expand_kernel<Bf16, 128>, grid, block, 0, st, p, x) : launch_pdl(paged_expand_kernel<Fp16, 128>, grid, block, 0, st, p, x);
+}
+
 }  // namespace tkphi
