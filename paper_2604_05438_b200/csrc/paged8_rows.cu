@@ -18,6 +18,8 @@
 //   - a warp takes 32 keys of a tile with a running softmax of its own; rows are rescaled only when a maximum moved.
 // Probabilities are scaled by 2^14 (the largest is then 2^14 or less: fp16 has few exponents) and rounded to fp16: bf16
 // outputs take that single rounding, an eighth of the output's own; fp16 ones enter as hi + lo pairs of numbers, 2^-22.
+#include <type_traits>
+
 #include "held8.cuh"
 #include "paged_walk.cuh"
 
@@ -27,17 +29,19 @@ template <int D, bool SPLIT>
 struct HeldRowCfg {
   static constexpr int WARPS = SPLIT ? 8 : 4;               // (cluster form: four warps for the even, four for the odd tiles)
   static constexpr int THREADS = (WARPS + 1) * 32;
-  static constexpr int CTAS = SPLIT ? 1 : 2;                // per multiprocessor
+  static constexpr int CTAS = SPLIT ? 1 : D == 64 ? 3 : 2;  // per multiprocessor
   static constexpr int TILE = kHeldKeys * D;                // codes of a tile's keys or values
   static constexpr int STAGE = 2 * TILE;
-  static constexpr int NS = (D == 128 ? 3 : 6) * (SPLIT ? 2 : 1) - (SPLIT && D == 128 ? 1 : 0);
+  static constexpr int NS = D == 128 ? (SPLIT ? 5 : 3) : (SPLIT ? 10 : 3);
   static constexpr size_t scales = (size_t)NS * STAGE;      // [NS][2][128] scale bytes
-  static constexpr size_t red = scales + NS * 2 * kHeldKeys;        // [warps][16 rows][32 dims] fp32
+  static constexpr size_t frags = scales + NS * 2 * kHeldKeys;      // [D / 16][32 lanes] queries as the lanes take them
+  static constexpr size_t red = frags + D * kRowTile * 2;           // [warps][16 rows][32 dims] fp32
   static constexpr size_t stat = red + WARPS * kRowTile * 32 * 4;   // [warps][16][2]
   static constexpr size_t bars = stat + WARPS * kRowTile * 2 * 4;
   static constexpr size_t total = bars + (2 * NS) * 8 + 16;
   static constexpr size_t keep = 0;                         // cluster form: this CTA's piece, over the ring's first tiles
   static_assert(kRowTile * (D + 2) * 4 <= NS * STAGE, "piece");
+  static_assert(CTAS * (total + 1024) <= 228 * 1024, "shared memory of a multiprocessor");
 };
 
 // Place of 16-byte chunk `chunk` of a row in a tile of rows of D bytes, as the TMA box with the swizzle of that width lies.
@@ -58,6 +62,7 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   constexpr float kShift = 14.f;                            // p = 2^kShift exp2(..)
   constexpr bool kPairs = !T::kBf16;
   extern __shared__ __align__(1024) unsigned char smem[];
+  uint4* q_frags = reinterpret_cast<uint4*>(smem + C::frags);
   float* red = reinterpret_cast<float*>(smem + C::red);
   float* stat = reinterpret_cast<float*>(smem + C::stat);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::bars);
@@ -148,8 +153,8 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     bool ok = true;
     int it = 0;
     while (w.next()) {
-      // ---- the unit's queries as A operands.  Operand columns 2j, 2j+1, 2j+8, 2j+9 of a group of 16 are dims 4j .. 4j+3.
-      uint32_t qf[D / 16][4];
+      // ---- the unit's queries as A operands in fp16.  Operand columns 2j, 2j+1, 2j+8, 2j+9 of a group of 16 are dims 4j .. 4j+3.
+      // They lie in shared memory, as a lane of each warp takes them: 2 or 4 KB that registers have no room for.
       float slA = p.scale_log2, slB = p.scale_log2;          // log2 units per unit of (operand q).(codes) * key scale
       {
         const uint2* qa = nullptr;
@@ -163,41 +168,44 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           const int r = w.r_first + rB;
           qb = q + ((size_t)(w.tok0 + r / p.group) * p.hq + w.h * p.group + r % p.group) * (D / 4);
         }
+        uint2 x[D / 16][2];                                  // [group of 16 dims][row]
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          const uint2 a = qa ? __ldg(qa + k * 4 + cj) : make_uint2(0, 0), b = qb ? __ldg(qb + k * 4 + cj) : make_uint2(0, 0);
-          qf[k][0] = a.x; qf[k][1] = b.x; qf[k][2] = a.y; qf[k][3] = b.y;
+          x[k][0] = qa ? __ldg(qa + k * 4 + cj) : make_uint2(0, 0);
+          x[k][1] = qb ? __ldg(qb + k * 4 + cj) : make_uint2(0, 0);
         }
+        float f[2] = {1.f, 1.f};
         if (T::kBf16) {
-          uint32_t mA = 0, mB = 0;                           // largest finite magnitudes (upper halves of their bits)
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k)
+          for (int r = 0; r < 2; ++r) {
+            float most = 0.f;                                // the largest finite magnitude
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int k = 0; k < D / 16; ++k)
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const uint32_t b = (e ? qf[k][i] >> 16 : qf[k][i]) & 0x7fffu;
-                if (b < 0x7f80u) { if (i & 1) mB = max(mB, b); else mA = max(mA, b); }
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t w = i < 2 ? x[k][r].x : x[k][r].y;
+                const float v = fabsf(i & 1 ? T::hi(w) : T::lo(w));
+                if (v < INFINITY) most = fmaxf(most, v);
               }
 #pragma unroll
-          for (int d = 1; d < 4; d <<= 1) {
-            mA = max(mA, __shfl_xor_sync(0xffffffffu, mA, d));
-            mB = max(mB, __shfl_xor_sync(0xffffffffu, mB, d));
+            for (int d = 1; d < 4; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+            // the largest goes to [2^14, 2^15); the exponent that is taken off is at least -100
+            const int e = max((int)(__float_as_uint(most) >> 23) - 127 - 14, -100);
+            f[r] = __uint_as_float((uint32_t)(127 - e) << 23);
+            (r ? slB : slA) *= __uint_as_float((uint32_t)(127 + e) << 23);
           }
-          // the largest goes to [2^14, 2^15); the exponent that is taken off is at least -100
-          const int eA = max((int)(mA >> 7) - 127 - 14, -100), eB = max((int)(mB >> 7) - 127 - 14, -100);
-          const float fA = __uint_as_float((uint32_t)(127 - eA) << 23), fB = __uint_as_float((uint32_t)(127 - eB) << 23);
+        }
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float f = i & 1 ? fB : fA;
-              qf[k][i] = Fp16::pack(T::lo(qf[k][i]) * f, T::hi(qf[k][i]) * f);
-            }
-          slA *= __uint_as_float((uint32_t)(127 + eA) << 23);
-          slB *= __uint_as_float((uint32_t)(127 + eB) << 23);
+        for (int k = 0; k < D / 16; ++k) {
+          if (k % WARPS != warp) continue;                   // the warps share the work
+          uint4 v = make_uint4(x[k][0].x, x[k][1].x, x[k][0].y, x[k][1].y);
+          if (T::kBf16)
+            v = make_uint4(Fp16::pack(T::lo(v.x) * f[0], T::hi(v.x) * f[0]), Fp16::pack(T::lo(v.y) * f[1], T::hi(v.y) * f[1]),
+                           Fp16::pack(T::lo(v.z) * f[0], T::hi(v.z) * f[0]), Fp16::pack(T::lo(v.w) * f[1], T::hi(v.w) * f[1]));
+          q_frags[k * 32 + lane] = v;
         }
       }
+      named_barrier(1, WARPS * 32);
       // last visible position of this thread's rows; -1: no such row
       int limA = -1, limB = -1;
       if (rA < w.rows) limA = BLOCK ? w.pos0 : p.causal ? w.pos0 + (w.r_first + rA) / p.group : w.len - 1;
@@ -234,48 +242,59 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             else key0[x] = w.len;                                                // past the list
           }
         }
-        if (key0[0] <= lim_last || key0[1] <= lim_last) {
-          const bool careful = key0[0] + 15 > lim_all || key0[1] + 15 > lim_all;
+        // (two copies: with keys that some row does not see, and without any)
+        auto step = [&](auto tag) {
+          constexpr bool careful = decltype(tag)::value;
           bool odd_values = false;                          // NaN codes that not every row sees
           float s[4][4];
+          // Scores of group x in s[2x], s[2x+1]: column 2j + e of s[2x + n] is key 4j + 2n + e of the group, so that a thread's
+          // four keys lie beside each other.
 #pragma unroll
-          for (int n = 0; n < 4; ++n) { s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f; }
+          for (int n = 0; n < 4; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+          const int kr = lane & 7, krow = kg + ((kr >> 1) << 2) + ((lane >> 4) << 1) + (kr & 1), ksub = (lane >> 3) & 1;
+          const uint32_t k_at[2] = {smem_u32(ks) + held_at<D>(krow, ksub), smem_u32(ks) + held_at<D>(krow + 16, ksub)};
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const int row = kg + x * 16 + ((lane >> 4) << 3) + (lane & 7), sub = (lane >> 3) & 1;
+          for (int k = 0; k < D / 32; ++k) {
+            uint32_t b0[2][4], b1[2][4];                    // words: (n = 0, dims 0-15), (0, 16-31), (1, 0-15), (1, 16-31)
 #pragma unroll
-            for (int k = 0; k < D / 32; ++k) {
-              uint32_t c[4], b0[4], b1[4];
-              ldmatrix_x4(c, smem_u32(ks) + held_at<D>(row, 2 * k + sub));
+            for (int x = 0; x < 2; ++x) {
+              uint32_t c[4];
+              ldmatrix_x4(c, k_at[x] ^ (k << 5));
 #pragma unroll
-              for (int i = 0; i < 4; ++i) unpack_codes(c[i], b0[i], b1[i]);
-              Fp16::mma(s[2 * x], qf[2 * k], b0[0], b1[0]);
-              Fp16::mma(s[2 * x], qf[2 * k + 1], b0[1], b1[1]);
-              Fp16::mma(s[2 * x + 1], qf[2 * k], b0[2], b1[2]);
-              Fp16::mma(s[2 * x + 1], qf[2 * k + 1], b0[3], b1[3]);
+              for (int i = 0; i < 4; ++i) unpack_codes(c[i], b0[x][i], b1[x][i]);
+            }
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              const uint4 q4 = q_frags[(2 * k + y) * 32 + lane];
+              const uint32_t qf[4] = {q4.x, q4.y, q4.z, q4.w};
+#pragma unroll
+              for (int n = 0; n < 4; ++n) Fp16::mma(s[n], qf, b0[n >> 1][2 * (n & 1) + y], b1[n >> 1][2 * (n & 1) + y]);
             }
           }
-          // scale bytes of this thread's keys: 8 n + 2 j, + 1
-          uint32_t vb[8];
-          uint32_t most = 0;
+          // this thread's keys: scale bytes of four at a time
+          uint32_t vw[2];
 #pragma unroll
-          for (int n = 0; n < 4; ++n) {
-            const uint32_t a = *reinterpret_cast<const uint16_t*>(ke + n * 8 + cc), b = *reinterpret_cast<const uint16_t*>(ve + n * 8 + cc);
-            const float f0 = held_scale(a & 255u), f1 = held_scale(a >> 8);
-            s[n][0] *= f0; s[n][2] *= f0;
-            s[n][1] *= f1; s[n][3] *= f1;
-            vb[2 * n] = b & 255u;
-            vb[2 * n + 1] = b >> 8;
+          for (int x = 0; x < 2; ++x) {
+            const uint32_t kw = *reinterpret_cast<const uint32_t*>(ke + x * 16 + 4 * cj);
+            vw[x] = *reinterpret_cast<const uint32_t*>(ve + x * 16 + 4 * cj);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              // (byte 255 gives infinity here, less itself no number; byte 0 gives 0 for 2^-127)
+              const float f = __uint_as_float((i == 3 ? kw >> 1 : kw << (23 - 8 * i)) & 0x7f800000u), z = f - f;
+              float (&a)[4] = s[2 * x + (i >> 1)];
+              a[i & 1] = fmaf(a[i & 1], f, z);
+              a[2 + (i & 1)] = fmaf(a[2 + (i & 1)], f, z);
+            }
           }
           if (careful) {
 #pragma unroll
-            for (int n = 0; n < 4; ++n)
+            for (int x = 0; x < 2; ++x)
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const int key = key0[n >> 1] + (n & 1) * 8 + cc + e;
-                if (key > limA) s[n][e] = -INFINITY;
-                if (key > limB) s[n][2 + e] = -INFINITY;
-                if (key > lim_last) vb[2 * n + e] = 0;
+              for (int i = 0; i < 4; ++i) {
+                const int key = key0[x] + 4 * cj + i;
+                if (key > limA) s[2 * x + (i >> 1)][i & 1] = -INFINITY;
+                if (key > limB) s[2 * x + (i >> 1)][2 + (i & 1)] = -INFINITY;
+                if (key > lim_last) vw[x] &= ~(0xffu << (8 * i));
               }
             // Values that no row sees may be anything (behind the sequence's end they may be left-overs): 0 times them must
             // not reach the product.  Those that some rows see are looked through.
@@ -297,16 +316,21 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
               odd_values = __any_sync(0xffffffffu, bad != 0);
             }
           }
-          // the largest value scale so far; the outputs follow when it grows
-#pragma unroll
-          for (int i = 0; i < 8; ++i) most = max(most, vb[i]);
-          most = __reduce_max_sync(0xffffffffu, most);
+          // the largest value scale so far; the outputs follow when it grows.  Bytes as pairs of 16 bits, keys 0, 2 and 1, 3.
+          uint32_t v2[4] = {vw[0] & 0x00ff00ffu, vw[0] >> 8 & 0x00ff00ffu, vw[1] & 0x00ff00ffu, vw[1] >> 8 & 0x00ff00ffu};
+          auto largest = [&]() {
+            const uint32_t m = __vmaxu2(__vmaxu2(v2[0], v2[1]), __vmaxu2(v2[2], v2[3]));
+            return __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
+          };
+          uint32_t most = largest();
           const bool bad_scale = most == 255u;
           if (bad_scale) {
-            most = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) most = max(most, vb[i] == 255u ? 0u : vb[i]);
-            most = __reduce_max_sync(0xffffffffu, most);
+            for (int i = 0; i < 4; ++i) {
+              if ((v2[i] & 0xffffu) == 255u) v2[i] &= 0xffff0000u;
+              if (v2[i] >> 16 == 255u) v2[i] &= 0xffffu;
+            }
+            most = largest();
           }
           if ((int)most > top) {
             const int d = 127 + top - (int)most;
@@ -315,6 +339,10 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             for (int n = 0; n < D / 8; ++n) { o[n][0] *= f; o[n][1] *= f; o[n][2] *= f; o[n][3] *= f; }
             top = (int)most;
           }
+          // exponent fields of the values' scales over the largest: 127 + byte - top, 0 if that is less
+          const uint32_t least = (uint32_t)max(top - 127, 0) * 0x00010001u, shift = (uint32_t)(127 - top) * 0x00010001u;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v2[i] = __vmaxu2(v2[i], least) + shift;
           float tA = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1])), tB = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
           tA = fmaxf(tA, fmaxf(fmaxf(s[2][0], s[2][1]), fmaxf(s[3][0], s[3][1])));
           tB = fmaxf(tB, fmaxf(fmaxf(s[2][2], s[2][3]), fmaxf(s[3][2], s[3][3])));
@@ -335,25 +363,33 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           // a row that has seen nothing yet: every term exp2(-inf - 0) = 0
           const float uA = mA == -INFINITY ? 0.f : mA, uB = mB == -INFINITY ? 0.f : mB;
 #pragma unroll
-          for (int n = 0; n < 4; ++n)
+          for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const float a = ex2_approx(fmaf(s[n][e] - uA, slA, kShift)), b = ex2_approx(fmaf(s[n][2 + e] - uB, slB, kShift));
+            for (int i = 0; i < 4; ++i) {
+              float& sa = s[2 * x + (i >> 1)][i & 1];
+              float& sb = s[2 * x + (i >> 1)][2 + (i & 1)];
+              const float a = ex2_approx(fmaf(sa - uA, slA, kShift)), b = ex2_approx(fmaf(sb - uB, slB, kShift));
               lA += a;
               lB += b;
-              // times the value's scale over the largest
-              const int d = 127 + (int)vb[2 * n + e] - top;
-              float f = d > 0 ? __uint_as_float((uint32_t)d << 23) : 0.f;
-              if (bad_scale && vb[2 * n + e] == 255u) f = __uint_as_float(0x7fc00000u);
-              s[n][e] = a * f;
-              s[n][2 + e] = b * f;
-              if (careful) {                                 // (a scale that is no number times a probability 0)
-                const int key = key0[n >> 1] + (n & 1) * 8 + cc + e;
-                if (key > limA) s[n][e] = 0.f;
-                if (key > limB) s[n][2 + e] = 0.f;
-              }
+              const uint32_t e = v2[2 * x + (i & 1)];
+              const float f = __uint_as_float(i < 2 ? e << 23 : e << 7 & 0x7f800000u);
+              sa = a * f;
+              sb = b * f;
             }
-          if (!BLOCK && odd_values) {
+          if (bad_scale || careful) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                float& sa = s[2 * x + (i >> 1)][i & 1];
+                float& sb = s[2 * x + (i >> 1)][2 + (i & 1)];
+                const int key = key0[x] + 4 * cj + i;
+                if ((vw[x] >> (8 * i) & 255u) == 255u) sa = sb = __uint_as_float(0x7fc00000u);
+                if (key > limA) sa = 0.f;                    // (unseen, whatever its scale)
+                if (key > limB) sb = 0.f;
+              }
+          }
+          if (careful && !BLOCK && odd_values) {
             // added to the rows that see them, and taken out of the product, where 0 times them would reach the others
             const float none = __uint_as_float(0x7fc00000u);
 #pragma unroll 1
@@ -386,12 +422,13 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
               ph[j] = Fp16::pack(u, v);
               if (kPairs) pl[j] = Fp16::pack(u - Fp16::lo(ph[j]), v - Fp16::hi(ph[j]));
             }
-            const int row = kg + x * 16 + (((lane >> 3) & 1) << 3) + (lane & 7), sub = lane >> 4;
+            const int r = lane & 7, row = kg + x * 16 + ((r >> 1) << 2) + (((lane >> 3) & 1) << 1) + (r & 1);
+            const uint32_t v_at = smem_u32(vs) + held_at<D>(row, lane >> 4);
 #pragma unroll
             for (int n = 0; n < D / 32; ++n) {
-              uint32_t c[4], b0[4], b1[4];                   // c: (keys 0-7, dims 0-15), (8-15, 0-15), (0-7, 16-31), (8-15, 16-31)
-              ldmatrix_x4_trans(c, smem_u32(vs) + held_at<D>(row, 2 * n + sub));
-              // a word: key 2j's dims 2g, 2g+1, then key 2j+1's; the two keys of a dim beside each other
+              uint32_t c[4], b0[4], b1[4];                   // c: (columns 0-7, dims 0-15), (8-15, 0-15), (0-7, 16-31), (8-15, 16-31)
+              ldmatrix_x4_trans(c, v_at ^ (n << 5));
+              // a word: column 2j's dims 2g, 2g+1, then column 2j+1's; the two keys of a dim beside each other
 #pragma unroll
               for (int i = 0; i < 4; ++i) unpack_codes(__byte_perm(c[i], 0, 0x3120), b0[i], b1[i]);
 #pragma unroll
@@ -405,7 +442,9 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
               }
             }
           }
-        }
+        };
+        if (key0[0] + 15 <= lim_all && key0[1] + 15 <= lim_all) step(std::false_type());
+        else if (key0[0] <= lim_last || key0[1] <= lim_last) step(std::true_type());
         __syncwarp();
         if (lane == 0) mbar_arrive(&empty[stage]);
       }
