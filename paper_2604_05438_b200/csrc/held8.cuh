@@ -89,9 +89,9 @@ struct ExpandProblem {
 cudaError_t launch_paged_expand(const PagedProblem& p, const ExpandProblem& x, int d, bool bf16, int pages, cudaStream_t st);
 
 constexpr int kHeldKeys = 128;               // keys of one tile of the row kernel
-int paged8_row_ctas(int d);                  // its CTAs per multiprocessor where units are dealt out as a line
+int paged8_row_ctas(int d, int max_rows);    // its CTAs per multiprocessor where units are dealt out as a line
 cudaError_t launch_paged8_rows(const PagedProblem& p, const HeldCache& held, const CUtensorMap& tk, const CUtensorMap& tv, int d,
-                               bool bf16, bool block, bool split, int grid, cudaStream_t st);
+                               bool bf16, bool block, bool split, int max_rows, int grid, cudaStream_t st);
 cudaError_t launch_paged8_rows_merge(const PagedProblem& p, int d, bool bf16, bool block, int units, int max_rows, cudaStream_t st);
 
 }  // namespace tkphi

@@ -1,23 +1,28 @@
-// Attention of few query rows over an 8-bit paged cache: sequences with at most 16 rows (tokens x query heads of a KV head),
+// Attention of few query rows over an 8-bit paged cache: sequences with at most 64 rows (tokens x query heads of a KV head),
 // and the page-selected form, where every token of a KV head reads a page list of its own.
 //
 //   y = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale * q.k_t - m),  lse = m + log sum_t p_t   over the visible keys t
 //   k_t = a_t * (its codes),  v_t = b_t * (its codes),  a_t and b_t powers of two
 //
 // in one pass with the running maximum m and sum.  Work is dealt out and joined as over a 16-bit cache (paged_walk.cuh), in
-// tiles of 128 keys.  Bound: memory, 2 * (head_dim + 1) bytes per key against 16 rows of work; with half the bytes of a
-// 16-bit cache the instructions per key count, too.  So:
-//   - both products run as fp16 products of the codes, which fp16 holds exactly: one conversion instruction per two codes.
-//     The dims of a code word are dealt to the operand's registers in the order in which the conversion leaves them, and the
-//     queries (first product) and outputs (second) are laid out to match, so that nothing is rearranged but one byte
-//     permutation per word of values.
+// tiles of 128 keys.  Bound: memory, 2 * (head_dim + 1) bytes per key against 8 or 16 rows of work; with half the bytes of a
+// 16-bit cache the instructions per key count as much.  So:
+//   - both products have the keys or dims of the cache as the 16 rows of the matrix instruction and 8 query rows as its
+//     columns (S^T = K Q^T, O^T = V^T P^T), once or twice: a single token of a group of up to 8 heads pays for 8 rows, where
+//     queries as the instruction's rows would pay for 16, in products, exponentials and registers.  P^T changes from
+//     accumulator to operand by a transpose of 8 x 8 blocks between lanes.
+//   - the products are fp16 products of the codes, which fp16 holds exactly: one conversion instruction per two codes.  The
+//     dims of a code word are dealt to the operand's registers in the order in which the conversion leaves them, and queries
+//     and outputs are laid out to match, so that nothing is rearranged but one byte permutation per word of values.
+//     (e4m3 instructions for the first product, with queries as sums of two or three codes, need no conversion of keys, but
+//     took 1.2x the time: they issue as more instructions.)
 //   - a key's power of two multiplies its score; a value's multiplies its probability, relative to the largest of the
 //     values that the warp has met (the outputs are rescaled when that grows), so that the fp16 operand stays in range.
 //   - bf16 queries are brought into fp16's range by a power of two per row, which the softmax scale takes back; elements
 //     below 2^-39 of the row's largest vanish.
 //   - a warp takes 32 keys of a tile with a running softmax of its own; rows are rescaled only when a maximum moved.
-// Probabilities are scaled by 2^14 (the largest is then 2^14 or less: fp16 has few exponents) and rounded to fp16: bf16
-// outputs take that single rounding, an eighth of the output's own; fp16 ones enter as hi + lo pairs of numbers, 2^-22.
+// Probabilities are scaled by 2^14 (the largest is then 2^14 or less: fp16 has few exponents) and rounded to fp16 once, 2^-12:
+// an eighth of a bf16 output's own rounding, as much as an fp16 one's.
 #include <type_traits>
 
 #include "held8.cuh"
@@ -25,8 +30,9 @@
 
 namespace tkphi {
 
-template <int D, bool SPLIT>
+template <int D, bool SPLIT, int NT>
 struct HeldRowCfg {
+  static constexpr int ROWS = 8 * NT;                       // query rows of a unit, at most
   static constexpr int WARPS = SPLIT ? 8 : 4;               // (cluster form: four warps for the even, four for the odd tiles)
   static constexpr int THREADS = (WARPS + 1) * 32;
   static constexpr int CTAS = SPLIT ? 1 : D == 64 ? 3 : 2;  // per multiprocessor
@@ -34,10 +40,11 @@ struct HeldRowCfg {
   static constexpr int STAGE = 2 * TILE;
   static constexpr int NS = D == 128 ? (SPLIT ? 5 : 3) : (SPLIT ? 10 : 3);
   static constexpr size_t scales = (size_t)NS * STAGE;      // [NS][2][128] scale bytes
-  static constexpr size_t frags = scales + NS * 2 * kHeldKeys;      // [D / 16][32 lanes] queries as the lanes take them
-  static constexpr size_t red = frags + D * kRowTile * 2;           // [warps][16 rows][32 dims] fp32
-  static constexpr size_t stat = red + WARPS * kRowTile * 32 * 4;   // [warps][16][2]
-  static constexpr size_t bars = stat + WARPS * kRowTile * 2 * 4;
+  static constexpr size_t frags = scales + NS * 2 * kHeldKeys;      // [D / 16][32 lanes][NT] queries as the lanes take them
+  static constexpr int CHUNK = 512 / ROWS;                  // dims of a row that are joined at a time
+  static constexpr size_t red = frags + D * ROWS * 2;       // [warps][ROWS][CHUNK] fp32
+  static constexpr size_t stat = red + WARPS * ROWS * CHUNK * 4;    // [warps][ROWS][2]
+  static constexpr size_t bars = stat + WARPS * ROWS * 2 * 4;
   static constexpr size_t total = bars + (2 * NS) * 8 + 16;
   static constexpr size_t keep = 0;                         // cluster form: this CTA's piece, over the ring's first tiles
   static_assert(kRowTile * (D + 2) * 4 <= NS * STAGE, "piece");
@@ -49,20 +56,25 @@ template <int D>
 __device__ __forceinline__ uint32_t held_at(uint32_t row, uint32_t chunk) {
   return D == 128 ? swz128(row, chunk) : row * 64u + ((chunk ^ ((row >> 1) & 3u)) << 4);
 }
+// Transpose of an 8 x 8 matrix of 16-bit elements: lane (g, j) gives elements (g, 2j), (g, 2j + 1) and gets (2j, g), (2j + 1, g).
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t a) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
 // The high bits of the bytes that are NaN codes.
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
-template <typename T, int D, bool BLOCK, bool SPLIT>
-__global__ void __launch_bounds__(HeldRowCfg<D, SPLIT>::THREADS, HeldRowCfg<D, SPLIT>::CTAS)
+template <typename T, int D, bool BLOCK, bool SPLIT, int NT>
+__global__ void __launch_bounds__(HeldRowCfg<D, SPLIT, NT>::THREADS, HeldRowCfg<D, SPLIT, NT>::CTAS)
 paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                    const __grid_constant__ PagedProblem p, const __grid_constant__ HeldCache held) {
-  using C = HeldRowCfg<D, SPLIT>;
+  using C = HeldRowCfg<D, SPLIT, NT>;
   using Walk = RowWalk<BLOCK, SPLIT, kHeldKeys>;
-  constexpr int WARPS = C::WARPS, NS = C::NS;
+  constexpr int WARPS = C::WARPS, NS = C::NS, ROWS = C::ROWS;
   constexpr float kShift = 14.f;                            // p = 2^kShift exp2(..)
-  constexpr bool kPairs = !T::kBf16;
   extern __shared__ __align__(1024) unsigned char smem[];
-  uint4* q_frags = reinterpret_cast<uint4*>(smem + C::frags);
+  uint2* q_frags = reinterpret_cast<uint2*>(smem + C::frags);
   float* red = reinterpret_cast<float*>(smem + C::red);
   float* stat = reinterpret_cast<float*>(smem + C::stat);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::bars);
@@ -148,79 +160,78 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     // ================================================================ compute
     Walk w(p, cta);
     const int ps = 1 << p.page_shift;
-    const int rA = lane >> 2, rB = rA + 8, cj = lane & 3, cc = 2 * cj;
+    const int g = lane >> 2, j = lane & 3;                   // query rows of this thread: 8 t + 2 j + i, i = 0, 1
     const int kg = (warp & 3) * 32;                          // this warp's keys of a tile
+    // the key row and the piece of it that this lane gives to ldmatrix, of the first group of 16 keys: even keys, odd ones
+    const int frag_row = kg + 2 * (lane & 7) + ((lane >> 3) & 1), frag_piece = lane >> 4;
     bool ok = true;
     int it = 0;
     while (w.next()) {
-      // ---- the unit's queries as A operands in fp16.  Operand columns 2j, 2j+1, 2j+8, 2j+9 of a group of 16 are dims 4j .. 4j+3.
-      // They lie in shared memory, as a lane of each warp takes them: 2 or 4 KB that registers have no room for.
-      float slA = p.scale_log2, slB = p.scale_log2;          // log2 units per unit of (operand q).(codes) * key scale
-      {
-        const uint2* qa = nullptr;
-        const uint2* qb = nullptr;
-        const uint2* q = static_cast<const uint2*>(p.q);
-        if (rA < w.rows) {
-          const int r = w.r_first + rA;
-          qa = q + ((size_t)(w.tok0 + r / p.group) * p.hq + w.h * p.group + r % p.group) * (D / 4);
-        }
-        if (rB < w.rows) {
-          const int r = w.r_first + rB;
-          qb = q + ((size_t)(w.tok0 + r / p.group) * p.hq + w.h * p.group + r % p.group) * (D / 4);
-        }
-        uint2 x[D / 16][2];                                  // [group of 16 dims][row]
+      // ---- the unit's queries as operands in fp16.  Operand rows 2j, 2j+1, 2j+8, 2j+9 of a group of 16 dims are dims 4j .. 4j+3.
+      // They lie in shared memory, as a lane of each warp takes them.
+      float sl[NT][2];                                       // log2 units per unit of (operand q).(codes) * key scale
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          x[k][0] = qa ? __ldg(qa + k * 4 + cj) : make_uint2(0, 0);
-          x[k][1] = qb ? __ldg(qb + k * 4 + cj) : make_uint2(0, 0);
-        }
-        float f[2] = {1.f, 1.f};
+      for (int t = 0; t < NT; ++t) {
+        const int r = w.r_first + 8 * t + g;
+        uint2 x[D / 16];
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+          x[k] = 8 * t + g < w.rows
+                     ? __ldg(static_cast<const uint2*>(p.q) + ((size_t)(w.tok0 + r / p.group) * p.hq + w.h * p.group + r % p.group) * (D / 4) + k * 4 + j)
+                     : make_uint2(0, 0);
+        float f = 1.f, back = p.scale_log2;
         if (T::kBf16) {
+          float most = 0.f;                                  // the largest finite magnitude
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            float most = 0.f;                                // the largest finite magnitude
+          for (int k = 0; k < D / 16; ++k)
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k)
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t u = i < 2 ? x[k].x : x[k].y;
+              const float v = fabsf(i & 1 ? T::hi(u) : T::lo(u));
+              if (v < INFINITY) most = fmaxf(most, v);
+            }
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const uint32_t w = i < 2 ? x[k][r].x : x[k][r].y;
-                const float v = fabsf(i & 1 ? T::hi(w) : T::lo(w));
-                if (v < INFINITY) most = fmaxf(most, v);
-              }
-#pragma unroll
-            for (int d = 1; d < 4; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-            // the largest goes to [2^14, 2^15); the exponent that is taken off is at least -100
-            const int e = max((int)(__float_as_uint(most) >> 23) - 127 - 14, -100);
-            f[r] = __uint_as_float((uint32_t)(127 - e) << 23);
-            (r ? slB : slA) *= __uint_as_float((uint32_t)(127 + e) << 23);
-          }
+          for (int d = 1; d < 4; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+          // the largest goes to [2^14, 2^15); the exponent that is taken off is at least -100
+          const int e = max((int)(__float_as_uint(most) >> 23) - 127 - 14, -100);
+          f = __uint_as_float((uint32_t)(127 - e) << 23);
+          back *= __uint_as_float((uint32_t)(127 + e) << 23);
         }
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
           if (k % WARPS != warp) continue;                   // the warps share the work
-          uint4 v = make_uint4(x[k][0].x, x[k][1].x, x[k][0].y, x[k][1].y);
-          if (T::kBf16)
-            v = make_uint4(Fp16::pack(T::lo(v.x) * f[0], T::hi(v.x) * f[0]), Fp16::pack(T::lo(v.y) * f[1], T::hi(v.y) * f[1]),
-                           Fp16::pack(T::lo(v.z) * f[0], T::hi(v.z) * f[0]), Fp16::pack(T::lo(v.w) * f[1], T::hi(v.w) * f[1]));
-          q_frags[k * 32 + lane] = v;
+          if (T::kBf16) x[k] = make_uint2(Fp16::pack(T::lo(x[k].x) * f, T::hi(x[k].x) * f), Fp16::pack(T::lo(x[k].y) * f, T::hi(x[k].y) * f));
+          q_frags[(k * 32 + lane) * NT + t] = x[k];
         }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) sl[t][i] = __shfl_sync(0xffffffffu, back, 8 * j + 4 * i);
       }
       named_barrier(1, WARPS * 32);
       // last visible position of this thread's rows; -1: no such row
-      int limA = -1, limB = -1;
-      if (rA < w.rows) limA = BLOCK ? w.pos0 : p.causal ? w.pos0 + (w.r_first + rA) / p.group : w.len - 1;
-      if (rB < w.rows) limB = BLOCK ? w.pos0 : p.causal ? w.pos0 + (w.r_first + rB) / p.group : w.len - 1;
+      int lim[NT][2];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int r = 8 * t + 2 * j + i;
+          lim[t][i] = r >= w.rows ? -1 : BLOCK ? w.pos0 : p.causal ? w.pos0 + (w.r_first + r) / p.group : w.len - 1;
+        }
       // keys up to lim_all are visible to every row of the unit, keys behind lim_last to none
       const int lim_all = BLOCK ? w.pos0 : p.causal ? w.pos0 + w.r_first / p.group : w.len - 1;
       const int lim_last = BLOCK ? w.pos0 : p.causal ? w.pos0 + (w.r_first + w.rows - 1) / p.group : w.len - 1;
-      // outputs: o[2x], o[2x+1] hold dims 16 x + 4 j, + 2 and 16 x + 4 j + 1, + 3 of rows A and B
-      float o[D / 8][4];
+      // outputs: o[t][b][0], [1] are dim 16 b + 2 g of this thread's rows, [2], [3] the dim behind it
+      float o[NT][D / 16][4];
+      float m[NT][2], l[NT][2];
 #pragma unroll
-      for (int n = 0; n < D / 8; ++n) { o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f; }
-      float mA = -INFINITY, mB = -INFINITY, lA = 0.f, lB = 0.f;
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int b = 0; b < D / 16; ++b) { o[t][b][0] = o[t][b][1] = o[t][b][2] = o[t][b][3] = 0.f; }
+        m[t][0] = m[t][1] = -INFINITY;
+        l[t][0] = l[t][1] = 0.f;
+      }
       int top = 0;                                           // the outputs' unit is 2^(top - 127)
 
-      for (int t = w.t0; t < w.t1; ++t, ++it) {
+      for (int tile = w.t0; tile < w.t1; ++tile, ++it) {
         if (SPLIT && (it & 1) != warp >> 2) continue;
         const int stage = it % NS;
         if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&full[stage], (uint32_t)(it / NS) & 1u, s_abort));
@@ -234,7 +245,7 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         int key0[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          key0[x] = t * kHeldKeys + kg + x * 16;
+          key0[x] = tile * kHeldKeys + kg + x * 16;
           if (BLOCK) {
             const int entry = key0[x] >> p.page_shift;
             if (entry < w.n_list - 1) key0[x] = 0 - 16;                          // all visible
@@ -246,55 +257,62 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         auto step = [&](auto tag) {
           constexpr bool careful = decltype(tag)::value;
           bool odd_values = false;                          // NaN codes that not every row sees
-          float s[4][4];
-          // Scores of group x in s[2x], s[2x+1]: column 2j + e of s[2x + n] is key 4j + 2n + e of the group, so that a thread's
-          // four keys lie beside each other.
+          // s[x][t][2 e + i]: key 16 x + 2 g + e of the warp's, row i of this thread's in row tile t
+          float s[2][NT][4];
 #pragma unroll
-          for (int n = 0; n < 4; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
-          const int kr = lane & 7, krow = kg + ((kr >> 1) << 2) + ((lane >> 4) << 1) + (kr & 1), ksub = (lane >> 3) & 1;
-          const uint32_t k_at[2] = {smem_u32(ks) + held_at<D>(krow, ksub), smem_u32(ks) + held_at<D>(krow + 16, ksub)};
+          for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (int k = 0; k < D / 32; ++k) {
-            uint32_t b0[2][4], b1[2][4];                    // words: (n = 0, dims 0-15), (0, 16-31), (1, 0-15), (1, 16-31)
+            for (int t = 0; t < NT; ++t) s[x][t][0] = s[x][t][1] = s[x][t][2] = s[x][t][3] = 0.f;
+          {
+            const uint32_t at[2] = {smem_u32(ks) + held_at<D>(frag_row, frag_piece), smem_u32(ks) + held_at<D>(frag_row + 16, frag_piece)};
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              uint32_t c[4];
-              ldmatrix_x4(c, k_at[x] ^ (k << 5));
+            for (int k = 0; k < D / 32; ++k) {
+              uint32_t a[2][2][4];                          // [x][group of 16 dims]: (even keys, dims 4j, 4j+1), (odd ..), (.., 4j+2, 4j+3)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) unpack_codes(c[i], b0[x][i], b1[x][i]);
-            }
+              for (int x = 0; x < 2; ++x) {
+                uint32_t c[4];                              // (even, dims 0-15), (odd, 0-15), (even, 16-31), (odd, 16-31)
+                ldmatrix_x4(c, at[x] ^ (k << 5));
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              const uint4 q4 = q_frags[(2 * k + y) * 32 + lane];
-              const uint32_t qf[4] = {q4.x, q4.y, q4.z, q4.w};
+                for (int i = 0; i < 4; ++i) unpack_codes(c[i], a[x][i >> 1][i & 1], a[x][i >> 1][2 + (i & 1)]);
+              }
 #pragma unroll
-              for (int n = 0; n < 4; ++n) Fp16::mma(s[n], qf, b0[n >> 1][2 * (n & 1) + y], b1[n >> 1][2 * (n & 1) + y]);
+              for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                  const uint2 q = q_frags[((2 * k + y) * 32 + lane) * NT + t];
+#pragma unroll
+                  for (int x = 0; x < 2; ++x) Fp16::mma(s[x][t], a[x][y], q.x, q.y);
+                }
             }
           }
-          // this thread's keys: scale bytes of four at a time
+          // this thread's keys, two of each group: scale bytes
           uint32_t vw[2];
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const uint32_t kw = *reinterpret_cast<const uint32_t*>(ke + x * 16 + 4 * cj);
-            vw[x] = *reinterpret_cast<const uint32_t*>(ve + x * 16 + 4 * cj);
+            const uint32_t kw = *reinterpret_cast<const uint16_t*>(ke + x * 16 + 2 * g);
+            vw[x] = *reinterpret_cast<const uint16_t*>(ve + x * 16 + 2 * g);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int e = 0; e < 2; ++e) {
               // (byte 255 gives infinity here, less itself no number; byte 0 gives 0 for 2^-127)
-              const float f = __uint_as_float((i == 3 ? kw >> 1 : kw << (23 - 8 * i)) & 0x7f800000u), z = f - f;
-              float (&a)[4] = s[2 * x + (i >> 1)];
-              a[i & 1] = fmaf(a[i & 1], f, z);
-              a[2 + (i & 1)] = fmaf(a[2 + (i & 1)], f, z);
+              const float f = __uint_as_float(kw << (23 - 8 * e) & 0x7f800000u), z = f - f;
+#pragma unroll
+              for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) s[x][t][2 * e + i] = fmaf(s[x][t][2 * e + i], f, z);
             }
           }
           if (careful) {
 #pragma unroll
             for (int x = 0; x < 2; ++x)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int key = key0[x] + 4 * cj + i;
-                if (key > limA) s[2 * x + (i >> 1)][i & 1] = -INFINITY;
-                if (key > limB) s[2 * x + (i >> 1)][2 + (i & 1)] = -INFINITY;
-                if (key > lim_last) vw[x] &= ~(0xffu << (8 * i));
+              for (int e = 0; e < 2; ++e) {
+                const int key = key0[x] + 2 * g + e;
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                  for (int i = 0; i < 2; ++i)
+                    if (key > lim[t][i]) s[x][t][2 * e + i] = -INFINITY;
+                if (key > lim_last) vw[x] &= e ? 0x00ffu : 0xff00u;
               }
             // Values that no row sees may be anything (behind the sequence's end they may be left-overs): 0 times them must
             // not reach the product.  Those that some rows see are looked through.
@@ -316,19 +334,19 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
               odd_values = __any_sync(0xffffffffu, bad != 0);
             }
           }
-          // the largest value scale so far; the outputs follow when it grows.  Bytes as pairs of 16 bits, keys 0, 2 and 1, 3.
-          uint32_t v2[4] = {vw[0] & 0x00ff00ffu, vw[0] >> 8 & 0x00ff00ffu, vw[1] & 0x00ff00ffu, vw[1] >> 8 & 0x00ff00ffu};
+          // the largest value scale so far; the outputs follow when it grows.  Bytes as pairs of 16 bits.
+          uint32_t v2[2] = {__byte_perm(vw[0], 0, 0x4140), __byte_perm(vw[1], 0, 0x4140)};
           auto largest = [&]() {
-            const uint32_t m = __vmaxu2(__vmaxu2(v2[0], v2[1]), __vmaxu2(v2[2], v2[3]));
-            return __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
+            const uint32_t u = __vmaxu2(v2[0], v2[1]);
+            return __reduce_max_sync(0xffffffffu, max(u & 0xffffu, u >> 16));
           };
           uint32_t most = largest();
           const bool bad_scale = most == 255u;
           if (bad_scale) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if ((v2[i] & 0xffffu) == 255u) v2[i] &= 0xffff0000u;
-              if (v2[i] >> 16 == 255u) v2[i] &= 0xffffu;
+            for (int x = 0; x < 2; ++x) {
+              if ((v2[x] & 0xffffu) == 255u) v2[x] &= 0xffff0000u;
+              if (v2[x] >> 16 == 255u) v2[x] &= 0xffffu;
             }
             most = largest();
           }
@@ -336,73 +354,87 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             const int d = 127 + top - (int)most;
             const float f = d > 0 ? __uint_as_float((uint32_t)d << 23) : 0.f;
 #pragma unroll
-            for (int n = 0; n < D / 8; ++n) { o[n][0] *= f; o[n][1] *= f; o[n][2] *= f; o[n][3] *= f; }
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int b = 0; b < D / 16; ++b) { o[t][b][0] *= f; o[t][b][1] *= f; o[t][b][2] *= f; o[t][b][3] *= f; }
             top = (int)most;
           }
           // exponent fields of the values' scales over the largest: 127 + byte - top, 0 if that is less
           const uint32_t least = (uint32_t)max(top - 127, 0) * 0x00010001u, shift = (uint32_t)(127 - top) * 0x00010001u;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v2[i] = __vmaxu2(v2[i], least) + shift;
-          float tA = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1])), tB = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
-          tA = fmaxf(tA, fmaxf(fmaxf(s[2][0], s[2][1]), fmaxf(s[3][0], s[3][1])));
-          tB = fmaxf(tB, fmaxf(fmaxf(s[2][2], s[2][3]), fmaxf(s[3][2], s[3][3])));
+          for (int x = 0; x < 2; ++x) v2[x] = __vmaxu2(v2[x], least) + shift;
+          // maxima over the warp's keys.  (They are kept before the scale: the largest score less the maximum is then exactly 0.)
+          float best[NT][2];
+          bool moved = false;
 #pragma unroll
-          for (int d = 1; d < 4; d <<= 1) {
-            tA = fmaxf(tA, __shfl_xor_sync(0xffffffffu, tA, d));
-            tB = fmaxf(tB, __shfl_xor_sync(0xffffffffu, tB, d));
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              float u = fmaxf(fmaxf(s[0][t][i], s[0][t][2 + i]), fmaxf(s[1][t][i], s[1][t][2 + i]));
+#pragma unroll
+              for (int d = 4; d < 32; d <<= 1) u = fmaxf(u, __shfl_xor_sync(0xffffffffu, u, d));
+              best[t][i] = fmaxf(m[t][i], u);
+              moved |= best[t][i] > m[t][i];
+            }
+          if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const float f = best[t][i] > m[t][i] ? ex2_approx((m[t][i] - best[t][i]) * sl[t][i]) : 1.f;
+                l[t][i] *= f;
+#pragma unroll
+                for (int b = 0; b < D / 16; ++b) { o[t][b][i] *= f; o[t][b][2 + i] *= f; }
+                m[t][i] = best[t][i];
+              }
           }
-          // (maxima are kept before the scale: the largest score less the maximum is then exactly 0)
-          const float nA = fmaxf(mA, tA), nB = fmaxf(mB, tB);
-          if (__any_sync(0xffffffffu, nA > mA || nB > mB)) {
-            const float fA = nA > mA ? ex2_approx((mA - nA) * slA) : 1.f, fB = nB > mB ? ex2_approx((mB - nB) * slB) : 1.f;
-            lA *= fA; lB *= fB;
 #pragma unroll
-            for (int n = 0; n < D / 8; ++n) { o[n][0] *= fA; o[n][1] *= fA; o[n][2] *= fB; o[n][3] *= fB; }
-            mA = nA; mB = nB;
-          }
-          // a row that has seen nothing yet: every term exp2(-inf - 0) = 0
-          const float uA = mA == -INFINITY ? 0.f : mA, uB = mB == -INFINITY ? 0.f : mB;
+          for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int x = 0; x < 2; ++x)
+            for (int i = 0; i < 2; ++i) {
+              // (a row that has seen nothing yet: every term exp2(-inf - 0) = 0)
+              const float u = m[t][i] == -INFINITY ? 0.f : m[t][i];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float& sa = s[2 * x + (i >> 1)][i & 1];
-              float& sb = s[2 * x + (i >> 1)][2 + (i & 1)];
-              const float a = ex2_approx(fmaf(sa - uA, slA, kShift)), b = ex2_approx(fmaf(sb - uB, slB, kShift));
-              lA += a;
-              lB += b;
-              const uint32_t e = v2[2 * x + (i & 1)];
-              const float f = __uint_as_float(i < 2 ? e << 23 : e << 7 & 0x7f800000u);
-              sa = a * f;
-              sb = b * f;
+              for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  float& a = s[x][t][2 * e + i];
+                  a = ex2_approx(fmaf(a - u, sl[t][i], kShift));
+                  l[t][i] += a;
+                  a *= __uint_as_float(e ? v2[x] << 7 & 0x7f800000u : v2[x] << 23);
+                }
             }
           if (bad_scale || careful) {
 #pragma unroll
             for (int x = 0; x < 2; ++x)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                float& sa = s[2 * x + (i >> 1)][i & 1];
-                float& sb = s[2 * x + (i >> 1)][2 + (i & 1)];
-                const int key = key0[x] + 4 * cj + i;
-                if ((vw[x] >> (8 * i) & 255u) == 255u) sa = sb = __uint_as_float(0x7fc00000u);
-                if (key > limA) sa = 0.f;                    // (unseen, whatever its scale)
-                if (key > limB) sb = 0.f;
+              for (int e = 0; e < 2; ++e) {
+                const int key = key0[x] + 2 * g + e;
+                const bool none = (vw[x] >> (8 * e) & 255u) == 255u;
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                  for (int i = 0; i < 2; ++i) {
+                    if (none) s[x][t][2 * e + i] = __uint_as_float(0x7fc00000u);
+                    if (key > lim[t][i]) s[x][t][2 * e + i] = 0.f;       // (unseen, whatever its scale)
+                  }
               }
           }
           if (careful && !BLOCK && odd_values) {
             // added to the rows that see them, and taken out of the product, where 0 times them would reach the others
-            const float none = __uint_as_float(0x7fc00000u);
 #pragma unroll 1
             for (int k = 0; k < 32; ++k) {
               const int key = key0[k >> 4] + (k & 15);
-              const bool a = key <= limA, b = key <= limB;
 #pragma unroll
-              for (int x = 0; x < D / 16; ++x) {
-                const uint32_t c = nan_codes(*reinterpret_cast<const uint32_t*>(vs + held_at<D>(kg + k, x) + 4 * cj));
-                if (c & 0x80u) { if (a) o[2 * x][0] = none; if (b) o[2 * x][2] = none; }
-                if (c & 0x8000u) { if (a) o[2 * x + 1][0] = none; if (b) o[2 * x + 1][2] = none; }
-                if (c & 0x800000u) { if (a) o[2 * x][1] = none; if (b) o[2 * x][3] = none; }
-                if (c >> 31) { if (a) o[2 * x + 1][1] = none; if (b) o[2 * x + 1][3] = none; }
+              for (int b = 0; b < D / 16; ++b) {
+                const uint32_t c = nan_codes(*reinterpret_cast<const uint16_t*>(vs + held_at<D>(kg + k, b) + 2 * g));
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                  for (int i = 0; i < 2; ++i) {
+                    if ((c & 0x80u) && key <= lim[t][i]) o[t][b][i] = __uint_as_float(0x7fc00000u);
+                    if ((c & 0x8000u) && key <= lim[t][i]) o[t][b][2 + i] = __uint_as_float(0x7fc00000u);
+                  }
               }
             }
             __syncwarp();
@@ -415,30 +447,25 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           }
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            uint32_t ph[4], pl[4];
+            uint32_t pt[NT][2];                              // P^T: even keys, odd keys of the group by rows
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {                    // A operand: (row, keys 0-7), (row + 8, 0-7), (row, 8-15), (row + 8, 8-15)
-              const float u = s[2 * x + (j >> 1)][(j & 1) * 2], v = s[2 * x + (j >> 1)][(j & 1) * 2 + 1];
-              ph[j] = Fp16::pack(u, v);
-              if (kPairs) pl[j] = Fp16::pack(u - Fp16::lo(ph[j]), v - Fp16::hi(ph[j]));
+            for (int t = 0; t < NT; ++t) {
+              pt[t][0] = transpose_8x8(Fp16::pack(s[x][t][0], s[x][t][1]));
+              pt[t][1] = transpose_8x8(Fp16::pack(s[x][t][2], s[x][t][3]));
             }
-            const int r = lane & 7, row = kg + x * 16 + ((r >> 1) << 2) + (((lane >> 3) & 1) << 1) + (r & 1);
-            const uint32_t v_at = smem_u32(vs) + held_at<D>(row, lane >> 4);
+            const uint32_t at = smem_u32(vs) + held_at<D>(frag_row + 16 * x, frag_piece);
 #pragma unroll
             for (int n = 0; n < D / 32; ++n) {
-              uint32_t c[4], b0[4], b1[4];                   // c: (columns 0-7, dims 0-15), (8-15, 0-15), (0-7, 16-31), (8-15, 16-31)
-              ldmatrix_x4_trans(c, v_at ^ (n << 5));
-              // a word: column 2j's dims 2g, 2g+1, then column 2j+1's; the two keys of a dim beside each other
-#pragma unroll
-              for (int i = 0; i < 4; ++i) unpack_codes(__byte_perm(c[i], 0, 0x3120), b0[i], b1[i]);
+              uint32_t c[4];                                 // (even keys, dims 0-15), (odd, 0-15), (even, 16-31), (odd, 16-31)
+              ldmatrix_x4_trans(c, at ^ (n << 5));
 #pragma unroll
               for (int y = 0; y < 2; ++y) {
-                Fp16::mma(o[4 * n + 2 * y], ph, b0[2 * y], b0[2 * y + 1]);
-                Fp16::mma(o[4 * n + 2 * y + 1], ph, b1[2 * y], b1[2 * y + 1]);
-                if (kPairs) {
-                  Fp16::mma(o[4 * n + 2 * y], pl, b0[2 * y], b0[2 * y + 1]);
-                  Fp16::mma(o[4 * n + 2 * y + 1], pl, b1[2 * y], b1[2 * y + 1]);
-                }
+                // a word: one key's dims 2g, 2g+1, then the next key's; the two keys of a dim beside each other
+                uint32_t a[4];
+                unpack_codes(__byte_perm(c[2 * y], 0, 0x3120), a[0], a[1]);
+                unpack_codes(__byte_perm(c[2 * y + 1], 0, 0x3120), a[2], a[3]);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) Fp16::mma(o[t][2 * n + y], a, pt[t][0], pt[t][1]);
               }
             }
           }
@@ -449,68 +476,75 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         if (lane == 0) mbar_arrive(&empty[stage]);
       }
 
-      // ---- the warps' softmaxes joined; a thread ends up with PER of 32 dims of one row
-      mA = mA * slA - kShift; mB = mB * slB - kShift;
+      // ---- the warps' softmaxes joined; a thread ends up with PER dims of a chunk of one row
 #pragma unroll
-      for (int d = 1; d < 4; d <<= 1) {
-        lA += __shfl_xor_sync(0xffffffffu, lA, d);
-        lB += __shfl_xor_sync(0xffffffffu, lB, d);
-      }
-      if (cj == 0) {
-        stat[(warp * kRowTile + rA) * 2] = mA; stat[(warp * kRowTile + rA) * 2 + 1] = lA;
-        stat[(warp * kRowTile + rB) * 2] = mB; stat[(warp * kRowTile + rB) * 2 + 1] = lB;
-      }
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          m[t][i] = m[t][i] * sl[t][i] - kShift;
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) l[t][i] += __shfl_xor_sync(0xffffffffu, l[t][i], d);
+          if (g == 0) {
+            stat[(warp * ROWS + 8 * t + 2 * j + i) * 2] = m[t][i];
+            stat[(warp * ROWS + 8 * t + 2 * j + i) * 2 + 1] = l[t][i];
+          }
+        }
       named_barrier(1, WARPS * 32);
-      float MA = -INFINITY, MB = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < WARPS; ++i) {
-        MA = fmaxf(MA, stat[(i * kRowTile + rA) * 2]);
-        MB = fmaxf(MB, stat[(i * kRowTile + rB) * 2]);
-      }
       // (a warp that has seen nothing has the sum 0; one that has seen no numbers alone has no maximum, but no 0 either)
       const float unit = held_scale((uint32_t)top);
-      const float sA = lA == 0.f ? 0.f : ex2_approx(mA - MA) * unit, sB = lB == 0.f ? 0.f : ex2_approx(mB - MB) * unit;
-      constexpr int PER = 16 / WARPS, TPR = 32 / PER;          // dims of a thread, threads of a row
+      float f[NT][2];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float M = -INFINITY;
+#pragma unroll
+          for (int k = 0; k < WARPS; ++k) M = fmaxf(M, stat[(k * ROWS + 8 * t + 2 * j + i) * 2]);
+          f[t][i] = l[t][i] == 0.f ? 0.f : ex2_approx(m[t][i] - M) * unit;
+        }
+      constexpr int PER = 16 / WARPS, TPR = C::CHUNK / PER;    // dims of a thread, threads of a row
       const int row = tid / TPR, dp = tid % TPR * PER;
       float M = -INFINITY, L = 0.f;
 #pragma unroll
-      for (int i = 0; i < WARPS; ++i) M = fmaxf(M, stat[(i * kRowTile + row) * 2]);
+      for (int k = 0; k < WARPS; ++k) M = fmaxf(M, stat[(k * ROWS + row) * 2]);
 #pragma unroll
-      for (int i = 0; i < WARPS; ++i) {
-        const float l = stat[(i * kRowTile + row) * 2 + 1];
-        if (l != 0.f) L += l * ex2_approx(stat[(i * kRowTile + row) * 2] - M);
+      for (int k = 0; k < WARPS; ++k) {
+        const float x = stat[(k * ROWS + row) * 2 + 1];
+        if (x != 0.f) L += x * ex2_approx(stat[(k * ROWS + row) * 2] - M);
       }
       const bool fin = w.whole();              // in a cluster: the unit is this CTA's alone
       const int slot = w.slot(cta);
       const int r = w.r_first + row;
       const size_t out_row = (size_t)(w.tok0 + r / p.group) * p.hq + w.h * p.group + r % p.group;
       const float inv = L != 0.f ? 1.f / L : 0.f;
+      // rows of CHUNK floats, each pair of rows turned by eight more, so that the accesses spread over the banks
+      auto place = [](int row, int dim) { return row * C::CHUNK + ((dim + 8 * (row >> 1)) & (C::CHUNK - 1)); };
 #pragma unroll
-      for (int x = 0; x < D / 32; ++x) {
-        // rows of 32 floats, 4-float pieces shifted by four in odd rows so that the accesses spread over the banks
-        float* mine = red + warp * kRowTile * 32;
+      for (int c = 0; c < D / C::CHUNK; ++c) {
+        float* mine = red + warp * 512;
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          const int at = ((4 * n + cj + 4 * (rA & 1)) & 7) * 4;
-          const float (&e)[4] = o[4 * x + 2 * n];
-          const float (&f)[4] = o[4 * x + 2 * n + 1];
-          *reinterpret_cast<float4*>(mine + rA * 32 + at) = make_float4(e[0] * sA, f[0] * sA, e[1] * sA, f[1] * sA);
-          *reinterpret_cast<float4*>(mine + rB * 32 + at) = make_float4(e[2] * sB, f[2] * sB, e[3] * sB, f[3] * sB);
-        }
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int b = 0; b < C::CHUNK / 16; ++b) {
+            const float (&x)[4] = o[t][c * (C::CHUNK / 16) + b];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              *reinterpret_cast<float2*>(mine + place(8 * t + 2 * j + i, 16 * b + 2 * g)) = make_float2(x[i] * f[t][i], x[2 + i] * f[t][i]);
+          }
         named_barrier(1, WARPS * 32);
         float a[PER];
 #pragma unroll
         for (int e = 0; e < PER; ++e) a[e] = 0.f;
 #pragma unroll
-        for (int i = 0; i < WARPS; ++i)
+        for (int k = 0; k < WARPS; ++k)
 #pragma unroll
           for (int e = 0; e < PER; e += 2) {
-            const float2 u = *reinterpret_cast<const float2*>(red + (i * kRowTile + row) * 32 + ((((dp >> 2) + 4 * (row & 1)) & 7) * 4) + (dp & 3) + e);
+            const float2 u = *reinterpret_cast<const float2*>(red + k * 512 + place(row, dp) + e);
             a[e] += u.x; a[e + 1] += u.y;
           }
         if (row < w.rows) {
-          float* part = (SPLIT ? keep + (size_t)row * D : p.row_part + ((size_t)slot * kRowTile + row) * D) + x * 32 + dp;
-          uint32_t* y = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.y) + out_row * D + x * 32 + dp);
+          float* part = (SPLIT ? keep + (size_t)row * D : p.row_part + ((size_t)slot * kRowTile + row) * D) + c * C::CHUNK + dp;
+          uint32_t* y = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.y) + out_row * D + c * C::CHUNK + dp);
 #pragma unroll
           for (int e = 0; e < PER; e += 2) {
             if (fin) y[e >> 1] = T::pack(a[e] * inv, a[e + 1] * inv);
@@ -538,12 +572,12 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   if (p.beside) pdl_wait();
 }
 
-template <typename T, int D, bool BLOCK, bool SPLIT>
-static cudaError_t launch_rows_s(const PagedProblem& p, const HeldCache& held, const CUtensorMap& tk, const CUtensorMap& tv, int grid,
+template <typename T, int D, bool BLOCK, bool SPLIT, int NT>
+static cudaError_t launch_rows_n(const PagedProblem& p, const HeldCache& held, const CUtensorMap& tk, const CUtensorMap& tv, int grid,
                                  cudaStream_t st) {
-  using C = HeldRowCfg<D, SPLIT>;
+  using C = HeldRowCfg<D, SPLIT, NT>;
   static PerDeviceFlag configured;
-  const cudaError_t e = set_max_dynamic_smem(configured, reinterpret_cast<const void*>(paged8_rows_kernel<T, D, BLOCK, SPLIT>), C::total);
+  const cudaError_t e = set_max_dynamic_smem(configured, reinterpret_cast<const void*>(paged8_rows_kernel<T, D, BLOCK, SPLIT, NT>), C::total);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
@@ -557,7 +591,15 @@ static cudaError_t launch_rows_s(const PagedProblem& p, const HeldCache& held, c
   attr[1].val.clusterDim.x = p.n_split; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = SPLIT && p.n_split > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, paged8_rows_kernel<T, D, BLOCK, SPLIT>, tk, tv, p, held);
+  return cudaLaunchKernelEx(&cfg, paged8_rows_kernel<T, D, BLOCK, SPLIT, NT>, tk, tv, p, held);
+}
+
+// Units of at most 8 rows by the kernel of one row tile, others by that of two.
+template <typename T, int D, bool BLOCK, bool SPLIT>
+static cudaError_t launch_rows_s(const PagedProblem& p, const HeldCache& held, const CUtensorMap& tk, const CUtensorMap& tv, int max_rows,
+                                 int grid, cudaStream_t st) {
+  return max_rows <= 8 ? launch_rows_n<T, D, BLOCK, SPLIT, 1>(p, held, tk, tv, grid, st)
+                       : launch_rows_n<T, D, BLOCK, SPLIT, 2>(p, held, tk, tv, grid, st);
 }
 
 #define TKPHI_BY_TYPE(call)                                                          \
@@ -566,11 +608,15 @@ static cudaError_t launch_rows_s(const PagedProblem& p, const HeldCache& held, c
            : (bf16 ? (block ? call(Bf16, 128, true) : call(Bf16, 128, false))         \
                    : (block ? call(Fp16, 128, true) : call(Fp16, 128, false))))
 
-int paged8_row_ctas(int d) { return d == 64 ? HeldRowCfg<64, false>::CTAS : HeldRowCfg<128, false>::CTAS; }
+int paged8_row_ctas(int d, int max_rows) {
+  return d == 64 ? (max_rows <= 8 ? HeldRowCfg<64, false, 1>::CTAS : HeldRowCfg<64, false, 2>::CTAS)
+                 : (max_rows <= 8 ? HeldRowCfg<128, false, 1>::CTAS : HeldRowCfg<128, false, 2>::CTAS);
+}
 
 cudaError_t launch_paged8_rows(const PagedProblem& p, const HeldCache& held, const CUtensorMap& tk, const CUtensorMap& tv, int d,
-                               bool bf16, bool block, bool split, int grid, cudaStream_t st) {
-#define ROWS(T, D, B) (split ? launch_rows_s<T, D, B, true>(p, held, tk, tv, grid, st) : launch_rows_s<T, D, B, false>(p, held, tk, tv, grid, st))
+                               bool bf16, bool block, bool split, int max_rows, int grid, cudaStream_t st) {
+#define ROWS(T, D, B) \
+  (split ? launch_rows_s<T, D, B, true>(p, held, tk, tv, max_rows, grid, st) : launch_rows_s<T, D, B, false>(p, held, tk, tv, max_rows, grid, st))
   return TKPHI_BY_TYPE(ROWS);
 #undef ROWS
 }

@@ -213,7 +213,7 @@ int split_rows(int64_t units, int64_t tiles, int n_sm, int most_tiles = 16) {
 
 tkphi_status plan_attend(const tkphi_paged_desc* kv, const PagedShape& sh, AttendPlan* pl, bool held = false) {
   const int n_sm = sm_count_current_device();
-  const int row_keys = held ? kHeldKeys : kRowKeys, row_ctas = held ? paged8_row_ctas(kv->head_dim) : 2;
+  const int row_keys = held ? kHeldKeys : kRowKeys;
   *pl = AttendPlan{};
   int64_t longest_row = 0, longest = 0;
   for (int b = 0; b < kv->batch; ++b) {
@@ -234,6 +234,7 @@ tkphi_status plan_attend(const tkphi_paged_desc* kv, const PagedShape& sh, Atten
   if (pl->row_tiles > INT_MAX / 2) return fail(TKPHI_ERR_UNSUPPORTED, "too many key tiles for one call");
   const int units = kv->batch * kv->n_kv_heads;
   pl->row_split = pl->max_rows <= kRowTile ? split_rows(units, longest_row, n_sm) : 0;     // (a cluster has one row tile)
+  const int row_ctas = held ? paged8_row_ctas(kv->head_dim, pl->max_rows) : 2;
   pl->row_ctas = pl->row_split ? 0 : (int)std::min<int64_t>(row_ctas * n_sm, pl->row_tiles);
   pl->row_grid = pl->row_split ? units * pl->row_split : pl->row_ctas;
   if (pl->any_tiles) {
@@ -286,7 +287,7 @@ struct BlockPlan {
 
 tkphi_status plan_block(const tkphi_paged_desc* kv, const PagedShape& sh, const tkphi_page_selection* sel, BlockPlan* pl,
                         bool held = false) {
-  const int row_keys = held ? kHeldKeys : kRowKeys, row_ctas = held ? paged8_row_ctas(kv->head_dim) : 2;
+  const int row_keys = held ? kHeldKeys : kRowKeys;
   if (!sel) return fail(TKPHI_ERR_INVALID_ARG, "selection is NULL");
   if (sel->n_sink_pages < 0 || sel->n_tail_pages < 1 || sel->topk_pages < 0)
     return fail(TKPHI_ERR_INVALID_ARG, "n_sink_pages (%d) and topk_pages (%d) must be >= 0, n_tail_pages (%d) >= 1",
@@ -303,7 +304,7 @@ tkphi_status plan_block(const tkphi_paged_desc* kv, const PagedShape& sh, const 
   const int n_sm = sm_count_current_device();
   pl->n_split = split_rows(units, tiles, n_sm);
   pl->cluster = pl->n_split > 0;
-  if (!pl->cluster) pl->n_split = (int)std::max<int64_t>(1, std::min<int64_t>((tiles + 1) / 2, units > 0 ? row_ctas * n_sm / units : 1));
+  if (!pl->cluster) pl->n_split = (int)std::max<int64_t>(1, std::min<int64_t>((tiles + 1) / 2, units > 0 ? (held ? paged8_row_ctas(kv->head_dim, sh.group) : 2) * n_sm / units : 1));
   size_t o = 0;
   // score row tiles: tokens of one sequence, 16 rows at a time
   const int tpt = kRowTile / padded_group(sh.group);
@@ -523,7 +524,7 @@ tkphi_status attend(const tkphi_paged_desc* kv, const HeldCache* held, const voi
   }
   if (e == cudaSuccess && pl.any_rows) {
     ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_ROWS);
-    e = held ? launch_paged8_rows(p, *held, tk, tv, kv->head_dim, bf16, false, pl.row_split > 0, pl.row_grid, cs)
+    e = held ? launch_paged8_rows(p, *held, tk, tv, kv->head_dim, bf16, false, pl.row_split > 0, pl.max_rows, pl.row_grid, cs)
              : launch_paged_rows(p, tk, tv, kv->head_dim, bf16, false, pl.row_split > 0, pl.row_grid, cs);
   }
   if (e == cudaSuccess && pl.max_chunks > 1) {
@@ -580,7 +581,7 @@ tkphi_status block_attend(const tkphi_paged_desc* kv, const HeldCache* held, con
   if (e != cudaSuccess) return cuda_fail(e, "page selection launch");
   {
     ScopedSpan sp(cs, TKPHI_KERNEL_PAGED_ROWS);
-    e = held ? launch_paged8_rows(p, *held, tk, tv, kv->head_dim, bf16, true, pl.cluster, units * pl.n_split, cs)
+    e = held ? launch_paged8_rows(p, *held, tk, tv, kv->head_dim, bf16, true, pl.cluster, sh.group, units * pl.n_split, cs)
              : launch_paged_rows(p, tk, tv, kv->head_dim, bf16, true, pl.cluster, units * pl.n_split, cs);
     if (e == cudaSuccess && pl.n_split > 1 && !pl.cluster)
       e = (held ? launch_paged8_rows_merge : launch_paged_rows_merge)(p, kv->head_dim, bf16, true, units, sh.group, cs);
