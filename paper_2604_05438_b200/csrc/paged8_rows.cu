@@ -35,10 +35,10 @@ struct HeldRowCfg {
   static constexpr int ROWS = 8 * NT;                       // query rows of a unit, at most
   static constexpr int WARPS = SPLIT ? 8 : 4;               // (cluster form: four warps for the even, four for the odd tiles)
   static constexpr int THREADS = (WARPS + 1) * 32;
-  static constexpr int CTAS = SPLIT ? 1 : D == 64 ? 3 : 2;  // per multiprocessor
+  static constexpr int CTAS = SPLIT ? 1 : D == 128 ? 2 : NT == 1 ? 4 : 3;  // per multiprocessor
   static constexpr int TILE = kHeldKeys * D;                // codes of a tile's keys or values
   static constexpr int STAGE = 2 * TILE;
-  static constexpr int NS = D == 128 ? (SPLIT ? 5 : 3) : (SPLIT ? 10 : 3);
+  static constexpr int NS = D == 128 ? (SPLIT ? 5 : 3) : SPLIT ? 10 : NT == 1 ? 2 : 3;
   static constexpr size_t scales = (size_t)NS * STAGE;      // [NS][2][128] scale bytes
   static constexpr size_t frags = scales + NS * 2 * kHeldKeys;      // [D / 16][32 lanes][NT] queries as the lanes take them
   static constexpr int CHUNK = 512 / ROWS;                  // dims of a row that are joined at a time

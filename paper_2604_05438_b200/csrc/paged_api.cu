@@ -170,9 +170,9 @@ struct AttendPlan {
 // Sequences with at most this many rows per KV head go to the row kernel.  Over a 16-bit cache: one tile of its matrix instruction.
 constexpr int kRowsLimit = 16;
 // Over an 8-bit cache: four.  The row kernel then reads such a sequence's cache once per tile, the other way writes it as 16-bit
-// pages first and reads those with the tile kernel.  One sequence of 128K rows, 24 / 8 heads of 128: 67 us with 16 rows, 205
-// with 64, 298 with 96, 391 with 128 against 328 to 332; eight of them 1505 us with 64, 2252 with 96 against 2000; 32 / 8 heads
-// of 64, eight of 128K: 1146 with 64 against 1106, eight of 32K: 315 against 300, of 4K: 61 against 66, 109 with 128 against 70.
+// pages first and reads those with the tile kernel.  One sequence of 128K rows, 24 / 8 heads of 128: 63 us with 16 rows, 177
+// with 64 (of 16-row tiles) against 328 to 332; eight of them 1325 us with 64, 2000 with 96 against 2006; 32 / 8 heads of 64, eight
+// of 128K: 770 with 64, 1155 with 96 against 1110, of 4K: 50 with 64 against 69, of 1K: 30 against 27.
 constexpr int kHeldRowsLimit = 64;
 constexpr int rows_limit(bool held) { return held ? kHeldRowsLimit : kRowsLimit; }
 
@@ -205,10 +205,21 @@ int choose_chunk(const tkphi_paged_desc* kv, const PagedShape& sh, int64_t longe
 }
 
 // CTAs per unit of the row kernel's cluster form, or 0 for the line: units of at most `tiles` tiles.
-int split_rows(int64_t units, int64_t tiles, int n_sm, int most_tiles = 16) {
+int split_rows(int64_t units, int64_t tiles, int n_sm) {
   int split = 1;
   while (split < 8 && tiles > 2 * split && units * split * 2 <= n_sm) split *= 2;
-  return tiles <= most_tiles * split ? split : 0;
+  return tiles <= 16 * split ? split : 0;
+}
+// The same for an 8-bit cache, `all` tiles of 128 keys in the call.  A cluster's CTA takes 0.75 us per tile, because a tile is a
+// chain of latencies; the line takes 2.4 or 3.1 us more for its join, and 0.9 or 0.53 us per tile of each multiprocessor
+// (head_dim 128 or 64).  Measured, cluster and line: one sequence of 4096 rows 9.6 / 10.2 and 8.0 / 8.2 us, of 8192 12.7 / 11.9
+// and 11.4 / 9.9, of 16384 18.6 / 14.2 and 17.1 / 11.9; eight of 2048 12.7 / 15.2 and 11.6 / 12.4, of 4096 18.7 / 21.8 and
+// 17.2 / 15.3; sixteen of 2048 16.6 / 22.0 and 15.1 / 15.0.  Beyond 16 tiles the line's even pieces count for more.
+int split_held_rows(int64_t units, int64_t tiles, int64_t all, int d, int n_sm) {
+  int split = 1;
+  while (split < 8 && tiles > 2 * split && units * split * 2 <= n_sm) split *= 2;
+  const double cta = 0.75 * (double)((tiles + split - 1) / split), line = (double)all / n_sm;
+  return tiles <= 16 * split && cta <= (d == 128 ? 2.4 + 0.9 * line : 3.1 + 0.53 * line) ? split : 0;
 }
 
 tkphi_status plan_attend(const tkphi_paged_desc* kv, const PagedShape& sh, AttendPlan* pl, bool held = false) {
@@ -233,7 +244,8 @@ tkphi_status plan_attend(const tkphi_paged_desc* kv, const PagedShape& sh, Atten
   }
   if (pl->row_tiles > INT_MAX / 2) return fail(TKPHI_ERR_UNSUPPORTED, "too many key tiles for one call");
   const int units = kv->batch * kv->n_kv_heads;
-  pl->row_split = pl->max_rows <= kRowTile ? split_rows(units, longest_row, n_sm) : 0;     // (a cluster has one row tile)
+  pl->row_split = pl->max_rows > kRowTile ? 0             // (a cluster has one row tile)
+                  : held ? split_held_rows(units, longest_row, pl->row_tiles, kv->head_dim, n_sm) : split_rows(units, longest_row, n_sm);
   const int row_ctas = held ? paged8_row_ctas(kv->head_dim, pl->max_rows) : 2;
   pl->row_ctas = pl->row_split ? 0 : (int)std::min<int64_t>(row_ctas * n_sm, pl->row_tiles);
   pl->row_grid = pl->row_split ? units * pl->row_split : pl->row_ctas;
