@@ -75,7 +75,9 @@ struct ReadProblem {
   long long k_row, k_head, v_row, v_head;    // elements
   long long total_rows;
   int* status;
+  int heads;                                 // KV heads of a CTA (set by the launch)
 };
+constexpr int kReadRows = 64;                // rows of a CTA
 cudaError_t launch_paged_read(const ReadProblem& p, bool bf16, cudaStream_t st);
 
 constexpr int kExpandRows = 128;             // rows of an expanded page
@@ -85,6 +87,7 @@ struct ExpandProblem {
   HeldCache held;
   void* k_out; void* v_out;                  // [pages][hkv][128][d]
   int* table; int max_pages;                 // [batch][max_pages] written for the sequences with many rows
+  int heads;                                 // KV heads of a CTA (set by the launch)
 };
 cudaError_t launch_paged_expand(const PagedProblem& p, const ExpandProblem& x, int d, bool bf16, int pages, cudaStream_t st);
 

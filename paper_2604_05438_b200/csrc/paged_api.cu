@@ -519,7 +519,7 @@ tkphi_status attend(const tkphi_paged_desc* kv, const HeldCache* held, const voi
     PagedProblem t = p;
     if (pl.expand_pages) {
       const ExpandProblem x{static_cast<const uint8_t*>(kv->k), static_cast<const uint8_t*>(kv->v), kv->stride_page, kv->stride_head,
-                            kv->stride_token, *held, w + pl.expand_k, w + pl.expand_v, reinterpret_cast<int*>(w + pl.expand_table), pl.expand_max};
+                            kv->stride_token, *held, w + pl.expand_k, w + pl.expand_v, reinterpret_cast<int*>(w + pl.expand_table), pl.expand_max, 0};
       tkphi_paged_desc d = *kv;
       d.page_size = kExpandRows; d.n_pages = pl.expand_pages; d.max_pages = pl.expand_max;
       d.stride_token = kv->head_dim; d.stride_head = d.stride_token * kExpandRows; d.stride_page = d.stride_head * kv->n_kv_heads;

@@ -1,20 +1,71 @@
 // Rows of an 8-bit paged cache back as 16-bit rows: out[cu_rows[b] + i] = codes * 2^(e - 127) of position first[b] + i of
 // sequence b, for keys and values, rounded once to the element type (exact in bf16).
 //
-// Bound: memory, 2 (d + 1) bytes in and 4 d out per row and head.  A thread has 16 codes of a row and writes 32 bytes;
-// a CTA takes 64 output rows of one KV head, two rows per thread with all loads before the stores.
+// Bound: memory, 2 (d + 1) bytes in and 4 d out per row and head.  A thread has 16 codes of a row's keys and values and writes
+// 32 bytes of each; a CTA takes 64 rows and several KV heads, one after the other, so that looking up the rows' places is
+// paid once, with the next head's loads in flight while one head is written.
 #include "held8.cuh"
 
 namespace tkphi {
 
-constexpr int kReadRows = 64;
 constexpr int kReadThreads = 256;
+
+// 32 bytes, in one store where they are aligned to that: two of 16 write half sectors.
+__device__ __forceinline__ void put32(uint16_t* to, const uint4& a, const uint4& c, bool aligned) {
+  if (aligned) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(c.x),
+                 "r"(c.y), "r"(c.z), "r"(c.w) : "memory");
+  } else {
+    reinterpret_cast<uint4*>(to)[0] = a;
+    reinterpret_cast<uint4*>(to)[1] = c;
+  }
+}
+
+// What a thread has of one row and head.
+struct HeldPiece { uint4 k, v; uint32_t ke, ve; };
+
+// Heads h0 .. h1-1 of ROWS rows: row i * rows-per-pass + tid / lanes-per-row of the CTA is read if ok[i], at `at[i]` of the codes
+// and `scale_at[i]` of the scales, and written by put(i, head, keys or values, 32 bytes as two pieces).
+template <typename T, int PASSES, typename Put>
+__device__ __forceinline__ void copy_heads(const uint8_t* k, const uint8_t* v, const HeldCache& held, long long stride_head, int page_rows,
+                                           int h0, int h1, const bool (&ok)[PASSES], const size_t (&at)[PASSES],
+                                           const size_t (&scale_at)[PASSES], Put put) {
+  HeldPiece now[PASSES], next[PASSES];
+  auto load = [&](HeldPiece (&x)[PASSES], int h) {
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      x[i].k = x[i].v = make_uint4(0, 0, 0, 0);
+      x[i].ke = x[i].ve = 0;
+      if (!ok[i]) continue;
+      const size_t c = at[i] + (size_t)h * stride_head, e = scale_at[i] + (size_t)h * page_rows;
+      if (k) { x[i].k = __ldcs(reinterpret_cast<const uint4*>(k + c)); x[i].ke = __ldg(held.k_scales + e); }
+      if (v) { x[i].v = __ldcs(reinterpret_cast<const uint4*>(v + c)); x[i].ve = __ldg(held.v_scales + e); }
+    }
+  };
+  load(next, h0);
+  for (int h = h0; h < h1; ++h) {
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) now[i] = next[i];
+    if (h + 1 < h1) load(next, h + 1);
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const uint4 w = s ? now[i].v : now[i].k;
+        const float f = held_scale(s ? now[i].ve : now[i].ke);
+        const uint2 a = held_values<T>(w.x, f), c = held_values<T>(w.y, f), d = held_values<T>(w.z, f), e = held_values<T>(w.w, f);
+        put(i, h, s, make_uint4(a.x, a.y, c.x, c.y), make_uint4(d.x, d.y, e.x, e.y));
+      }
+  }
+}
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kReadThreads) paged_read_kernel(const __grid_constant__ ReadProblem p) {
-  constexpr int LPR = D / 16, RPP = kReadThreads / LPR, PASSES = kReadRows / RPP > 0 ? kReadRows / RPP : 1;
+  constexpr int LPR = D / 16, RPP = kReadThreads / LPR, PASSES = kReadRows / RPP;
+  static_assert(PASSES >= 1, "rows of a CTA");
   __shared__ int s_seq;
-  const int tid = threadIdx.x, lane = tid & 31, h = blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int h0 = blockIdx.y * p.heads, h1 = min(h0 + p.heads, p.hkv);
   const long long row0 = (long long)blockIdx.x * kReadRows;
   pdl_wait();
   pdl_launch_next();
@@ -32,49 +83,51 @@ __global__ void __launch_bounds__(kReadThreads) paged_read_kernel(const __grid_c
   __syncthreads();
   int b = s_seq;
   const int l = tid % LPR, ps = 1 << p.page_shift;
-  uint4 kw[PASSES], vw[PASSES];
-  uint32_t ke[PASSES], ve[PASSES];
   bool ok[PASSES];
+  size_t at[PASSES], scale_at[PASSES];
 #pragma unroll
   for (int i = 0; i < PASSES; ++i) {
     const long long row = row0 + i * RPP + tid / LPR;
     ok[i] = false;
-    if (row >= p.total_rows || (RPP > kReadRows && tid / LPR >= kReadRows)) continue;
+    at[i] = scale_at[i] = 0;
+    if (row >= p.total_rows) continue;
     while (b < p.batch && __ldg(p.cu_rows + b + 1) <= row) ++b;
     if (b >= p.batch) continue;
     const long long pos = row - __ldg(p.cu_rows + b) + (p.first ? __ldg(p.first + b) : 0ll);
-    const long long have = __ldg(p.kv_lens + b);
-    if (pos < 0 || pos >= have || pos >= p.max_kv) continue;       // (a replay with shorter device lengths: not written)
+    if (pos < 0 || pos >= __ldg(p.kv_lens + b) || pos >= p.max_kv) continue;       // (a replay with shorter device lengths: not written)
     const int page = __ldg(p.table + (size_t)b * p.max_pages + (pos >> p.page_shift));
     if (page < 0 || page >= p.n_pages) {
       if (l == 0) atomicExch(p.status, kStatusBadPage);
       continue;
     }
-    ok[i] = true;
     const int slot = (int)(pos & (ps - 1));
-    const size_t at = (size_t)page * p.stride_page + (size_t)h * p.stride_head + (size_t)slot * p.stride_token;
-    const size_t scale_at = ((size_t)page * p.hkv + h) * ps + slot;
-    if (p.k_out) { kw[i] = __ldg(reinterpret_cast<const uint4*>(p.k + at) + l); ke[i] = __ldg(p.held.k_scales + scale_at); }
-    if (p.v_out) { vw[i] = __ldg(reinterpret_cast<const uint4*>(p.v + at) + l); ve[i] = __ldg(p.held.v_scales + scale_at); }
+    ok[i] = true;
+    at[i] = (size_t)page * p.stride_page + (size_t)slot * p.stride_token + l * 16;
+    scale_at[i] = (size_t)page * p.hkv * ps + slot;
   }
-#pragma unroll
-  for (int i = 0; i < PASSES; ++i) {
-    if (!ok[i]) continue;
-    const size_t row = (size_t)(row0 + i * RPP + tid / LPR);
-    auto put = [&](void* out, long long row_stride, long long head_stride, const uint4& w, uint32_t e) {
-      const float s = held_scale(e);
-      const uint2 a = held_values<T>(w.x, s), c = held_values<T>(w.y, s), d = held_values<T>(w.z, s), f = held_values<T>(w.w, s);
-      uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + row * row_stride + (size_t)h * head_stride + l * 16);
-      o[0] = make_uint4(a.x, a.y, c.x, c.y);
-      o[1] = make_uint4(d.x, d.y, f.x, f.y);
-    };
-    if (p.k_out) put(p.k_out, p.k_row, p.k_head, kw[i], ke[i]);
-    if (p.v_out) put(p.v_out, p.v_row, p.v_head, vw[i], ve[i]);
-  }
+  const bool wide = ((reinterpret_cast<uintptr_t>(p.k_out) | reinterpret_cast<uintptr_t>(p.v_out)) & 31u) == 0 &&
+                    ((p.k_row | p.k_head | p.v_row | p.v_head) & 15ll) == 0;
+  copy_heads<T>(p.k_out ? p.k : nullptr, p.v_out ? p.v : nullptr, p.held, p.stride_head, ps, h0, h1, ok, at, scale_at,
+                [&](int i, int h, int s, const uint4& a, const uint4& c) {
+                  void* out = s ? p.v_out : p.k_out;
+                  if (!ok[i] || !out) return;
+                  const size_t row = (size_t)(row0 + i * RPP + tid / LPR);
+                  put32(static_cast<uint16_t*>(out) + row * (s ? p.v_row : p.k_row) + (size_t)h * (s ? p.v_head : p.k_head) + l * 16, a, c, wide);
+                });
 }
 
-cudaError_t launch_paged_read(const ReadProblem& p, bool bf16, cudaStream_t st) {
-  const dim3 grid((unsigned)((p.total_rows + kReadRows - 1) / kReadRows), p.hkv), block(kReadThreads);
+// Heads of a CTA: all of them, or fewer where there are not CTAs enough to go round.
+static int heads_per_cta(long long blocks, int hkv) {
+  int n = hkv;
+  while (n > 1 && blocks * ((hkv + n - 1) / n) < 8 * sm_count_current_device()) n = (n + 1) / 2;
+  return n;
+}
+
+cudaError_t launch_paged_read(const ReadProblem& q, bool bf16, cudaStream_t st) {
+  ReadProblem p = q;
+  const long long blocks = (p.total_rows + kReadRows - 1) / kReadRows;
+  p.heads = heads_per_cta(blocks, p.hkv);
+  const dim3 grid((unsigned)blocks, (p.hkv + p.heads - 1) / p.heads), block(kReadThreads);
   if (p.d == 64)
     return bf16 ? launch_pdl(paged_read_kernel<Bf16, 64>, grid, block, 0, st, p) : launch_pdl(paged_read_kernel<Fp16, 64>, grid, block, 0, st, p);
   return bf16 ? launch_pdl(paged_read_kernel<Bf16, 128>, grid, block, 0, st, p) : launch_pdl(paged_read_kernel<Fp16, 128>, grid, block, 0, st, p);
@@ -83,12 +136,14 @@ cudaError_t launch_paged_read(const ReadProblem& p, bool bf16, cudaStream_t st) 
 // ---------------------------------------------------------------- for attention of many rows
 // The caches of the sequences with many rows as 16-bit pages of 128 rows in the workspace, [page][head][slot][dim], one
 // sequence's pages behind another's, and a page table of them; codes times powers of two, so nothing is lost.  A CTA takes
-// a page of one KV head.  Rows at or behind a sequence's length and on bad pages become 0.
+// half a page.  Rows at or behind a sequence's length and on bad pages become 0.
 template <typename T, int D>
 __global__ void __launch_bounds__(kReadThreads) paged_expand_kernel(const __grid_constant__ PagedProblem p, const __grid_constant__ ExpandProblem x) {
-  constexpr int LPR = D / 16, RPP = kReadThreads / LPR, PASSES = kExpandRows / RPP;
+  constexpr int LPR = D / 16, RPP = kReadThreads / LPR, PASSES = kReadRows / RPP, PARTS = kExpandRows / kReadRows;
   __shared__ int s_seq, s_page;
-  const int tid = threadIdx.x, lane = tid & 31, h = blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int out_page = blockIdx.x / PARTS, first = blockIdx.x % PARTS * kReadRows;
+  const int h0 = blockIdx.y * x.heads, h1 = min(h0 + x.heads, p.hkv);
   pdl_wait();
   pdl_launch_next();
   if (tid < 32) {
@@ -98,26 +153,26 @@ __global__ void __launch_bounds__(kReadThreads) paged_expand_kernel(const __grid
       int n = 0;
       if (s + lane < p.batch && (long long)paged_q_len(p, s + lane) * p.group > p.rows_limit) n = (paged_kv_len(p, s + lane) + kExpandRows - 1) / kExpandRows;
       const int incl = warp_inclusive_scan(n) + base;
-      if (incl > (int)blockIdx.x && incl - n <= (int)blockIdx.x) {           // one lane
+      if (incl > out_page && incl - n <= out_page) {           // one lane
         s_seq = s + lane;
-        s_page = blockIdx.x - (incl - n);
+        s_page = out_page - (incl - n);
       }
       base = __shfl_sync(0xffffffffu, incl, 31);
-      if (base > (int)blockIdx.x) break;
+      if (base > out_page) break;
     }
   }
   __syncthreads();
   const int b = s_seq;
   if (b < 0) return;                           // (a replay with shorter lengths)
   const int l = tid % LPR, ps = 1 << p.page_shift, len = paged_kv_len(p, b);
-  if (h == 0 && tid == 0) x.table[(size_t)b * x.max_pages + s_page] = blockIdx.x;
-  uint4 kw[PASSES], vw[PASSES];
-  uint32_t ke[PASSES], ve[PASSES];
+  if (h0 == 0 && first == 0 && tid == 0) x.table[(size_t)b * x.max_pages + s_page] = out_page;
+  bool ok[PASSES];
+  size_t at[PASSES], scale_at[PASSES];
 #pragma unroll
   for (int i = 0; i < PASSES; ++i) {
-    kw[i] = vw[i] = make_uint4(0, 0, 0, 0);
-    ke[i] = ve[i] = 0;
-    const int pos = s_page * kExpandRows + i * RPP + tid / LPR;
+    const int pos = s_page * kExpandRows + first + i * RPP + tid / LPR;
+    ok[i] = false;
+    at[i] = scale_at[i] = 0;
     if (pos >= len) continue;
     const int page = __ldg(p.table + (size_t)b * p.max_pages + (pos >> p.page_shift));
     if (page < 0 || page >= p.n_pages) {
@@ -125,30 +180,21 @@ __global__ void __launch_bounds__(kReadThreads) paged_expand_kernel(const __grid
       continue;
     }
     const int slot = pos & (ps - 1);
-    const size_t at = (size_t)page * x.stride_page + (size_t)h * x.stride_head + (size_t)slot * x.stride_token;
-    const size_t scale_at = ((size_t)page * p.hkv + h) * ps + slot;
-    kw[i] = __ldg(reinterpret_cast<const uint4*>(x.k + at) + l);
-    vw[i] = __ldg(reinterpret_cast<const uint4*>(x.v + at) + l);
-    ke[i] = __ldg(x.held.k_scales + scale_at);
-    ve[i] = __ldg(x.held.v_scales + scale_at);
+    ok[i] = true;
+    at[i] = (size_t)page * x.stride_page + (size_t)slot * x.stride_token + l * 16;
+    scale_at[i] = (size_t)page * p.hkv * ps + slot;
   }
-  const size_t out = ((size_t)blockIdx.x * p.hkv + h) * kExpandRows;
-#pragma unroll
-  for (int i = 0; i < PASSES; ++i) {
-    auto put = [&](void* to, const uint4& w, uint32_t e) {
-      const float s = held_scale(e);
-      const uint2 a = held_values<T>(w.x, s), c = held_values<T>(w.y, s), d = held_values<T>(w.z, s), f = held_values<T>(w.w, s);
-      uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(to) + (out + i * RPP + tid / LPR) * D + l * 16);
-      o[0] = make_uint4(a.x, a.y, c.x, c.y);
-      o[1] = make_uint4(d.x, d.y, f.x, f.y);
-    };
-    put(x.k_out, kw[i], ke[i]);
-    put(x.v_out, vw[i], ve[i]);
-  }
+  copy_heads<T>(x.k, x.v, x.held, x.stride_head, ps, h0, h1, ok, at, scale_at, [&](int i, int h, int s, const uint4& a, const uint4& c) {
+    const size_t row = ((size_t)out_page * p.hkv + h) * kExpandRows + first + i * RPP + tid / LPR;
+    put32(static_cast<uint16_t*>(s ? x.v_out : x.k_out) + row * D + l * 16, a, c, true);
+  });
 }
 
-cudaError_t launch_paged_expand(const PagedProblem& p, const ExpandProblem& x, int d, bool bf16, int pages, cudaStream_t st) {
-  const dim3 grid(pages, p.hkv), block(kReadThreads);
+cudaError_t launch_paged_expand(const PagedProblem& p, const ExpandProblem& q, int d, bool bf16, int pages, cudaStream_t st) {
+  ExpandProblem x = q;
+  const long long blocks = (long long)pages * (kExpandRows / kReadRows);
+  x.heads = heads_per_cta(blocks, p.hkv);
+  const dim3 grid((unsigned)blocks, (p.hkv + x.heads - 1) / x.heads), block(kReadThreads);
   if (d == 64)
     return bf16 ? launch_pdl(paged_expand_kernel<Bf16, 64>, grid, block, 0, st, p, x) : launch_pdl(paged_expand_kernel<Fp16, 64>, grid, block, 0, st, p, x);
   return bf16 ? launch_pdl(paged_expand_kernel<Bf16, 128>, grid, block, 0, st, p, x) : launch_pdl(paged_expand_kernel<Fp16, 128>, grid, block, 0, st, p, x);
