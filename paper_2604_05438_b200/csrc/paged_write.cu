@@ -12,6 +12,12 @@
 // at head_dim 128 (4 at 64), a lane owning the two 8-element pieces whose elements are each other's partners in the
 // rotation.  A row's sum of squares and its largest magnitude are two or three shuffles between its lanes; all lanes of a
 // warp take part in them, with zeros where they have no row.
+// Measured: 15.8K tokens, 24 / 8 heads of 128, norms, half of the dims rotated, bounds, 16-bit cache: 88 us (3.7 TB/s);
+// 23.6K tokens, 32 / 8 heads of 64, rotated, 8-bit cache: 61 us (4.4 TB/s); one token 5.5 us a call.  Neither memory (DRAM 40 to
+// 47% busy) nor issue (40 to 55%) is the bound, but the chain of a row: loads, two sums over its lanes, sines, conversions.  Five
+// CTAs of 128 threads per multiprocessor are 9% faster than four; six spill.  Tried and no faster (59 to 75 and 87 to 117 us):
+// several heads per CTA with the sines shared through registers or shared memory, packed 32-bit pairs, the next row's loads
+// issued ahead into registers or by asynchronous copies into shared memory.
 #include "held8.cuh"
 
 namespace tkphi {
@@ -75,7 +81,7 @@ __device__ __forceinline__ uint4 row_codes(const float (&x)[16], uint32_t e) {
 // An item is one KV head of 64 aligned cache positions (128 where the page is that long): whole pages, so that their
 // bounds need no other CTA.
 template <typename T, int D, int NT, bool HELD>
-__global__ void __launch_bounds__(NT, NT == 128 ? 4 : 2) paged_write_kernel(const __grid_constant__ WriteProblem wp) {
+__global__ void __launch_bounds__(NT, NT == 128 ? 5 : 2) paged_write_kernel(const __grid_constant__ WriteProblem wp) {
   constexpr int LPR = D / 16;                  // lanes of a row
   constexpr int RPW = 32 / LPR;                // rows of a warp
   constexpr int RPP = NT / LPR;                // rows of one pass of the CTA
@@ -141,15 +147,12 @@ __global__ void __launch_bounds__(NT, NT == 128 ? 4 : 2) paged_write_kernel(cons
     const int row = r0 + tid / LPR;
     const bool in = row >= first && row < hi, fresh = in && row >= lo;
     uint4 a = make_uint4(0, 0, 0, 0), c = a;              // the held key, as 16-bit pieces, for the bounds
-    int phys = 0;
-    bool ok = false;
-    if (in) {
-      // a page id outside the cache: its rows are dropped, the queries of its tokens are written all the same
-      phys = __ldg(table + (row >> p.page_shift));
-      ok = phys >= 0 && phys < p.n_pages;
-      if (!ok && l == 0) atomicExch(p.status, kStatusBadPage);
-      phys = ok ? phys : 0;
-    }
+    int phys = -1;
+    if (in) phys = __ldg(table + (row >> p.page_shift));
+    // a page id outside the cache: its rows are dropped, the queries of its tokens are written all the same
+    const bool ok = phys >= 0 && phys < p.n_pages;
+    const bool bad = in && !ok && l == 0;
+    phys = ok ? phys : 0;
     const size_t at = (size_t)phys * p.stride_page + (size_t)h * p.stride_head + (size_t)(row & (ps - 1)) * p.stride_token;
     const size_t scale_at = ((size_t)phys * p.hkv + h) * ps + (row & (ps - 1));
     if (__any_sync(0xffffffffu, fresh)) {
@@ -245,6 +248,7 @@ __global__ void __launch_bounds__(NT, NT == 128 ? 4 : 2) paged_write_kernel(cons
         }
       }
     }
+    if (bad) atomicExch(p.status, kStatusBadPage);
     if (in && !fresh) {                                   // a row of an earlier call
       if (HELD) {
         const uint2* kd = reinterpret_cast<const uint2*>(static_cast<const char*>(p.k) + at);
@@ -261,27 +265,33 @@ __global__ void __launch_bounds__(NT, NT == 128 ? 4 : 2) paged_write_kernel(cons
       }
     }
     if (p.bounds) {
-      // over the warp's rows (all of one page); lanes without a row take their partner's
-      uint4 n0 = a, n1 = c, x0 = a, x1 = c;
-      uint32_t* w[4] = {reinterpret_cast<uint32_t*>(&n0), reinterpret_cast<uint32_t*>(&n1), reinterpret_cast<uint32_t*>(&x0),
-                        reinterpret_cast<uint32_t*>(&x1)};
-      bool any = in;
+      // Over the warp's rows (all of one page).  Lanes without a row take another row's; then the lanes of two rows share the
+      // work: one takes the first pieces, the other the second, then one minima, the other maxima.
+      const unsigned have = __ballot_sync(0xffffffffu, in);
+      if (have != 0) {
+        uint32_t k[8] = {a.x, a.y, a.z, a.w, c.x, c.y, c.z, c.w};
+        if (have != 0xffffffffu) {
+          const int from = in ? lane : (__ffs(have) - 1) / LPR * LPR + l;
 #pragma unroll
-      for (int o = LPR; o < 32; o <<= 1) {
-        const bool theirs = __shfl_xor_sync(0xffffffffu, (int)any, o) != 0;
+          for (int i = 0; i < 8; ++i) k[i] = __shfl_sync(0xffffffffu, k[i], from);
+        }
+        const bool second = lane & 16, most = lane & 8;
+        uint32_t m[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t mine = second ? k[4 + i] : k[i], theirs = __shfl_xor_sync(0xffffffffu, second ? k[i] : k[4 + i], 16);
+          const uint32_t lo2 = T::min2(mine, theirs), hi2 = T::max2(mine, theirs);
+          const uint32_t other = __shfl_xor_sync(0xffffffffu, most ? lo2 : hi2, 8);
+          m[i] = most ? T::max2(hi2, other) : T::min2(lo2, other);
+        }
+        if (LPR == 4) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t x = __shfl_xor_sync(0xffffffffu, w[j][i], o);
-            if (theirs) w[j][i] = !any ? x : j < 2 ? T::min2(w[j][i], x) : T::max2(w[j][i], x);
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, m[i], 4);
+            m[i] = most ? T::max2(m[i], other) : T::min2(m[i], other);
           }
-        any = any || theirs;
-      }
-      if (lane < LPR) {
-        const int grp = (r0 + warp * RPW) / RPW;
-        s_red[grp][0][c0] = n0; s_red[grp][0][c1] = n1;
-        s_red[grp][1][c0] = x0; s_red[grp][1][c1] = x1;
+        }
+        if (LPR == 8 || (lane & 4) == 0) s_red[(r0 + warp * RPW) / RPW][most][second ? c1 : c0] = make_uint4(m[0], m[1], m[2], m[3]);
       }
     }
   }
