@@ -32,6 +32,18 @@ template <typename T>
 __device__ __forceinline__ uint4 pack_piece(const float* x) {
   return make_uint4(T::pack(x[0], x[1]), T::pack(x[2], x[3]), T::pack(x[4], x[5]), T::pack(x[6], x[7]));
 }
+// Cosine and sine of an angle of a / 2^32 turns: less the nearest quarter turn, an angle |y| <= pi / 4 is left, of which the
+// Taylor polynomials of degree 9 and 10 are off by y^11 / 11! = 1.8e-9 and y^12 / 12! = 1.1e-10, less than 32 bits hold.
+// (sincospif took about 125 instructions of a pair, two thirds of the kernel's.)
+__device__ __forceinline__ void turn_cos_sin(uint32_t a, float& cs, float& sn) {
+  const uint32_t quarter = a + 0x20000000u;                  // its top two bits: the quarter
+  const float y = (float)(int)(a - (quarter & 0xc0000000u)) * 1.46291807926715968e-9f, z = y * y;      // 2 pi / 2^32
+  const float s = fmaf(y * z, fmaf(z, fmaf(z, fmaf(z, 2.75573192e-6f, -1.98412698e-4f), 8.33333333e-3f), -1.66666667e-1f), y);
+  const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -2.75573192e-7f, 2.48015873e-5f), -1.38888889e-3f), 4.16666667e-2f), -0.5f), 1.f);
+  const bool odd = quarter & 0x40000000u;
+  sn = __uint_as_float(__float_as_uint(odd ? c : s) ^ (quarter & 0x80000000u));
+  cs = __uint_as_float(__float_as_uint(odd ? s : c) ^ ((quarter + 0x40000000u) & 0x80000000u));
+}
 // x: the lane's two pieces of 8 dims.
 __device__ __forceinline__ void rotate16(float (&x)[16], const float (&cs)[8], const float (&sn)[8], bool pairs) {
 #pragma unroll
@@ -89,11 +101,18 @@ __global__ void __launch_bounds__(NT, NT == 128 ? 5 : 2) paged_write_kernel(cons
   const AppendProblem& p = wp.a;
   __shared__ long long s_find[4];              // sequence, its first token row, cache length, first new position
   __shared__ int s_item;
+  __shared__ __align__(16) unsigned long long s_turn[D / 2];
   __shared__ uint4 s_red[128 / RPW][2][2 * LPR];     // a warp's rows: their minimum and maximum
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int h = blockIdx.y, span_shift = p.page_shift > 6 ? p.page_shift : 6;
   pdl_wait();
   pdl_launch_next();
+  // Turns per position of the rotated pairs, less whole ones, in units of 2^-64.  The product with a position then drops whole
+  // turns by itself, exactly: the angle is off by position * 2^-65 turns, and by the product's rounding to 2^-53 of inv_freq.
+  if (tid >= NT / 2 && tid - NT / 2 < p.rot / 2) {
+    const double t = (double)__ldg(p.inv_freq + tid - NT / 2) * 0.15915494309189533577;
+    s_turn[tid - NT / 2] = __double2ull_rz((t - floor(t)) * 18446744073709551616.0);
+  }
 
   // ---- which positions: a sequence holds (q_len + span - 2) / span + 1 items, enough for every start inside one
   if (warp == 0) {
@@ -137,18 +156,20 @@ __global__ void __launch_bounds__(NT, NT == 128 ? 5 : 2) paged_write_kernel(cons
   const int turned = p.rot / 16;                          // lanes whose pieces are rotated
   const bool rotate = l < turned;
   if (rotate && !p.pairs) { c0 = l; c1 = l + turned; }
-  double turn[8];
-  if (rotate) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) turn[i] = (double)__ldg(p.inv_freq + 8 * l + i) * 0.15915494309189533577;
-  }
   const float* kw = wp.k_weight ? wp.k_weight + h * wp.k_weight_head : nullptr;
-  for (int r0 = 0; r0 < hi; r0 += RPP) {
+  // page ids one pass ahead
+  auto page_of = [&](int r0) {
+    const int row = r0 + tid / LPR;
+    return row >= first && row < hi ? __ldg(table + (row >> p.page_shift)) : -1;
+  };
+  const int r_begin = first / RPP * RPP;
+  int page_next = page_of(r_begin);
+  for (int r0 = r_begin; r0 < hi; r0 += RPP) {
     const int row = r0 + tid / LPR;
     const bool in = row >= first && row < hi, fresh = in && row >= lo;
     uint4 a = make_uint4(0, 0, 0, 0), c = a;              // the held key, as 16-bit pieces, for the bounds
-    int phys = -1;
-    if (in) phys = __ldg(table + (row >> p.page_shift));
+    int phys = page_next;
+    page_next = page_of(r0 + RPP);
     // a page id outside the cache: its rows are dropped, the queries of its tokens are written all the same
     const bool ok = phys >= 0 && phys < p.n_pages;
     const bool bad = in && !ok && l == 0;
@@ -167,12 +188,9 @@ __global__ void __launch_bounds__(NT, NT == 128 ? 5 : 2) paged_write_kernel(cons
         v0 = __ldg(vs + 2 * l);
         v1 = __ldg(vs + 2 * l + 1);
         if (rotate) {
-          const double x = (double)(p.positions ? __ldg(p.positions + tok) : t);
+          const unsigned long long x = (unsigned long long)(p.positions ? __ldg(p.positions + tok) : t);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const double w = x * turn[i];
-            sincospif(2.f * (float)(w - rint(w)), &sn[i], &cs[i]);
-          }
+          for (int i = 0; i < 8; ++i) turn_cos_sin((uint32_t)((x * s_turn[8 * l + i] + 0x80000000ull) >> 32), cs[i], sn[i]);
         }
       }
       float x[16];
