@@ -57,6 +57,7 @@ struct WriteProblem {
   const float* k_weight; long long k_weight_head;
   float eps;
   HeldCache held;                            // k_scales null: a 16-bit cache
+  bool wide;                                 // all 16-bit rows that are written lie on 32-byte boundaries (set by the launch)
 };
 cudaError_t launch_paged_write(const WriteProblem& p, bool bf16, cudaStream_t st);
 

@@ -12,16 +12,27 @@
 // at head_dim 128 (4 at 64), a lane owning the two 8-element pieces whose elements are each other's partners in the
 // rotation.  A row's sum of squares and its largest magnitude are two or three shuffles between its lanes; all lanes of a
 // warp take part in them, with zeros where they have no row.
-// Measured: 15.8K tokens, 24 / 8 heads of 128, norms, half of the dims rotated, bounds, 16-bit cache: 88 us (3.7 TB/s);
-// 23.6K tokens, 32 / 8 heads of 64, rotated, 8-bit cache: 61 us (4.4 TB/s); one token 5.5 us a call.  Neither memory (DRAM 40 to
-// 47% busy) nor issue (40 to 55%) is the bound, but the chain of a row: loads, two sums over its lanes, sines, conversions.  Five
-// CTAs of 128 threads per multiprocessor are 9% faster than four; six spill.  Tried and no faster (59 to 75 and 87 to 117 us):
-// several heads per CTA with the sines shared through registers or shared memory, packed 32-bit pairs, the next row's loads
-// issued ahead into registers or by asynchronous copies into shared memory.
+// Measured: 15.8K tokens, 24 / 8 heads of 128, norms, half of the dims rotated, bounds, 16-bit cache: 80 us (4.1 TB/s);
+// 23.6K tokens, 32 / 8 heads of 64, rotated, 8-bit cache: 54 us (4.9 TB/s); one token 4.8 us a call.  The chain of a row is the
+// bound (loads, sums over its lanes, conversions) at the occupancy that its registers leave: what helped were all loads of a row
+// before anything else, no spilled registers, angles in fixed point with frequencies in shared memory, 32-byte stores.  Tried
+// and no faster: several heads per CTA with the sines shared, packed 32-bit pairs, the next row's loads issued ahead into
+// registers or by asynchronous copies into shared memory, weights in shared memory, five CTAs with 96 registers.
 #include "held8.cuh"
 
 namespace tkphi {
 
+// Writes pieces c0 and c1 of a row.  Neighbours are 32 bytes: two stores of 16 would each write half of every sector.
+__device__ __forceinline__ void put_pieces(void* row, int c0, int c1, bool wide, const uint4& a, const uint4& c) {
+  uint4* p = static_cast<uint4*>(row);
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + c0), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(c.x),
+                 "r"(c.y), "r"(c.z), "r"(c.w) : "memory");
+  } else {
+    p[c0] = a;
+    p[c1] = c;
+  }
+}
 template <typename T>
 __device__ __forceinline__ void unpack_piece(const uint4& v, float* x) {
   const uint32_t* w = reinterpret_cast<const uint32_t*>(&v);
@@ -93,7 +104,7 @@ __device__ __forceinline__ uint4 row_codes(const float (&x)[16], uint32_t e) {
 // An item is one KV head of 64 aligned cache positions (128 where the page is that long): whole pages, so that their
 // bounds need no other CTA.
 template <typename T, int D, int NT, bool HELD>
-__global__ void __launch_bounds__(NT, NT == 128 ? 5 : 2) paged_write_kernel(const __grid_constant__ WriteProblem wp) {
+__global__ void __launch_bounds__(NT, NT == 128 ? 4 : 2) paged_write_kernel(const __grid_constant__ WriteProblem wp) {
   constexpr int LPR = D / 16;                  // lanes of a row
   constexpr int RPW = 32 / LPR;                // rows of a warp
   constexpr int RPP = NT / LPR;                // rows of one pass of the CTA
@@ -156,6 +167,8 @@ __global__ void __launch_bounds__(NT, NT == 128 ? 5 : 2) paged_write_kernel(cons
   const int turned = p.rot / 16;                          // lanes whose pieces are rotated
   const bool rotate = l < turned;
   if (rotate && !p.pairs) { c0 = l; c1 = l + turned; }
+  // (in the form for many rows: where latency counts, the choice costs more than it gives)
+  const bool wide = NT == 128 && wp.wide && c1 == c0 + 1;
   const float* kw = wp.k_weight ? wp.k_weight + h * wp.k_weight_head : nullptr;
   // page ids one pass ahead
   auto page_of = [&](int r0) {
@@ -181,12 +194,29 @@ __global__ void __launch_bounds__(NT, NT == 128 ? 5 : 2) paged_write_kernel(cons
       const uint4* ks = reinterpret_cast<const uint4*>(static_cast<const char*>(p.k_new) + ((size_t)tok * p.k_new_token + (size_t)h * p.k_new_head) * es);
       const uint4* vs = reinterpret_cast<const uint4*>(static_cast<const char*>(p.v_new) + ((size_t)tok * p.v_new_token + (size_t)h * p.v_new_head) * es);
       uint4 ka = a, kc = a, v0 = a, v1 = a;
+      const char* qs = static_cast<const char*>(p.q) + ((size_t)tok * p.q_token + (size_t)h * p.group * p.q_head) * es;
+      char* qd = static_cast<char*>(p.q_out) + ((size_t)tok * p.q_out_token + (size_t)h * p.group * p.q_out_head) * es;
+      uint4 u[4], w[4];
+      auto load_queries = [&](int g) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          u[i] = w[i] = make_uint4(0, 0, 0, 0);
+          if (g + i < p.group && fresh) {
+            const uint4* s = reinterpret_cast<const uint4*>(qs + (size_t)(g + i) * p.q_head * es);
+            u[i] = s[c0];
+            w[i] = s[c1];
+          }
+        }
+      };
       float cs[8], sn[8];
       if (fresh) {
         ka = __ldg(ks + c0);
         kc = __ldg(ks + c1);
         v0 = __ldg(vs + 2 * l);
         v1 = __ldg(vs + 2 * l + 1);
+      }
+      if (p.q) load_queries(0);
+      if (fresh) {
         if (rotate) {
           const unsigned long long x = (unsigned long long)(p.positions ? __ldg(p.positions + tok) : t);
 #pragma unroll
@@ -226,29 +256,14 @@ __global__ void __launch_bounds__(NT, NT == 128 ? 5 : 2) paged_write_kernel(cons
         a = pack_piece<T>(x);
         c = pack_piece<T>(x + 8);
         if (ok) {
-          uint4* kd = reinterpret_cast<uint4*>(static_cast<char*>(p.k) + at * es);
-          uint4* vd = reinterpret_cast<uint4*>(static_cast<char*>(p.v) + at * es);
-          kd[c0] = a;
-          kd[c1] = c;
-          vd[2 * l] = v0;
-          vd[2 * l + 1] = v1;
+          put_pieces(static_cast<char*>(p.k) + at * es, c0, c1, wide, a, c);
+          put_pieces(static_cast<char*>(p.v) + at * es, 2 * l, 2 * l + 1, NT == 128 && wp.wide, v0, v1);
         }
       }
       if (p.q) {
-        const char* qs = static_cast<const char*>(p.q) + ((size_t)tok * p.q_token + (size_t)h * p.group * p.q_head) * es;
-        char* qd = static_cast<char*>(p.q_out) + ((size_t)tok * p.q_out_token + (size_t)h * p.group * p.q_out_head) * es;
         // four heads at a time, all loads before the stores (plain loads: q_out may be q itself)
         for (int g = 0; g < p.group; g += 4) {
-          uint4 u[4], w[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            u[i] = w[i] = make_uint4(0, 0, 0, 0);
-            if (g + i < p.group && fresh) {
-              const uint4* s = reinterpret_cast<const uint4*>(qs + (size_t)(g + i) * p.q_head * es);
-              u[i] = s[c0];
-              w[i] = s[c1];
-            }
-          }
+          if (g > 0) load_queries(g);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             if (g + i < p.group) {
@@ -258,9 +273,7 @@ __global__ void __launch_bounds__(NT, NT == 128 ? 5 : 2) paged_write_kernel(cons
               if (wp.q_weight) norm16<LPR>(z, wp.q_weight + (h * p.group + g + i) * wp.q_weight_head, c0, c1, wp.eps);
               if (fresh) {
                 if (rotate) rotate16(z, cs, sn, p.pairs);
-                uint4* o = reinterpret_cast<uint4*>(qd + (size_t)(g + i) * p.q_out_head * es);
-                o[c0] = pack_piece<T>(z);
-                o[c1] = pack_piece<T>(z + 8);
+                put_pieces(qd + (size_t)(g + i) * p.q_out_head * es, c0, c1, wide, pack_piece<T>(z), pack_piece<T>(z + 8));
               }
             }
         }
@@ -346,7 +359,16 @@ static cudaError_t launch_write_d(const WriteProblem& p, cudaStream_t st) {
   return p.held.k_scales ? launch_write_t<T, D, true>(p, st) : launch_write_t<T, D, false>(p, st);
 }
 
-cudaError_t launch_paged_write(const WriteProblem& p, bool bf16, cudaStream_t st) {
+cudaError_t launch_paged_write(const WriteProblem& q, bool bf16, cudaStream_t st) {
+  WriteProblem p = q;
+  const AppendProblem& a = p.a;
+  uintptr_t bits = reinterpret_cast<uintptr_t>(a.q_out);
+  long long strides = a.q ? a.q_out_token | a.q_out_head : 0;
+  if (!p.held.k_scales) {
+    bits |= reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v);
+    strides |= a.stride_page | a.stride_head | a.stride_token;
+  }
+  p.wide = (bits & 31u) == 0 && (strides & 15) == 0;
   if (p.a.d == 64) return bf16 ? launch_write_d<Bf16, 64>(p, st) : launch_write_d<Fp16, 64>(p, st);
   return bf16 ? launch_write_d<Bf16, 128>(p, st) : launch_write_d<Fp16, 128>(p, st);
 }
