@@ -13,8 +13,9 @@ LIB = os.path.join(HERE, "libtkphi.so")
 SOURCES = ["api.cu", "score.cu", "select_cluster.cu", "exact_residual.cu", "build_summaries.cu", "static_scratch.cu",
            "selftest.cu", "cached_features.cu",
            "mlp_features.cu", "mlp_query.cu", "paged_api.cu", "paged_append.cu", "paged_rows.cu",
-           "paged_tiles.cu", "paged_select.cu", "paged_write.cu", "paged_read.cu"]
-HEADERS = ["common.cuh", "sm100.cuh", "feature_jobs.cuh", "host.cuh", "paged.cuh", "paged_walk.cuh", "held8.cuh", os.path.join("..", "..", "include", "tkphi.h")]
+           "paged_tiles.cu", "paged_select.cu", "paged_write.cu", "paged_read.cu", "paged8_rows.cu"]
+HEADERS = ["common.cuh", "sm100.cuh", "feature_jobs.cuh", "host.cuh", "paged.cuh", "paged_walk.cuh", "held8.cuh",
+           os.path.join("..", "..", "include", "tkphi.h")]
 
 
 BINDING = os.path.join(HERE, "_paged_binding.so")

@@ -231,3 +231,13 @@ def test_calls_that_the_binding_refuses(lib):
         T.CacheRows([0, 1], [0, 0])
     with pytest.raises(AssertionError):
         T.CacheRows([0, 1], None, first_dev=torch.zeros(1, dtype=torch.int64))
+
+
+def test_the_build_takes_every_kernel_source():
+    import os
+
+    from paper_2604_05438_b200 import build
+
+    assert sorted(f for f in os.listdir(build.CSRC) if f.endswith(".cu")) == sorted(build.SOURCES)
+    assert sorted(f for f in os.listdir(build.CSRC) if f.endswith(".cuh")) == sorted(os.path.basename(h) for h in build.HEADERS
+                                                                                      if h.endswith(".cuh"))
