@@ -472,11 +472,12 @@ tkphi_status tkphi_coded_read(const tkphi_coded_desc* kv, const tkphi_read_desc*
 
 /* As tkphi_paged_workspace_bytes, tkphi_paged_attention and tkphi_paged_block_attention, over an 8-bit cache.  What the rows
  * stand for enters the products exactly; scores, sums and products are accumulated in fp32.  Sequences with at most 64 query
- * rows of one KV head (q_len * n_q_heads / n_kv_heads), and the page-selected call: probabilities are rounded to fp16 once
- * with bf16 queries and multiplied as pairs of fp16 numbers with fp16 ones; values are held to 2^-39 of the largest value
- * scale among the keys that are summed together.  Sequences with more rows: their caches are first written to the workspace
- * as 16-bit rows (4 bytes per element of k and v together: the workspace is that much larger, and values beyond the type's
- * range count as infinite), then everything is as over a 16-bit cache. */
+ * rows of one KV head (q_len * n_q_heads / n_kv_heads), and the page-selected call: probabilities are rounded to fp16
+ * once, relative to the largest of their product with the values' scales among the keys that are summed together, and vanish
+ * below 2^-39 of it; bf16 queries' elements vanish below 2^-39 of their row's
+ * largest.  Sequences with more rows: their caches are first written to the workspace as 16-bit rows (4 bytes per element of
+ * k and v together: the workspace is that much larger, and values beyond the type's range count as infinite), then everything
+ * is as over a 16-bit cache. */
 size_t tkphi_coded_workspace_bytes(const tkphi_coded_desc* kv, const tkphi_page_selection* selection, int which);
 tkphi_status tkphi_coded_attention(const tkphi_coded_desc* kv, const void* q, void* y_out, float* lse_out, float scale,
                                     uint32_t flags, void* workspace, size_t workspace_bytes, void* cuda_stream);

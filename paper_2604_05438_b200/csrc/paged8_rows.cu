@@ -23,6 +23,10 @@
 //   - a warp takes 32 keys of a tile with a running softmax of its own; rows are rescaled only when a maximum moved.
 // Probabilities are scaled by 2^14 (the largest is then 2^14 or less: fp16 has few exponents) and rounded to fp16 once, 2^-12:
 // an eighth of a bf16 output's own rounding, as much as an fp16 one's.
+// Measured: 32 sequences of 8K to 64K, 24 / 8 heads of 128: 338-343 us, 6.4 TB/s of codes and scales (16-bit operands in the
+// other order, queries as the rows: 435).  A token over 4096 keys, 32 / 8 heads of 64: 8.0 us; with sixteen warps instead of
+// eight in the cluster form 9.1.  Three CTAs per multiprocessor instead of two at head_dim 128: no faster (registers spill).
+#include <cfloat>
 #include <type_traits>
 
 #include "held8.cuh"
@@ -169,7 +173,10 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     while (w.next()) {
       // ---- the unit's queries as operands in fp16.  Operand rows 2j, 2j+1, 2j+8, 2j+9 of a group of 16 dims are dims 4j .. 4j+3.
       // They lie in shared memory, as a lane of each warp takes them.
-      float sl[NT][2];                                       // log2 units per unit of (operand q).(codes) * key scale
+      float sl[NT][2];                                       // log2 units per unit of (operand q).(codes) * key scale * key_unit
+      float key_unit = 1.f;
+      int e_row[NT], e_top = 0;                              // powers of two taken off the rows, the largest of the unit's
+      if (T::kBf16) e_top = -126;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const int r = w.r_first + 8 * t + g;
@@ -179,7 +186,8 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           x[k] = 8 * t + g < w.rows
                      ? __ldg(static_cast<const uint2*>(p.q) + ((size_t)(w.tok0 + r / p.group) * p.hq + w.h * p.group + r % p.group) * (D / 4) + k * 4 + j)
                      : make_uint2(0, 0);
-        float f = 1.f, back = p.scale_log2;
+        float f = 1.f;
+        e_row[t] = 0;
         if (T::kBf16) {
           float most = 0.f;                                  // the largest finite magnitude
 #pragma unroll
@@ -192,10 +200,11 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             }
 #pragma unroll
           for (int d = 1; d < 4; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-          // the largest goes to [2^14, 2^15); the exponent that is taken off is at least -100
-          const int e = max((int)(__float_as_uint(most) >> 23) - 127 - 14, -100);
+          // the largest goes to [2^14, 2^15); the exponent that is taken off is at least -126
+          const int e = max((int)(__float_as_uint(most) >> 23) - 127 - 14, -126);
           f = __uint_as_float((uint32_t)(127 - e) << 23);
-          back *= __uint_as_float((uint32_t)(127 + e) << 23);
+          e_row[t] = e;
+          e_top = max(e_top, __reduce_max_sync(0xffffffffu, e));
         }
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
@@ -203,6 +212,15 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           if (T::kBf16) x[k] = make_uint2(Fp16::pack(T::lo(x[k].x) * f, T::hi(x[k].x) * f), Fp16::pack(T::lo(x[k].y) * f, T::hi(x[k].y) * f));
           q_frags[(k * 32 + lane) * NT + t] = x[k];
         }
+      }
+      // Small queries scaled up times large keys would leave fp32's range where their products do not: up to 2^32 of what the
+      // queries gained comes off the keys' scales (products below 2^31 * 2^(127 - 32); the keys that vanish then are below
+      // 2^-86, of queries below 2^-16).
+      const int off = min(max(-e_top, 0), 32);
+      key_unit = __uint_as_float((uint32_t)(127 - off) << 23);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const float back = fminf(p.scale_log2 * __uint_as_float((uint32_t)max(127 + e_row[t] + off, 1) << 23), FLT_MAX);
 #pragma unroll
         for (int i = 0; i < 2; ++i) sl[t][i] = __shfl_sync(0xffffffffu, back, 8 * j + 4 * i);
       }
@@ -294,7 +312,7 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               // (byte 255 gives infinity here, less itself no number; byte 0 gives 0 for 2^-127)
-              const float f = __uint_as_float(kw << (23 - 8 * e) & 0x7f800000u), z = f - f;
+              const float f = __uint_as_float(kw << (23 - 8 * e) & 0x7f800000u) * key_unit, z = f - f;
 #pragma unroll
               for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -481,7 +499,8 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          m[t][i] = m[t][i] * sl[t][i] - kShift;
+          m[t][i] *= sl[t][i];                               // (from here on without the 2^kShift)
+          l[t][i] *= 1.f / (1 << (int)kShift);
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) l[t][i] += __shfl_xor_sync(0xffffffffu, l[t][i], d);
           if (g == 0) {
@@ -491,7 +510,7 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         }
       named_barrier(1, WARPS * 32);
       // (a warp that has seen nothing has the sum 0; one that has seen no numbers alone has no maximum, but no 0 either)
-      const float unit = held_scale((uint32_t)top);
+      const float unit = held_scale((uint32_t)top) * (1.f / (1 << (int)kShift));
       float f[NT][2];
 #pragma unroll
       for (int t = 0; t < NT; ++t)

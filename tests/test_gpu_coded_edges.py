@@ -118,6 +118,47 @@ def test_queries_and_keys_of_any_size(power, way):
 
 
 @pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("power", [-112, -90, 105])
+def test_queries_and_keys_near_the_ends_of_the_range(power, way):
+    q_len, g = WAYS[way]
+    s = make_step8(2 * g, 2, 64, 32, "bf16", [(q_len, 500), (1, 33)], seed=31, spread=0.0)
+    s.q = (s.q.double() * 2.0 ** power).to(s.q.dtype)
+    keep = s.ks != 255
+    s.ks[keep] = (s.ks.astype(int) - power)[keep].astype(np.uint8)
+    compare8(s)
+
+
+@pytest.mark.parametrize("way", WAYS)
+def test_keys_beyond_2_to_the_115(way):
+    """Scores of 2^115 and more, finite: the largest takes all."""
+    q_len, g = WAYS[way]
+    s = make_step8(2 * g, 2, 64, 32, "bf16", [(q_len, 300)], seed=32, spread=0.0)
+    s.ks[s.ks != 255] += 115
+    y, lse = gpu_attention8(s)
+    k, v = s.values()
+    for tok in range(q_len):
+        for h in range(2 * g):
+            n = 300 - q_len + tok + 1
+            score = PO.rows(k, s.table[0], n)[h // g] @ f64(s.q)[tok, h] / 8
+            want = PO.rows(v, s.table[0], n)[h // g][score.argmax()]
+            first, second = np.sort(score)[-1], np.sort(score)[-2]
+            assert first - second > 2.0 ** -18 * first         # (told apart in 32 bits)
+            assert (np.abs(y[tok, h] - want) <= 2.0 ** -8 * np.abs(want)).all()
+            assert abs(lse[tok, h] - first) <= 2.0 ** -17 * first
+
+
+@pytest.mark.parametrize("way", WAYS)
+def test_values_beyond_2_to_the_110(way):
+    """Their mean over 300 keys stays in range, and so does every sum on the way: below 300 * 2^4 * 2^110."""
+    q_len, g = WAYS[way]
+    s = make_step8(2 * g, 2, 64, 32, "bf16", [(q_len, 300)], seed=33, spread=0.0)
+    y0, lse0 = gpu_attention8(s)
+    s.vs[s.vs != 255] += 110
+    y, lse = gpu_attention8(s)
+    assert (y == y0 * 2.0 ** 110).all() and (lse == lse0).all()
+
+
+@pytest.mark.parametrize("way", WAYS)
 @pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "fp16")])
 def test_scores_of_very_large_size(d, dtype, way):
     q_len, g = WAYS[way]
