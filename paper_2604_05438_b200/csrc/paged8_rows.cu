@@ -220,7 +220,8 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       key_unit = __uint_as_float((uint32_t)(127 - off) << 23);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const float back = fminf(p.scale_log2 * __uint_as_float((uint32_t)max(127 + e_row[t] + off, 1) << 23), FLT_MAX);
+        // (not 0, not infinite: either would make no numbers of infinite and of equal scores)
+        const float back = fminf(fmaxf(p.scale_log2 * __uint_as_float((uint32_t)max(127 + e_row[t] + off, 1) << 23), FLT_TRUE_MIN), FLT_MAX);
 #pragma unroll
         for (int i = 0; i < 2; ++i) sl[t][i] = __shfl_sync(0xffffffffu, back, 8 * j + 4 * i);
       }

@@ -9,7 +9,7 @@ import torch
 
 from oracle import paged8_oracle as P8
 from oracle import paged_oracle as PO
-from paged8_utils import E8, F8, bounds_of, device_cache, gpu_attention8, make_step8, to_device8
+from paged8_utils import E8, F8, bounds_of, device_cache, gpu_attention8, gpu_block_attention8, make_step8, to_device8
 from paged_utils import DT, check_attention, f64
 
 pytestmark = pytest.mark.gpu
@@ -44,6 +44,20 @@ def at(s, b, t):
 @pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "fp16")])
 def test_every_group(d, dtype, hq, hkv):
     compare8(make_step8(hq, hkv, d, 64, dtype, [(1, 1500), (3, 77), (6, 400), (20, 2100)], seed=20))
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 1), (9, 1), (12, 1), (16, 1), (32, 2)])
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "bf16"), (64, "fp16"), (128, "fp16")])
+@pytest.mark.parametrize("lens", [[(1, 1500), (3, 77), (6, 400)],                 # few units: clusters
+                                  [(40, 3000)] + [(1, 900 + 64 * i) for i in range(90)]])     # many: pieces of a line
+def test_every_group_over_selected_pages(lens, d, dtype, hq, hkv):
+    sink, tail, topk, ps = 1, 2, 4, 64
+    s = make_step8(hq, hkv, d, ps, dtype, lens, seed=35, with_bounds=True)
+    y, lse, idx = gpu_block_attention8(s, sink, tail, topk)
+    k, v = s.values()
+    wy, wl, A, C, pages = PO.block_attention(f64(s.q), k, v, s.table, s.kv_lens, s.cu_q, f64(s.bounds), sink, tail, topk)
+    assert (idx == pages).all()
+    check_attention(dtype, d, y, lse, wy, wl, A, C, (sink + tail + topk) * ps)
 
 
 def test_a_very_long_sequence():
@@ -145,6 +159,19 @@ def test_keys_beyond_2_to_the_115(way):
             assert first - second > 2.0 ** -18 * first         # (told apart in 32 bits)
             assert (np.abs(y[tok, h] - want) <= 2.0 ** -8 * np.abs(want)).all()
             assert abs(lse[tok, h] - first) <= 2.0 ** -17 * first
+
+
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("scale,power", [(1e-20, None), (2.0 ** -100, None), (2.0 ** 100, 60), (2.0 ** 60, -60)])
+def test_scales_of_any_size(scale, power, way):
+    """Queries of zeros with a very small scale: every key counts the same.  Others with a very large one: finite scores are
+    told apart, or (their product with the scale is of usual size) as ever."""
+    q_len, g = WAYS[way]
+    s = make_step8(2 * g, 2, 64, 32, "bf16", [(q_len, 300), (1, 5)], seed=34, spread=0.0)
+    s.q = torch.zeros_like(s.q) if power is None else (s.q.double() * 2.0 ** power).to(s.q.dtype)
+    if power == 60:
+        s.k[:] = 0                                           # scores of 0 times 2^100
+    compare8(s, scale=scale)
 
 
 @pytest.mark.parametrize("way", WAYS)
