@@ -54,6 +54,7 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kScoreThreads, 2) paged_score_kernel(const __grid_constant__ PagedProblem p) {
   constexpr int CH = D / 32;                 // 16-byte pieces of a lane per bound
   __shared__ int s_find[2];
+  __shared__ uint4 s_q[2 * CH][2][32];       // [step of 16 dims][q+, q-][lane]
   __shared__ int s_mag[16], s_min[16], s_max[16];      // per token: largest magnitude; smallest and largest ordered score
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int gp = padded_group(p.group), tpt = kRowTile / gp;         // tokens of a tile
@@ -86,7 +87,7 @@ __global__ void __launch_bounds__(kScoreThreads, 2) paged_score_kernel(const __g
   if (last.n <= p.topk || j0 >= last.n) return;          // all are taken, or none is left for this CTA
   const int n_all = last.n, stride = gridDim.y * kScorePages;
   const int* table = p.table + (size_t)b * p.max_pages + last.first;
-  int ids[2];                                // of this round's pages; the next round's are fetched a round ahead
+  int ids[2];                                // of the pages whose bounds are loaded next
   auto load_ids = [&](int j) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -96,25 +97,16 @@ __global__ void __launch_bounds__(kScoreThreads, 2) paged_score_kernel(const __g
   };
   load_ids(j0);
 
-  // ---- query rows as A operands: q+ against hi, q- against lo
+  // ---- query rows as A operands: q+ against hi, q- against lo, in shared memory as a lane takes them; a warp makes one step's
   const int r = lane >> 2, kq = lane & 3;
-  uint32_t ap[CH][2][4], an[CH][2][4];
+  uint2 q_own[2] = {make_uint2(0, 0), make_uint2(0, 0)};
+  if (warp < 2 * CH) {
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const int row = r + half * 8, t = row / gp, g = row % gp;
-    const bool live = t < n_tok && g < p.group;
-    const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.q) + ((size_t)(tok0 + (live ? t : 0)) * p.hq + h * p.group + (live ? g : 0)) * D);
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const uint4 v = live ? __ldg(q + kq + 4 * i) : make_uint4(0, 0, 0, 0);
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        // fragment e & 1 of the step e >> 1: registers half (dims 2k, 2k+1) and 2 + half (the upper eight)
-        const uint32_t neg = T::min2(w[e], 0u), pos = T::max2(w[e], 0u);
-        ap[i][e >> 1][(e & 1) * 2 + half] = pos;
-        an[i][e >> 1][(e & 1) * 2 + half] = neg;
-      }
+    for (int half = 0; half < 2; ++half) {
+      const int row = r + half * 8, t = row / gp, g = row % gp;
+      if (t < n_tok && g < p.group)
+        q_own[half] = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p.q) + ((size_t)(tok0 + t) * p.hq + h * p.group + g) * D) +
+                            2 * (kq + 4 * (warp >> 1)) + (warp & 1));
     }
   }
   const uint4* bounds = static_cast<const uint4*>(p.bounds) + (size_t)h * (2 * D / 8) + kq;
@@ -130,19 +122,28 @@ __global__ void __launch_bounds__(kScoreThreads, 2) paged_score_kernel(const __g
   float* keysA = p.page_scores + ((size_t)(tok0 + tA) * p.hkv + h) * p.key_stride;
   float* keysB = p.page_scores + ((size_t)(tok0 + tB) * p.hkv + h) * p.key_stride;
   float magA = 0.f, magB = 0.f, minA = INFINITY, minB = INFINITY, maxA = -INFINITY, maxB = -INFINITY;
+  // A warp's two steps of a round each have a buffer, which is filled with the next round's bounds as soon as it has been used.
+  uint4 lo[2][CH], hi[2][CH];
+  bool ok[2];
+  auto load_bounds = [&](int s) {
+    const int phys = ids[s];
+    ok[s] = phys >= 0 && phys < p.n_pages;
+    if (!ok[s] && kq == 0) atomicExch(p.status, kStatusBadPage);
+    const uint4* src = bounds + (ok[s] ? phys : 0) * page_step;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) { lo[s][i] = __ldg(src + 4 * i); hi[s][i] = __ldg(src + D / 8 + 4 * i); }
+  };
+  load_bounds(0);
+  load_bounds(1);
+  load_ids(j0 + stride);
+  if (warp < 2 * CH) {
+    // registers of a fragment: rows r and r + 8 of the lower eight dims of the step, then of the upper eight
+    const uint2 a = q_own[0], c = q_own[1];
+    s_q[warp][0][lane] = make_uint4(T::max2(a.x, 0u), T::max2(c.x, 0u), T::max2(a.y, 0u), T::max2(c.y, 0u));
+    s_q[warp][1][lane] = make_uint4(T::min2(a.x, 0u), T::min2(c.x, 0u), T::min2(a.y, 0u), T::min2(c.y, 0u));
+  }
+  __syncthreads();
   for (; j0 < n_all; j0 += stride) {
-    uint4 lo[2][CH], hi[2][CH];
-    bool ok[2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int phys = ids[s];
-      ok[s] = phys >= 0 && phys < p.n_pages;
-      if (!ok[s] && kq == 0) atomicExch(p.status, kStatusBadPage);
-      const uint4* src = bounds + (ok[s] ? phys : 0) * page_step;
-#pragma unroll
-      for (int i = 0; i < CH; ++i) { lo[s][i] = __ldg(src + 4 * i); hi[s][i] = __ldg(src + D / 8 + 4 * i); }
-    }
-    load_ids(j0 + stride);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       float v[4] = {0.f, 0.f, 0.f, 0.f}, m[4] = {0.f, 0.f, 0.f, 0.f};
@@ -152,13 +153,17 @@ __global__ void __launch_bounds__(kScoreThreads, 2) paged_score_kernel(const __g
         const uint32_t* wh = reinterpret_cast<const uint32_t*>(&hi[s][i]);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          T::mma(v, ap[i][u], wh[2 * u], wh[2 * u + 1]);
-          T::mma(v, an[i][u], wl[2 * u], wl[2 * u + 1]);
+          const uint4 x = s_q[2 * i + u][0][lane], y = s_q[2 * i + u][1][lane];
+          const uint32_t ap[4] = {x.x, x.y, x.z, x.w}, an[4] = {y.x, y.y, y.z, y.w};
+          T::mma(v, ap, wh[2 * u], wh[2 * u + 1]);
+          T::mma(v, an, wl[2 * u], wl[2 * u + 1]);
           // magnitudes: q+ |hi| and q- (-|lo|)
-          T::mma(m, ap[i][u], wh[2 * u] & 0x7fff7fffu, wh[2 * u + 1] & 0x7fff7fffu);
-          T::mma(m, an[i][u], wl[2 * u] | 0x80008000u, wl[2 * u + 1] | 0x80008000u);
+          T::mma(m, ap, wh[2 * u] & 0x7fff7fffu, wh[2 * u + 1] & 0x7fff7fffu);
+          T::mma(m, an, wl[2 * u] | 0x80008000u, wl[2 * u + 1] | 0x80008000u);
         }
       }
+      const unsigned bad = __ballot_sync(0xffffffffu, !ok[s]);
+      if (j0 + stride < n_all) load_bounds(s);
       // rows of padding repeat nothing of a real row: they must not win
       if (r % gp >= p.group) { v[0] = v[1] = -INFINITY; if (gp < 16) v[2] = v[3] = -INFINITY; }
       if (gp == 16 && 8 + r >= p.group) v[2] = v[3] = -INFINITY;
@@ -174,7 +179,6 @@ __global__ void __launch_bounds__(kScoreThreads, 2) paged_score_kernel(const __g
         for (int e = 0; e < 2; ++e) { v[e] = fmaxf(v[e], v[2 + e]); m[e] = max_nan(m[e], m[2 + e]); }
       }
       // a page with a bad id comes last (its lanes hold page r, its results are in lanes of every row)
-      const unsigned bad = __ballot_sync(0xffffffffu, !ok[s]);
       const int j = j0 + warp * 16 + s * 8 + 2 * kq;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -189,6 +193,7 @@ __global__ void __launch_bounds__(kScoreThreads, 2) paged_score_kernel(const __g
         }
       }
     }
+    load_ids(j0 + 2 * stride);
   }
   // each token's largest magnitude and range of scores here (non-negative floats order like their bits, NaN last)
   auto note = [&](int t, float mag, float lo, float hi) {
