@@ -23,7 +23,7 @@
 //   - a warp takes 32 keys of a tile with a running softmax of its own; rows are rescaled only when a maximum moved.
 // Probabilities are scaled by 2^14 (the largest is then 2^14 or less: fp16 has few exponents) and rounded to fp16 once, 2^-12:
 // an eighth of a bf16 output's own rounding, as much as an fp16 one's.
-// Measured: 32 sequences of 8K to 64K, 24 / 8 heads of 128: 338-343 us, 6.4 TB/s of codes and scales (16-bit operands in the
+// Measured: 32 sequences of 8K to 64K, 24 / 8 heads of 128: 338-348 us, 6.2-6.4 TB/s of codes and scales (16-bit operands in the
 // other order, queries as the rows: 435).  A token over 4096 keys, 32 / 8 heads of 64: 8.0 us; with sixteen warps instead of
 // eight in the cluster form 9.1.  Three CTAs per multiprocessor instead of two at head_dim 128: no faster (registers spill).
 #include <cfloat>

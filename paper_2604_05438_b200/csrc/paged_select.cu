@@ -49,7 +49,9 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 
 // Bounds of all candidate pages.  A tile of the matrix instruction is 16 query rows x 8 pages; a lane reads 16 bytes of
 // its page at a time and uses them as they lie: which of the 16 terms of a step an element is does not matter as long as
-// the query's fragment holds its partner there.  Bound: DRAM, the bounds are read once per tile of rows.
+// the query's fragment holds its partner there.  Bound: the chain of a round (page ids, bounds, products) at two CTAs per
+// multiprocessor; the next round's bounds are on the way meanwhile.  32 tokens over 8K-64K, 24 / 8 heads of 128: 26 us (29
+// without that, its registers taken by query fragments); the bounds are read once per tile of rows.
 template <typename T, int D>
 __global__ void __launch_bounds__(kScoreThreads, 2) paged_score_kernel(const __grid_constant__ PagedProblem p) {
   constexpr int CH = D / 32;                 // 16-byte pieces of a lane per bound
