@@ -475,7 +475,7 @@ tkphi_status tkphi_coded_read(const tkphi_coded_desc* kv, const tkphi_read_desc*
  * rows of one KV head (q_len * n_q_heads / n_kv_heads), and the page-selected call: probabilities are rounded to fp16
  * once, relative to the largest of their product with the values' scales among the keys that are summed together, and vanish
  * below 2^-39 of it; bf16 queries' elements vanish below 2^-39 of their row's
- * largest.  Sequences with more rows: their caches are first written to the workspace as 16-bit rows (4 bytes per element of
+ * largest; keys whose scale byte is 0 score 0.  Sequences with more rows: their caches are first written to the workspace as 16-bit rows (4 bytes per element of
  * k and v together: the workspace is that much larger, and values beyond the type's range count as infinite), then everything
  * is as over a 16-bit cache. */
 size_t tkphi_coded_workspace_bytes(const tkphi_coded_desc* kv, const tkphi_page_selection* selection, int which);
