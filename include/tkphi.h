@@ -472,9 +472,9 @@ tkphi_status tkphi_coded_read(const tkphi_coded_desc* kv, const tkphi_read_desc*
 
 /* As tkphi_paged_workspace_bytes, tkphi_paged_attention and tkphi_paged_block_attention, over an 8-bit cache.  What the rows
  * stand for enters the products exactly; scores, sums and products are accumulated in fp32.  Sequences with at most 64 query
- * rows of one KV head (q_len * n_q_heads / n_kv_heads), and the page-selected call: probabilities are rounded to fp16
- * once, relative to the largest of their product with the values' scales among the keys that are summed together, and vanish
- * below 2^-39 of it; bf16 queries' elements vanish below 2^-39 of their row's
+ * rows of one KV head (q_len * n_q_heads / n_kv_heads), and the page-selected call: a probability's product with its value's
+ * scale is rounded to fp16 once, and vanishes below 2^-29 of the largest such product of the query row's visible keys (keys that
+ * it does not see have no part in that); bf16 queries' elements vanish below 2^-39 of their row's
  * largest; keys whose scale byte is 0 score 0.  Sequences with more rows: their caches are first written to the workspace as 16-bit rows (4 bytes per element of
  * k and v together: the workspace is that much larger, and values beyond the type's range count as infinite), then everything
  * is as over a 16-bit cache. */

@@ -16,13 +16,18 @@
 //     and outputs are laid out to match, so that nothing is rearranged but one byte permutation per word of values.
 //     (e4m3 instructions for the first product, with queries as sums of two or three codes, need no conversion of keys, but
 //     took 1.2x the time: they issue as more instructions.)
-//   - a key's power of two multiplies its score; a value's multiplies its probability, relative to the largest of the
-//     values that the warp has met (the outputs are rescaled when that grows), so that the fp16 operand stays in range.
+//   - a key's power of two multiplies its score; a value's multiplies its probability, in units of the row's reference: a power
+//     of two that the row's largest product of the two does not exceed and is at most 2^10 below, so that the products that
+//     count are normal numbers of the fp16 operand, whatever the sizes of values that nothing attends to or of later tokens'
+//     values.  Scales below the reference change nothing in that, unless a maximum moves to a key with a very small one.  So a
+//     warp, whose rows have one reference as a rule, looks for scales above it only; where there is one, each row takes the
+//     reference that its own keys allow, with room for larger scales, and its outputs follow.
 //   - bf16 queries are brought into fp16's range by a power of two per row, which the softmax scale takes back; elements
 //     below 2^-39 of the row's largest vanish.
 //   - a warp takes 32 keys of a tile with a running softmax of its own; rows are rescaled only when a maximum moved.
-// Probabilities are scaled by 2^14 (the largest is then 2^14 or less: fp16 has few exponents) and rounded to fp16 once, 2^-12:
-// an eighth of a bf16 output's own rounding, as much as an fp16 one's.
+// Probabilities are scaled by 2^14 (a row's largest product is then from 2^4 to 2^15: fp16 has few exponents) and rounded to
+// fp16 once, 2^-12: an eighth of a bf16 output's own rounding, as much as an fp16 one's.  Products below 2^-29 of the row's
+// largest vanish.
 // Measured: 32 sequences of 8K to 64K, 24 / 8 heads of 128: 338-348 us, 6.2-6.4 TB/s of codes and scales (16-bit operands in the
 // other order, queries as the rows: 435).  A token over 4096 keys, 32 / 8 heads of 64: 8.0 us; with sixteen warps instead of
 // eight in the cluster form 9.1.  Three CTAs per multiprocessor instead of two at head_dim 128: no faster (registers spill).
@@ -77,6 +82,9 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   using Walk = RowWalk<BLOCK, SPLIT, kHeldKeys>;
   constexpr int WARPS = C::WARPS, NS = C::NS, ROWS = C::ROWS;
   constexpr float kShift = 14.f;                            // p = 2^kShift exp2(..)
+  constexpr int kLoose = 10;                                // powers of two that a row's reference may be above its largest product
+  constexpr int kRoom = 3;                                  // .. and is above the scales where that allows it
+  constexpr int kNone = -10000;
   extern __shared__ __align__(1024) unsigned char smem[];
   uint2* q_frags = reinterpret_cast<uint2*>(smem + C::frags);
   float* red = reinterpret_cast<float*>(smem + C::red);
@@ -248,7 +256,12 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         m[t][0] = m[t][1] = -INFINITY;
         l[t][0] = l[t][1] = 0.f;
       }
-      int top = 0;                                           // the outputs' unit is 2^(top - 127)
+      // A row's outputs are in units of 2^(reference - 127), and so are the values' scales in its probabilities' operands: `top`
+      // for all rows, or (mixed) one for each, of which it is the largest (in this warp's part of stat, since it is seldom used).
+      // Each row's largest product so far is 2^(low - 127) at least, top - kLoose <= low (mixed: 2^(its reference - kLoose - 127)).
+      int top = 0, low = 0;
+      bool mixed = false, fresh = true;                      // fresh: no keys yet
+      int* refs = reinterpret_cast<int*>(stat) + (warp * ROWS + 2 * j) * 2;      // this thread's rows: [16 t + 2 i]
 
       for (int tile = w.t0; tile < w.t1; ++tile, ++it) {
         if (SPLIT && (it & 1) != warp >> 2) continue;
@@ -272,9 +285,33 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             else key0[x] = w.len;                                                // past the list
           }
         }
-        // (two copies: with keys that some row does not see, and without any)
-        auto step = [&](auto tag) {
+        // the scale bytes of this thread's values, two keys of each group, as pairs of 16 bits
+        const bool all_seen = key0[0] + 15 <= lim_all && key0[1] + 15 <= lim_all;
+        uint32_t v2[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) v2[x] = __byte_perm(*reinterpret_cast<const uint16_t*>(ve + x * 16 + 2 * g), 0, 0x4140);
+        auto smallest = [](uint32_t a, uint32_t b) {
+          const uint32_t u = __vminu2(a, b);
+          return (int)__reduce_min_sync(0xffffffffu, min(u & 0xffffu, u >> 16));
+        };
+        auto above_top = [&]() { const uint32_t u = (uint32_t)top * 0x00010001u; return __any_sync(0xffffffffu, __vmaxu2(__vmaxu2(v2[0], v2[1]), u) != u); };
+        bool plain = all_seen && !mixed;
+        if (plain && fresh) {
+          // the first keys: in most cases one reference does for all rows
+          const uint32_t u = __vmaxu2(v2[0], v2[1]);
+          const int most = (int)__reduce_max_sync(0xffffffffu, max(u & 0xffffu, u >> 16));
+          low = smallest(v2[0], v2[1]);
+          plain = most < 255 && most - low <= kLoose;
+          if (plain) { top = min(min(most + kRoom, low + kLoose), 254); fresh = false; }
+        } else if (plain) {
+          plain = !above_top();
+        }
+        // (two copies: with keys that some row does not see or scales that need other references, and without any.  The latter
+        // is the false one, and returns whether the other has to do the tile: nothing has changed then.)
+        auto step = [&](auto tag) -> bool {
           constexpr bool careful = decltype(tag)::value;
+          int least = 0;                                    // the smallest scale byte of the keys that some row sees
+          bool other = mixed || fresh;                      // other references are needed
           bool odd_values = false;                          // NaN codes that not every row sees
           // s[x][t][2 e + i]: key 16 x + 2 g + e of the warp's, row i of this thread's in row tile t
           float s[2][NT][4];
@@ -304,12 +341,9 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 }
             }
           }
-          // this thread's keys, two of each group: scale bytes
-          uint32_t vw[2];
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const uint32_t kw = *reinterpret_cast<const uint16_t*>(ke + x * 16 + 2 * g);
-            vw[x] = *reinterpret_cast<const uint16_t*>(ve + x * 16 + 2 * g);
+            const uint32_t kw = *reinterpret_cast<const uint16_t*>(ke + x * 16 + 2 * g);     // this thread's keys' scale bytes
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               // (byte 255 gives infinity here, less itself no number; byte 0 gives 0 for 2^-127)
@@ -331,8 +365,15 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 #pragma unroll
                   for (int i = 0; i < 2; ++i)
                     if (key > lim[t][i]) s[x][t][2 * e + i] = -INFINITY;
-                if (key > lim_last) vw[x] &= e ? 0x00ffu : 0xff00u;
               }
+            uint32_t unseen[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              unseen[x] = (key0[x] + 2 * g > lim_last ? 0xffffu : 0u) | (key0[x] + 2 * g + 1 > lim_last ? 0xffff0000u : 0u);
+              v2[x] &= ~unseen[x];
+            }
+            least = smallest(v2[0] | unseen[0], v2[1] | unseen[1]);
+            other |= above_top();
             // Values that no row sees may be anything (behind the sequence's end they may be left-overs): 0 times them must
             // not reach the product.  Those that some rows see are looked through.
             constexpr int CPR = D / 16;                     // 16-byte chunks of a row
@@ -344,7 +385,7 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             }
             fence_proxy_async_smem();                       // before the slot's next copy
             __syncwarp();
-            if (!BLOCK && lim_all < lim_last) {
+            if (!BLOCK && !all_seen && lim_all < lim_last) {
               uint32_t bad = 0;
               for (int i = lane; i < 32 * CPR; i += 32) {
                 const uint4 c = *reinterpret_cast<const uint4*>(vs + held_at<D>(kg + i / CPR, i % CPR));
@@ -353,35 +394,6 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
               odd_values = __any_sync(0xffffffffu, bad != 0);
             }
           }
-          // the largest value scale so far; the outputs follow when it grows.  Bytes as pairs of 16 bits.
-          uint32_t v2[2] = {__byte_perm(vw[0], 0, 0x4140), __byte_perm(vw[1], 0, 0x4140)};
-          auto largest = [&]() {
-            const uint32_t u = __vmaxu2(v2[0], v2[1]);
-            return __reduce_max_sync(0xffffffffu, max(u & 0xffffu, u >> 16));
-          };
-          uint32_t most = largest();
-          const bool bad_scale = most == 255u;
-          if (bad_scale) {
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              if ((v2[x] & 0xffffu) == 255u) v2[x] &= 0xffff0000u;
-              if (v2[x] >> 16 == 255u) v2[x] &= 0xffffu;
-            }
-            most = largest();
-          }
-          if ((int)most > top) {
-            const int d = 127 + top - (int)most;
-            const float f = d > 0 ? __uint_as_float((uint32_t)d << 23) : 0.f;
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-              for (int b = 0; b < D / 16; ++b) { o[t][b][0] *= f; o[t][b][1] *= f; o[t][b][2] *= f; o[t][b][3] *= f; }
-            top = (int)most;
-          }
-          // exponent fields of the values' scales over the largest: 127 + byte - top, 0 if that is less
-          const uint32_t least = (uint32_t)max(top - 127, 0) * 0x00010001u, shift = (uint32_t)(127 - top) * 0x00010001u;
-#pragma unroll
-          for (int x = 0; x < 2; ++x) v2[x] = __vmaxu2(v2[x], least) + shift;
           // maxima over the warp's keys.  (They are kept before the scale: the largest score less the maximum is then exactly 0.)
           float best[NT][2];
           bool moved = false;
@@ -395,12 +407,40 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
               best[t][i] = fmaxf(m[t][i], u);
               moved |= best[t][i] > m[t][i];
             }
+          bool had[NT][2], rose[NT][2];                     // the row had a key before; its maximum moved
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) { had[t][i] = m[t][i] > -INFINITY; rose[t][i] = best[t][i] > m[t][i]; }
           if (__any_sync(0xffffffffu, moved)) {
+            // a largest score's key has its value's scale as product
+            if (!careful) least = smallest(v2[0], v2[1]);
+            if (least < top - kLoose) {
+              if (careful) {
+                other = true;
+              } else {
+                // (where that is not another key's)
+                least = 1000;
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                  for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                      for (int e = 0; e < 2; ++e)
+                        if (rose[t][i] && lim[t][i] >= 0 && s[x][t][2 * e + i] == best[t][i])
+                          least = min(least, (int)(e ? v2[x] >> 16 : v2[x] & 0xffffu));
+                least = __reduce_min_sync(0xffffffffu, least);
+                if (least < top - kLoose) return true;
+              }
+            }
+            low = min(low, least);
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
               for (int i = 0; i < 2; ++i) {
-                const float f = best[t][i] > m[t][i] ? ex2_approx((m[t][i] - best[t][i]) * sl[t][i]) : 1.f;
+                const float f = rose[t][i] ? ex2_approx((m[t][i] - best[t][i]) * sl[t][i]) : 1.f;
                 l[t][i] *= f;
 #pragma unroll
                 for (int b = 0; b < D / 16; ++b) { o[t][b][i] *= f; o[t][b][2 + i] *= f; }
@@ -420,16 +460,107 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                   float& a = s[x][t][2 * e + i];
                   a = ex2_approx(fmaf(a - u, sl[t][i], kShift));
                   l[t][i] += a;
-                  a *= __uint_as_float(e ? v2[x] << 7 & 0x7f800000u : v2[x] << 23);
                 }
             }
-          if (bad_scale || careful) {
+          // probabilities times the values' scales
+          if (!careful || !other) {
+            const uint32_t floor2 = (uint32_t)max(top - 127, 0) * 0x00010001u, shift2 = (uint32_t)(127 - top) * 0x00010001u;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const uint32_t w = __vmaxu2(v2[x], floor2) + shift2;      // exponent fields, 0 if that is less
+#pragma unroll
+              for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                  for (int i = 0; i < 2; ++i) s[x][t][2 * e + i] *= __uint_as_float(e ? w << 7 & 0x7f800000u : w << 23);
+            }
+          } else {
+            int most[NT][2], product[NT][2], mine[NT][2];    // of the keys that a row sees: largest byte, largest product; its own `low`
+            int all_product = 0, all_most = -1, all_low = 1000;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const int ref = mixed ? refs[16 * t + 2 * i] : top;
+                int u = -1, v = kNone;
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                  for (int e = 0; e < 2; ++e) {
+                    const int byte = (int)(e ? v2[x] >> 16 : v2[x] & 0xffffu), field = (int)(__float_as_uint(s[x][t][2 * e + i]) >> 23);
+                    if (byte < 255 && key0[x] + 2 * g + e <= lim[t][i]) {
+                      u = max(u, byte);
+                      if (field > 0) v = max(v, field - 127 - (int)kShift + byte);     // (0, or below what 32 bits hold well)
+                    }
+                  }
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) {
+                  u = max(u, __shfl_xor_sync(0xffffffffu, u, d));
+                  v = max(v, __shfl_xor_sync(0xffffffffu, v, d));
+                }
+                most[t][i] = u;
+                product[t][i] = v;
+                // (a new maximum is among the products)
+                mine[t][i] = max(v, rose[t][i] && u >= 0 ? kNone : mixed ? ref - kLoose : low);
+                if (lim[t][i] >= 0 && m[t][i] > -INFINITY) {
+                  all_product = max(all_product, v);
+                  all_most = max(all_most, u);
+                  all_low = min(all_low, mine[t][i]);
+                }
+              }
+            // One reference for all rows if there is one that their largest products allow, with room for larger scales, so that it
+            // seldom moves.  (Not where some rows do not see all keys: those must not matter to them.)
+            all_most = __reduce_max_sync(0xffffffffu, all_most);
+            all_product = max((int)__reduce_max_sync(0xffffffffu, all_product), all_most);
+            all_low = __reduce_min_sync(0xffffffffu, all_low);
+            const int common = min(all_low + kLoose, max(fresh ? 0 : top, all_most + kRoom));
+            const bool same = all_seen && common >= all_product && common <= 254;
+            int ref_max = -1, ref_min = 1000;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                int ref = mixed ? refs[16 * t + 2 * i] : top;
+                if (most[t][i] >= 0) {
+                  const int want = !had[t][i] ? most[t][i] + kRoom : mixed || most[t][i] > ref ? max(top, most[t][i] + kRoom) : top;
+                  const int own = min(max(max(product[t][i], 0), min(mine[t][i] + kLoose, want)), 254), to = same ? common : own;
+                  const int by = ref - to, half = by / 2;
+                  const float f0 = __uint_as_float((uint32_t)(127 + half) << 23), f1 = __uint_as_float((uint32_t)(127 + by - half) << 23);
+#pragma unroll
+                  for (int b = 0; b < D / 16; ++b) { o[t][b][i] = o[t][b][i] * f0 * f1; o[t][b][2 + i] = o[t][b][2 + i] * f0 * f1; }
+                  ref = to;
+                }
+                __syncwarp();
+                refs[16 * t + 2 * i] = ref;                  // (the same from all lanes of the row)
+                if (lim[t][i] >= 0 && m[t][i] > -INFINITY) {
+                  ref_max = max(ref_max, ref);
+                  ref_min = min(ref_min, ref);
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                  for (int e = 0; e < 2; ++e) {
+                    const int byte = (int)(e ? v2[x] >> 16 : v2[x] & 0xffffu);
+                    s[x][t][2 * e + i] *= __uint_as_float((uint32_t)min(max(127 + byte - ref, 0), 254) << 23);
+                  }
+              }
+            ref_max = __reduce_max_sync(0xffffffffu, ref_max);
+            ref_min = __reduce_min_sync(0xffffffffu, ref_min);
+            low = all_low;
+            if (ref_max >= 0) {                              // (some row has a key)
+              mixed = ref_max != ref_min;
+              top = ref_max;
+              fresh = false;
+            }
+          }
+          if (careful) {
 #pragma unroll
             for (int x = 0; x < 2; ++x)
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
                 const int key = key0[x] + 2 * g + e;
-                const bool none = (vw[x] >> (8 * e) & 255u) == 255u;
+                const bool none = (v2[x] >> (16 * e) & 0xffffu) == 255u;
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -488,14 +619,21 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
               }
             }
           }
+          return false;
         };
-        if (key0[0] + 15 <= lim_all && key0[1] + 15 <= lim_all) step(std::false_type());
-        else if (key0[0] <= lim_last || key0[1] <= lim_last) step(std::true_type());
+        if (plain) plain = !step(std::false_type());
+        if (!plain && (key0[0] <= lim_last || key0[1] <= lim_last)) step(std::true_type());
         __syncwarp();
         if (lane == 0) mbar_arrive(&empty[stage]);
       }
 
       // ---- the warps' softmaxes joined; a thread ends up with PER dims of a chunk of one row
+      float unit[NT][2];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) unit[t][i] = held_scale((uint32_t)(mixed ? refs[16 * t + 2 * i] : top)) * (1.f / (1 << (int)kShift));
+      __syncwarp();
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -511,7 +649,6 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         }
       named_barrier(1, WARPS * 32);
       // (a warp that has seen nothing has the sum 0; one that has seen no numbers alone has no maximum, but no 0 either)
-      const float unit = held_scale((uint32_t)top) * (1.f / (1 << (int)kShift));
       float f[NT][2];
 #pragma unroll
       for (int t = 0; t < NT; ++t)
@@ -520,7 +657,7 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           float M = -INFINITY;
 #pragma unroll
           for (int k = 0; k < WARPS; ++k) M = fmaxf(M, stat[(k * ROWS + 8 * t + 2 * j + i) * 2]);
-          f[t][i] = l[t][i] == 0.f ? 0.f : ex2_approx(m[t][i] - M) * unit;
+          f[t][i] = l[t][i] == 0.f ? 0.f : ex2_approx(m[t][i] - M) * unit[t][i];
         }
       constexpr int PER = 16 / WARPS, TPR = C::CHUNK / PER;    // dims of a thread, threads of a row
       const int row = tid / TPR, dp = tid % TPR * PER;
