@@ -412,8 +412,9 @@ tkphi_status tkphi_paged_block_attention(const tkphi_paged_desc* kv, const tkphi
 
 /* Norms of the new tokens' heads, each head on its own: x -> x * weight / sqrt(mean(x^2) + eps), before the rotation.  Weights
  * are fp32 device arrays, 16-byte aligned, [heads][head_dim] with a stride between heads (a multiple of 4 elements, at least
- * head_dim, or 0: one [head_dim] for all).  A NULL side is not normed.  The sum of squares is taken in 32 bits: elements
- * beyond 2^60 overflow it. */
+ * head_dim, or 0: one [head_dim] for all).  A NULL side is not normed.  The sum of squares is taken in 32 bits, of a head
+ * scaled by a power of two where they would not hold it, so that heads of any finite size get their norm.  With eps 0 a head of
+ * zeros becomes NaN (0 / 0). */
 typedef struct {
   const float* q_weight; int64_t q_stride_head;
   const float* k_weight; int64_t k_stride_head;

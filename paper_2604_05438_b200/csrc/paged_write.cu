@@ -66,13 +66,15 @@ __device__ __forceinline__ void rotate16(float (&x)[16], const float (&cs)[8], c
   }
 }
 template <int LPR>
-__device__ __forceinline__ void norm16(float (&x)[16], const float* weight, int c0, int c1, float eps) {
+__device__ __forceinline__ float row_squares(const float (&x)[16]) {
   float s = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) s = fmaf(x[i], x[i], s);
 #pragma unroll
   for (int o = 1; o < LPR; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  const float r = rsqrtf(fmaf(s, 1.f / (16 * LPR), eps));
+  return s;
+}
+__device__ __forceinline__ void weigh16(float (&x)[16], float r, const float* weight, int c0, int c1) {
   float w[16];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -81,6 +83,29 @@ __device__ __forceinline__ void norm16(float (&x)[16], const float* weight, int 
   }
 #pragma unroll
   for (int i = 0; i < 16; ++i) x[i] = x[i] * r * w[i];
+}
+// Norm of a head.  True if the result is not to be used: v = mean(x^2) + eps is right where squares that 32 bits do not hold do not
+// count beside it and none overflows, which leaves out bf16 elements beyond 2^60, or of 2^-40 and less with as small an eps.
+template <typename T, int LPR>
+__device__ __forceinline__ bool norm16(float (&x)[16], const float* weight, int c0, int c1, float eps) {
+  const float v = fmaf(row_squares<LPR>(x), 1.f / (16 * LPR), eps);
+  weigh16(x, rsqrtf(v), weight, c0, c1);
+  return T::kBf16 && !(v >= 0x1p-80f && v < INFINITY);
+}
+// Norm of any head: scaled by a power of two, so that its largest element or the root of eps is about 1.  (A head of zeros without
+// eps, infinities and NaN: as they are.)
+template <int LPR>
+__device__ __forceinline__ void norm16_scaled(float (&x)[16], const float* weight, int c0, int c1, float eps) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
+#pragma unroll
+  for (int o = 1; o < LPR; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+  const uint32_t field = min(max(max(most, __float_as_uint(sqrtf(eps))) >> 23, 1u), 253u);
+  const float f = most < 0x7f800000u ? __uint_as_float((254u - field) << 23) : 1.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] *= f;
+  weigh16(x, rsqrtf(fmaf(row_squares<LPR>(x), 1.f / (16 * LPR), eps * f * f)), weight, c0, c1);
 }
 // Scale byte of the row that LPR lanes hold.
 template <int LPR>
@@ -101,6 +126,128 @@ __device__ __forceinline__ uint4 row_codes(const float (&x)[16], uint32_t e) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// A row's key as the cache holds it, as 16-bit pieces.
+template <typename T, bool HELD>
+__device__ __forceinline__ void held_key(const WriteProblem& wp, size_t at, size_t scale_at, int c0, int c1, uint4& a, uint4& c) {
+  if (HELD) {
+    const uint2* kd = reinterpret_cast<const uint2*>(static_cast<const char*>(wp.a.k) + at);
+    const uint2 k0 = kd[c0], k1 = kd[c1];
+    const float s = held_scale(wp.held.k_scales[scale_at]);
+    const uint2 w0 = held_values<T>(k0.x, s), w1 = held_values<T>(k0.y, s);
+    const uint2 w2 = held_values<T>(k1.x, s), w3 = held_values<T>(k1.y, s);
+    a = make_uint4(w0.x, w0.y, w1.x, w1.y);
+    c = make_uint4(w2.x, w2.y, w3.x, w3.y);
+  } else {
+    const uint4* kd = reinterpret_cast<const uint4*>(static_cast<const char*>(wp.a.k) + at * 2);
+    a = kd[c0];
+    c = kd[c1];
+  }
+}
+// Minimum and maximum over the warp's rows (all of one page).  Lanes without a row take another row's; then the lanes of two rows
+// share the work: one takes the first pieces, the other the second, then one minima, the other maxima.
+template <typename T, int LPR>
+__device__ __forceinline__ void warp_bounds(bool in, const uint4& a, const uint4& c, int c0, int c1, uint4 (*to)[2 * LPR]) {
+  const int lane = threadIdx.x & 31, l = lane % LPR;
+  const unsigned have = __ballot_sync(0xffffffffu, in);
+  if (have == 0) return;
+  uint32_t k[8] = {a.x, a.y, a.z, a.w, c.x, c.y, c.z, c.w};
+  if (have != 0xffffffffu) {
+    const int from = in ? lane : (__ffs(have) - 1) / LPR * LPR + l;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) k[i] = __shfl_sync(0xffffffffu, k[i], from);
+  }
+  const bool second = lane & 16, most = lane & 8;
+  uint32_t m[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t mine = second ? k[4 + i] : k[i], theirs = __shfl_xor_sync(0xffffffffu, second ? k[i] : k[4 + i], 16);
+    const uint32_t lo2 = T::min2(mine, theirs), hi2 = T::max2(mine, theirs);
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, most ? lo2 : hi2, 8);
+    m[i] = most ? T::max2(hi2, other) : T::min2(lo2, other);
+  }
+  if (LPR == 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t other = __shfl_xor_sync(0xffffffffu, m[i], 4);
+      m[i] = most ? T::max2(m[i], other) : T::min2(m[i], other);
+    }
+  }
+  if (LPR == 8 || (lane & 4) == 0) to[most][second ? c1 : c0] = make_uint4(m[0], m[1], m[2], m[3]);
+}
+
+// The heads of the warp's rows that s_again marks, once more, with scaled squares; then those rows' part of the bounds from the cache.
+// One head after the other in one copy of the code, called after everything else, because it is seldom needed: a branch in
+// each norm, or a call in the loop over rows, takes a single token 0.5 to 1.8 us.
+struct AgainRows {
+  int h, c0, c1;
+  bool rotate;
+  int b;
+  long long tok0, begin, t0;
+  int first, lo, hi;
+};
+template <typename T, int D, int NT, bool HELD>
+__device__ __noinline__ void write_again(const WriteProblem& wp, const AgainRows& r, const uint32_t* s_again, const unsigned long long* s_turn,
+                                         uint4 (*s_red)[2][2 * (D / 16)]) {
+  constexpr int LPR = D / 16, RPW = 32 / LPR, RPP = NT / LPR;
+  const AppendProblem& p = wp.a;
+  const int tid = threadIdx.x, warp = tid >> 5, l = tid % LPR, ps = 1 << p.page_shift;
+  const int* table = p.table + (size_t)r.b * p.max_pages + (r.t0 >> p.page_shift);
+  __syncwarp();
+#pragma unroll 1
+  for (int r0 = r.first / RPP * RPP; r0 < r.hi; r0 += RPP) {
+    const int row = r0 + tid / LPR;
+    const bool in = row >= r.first && row < r.hi, fresh = in && row >= r.lo;
+    const uint32_t again = fresh ? s_again[row] : 0;
+    if (!__any_sync(0xffffffffu, again != 0)) continue;
+    const int page = in ? __ldg(table + (row >> p.page_shift)) : -1;
+    const bool ok = page >= 0 && page < p.n_pages;
+    const int phys = ok ? page : 0;
+    const size_t at = (size_t)phys * p.stride_page + (size_t)r.h * p.stride_head + (size_t)(row & (ps - 1)) * p.stride_token;
+    const size_t scale_at = ((size_t)phys * p.hkv + r.h) * ps + (row & (ps - 1));
+    const long long t = r.t0 + row, tok = fresh ? r.tok0 + (t - r.begin) : r.tok0;
+    float cs[8], sn[8];
+    if (r.rotate) {
+      const unsigned long long x = (unsigned long long)(p.positions ? __ldg(p.positions + tok) : t);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) turn_cos_sin((uint32_t)((x * s_turn[8 * l + i] + 0x80000000ull) >> 32), cs[i], sn[i]);
+    }
+#pragma unroll 1
+    for (int n = 0; n <= p.group; ++n) {
+      const bool mine = again >> n & 1u;
+      if (!__any_sync(0xffffffffu, mine)) continue;
+      const int head = n == 0 ? r.h : r.h * p.group + n - 1;
+      const size_t from = n == 0 ? (size_t)tok * p.k_new_token + (size_t)head * p.k_new_head : (size_t)tok * p.q_token + (size_t)head * p.q_head;
+      const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(n == 0 ? p.k_new : p.q) + from * 2);
+      uint4 a = make_uint4(0, 0, 0, 0), c = a;
+      if (mine) { a = src[r.c0]; c = src[r.c1]; }
+      float x[16];
+      unpack_piece<T>(a, x);
+      unpack_piece<T>(c, x + 8);
+      norm16_scaled<LPR>(x, n == 0 ? wp.k_weight + head * wp.k_weight_head : wp.q_weight + head * wp.q_weight_head, r.c0, r.c1, wp.eps);
+      if (r.rotate) rotate16(x, cs, sn, p.pairs);
+      if (HELD && n == 0) {
+        const uint32_t e = row_byte<LPR>(x);
+        const uint4 code = row_codes(x, e);
+        if (mine && ok) {
+          uint2* kd = reinterpret_cast<uint2*>(static_cast<char*>(p.k) + at);
+          kd[r.c0] = make_uint2(code.x, code.y);
+          kd[r.c1] = make_uint2(code.z, code.w);
+          if (l == 0) wp.held.k_scales[scale_at] = (uint8_t)e;
+        }
+      } else if (mine && (n > 0 || ok)) {
+        char* to = n == 0 ? static_cast<char*>(p.k) + at * 2 : static_cast<char*>(p.q_out) + ((size_t)tok * p.q_out_token + (size_t)head * p.q_out_head) * 2;
+        put_pieces(to, r.c0, r.c1, false, pack_piece<T>(x), pack_piece<T>(x + 8));
+      }
+    }
+    if (p.bounds && __any_sync(0xffffffffu, again & 1u)) {
+      __syncwarp();
+      uint4 a = make_uint4(0, 0, 0, 0), c = a;
+      if (in && ok) held_key<T, HELD>(wp, at, scale_at, r.c0, r.c1, a, c);
+      warp_bounds<T, LPR>(in, a, c, r.c0, r.c1, s_red[(r0 + warp * RPW) / RPW]);
+    }
+  }
+}
+
 // An item is one KV head of 64 aligned cache positions (128 where the page is that long): whole pages, so that their
 // bounds need no other CTA.
 template <typename T, int D, int NT, bool HELD>
@@ -114,7 +261,9 @@ __global__ void __launch_bounds__(NT, NT == 128 ? 4 : 2) paged_write_kernel(cons
   __shared__ int s_item;
   __shared__ __align__(16) unsigned long long s_turn[D / 2];
   __shared__ uint4 s_red[128 / RPW][2][2 * LPR];     // a warp's rows: their minimum and maximum
+  __shared__ uint32_t s_again[T::kBf16 ? 128 : 1];   // of a new row of the item: heads to be written once more
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (T::kBf16 && tid < 128) s_again[tid] = 0;
   const int h = blockIdx.y, span_shift = p.page_shift > 6 ? p.page_shift : 6;
   pdl_wait();
   pdl_launch_next();
@@ -177,6 +326,7 @@ __global__ void __launch_bounds__(NT, NT == 128 ? 4 : 2) paged_write_kernel(cons
   };
   const int r_begin = first / RPP * RPP;
   int page_next = page_of(r_begin);
+  bool any_again = false;
   for (int r0 = r_begin; r0 < hi; r0 += RPP) {
     const int row = r0 + tid / LPR;
     const bool in = row >= first && row < hi, fresh = in && row >= lo;
@@ -226,7 +376,8 @@ __global__ void __launch_bounds__(NT, NT == 128 ? 4 : 2) paged_write_kernel(cons
       float x[16];
       unpack_piece<T>(ka, x);
       unpack_piece<T>(kc, x + 8);
-      if (kw) norm16<LPR>(x, kw, c0, c1, wp.eps);
+      uint32_t again = 0;                                 // heads whose norm needs scaled squares: the key, the group's queries
+      if (kw && norm16<T, LPR>(x, kw, c0, c1, wp.eps)) again = 1;
       if (fresh && rotate) rotate16(x, cs, sn, p.pairs);
       if (HELD) {
         const uint32_t ke = row_byte<LPR>(x);
@@ -270,61 +421,32 @@ __global__ void __launch_bounds__(NT, NT == 128 ? 4 : 2) paged_write_kernel(cons
               float z[16];
               unpack_piece<T>(u[i], z);
               unpack_piece<T>(w[i], z + 8);
-              if (wp.q_weight) norm16<LPR>(z, wp.q_weight + (h * p.group + g + i) * wp.q_weight_head, c0, c1, wp.eps);
-              if (fresh) {
+              // (such a head stays as it is for now: q_out may be q itself)
+              const bool scale = wp.q_weight && norm16<T, LPR>(z, wp.q_weight + (h * p.group + g + i) * wp.q_weight_head, c0, c1, wp.eps);
+              if (scale) again |= 2u << (g + i);
+              if (fresh && !scale) {
                 if (rotate) rotate16(z, cs, sn, p.pairs);
                 put_pieces(qd + (size_t)(g + i) * p.q_out_head * es, c0, c1, wide, pack_piece<T>(z), pack_piece<T>(z + 8));
               }
             }
         }
       }
+      if (T::kBf16 && fresh && again) {
+        any_again = true;
+        if (l == 0) s_again[row] = again;
+      }
     }
     if (bad) atomicExch(p.status, kStatusBadPage);
     if (in && !fresh) {                                   // a row of an earlier call
-      if (HELD) {
-        const uint2* kd = reinterpret_cast<const uint2*>(static_cast<const char*>(p.k) + at);
-        const uint2 k0 = kd[c0], k1 = kd[c1];
-        const float s = held_scale(wp.held.k_scales[scale_at]);
-        const uint2 w0 = held_values<T>(k0.x, s), w1 = held_values<T>(k0.y, s);
-        const uint2 w2 = held_values<T>(k1.x, s), w3 = held_values<T>(k1.y, s);
-        a = make_uint4(w0.x, w0.y, w1.x, w1.y);
-        c = make_uint4(w2.x, w2.y, w3.x, w3.y);
-      } else {
-        const uint4* kd = reinterpret_cast<const uint4*>(static_cast<const char*>(p.k) + at * es);
-        a = kd[c0];
-        c = kd[c1];
-      }
+      held_key<T, HELD>(wp, at, scale_at, c0, c1, a, c);
     }
     if (p.bounds) {
-      // Over the warp's rows (all of one page).  Lanes without a row take another row's; then the lanes of two rows share the
-      // work: one takes the first pieces, the other the second, then one minima, the other maxima.
-      const unsigned have = __ballot_sync(0xffffffffu, in);
-      if (have != 0) {
-        uint32_t k[8] = {a.x, a.y, a.z, a.w, c.x, c.y, c.z, c.w};
-        if (have != 0xffffffffu) {
-          const int from = in ? lane : (__ffs(have) - 1) / LPR * LPR + l;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) k[i] = __shfl_sync(0xffffffffu, k[i], from);
-        }
-        const bool second = lane & 16, most = lane & 8;
-        uint32_t m[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t mine = second ? k[4 + i] : k[i], theirs = __shfl_xor_sync(0xffffffffu, second ? k[i] : k[4 + i], 16);
-          const uint32_t lo2 = T::min2(mine, theirs), hi2 = T::max2(mine, theirs);
-          const uint32_t other = __shfl_xor_sync(0xffffffffu, most ? lo2 : hi2, 8);
-          m[i] = most ? T::max2(hi2, other) : T::min2(lo2, other);
-        }
-        if (LPR == 4) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t other = __shfl_xor_sync(0xffffffffu, m[i], 4);
-            m[i] = most ? T::max2(m[i], other) : T::min2(m[i], other);
-          }
-        }
-        if (LPR == 8 || (lane & 4) == 0) s_red[(r0 + warp * RPW) / RPW][most][second ? c1 : c0] = make_uint4(m[0], m[1], m[2], m[3]);
-      }
+      warp_bounds<T, LPR>(in, a, c, c0, c1, s_red[(r0 + warp * RPW) / RPW]);
     }
+  }
+  if (T::kBf16 && __any_sync(0xffffffffu, any_again)) {
+    const AgainRows r{h, c0, c1, rotate, b, tok0, begin, t0, first, lo, hi};
+    write_again<T, D, NT, HELD>(wp, r, s_again, s_turn, s_red);
   }
   if (!p.bounds) return;
   __syncthreads();

@@ -6,8 +6,8 @@ import torch
 
 from oracle import paged8_oracle as P8
 from oracle import paged_oracle as PO
-from paged8_utils import F8, gpu_attention8, gpu_block_attention8, make_step8
-from paged_utils import DT, check_attention, f64
+from paged8_utils import F8, gpu_attention8, gpu_block_attention8, make_step8, to_device8
+from paged_utils import DT, check_attention, f64, make_step, to_device
 
 pytestmark = pytest.mark.gpu
 
@@ -138,3 +138,105 @@ def test_a_later_tokens_values_do_not_reach_the_tokens_before_it(kv_len, power, 
     assert (y[:q_len - 1] == clean[0][:q_len - 1]).all() and (lse == clean[1]).all()
     assert (y[q_len:] == clean[0][q_len:]).all()
     check_attention("bf16", 64, y, lse, *oracle8(s), kv_len)
+
+
+# ---------------------------------------------------------------------------------------------- head norms
+# a norm's error relative to the head's largest element: the sum of squares d/2 2^-24, the root 2^-22, four products
+def norm_slack(d):
+    return (d / 2 + 4 + 4) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-40, 1e-30, 1e-6])
+@pytest.mark.parametrize("d,held", [(64, True), (128, False)])
+def test_norms_of_heads_of_any_size(d, held, eps):
+    """bf16 heads of 2^-130 to 2^120, some elements far below the others; eps 0, below and above their squares."""
+    powers = [-130, -126, -120, -100, -76, -75, -64, -63, -50, -40, -30, -10, 0, 40, 60, 62, 63, 64, 90, 120]
+    hq, hkv, ps, n = 4, 2, 16, len(powers)
+    g = torch.Generator().manual_seed(90)
+    x = torch.randn(n, hq + 2 * hkv, d, generator=g, dtype=torch.float64)
+    x[:, :, ::7] *= 2.0 ** -20
+    x = (x * torch.exp2(torch.tensor(powers, dtype=torch.float64))[:, None, None]).to(torch.bfloat16)
+    k_new, v_new, q = x[:, hq:hq + hkv], x[:, hq + hkv:], x[:, :hq]
+    w = 1 + 0.3 * torch.randn(d, generator=g)
+    if held:
+        s = make_step8(hq, hkv, d, ps, "bf16", [(n, n)], seed=91)
+        kv = to_device8(s)
+    else:
+        s = make_step(hq, hkv, d, ps, "bf16", [(n, n)], seed=91)
+        kv = to_device(s)
+    out = torch.full((n, hq, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    T().paged_append(kv, k_new.cuda(), v_new.cuda(), None, q.cuda(), out, norms=T().HeadNorms(w.cuda(), w.cuda(), eps))
+    assert kv.device_status() == 0
+    eps32 = float(np.float32(eps))
+    qy, ky = (P8.norm(t.double().numpy(), w.double().numpy(), eps32) for t in (q, k_new))
+    u, tiny = torch.finfo(torch.bfloat16).eps / 2, 2.0 ** -134      # half a step of bf16 (8 bits: 2^-8), half of its smallest number
+    most = np.abs(qy).max(-1, keepdims=True)
+    assert (np.abs(f64(out) - qy) <= u * np.abs(qy) + norm_slack(d) * most + tiny).all()
+    for t in range(n):
+        page, slot = s.table[0, t // ps], t % ps
+        most = np.abs(ky[t]).max(-1, keepdims=True)
+        if held:
+            c, e = kv.k.view(torch.uint8).cpu().numpy()[page, :, slot], kv.k_scales.view(torch.uint8).cpu().numpy()[page, :, slot]
+            got, tol = P8.values(c, e), 2.0 ** -4 * np.abs(ky[t]) + 2.0 ** -10 * P8.power(e)[:, None]
+        else:
+            got, tol = f64(kv.k)[page, :, slot], u * np.abs(ky[t])
+        assert (np.abs(got - ky[t]) <= tol + 1.1 * norm_slack(d) * most + tiny).all(), powers[t]
+
+
+def test_norms_of_heads_without_a_size():
+    """eps 0: a head of zeros is 0 / 0, as is an infinite element; the others of that head are 0.  Neighbours are as ever."""
+    d, ps = 64, 16
+    s = make_step(2, 1, d, ps, "bf16", [(3, 3)], seed=92)
+    q = torch.ones(3, 2, d)
+    q[0, 0] = 0
+    q[1, 1, 3] = float("inf")
+    q[2, 0, 5] = float("nan")
+    q, out = q.bfloat16().cuda(), torch.empty(3, 2, d, dtype=torch.bfloat16, device="cuda")
+    kv, w = to_device(s), torch.ones(d).cuda()
+    T().paged_append(kv, torch.ones(3, 1, d).bfloat16().cuda(), torch.ones(3, 1, d).bfloat16().cuda(), None, q, out, norms=T().HeadNorms(w, None, 0.0))
+    got = f64(out)
+    want = np.ones((3, 2, d))
+    want[0, 0], want[2, 0], want[1, 1], want[1, 1, 3] = np.nan, np.nan, 0, np.nan
+    assert np.array_equal(got, want, equal_nan=True)
+
+
+@pytest.mark.parametrize("held,ps,d,pairs", [(True, 16, 128, False), (True, 128, 64, True), (False, 32, 64, False), (False, 128, 128, True)])
+def test_heads_of_any_size_beside_others(held, ps, d, pairs):
+    """Some heads of some tokens are very small or large: rotated, queries in place, weights of each head, bounds of pages that hold
+    rows of earlier calls, a group of more than four heads."""
+    hq, hkv, lens = 12, 2, [(5, 90), (1, 33), (150, 200), (0, 4)]
+    if held:
+        s = make_step8(hq, hkv, d, ps, "bf16", lens, seed=99, with_bounds=True)
+        kv = to_device8(s)
+    else:
+        s = make_step(hq, hkv, d, ps, "bf16", lens, seed=99, with_bounds=True)
+        kv = to_device(s)
+    n = s.total_q
+    g = torch.Generator().manual_seed(100)
+    x = torch.randn(n, hq + 2 * hkv, d, generator=g, dtype=torch.float64)
+    power = torch.tensor([0, -100, 0, 0, 80, 0, -70, 0], dtype=torch.float64)[torch.randint(0, 8, (n, hq + 2 * hkv), generator=g)]
+    power[:, hq + hkv:] = 0                                  # values are not normed
+    x = (x * torch.exp2(power)[..., None]).bfloat16()
+    k_new, v_new, q = x[:, hq:hq + hkv], x[:, hq + hkv:], x[:, :hq].contiguous()
+    wq, wk = (1 + 0.3 * torch.randn(m, d, generator=g) for m in (hq, hkv))
+    inv = 0.5 ** torch.arange(d // 4, dtype=torch.float32)
+    q_dev = q.cuda()
+    T().paged_append(kv, k_new.cuda(), v_new.cuda(), T().RotaryMap(inv.cuda(), pairs), q_dev, q_dev, norms=T().HeadNorms(wq.cuda(), wk.cuda(), 0.0))
+    assert kv.device_status() == 0
+    u, slack = torch.finfo(torch.bfloat16).eps / 2, norm_slack(d) + 16 * 2.0 ** -24        # (sine and cosine: 2^-22 each, their angle 2^-22)
+    got_k = P8.values(kv.k.view(torch.uint8).cpu().numpy(), kv.k_scales.view(torch.uint8).cpu().numpy()) if held else f64(kv.k)
+    for b, (m, length) in enumerate(lens):
+        for i in range(m):
+            tok, t = int(s.cu_q[b]) + i, length - m + i
+            y = PO.rotate(P8.norm(q[tok].double().numpy(), wq.double().numpy(), 0.0), t, inv.double().numpy(), pairs)
+            assert (np.abs(f64(q_dev)[tok] - y) <= u * np.abs(y) + 1.1 * slack * np.abs(y).max(-1, keepdims=True)).all()
+            y = PO.rotate(P8.norm(k_new[tok].double().numpy(), wk.double().numpy(), 0.0), t, inv.double().numpy(), pairs)
+            got = got_k[s.table[b, t // ps], :, t % ps]
+            tol = 2.0 ** -4 * np.abs(y) + 2.0 ** -10 * P8.power(P8.scale_byte(got))[:, None] if held else u * np.abs(y)
+            assert (np.abs(got - y) <= tol + 1.1 * slack * np.abs(y).max(-1, keepdims=True)).all()
+    want = PO.page_bounds(got_k, s.table, s.kv_lens)
+    for b, (m, length) in enumerate(lens):
+        for p in range((length - m) // ps, (length + ps - 1) // ps if m else 0):
+            page = int(s.table[b, p])
+            lo, hi = (torch.from_numpy(w).bfloat16().double().numpy() for w in want[page])
+            assert (f64(kv.key_bounds)[page, :, 0] == lo).all() and (f64(kv.key_bounds)[page, :, 1] == hi).all()
