@@ -464,21 +464,24 @@ typedef struct {
 } tkphi_read_desc;
 
 /*
- * What rows of an 8-bit cache stand for, as 16-bit rows (rounded once: exact in bf16; in fp16 infinite beyond 65504).
+ * What rows of an 8-bit cache stand for, as 16-bit rows, rounded once.  bf16: exact from 2^-130 to the largest number, infinite
+ * beyond.  fp16: exact from 2^-21 to 65504, and beyond it 65504 (fp16 elements from 63488 on are held as 65536).
  * Written to a head-major or token-major array this is a cache as tkphi_build_summaries and the decode calls take it.
  * kv's cu_q plays no part.  Rows of positions at or behind a sequence's device length, or on a bad page, are left as they
  * were.  No workspace.
  */
 tkphi_status tkphi_coded_read(const tkphi_coded_desc* kv, const tkphi_read_desc* rows, void* cuda_stream);
 
-/* As tkphi_paged_workspace_bytes, tkphi_paged_attention and tkphi_paged_block_attention, over an 8-bit cache.  What the rows
- * stand for enters the products exactly; scores, sums and products are accumulated in fp32.  Sequences with at most 64 query
- * rows of one KV head (q_len * n_q_heads / n_kv_heads), and the page-selected call: a probability's product with its value's
- * scale is rounded to fp16 once, and vanishes below 2^-29 of the largest such product of the query row's visible keys (keys that
- * it does not see have no part in that); bf16 queries' elements vanish below 2^-39 of their row's
- * largest; keys whose scale byte is 0 score 0.  Sequences with more rows: their caches are first written to the workspace as 16-bit rows (4 bytes per element of
- * k and v together: the workspace is that much larger, and values beyond the type's range count as infinite), then everything
- * is as over a 16-bit cache. */
+/* As tkphi_paged_workspace_bytes, tkphi_paged_attention and tkphi_paged_block_attention, over an 8-bit cache.  Scores, sums
+ * and products are accumulated in fp32.  fp16 outputs beyond 65504 are 65504.
+ *  - Sequences with at most 64 query rows of one KV head (q_len * n_q_heads / n_kv_heads), and the page-selected call: what the
+ *    rows stand for enters the products exactly, but keys whose scale byte is 0 score 0.  A probability's product with its value's
+ *    scale is rounded to fp16 once, and vanishes below 2^-29 of the largest such product of the query row's visible keys (keys
+ *    that it does not see have no part in that).  Elements of bf16 queries lose digits below 2^-31 of their row's largest and
+ *    vanish below 2^-39 of it.
+ *  - Sequences with more rows: their caches are first written to the workspace as 16-bit rows (4 bytes per element of k and v
+ *    together: the workspace is that much larger, twice the sequences' 8-bit caches), rounded as tkphi_coded_read does it; then
+ *    everything is as over a 16-bit cache. */
 size_t tkphi_coded_workspace_bytes(const tkphi_coded_desc* kv, const tkphi_page_selection* selection, int which);
 tkphi_status tkphi_coded_attention(const tkphi_coded_desc* kv, const void* q, void* y_out, float* lse_out, float scale,
                                     uint32_t flags, void* workspace, size_t workspace_bytes, void* cuda_stream);

@@ -2,8 +2,7 @@
 //
 // A row x is held as codes c and a byte e, x_i ~ c_i 2^(e - 127), with e the smallest in [1, 254] for which the largest
 // |x_i| is at most 448 * 2^(e - 127): 448 is the largest code.  Scaling by a power of two is exact, so a value is rounded
-// once, by the code, to 2^-4 of itself at most (2^-10 of 2^(e-127) where the code is below 2^-6), and what a row stands for
-// is exact in 32 and in bf16.  (A scale of 32 bits would use the codes' range up to 448 in every row, which gains
+// once, by the code, to 2^-4 of itself at most (2^-10 of 2^(e-127) where the code is below 2^-6).  (A scale of 32 bits would use the codes' range up to 448 in every row, which gains
 // nothing: the codes are floating-point numbers, their relative steps are the same everywhere but at the bottom.)
 // A row with an element that is infinite or no number is held as NaN codes with e = 255, which stands for NaN.
 #pragma once
@@ -38,12 +37,25 @@ __device__ __forceinline__ void unpack_codes(uint32_t w, uint32_t& lo, uint32_t&
   asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n cvt.rn.f16x2.e4m3x2 %1, h;\n}"
       : "=r"(lo), "=r"(hi) : "r"(w));
 }
+// The element type as what comes out of an 8-bit cache is rounded to it: finite fp16 numbers from 63488 on are held as 65536, which
+// fp16 does not have, so what is finite becomes its largest number, not infinite.
+struct Fp16Held : Fp16 {
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    uint32_t r;
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
+  }
+};
+template <typename T> struct OutOfHeld { using type = T; };
+template <> struct OutOfHeld<Fp16> { using type = Fp16Held; };
+
 // Four codes times a scale, as two pairs of the element type.
 template <typename T>
 __device__ __forceinline__ uint2 held_values(uint32_t w, float scale) {
   uint32_t lo, hi;
   unpack_codes(w, lo, hi);
-  return make_uint2(T::pack(Fp16::lo(lo) * scale, Fp16::hi(lo) * scale), T::pack(Fp16::lo(hi) * scale, Fp16::hi(hi) * scale));
+  using Out = typename OutOfHeld<T>::type;
+  return make_uint2(Out::pack(Fp16::lo(lo) * scale, Fp16::hi(lo) * scale), Out::pack(Fp16::lo(hi) * scale, Fp16::hi(hi) * scale));
 }
 
 // ---------------------------------------------------------------- launches (host)

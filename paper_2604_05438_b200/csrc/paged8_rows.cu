@@ -704,7 +704,7 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           uint32_t* y = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.y) + out_row * D + c * C::CHUNK + dp);
 #pragma unroll
           for (int e = 0; e < PER; e += 2) {
-            if (fin) y[e >> 1] = T::pack(a[e] * inv, a[e + 1] * inv);
+            if (fin) y[e >> 1] = OutOfHeld<T>::type::pack(a[e] * inv, a[e + 1] * inv);
             else *reinterpret_cast<float2*>(part + e) = make_float2(a[e], a[e + 1]);
           }
         }
@@ -721,7 +721,7 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       }
     }
   }
-  if (SPLIT && p.n_split > 1) join_cluster<T, D, BLOCK, kHeldKeys, WARPS>(p, cta, keep, keep_stat);
+  if (SPLIT && p.n_split > 1) join_cluster<typename OutOfHeld<T>::type, D, BLOCK, kHeldKeys, WARPS>(p, cta, keep, keep_stat);
   __syncthreads();
   if (*s_abort && tid == 0) atomicExch(p.status, kStatusTimeout);
   // (beside a tile-kernel launch this grid may run next to it: it must not be complete before that one is, because the
@@ -780,7 +780,7 @@ cudaError_t launch_paged8_rows(const PagedProblem& p, const HeldCache& held, con
 
 cudaError_t launch_paged8_rows_merge(const PagedProblem& p, int d, bool bf16, bool block, int units, int max_rows, cudaStream_t st) {
 #define MERGE(T, D, B) \
-  launch_pdl(paged_rows_merge_kernel<T, D, B, kHeldKeys>, dim3(units, max_rows), dim3(kMergeThreads), 0, st, p)
+  launch_pdl(paged_rows_merge_kernel<OutOfHeld<T>::type, D, B, kHeldKeys>, dim3(units, max_rows), dim3(kMergeThreads), 0, st, p)
   return TKPHI_BY_TYPE(MERGE);
 #undef MERGE
 }

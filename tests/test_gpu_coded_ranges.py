@@ -240,3 +240,81 @@ def test_heads_of_any_size_beside_others(held, ps, d, pairs):
             page = int(s.table[b, p])
             lo, hi = (torch.from_numpy(w).bfloat16().double().numpy() for w in want[page])
             assert (f64(kv.key_bounds)[page, :, 0] == lo).all() and (f64(kv.key_bounds)[page, :, 1] == hi).all()
+
+
+# ---------------------------------------------------------------------------------------------- fp16 near the end of its range
+def big_rows(s, hkv, d, seed):
+    """New tokens with elements up to the largest fp16 number; those from 63488 on are held as 65536."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(s.total_q, hkv, d, generator=g)
+    for t in range(s.total_q):
+        x[t, :, (3 * t) % d] = [65504, -65504, 63488, -63520, 60000, 65504][t % 6]
+    return x.half()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_fp16_rows_at_the_end_of_the_range_stay_finite(d):
+    hkv, ps, n = 2, 16, 70
+    s = make_step8(4, hkv, d, ps, "fp16", [(n, n)], seed=95, with_bounds=True)
+    x = big_rows(s, hkv, d, 96)
+    kv = to_device8(s)
+    T().paged_append(kv, x.cuda(), x.flip(0).contiguous().cuda())
+    out = [torch.empty(n, hkv, d, dtype=torch.float16, device="cuda") for _ in range(2)]
+    T().paged_read(kv, T().CacheRows([0, n], device="cuda"), *out)
+    assert kv.device_status() == 0
+    for got, rows in ((f64(out[0]), f64(x)), (f64(out[1]), f64(x.flip(0)))):
+        held = P8.hold(rows)[0]
+        assert np.abs(held).max() == 65536                   # (it is what this test is about)
+        # (2^-14: the smallest normal number; elements beside one of 65504 are held to 2^-10 * 2^8)
+        want = np.clip(held, -65504, 65504)
+        assert (got == want).all()
+        assert (np.abs(got - rows) <= 2.0 ** -4 * np.abs(rows) + 2.0 ** -2).all()
+    for p in range((n + ps - 1) // ps):
+        have = f64(out[0])[p * ps:(p + 1) * ps]
+        b = f64(kv.key_bounds)[s.table[0, p]]
+        assert (b[:, 0] == have.min(0)).all() and (b[:, 1] == have.max(0)).all()
+
+
+def test_fp16_rows_beyond_the_range_read_as_its_ends():
+    """Every scale byte from that of 65504 on; NaN codes and byte 255 stay NaN."""
+    d, ps = 64, 128
+    s = make_step8(1, 1, d, ps, "fp16", [(0, 1024)], seed=97)
+    codes = np.tile(np.arange(256, dtype=np.uint8).reshape(4, 64), (256, 1))
+    scales = np.repeat(np.arange(256, dtype=np.uint8), 4)
+    for t in range(1024):
+        p = s.table[0, t // ps]
+        s.v[p, 0, t % ps], s.vs[p, 0, t % ps] = codes[t], scales[t]
+    out = torch.empty(1024, 1, d, dtype=torch.float16, device="cuda")
+    T().paged_read(to_device8(s), T().CacheRows([0, 1024], device="cuda"), None, out)
+    x = P8.values(codes, scales)
+    want = torch.from_numpy(np.clip(x, -65504, 65504)).half()
+    assert np.array_equal(f64(out[:, 0]), f64(want), equal_nan=True)
+
+
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("side", ["values", "keys"])
+def test_attention_over_fp16_rows_at_the_end_of_the_range(side, way):
+    """Values held as 65536 count as that or as 65504, 2^-11 less; so do keys, here in a dim in which the queries are 0.  Outputs
+    are finite."""
+    q_len, g = WAYS[way]
+    n = 200
+    s = make_step8(2 * g, 2, 64, 32, "fp16", [(q_len, n), (1, 40)], seed=98, spread=0.0)
+    codes, scales = (s.v, s.vs) if side == "values" else (s.k, s.ks)
+    if side == "values":
+        for t in range(n):                                   # all of them: the output is 65504 or what lies near
+            codes[at(s, 0, t)], scales[at(s, 0, t)] = code(256), 127 + 8
+            s.v[s.table[0, t // 32], :, t % 32, ::2] = code(-256)
+    else:
+        s.q[:, :, 5] = 0
+        for t in range(0, n, 3):
+            codes[at(s, 0, t)], scales[at(s, 0, t)] = 0, 127 + 8
+            s.k[s.table[0, t // 32], :, t % 32, 5] = code(256)
+    y, lse = gpu_attention8(s)
+    wy, wl, A, C = oracle8(s)
+    assert np.isfinite(y).all() and np.isfinite(lse).all()
+    u = 2.0 ** -11
+    C = C if side == "values" else np.minimum(C, 40.0)       # (products with 0 are exact)
+    e = (64 * 2.0 ** -22 * C + 2.0 ** -21)[..., None]
+    assert (np.abs(y - np.clip(wy, -65504, 65504)) <= u * np.abs(wy) + (2 * u + 2 * e + 2 * n * 2.0 ** -24) * A + 2.0 ** -24).all()
+    assert np.abs(lse - wl).max() <= e.max() + n * 2.0 ** -24 + 2.0 ** -18
+    assert (np.abs(y[:q_len]) >= 65000).all() or side == "keys"
