@@ -43,17 +43,29 @@ template <typename T>
 __device__ __forceinline__ uint4 pack_piece(const float* x) {
   return make_uint4(T::pack(x[0], x[1]), T::pack(x[2], x[3]), T::pack(x[4], x[5]), T::pack(x[6], x[7]));
 }
-// Cosine and sine of an angle of a / 2^32 turns: less the nearest quarter turn, an angle |y| <= pi / 4 is left, of which the
+// A rotated pair: turns per position, less whole ones, in units of 2^-64, and 2 pi / 2^32; that is NaN where the frequency is infinite
+// or no number, for which fixed point has nothing.
+struct __align__(16) Turn { unsigned long long per; float unit; };
+// Cosine and sine of an angle of a / 2^32 turns (unit: 2 pi / 2^32): less the nearest quarter turn, an angle |y| <= pi / 4 is left, of which the
 // Taylor polynomials of degree 9 and 10 are off by y^11 / 11! = 1.8e-9 and y^12 / 12! = 1.1e-10, less than 32 bits hold.
 // (sincospif took about 125 instructions of a pair, two thirds of the kernel's.)
-__device__ __forceinline__ void turn_cos_sin(uint32_t a, float& cs, float& sn) {
+__device__ __forceinline__ void turn_cos_sin(uint32_t a, float unit, float& cs, float& sn) {
   const uint32_t quarter = a + 0x20000000u;                  // its top two bits: the quarter
-  const float y = (float)(int)(a - (quarter & 0xc0000000u)) * 1.46291807926715968e-9f, z = y * y;      // 2 pi / 2^32
+  const float y = (float)(int)(a - (quarter & 0xc0000000u)) * unit, z = y * y;
   const float s = fmaf(y * z, fmaf(z, fmaf(z, fmaf(z, 2.75573192e-6f, -1.98412698e-4f), 8.33333333e-3f), -1.66666667e-1f), y);
   const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -2.75573192e-7f, 2.48015873e-5f), -1.38888889e-3f), 4.16666667e-2f), -0.5f), 1.f);
   const bool odd = quarter & 0x40000000u;
   sn = __uint_as_float(__float_as_uint(odd ? c : s) ^ (quarter & 0x80000000u));
   cs = __uint_as_float(__float_as_uint(odd ? s : c) ^ ((quarter + 0x40000000u) & 0x80000000u));
+}
+// Of a lane's eight pairs at position x.
+template <int LPR>
+__device__ __forceinline__ void row_angles(float (&cs)[8], float (&sn)[8], unsigned long long x, const Turn* turn) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const Turn t = turn[i * LPR];
+    turn_cos_sin((uint32_t)((x * t.per + 0x80000000ull) >> 32), t.unit, cs[i], sn[i]);
+  }
 }
 // x: the lane's two pieces of 8 dims.
 __device__ __forceinline__ void rotate16(float (&x)[16], const float (&cs)[8], const float (&sn)[8], bool pairs) {
@@ -186,7 +198,7 @@ struct AgainRows {
   int first, lo, hi;
 };
 template <typename T, int D, int NT, bool HELD>
-__device__ __noinline__ void write_again(const WriteProblem& wp, const AgainRows& r, const uint32_t* s_again, const unsigned long long* s_turn,
+__device__ __noinline__ void write_again(const WriteProblem& wp, const AgainRows& r, const uint32_t* s_again, const Turn* s_turn,
                                          uint4 (*s_red)[2][2 * (D / 16)]) {
   constexpr int LPR = D / 16, RPW = 32 / LPR, RPP = NT / LPR;
   const AppendProblem& p = wp.a;
@@ -208,8 +220,7 @@ __device__ __noinline__ void write_again(const WriteProblem& wp, const AgainRows
     float cs[8], sn[8];
     if (r.rotate) {
       const unsigned long long x = (unsigned long long)(p.positions ? __ldg(p.positions + tok) : t);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) turn_cos_sin((uint32_t)((x * s_turn[8 * l + i] + 0x80000000ull) >> 32), cs[i], sn[i]);
+      row_angles<LPR>(cs, sn, x, s_turn + l);
     }
 #pragma unroll 1
     for (int n = 0; n <= p.group; ++n) {
@@ -259,7 +270,7 @@ __global__ void __launch_bounds__(NT, NT == 128 ? 4 : 2) paged_write_kernel(cons
   const AppendProblem& p = wp.a;
   __shared__ long long s_find[4];              // sequence, its first token row, cache length, first new position
   __shared__ int s_item;
-  __shared__ __align__(16) unsigned long long s_turn[D / 2];
+  __shared__ Turn s_turn[D / 2];
   __shared__ uint4 s_red[128 / RPW][2][2 * LPR];     // a warp's rows: their minimum and maximum
   __shared__ uint32_t s_again[T::kBf16 ? 128 : 1];   // of a new row of the item: heads to be written once more
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -267,11 +278,14 @@ __global__ void __launch_bounds__(NT, NT == 128 ? 4 : 2) paged_write_kernel(cons
   const int h = blockIdx.y, span_shift = p.page_shift > 6 ? p.page_shift : 6;
   pdl_wait();
   pdl_launch_next();
-  // Turns per position of the rotated pairs, less whole ones, in units of 2^-64.  The product with a position then drops whole
-  // turns by itself, exactly: the angle is off by position * 2^-65 turns, and by the product's rounding to 2^-53 of inv_freq.
+  // The product of a pair's turns with a position drops whole turns by itself, exactly: the angle is off by position * 2^-64 turns,
+  // and by the product's rounding to 2^-53 of inv_freq.
   if (tid >= NT / 2 && tid - NT / 2 < p.rot / 2) {
-    const double t = (double)__ldg(p.inv_freq + tid - NT / 2) * 0.15915494309189533577;
-    s_turn[tid - NT / 2] = __double2ull_rz((t - floor(t)) * 18446744073709551616.0);
+    const float freq = __ldg(p.inv_freq + tid - NT / 2);
+    const double t = (double)freq * 0.15915494309189533577;
+    // (the pairs of one place in all lanes beside each other, so that a warp's reads of them spread over the banks)
+    s_turn[(tid & 7) * LPR + (tid - NT / 2) / 8] = Turn{__double2ull_rz((t - floor(t)) * 18446744073709551616.0),
+                                fabsf(freq) < INFINITY ? 1.46291807926715968e-9f : __uint_as_float(0x7fc00000u)};
   }
 
   // ---- which positions: a sequence holds (q_len + span - 2) / span + 1 items, enough for every start inside one
@@ -369,8 +383,7 @@ __global__ void __launch_bounds__(NT, NT == 128 ? 4 : 2) paged_write_kernel(cons
       if (fresh) {
         if (rotate) {
           const unsigned long long x = (unsigned long long)(p.positions ? __ldg(p.positions + tok) : t);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) turn_cos_sin((uint32_t)((x * s_turn[8 * l + i] + 0x80000000ull) >> 32), cs[i], sn[i]);
+          row_angles<LPR>(cs, sn, x, s_turn + l);
         }
       }
       float x[16];

@@ -318,3 +318,42 @@ def test_attention_over_fp16_rows_at_the_end_of_the_range(side, way):
     assert (np.abs(y - np.clip(wy, -65504, 65504)) <= u * np.abs(wy) + (2 * u + 2 * e + 2 * n * 2.0 ** -24) * A + 2.0 ** -24).all()
     assert np.abs(lse - wl).max() <= e.max() + n * 2.0 ** -24 + 2.0 ** -18
     assert (np.abs(y[:q_len]) >= 65000).all() or side == "keys"
+
+
+# ---------------------------------------------------------------------------------------------- angles
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("held,norm", [(True, False), (True, True), (False, True)])
+def test_frequencies_that_are_no_numbers(held, norm, pairs):
+    """Pairs with an infinite or NaN frequency become NaN, as in the append without norms, and a row of an 8-bit cache with them."""
+    hq, hkv, d, ps, n = 4, 2, 64, 16, 5
+    g = torch.Generator().manual_seed(93)
+    x = torch.randn(n, hq + 2 * hkv, d, generator=g).bfloat16()
+    k_new, v_new, q = x[:, hq:hq + hkv], x[:, hq + hkv:], x[:, :hq]
+    inv = 0.5 ** torch.arange(16, dtype=torch.float32)
+    bad = [2, 7, 15]
+    for i, b in zip(bad, (float("inf"), float("nan"), -float("inf"))):
+        inv[i] = b
+    if held:
+        s = make_step8(hq, hkv, d, ps, "bf16", [(n, n)], seed=94)
+        kv = to_device8(s)
+    else:
+        s = make_step(hq, hkv, d, ps, "bf16", [(n, n)], seed=94)
+        kv = to_device(s)
+    out = torch.empty(n, hq, d, dtype=torch.bfloat16, device="cuda")
+    w = torch.ones(d).cuda()
+    T().paged_append(kv, k_new.cuda(), v_new.cuda(), T().RotaryMap(inv.cuda(), pairs), q.cuda(), out, norms=T().HeadNorms(w, w, 1e-6) if norm else None)
+    assert kv.device_status() == 0
+    none = np.zeros(d, bool)
+    for i in bad:
+        none[[2 * i, 2 * i + 1] if pairs else [i, i + 16]] = True
+    assert np.array_equal(np.isnan(f64(out)), np.broadcast_to(none, (n, hq, d)))
+    page = int(s.table[0, 0])
+    if held:
+        assert (kv.k_scales.view(torch.uint8).cpu().numpy()[page, :, :n] == 255).all()
+    else:
+        assert np.array_equal(np.isnan(f64(kv.k)[page, :, :n]), np.broadcast_to(none, (hkv, n, d)))
+    clean = inv.double().numpy()
+    clean[bad] = 0
+    for t in range(n):
+        y = PO.rotate(P8.norm(q[t].double().numpy(), np.ones(d) if norm else None, 1e-6), t, clean, pairs)
+        assert (np.abs(f64(out)[t] - y)[:, ~none] <= 2.0 ** -8 * np.abs(y)[:, ~none] + 2.0 ** -14).all()
