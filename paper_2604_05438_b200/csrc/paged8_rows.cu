@@ -373,7 +373,44 @@ paged8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
               v2[x] &= ~unseen[x];
             }
             least = smallest(v2[0] | unseen[0], v2[1] | unseen[1]);
-            other |= above_top();
+            if (fresh) {
+              // The first keys: where scales are near each other, and the largest is the same for every row that sees a key, one
+              // reference does for all rows.
+              const uint32_t u = __vmaxu2(v2[0], v2[1]);
+              const int hi = (int)__reduce_max_sync(0xffffffffu, max(u & 0xffffu, u >> 16));
+              if (hi < 255 && hi - least <= kLoose - kRoom) {
+                uint32_t row_most = 0, row_least = 0x7fffu;  // (bytes + 1; 0: no key)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                  uint32_t w = 0;                            // of the thread's two rows
+#pragma unroll
+                  for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                      const int key = key0[x] + 2 * g + e;
+                      const uint32_t b = (e ? v2[x] >> 16 : v2[x] & 0xffffu) + 1;
+                      w = __vmaxu2(w, (key <= lim[t][0] ? b : 0) | (key <= lim[t][1] ? b << 16 : 0));
+                    }
+#pragma unroll
+                  for (int d = 4; d < 32; d <<= 1) w = __vmaxu2(w, __shfl_xor_sync(0xffffffffu, w, d));
+#pragma unroll
+                  for (int i = 0; i < 2; ++i) {
+                    const uint32_t b = i ? w >> 16 : w & 0xffffu;
+                    row_most = max(row_most, b);
+                    if (b > 0) row_least = min(row_least, b);
+                  }
+                }
+                row_most = __reduce_max_sync(0xffffffffu, row_most);
+                row_least = __reduce_min_sync(0xffffffffu, row_least);
+                if (row_most == row_least) {
+                  top = min((int)row_most - 1 + kRoom, 254);
+                  low = least;
+                  fresh = other = false;
+                }
+              }
+            } else {
+              other |= above_top();
+            }
             // Values that no row sees may be anything (behind the sequence's end they may be left-overs): 0 times them must
             // not reach the product.  Those that some rows see are looked through.
             constexpr int CPR = D / 16;                     // 16-byte chunks of a row
