@@ -473,7 +473,8 @@ typedef struct {
 tkphi_status tkphi_coded_read(const tkphi_coded_desc* kv, const tkphi_read_desc* rows, void* cuda_stream);
 
 /* As tkphi_paged_workspace_bytes, tkphi_paged_attention and tkphi_paged_block_attention, over an 8-bit cache.  Scores, sums
- * and products are accumulated in fp32.  fp16 outputs beyond 65504 are 65504.
+ * and products are accumulated in fp32; sums of values times probabilities (relative to the largest) beyond 2^128 are infinite.
+ * fp16 outputs beyond 65504 are 65504.
  *  - Sequences with at most 64 query rows of one KV head (q_len * n_q_heads / n_kv_heads), and the page-selected call: what the
  *    rows stand for enters the products exactly, but keys whose scale byte is 0 score 0.  A probability's product with its value's
  *    scale is rounded to fp16 once, and vanishes below 2^-29 of the largest such product of the query row's visible keys (keys

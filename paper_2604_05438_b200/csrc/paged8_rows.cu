@@ -28,8 +28,10 @@
 // Probabilities are scaled by 2^14 (a row's largest product is then from 2^4 to 2^15: fp16 has few exponents) and rounded to
 // fp16 once, 2^-12: an eighth of a bf16 output's own rounding, as much as an fp16 one's.  Products below 2^-29 of the row's
 // largest vanish.
-// Measured: 32 sequences of 8K to 64K, 24 / 8 heads of 128: 338-348 us, 6.2-6.4 TB/s of codes and scales (16-bit operands in the
-// other order, queries as the rows: 435).  A token over 4096 keys, 32 / 8 heads of 64: 8.0 us; with sixteen warps instead of
+// Measured: 32 sequences of 8K to 64K, 24 / 8 heads of 128: 330-345 us, 6.3-6.5 TB/s of codes and scales (16-bit operands in the
+// other order, queries as the rows: 435; scales looked at on both sides of the reference and references tracked row by row in
+// every tile: 395-445).  Scales spread by a standard deviation of 12 powers instead of 1: 204 against 198 us for 32 sequences of
+// 16K; with two row tiles and a deviation of 4, 157 against 72 for eight of 32K, because each row then keeps a reference of its own.  A token over 4096 keys, 32 / 8 heads of 64: 8.0 us; with sixteen warps instead of
 // eight in the cluster form 9.1.  Three CTAs per multiprocessor instead of two at head_dim 128: no faster (registers spill).
 #include <cfloat>
 #include <type_traits>

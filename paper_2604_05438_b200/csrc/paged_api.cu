@@ -170,9 +170,9 @@ struct AttendPlan {
 // Sequences with at most this many rows per KV head go to the row kernel.  Over a 16-bit cache: one tile of its matrix instruction.
 constexpr int kRowsLimit = 16;
 // Over an 8-bit cache: four.  The row kernel then reads such a sequence's cache once per tile, the other way writes it as 16-bit
-// pages first and reads those with the tile kernel.  One sequence of 128K rows, 24 / 8 heads of 128: 63 us with 16 rows, 177
-// with 64 (of 16-row tiles) against 328 to 332; eight of them 1325 us with 64, 2000 with 96 against 2006; 32 / 8 heads of 64, eight
-// of 128K: 770 with 64, 1155 with 96 against 1110, of 4K: 50 with 64 against 69, of 1K: 30 against 27.
+// pages first and reads those with the tile kernel.  One sequence of 128K rows, 24 / 8 heads of 128: 64 us with 16 rows, 172
+// with 64 (of 16-row tiles), by the other way 285 with 96; eight of them 1300 us with 64, 1710 with 96; 32 / 8 heads of 64, eight
+// of 128K: 783 and 998, of 4K: 51-54 and 62-64, of 1K: 31 and 22.
 constexpr int kHeldRowsLimit = 64;
 constexpr int rows_limit(bool held) { return held ? kHeldRowsLimit : kRowsLimit; }
 

@@ -1,5 +1,5 @@
 // Rows of an 8-bit paged cache back as 16-bit rows: out[cu_rows[b] + i] = codes * 2^(e - 127) of position first[b] + i of
-// sequence b, for keys and values, rounded once to the element type (exact in bf16).
+// sequence b, for keys and values, rounded once to the element type (exact in bf16 from 2^-130 to its largest number).
 //
 // Bound: memory, 2 (d + 1) bytes in and 4 d out per row and head.  A thread has 16 codes of a row's keys and values and writes
 // 32 bytes of each; a CTA takes 64 rows and several KV heads, one after the other, so that looking up the rows' places is
@@ -145,8 +145,7 @@ cudaError_t launch_paged_read(const ReadProblem& q, bool bf16, cudaStream_t st) 
 
 // ---------------------------------------------------------------- for attention of many rows
 // The caches of the sequences with many rows as 16-bit pages of 128 rows in the workspace, [page][head][slot][dim], one
-// sequence's pages behind another's, and a page table of them; codes times powers of two, so nothing is lost.  A CTA takes
-// half a page.  Rows at or behind a sequence's length and on bad pages become 0.
+// sequence's pages behind another's, and a page table of them; rounded as the rows that are read back.  A CTA takes half a page.  Rows at or behind a sequence's length and on bad pages become 0.
 template <typename T, int D>
 __global__ void __launch_bounds__(kReadThreads) paged_expand_kernel(const __grid_constant__ PagedProblem p, const __grid_constant__ ExpandProblem x) {
   constexpr int LPR = D / 16, RPP = kReadThreads / LPR, PASSES = kReadRows / RPP, PARTS = kExpandRows / kReadRows;

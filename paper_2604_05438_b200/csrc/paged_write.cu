@@ -13,7 +13,7 @@
 // rotation.  A row's sum of squares and its largest magnitude are two or three shuffles between its lanes; all lanes of a
 // warp take part in them, with zeros where they have no row.
 // Measured: 15.8K tokens, 24 / 8 heads of 128, norms, half of the dims rotated, bounds, 16-bit cache: 80 us (4.1 TB/s);
-// 23.6K tokens, 32 / 8 heads of 64, rotated, 8-bit cache: 54 us (4.9 TB/s); one token 4.8 us a call.  The chain of a row is the
+// 23.6K tokens, 32 / 8 heads of 64, rotated, 8-bit cache: 56 us (4.8 TB/s); one token 4.8-5.0 us a call.  The chain of a row is the
 // bound (loads, sums over its lanes, conversions) at the occupancy that its registers leave: what helped were all loads of a row
 // before anything else, no spilled registers, angles in fixed point with frequencies in shared memory, 32-byte stores.  Tried
 // and no faster: several heads per CTA with the sines shared, packed 32-bit pairs, the next row's loads issued ahead into
@@ -46,8 +46,8 @@ __device__ __forceinline__ uint4 pack_piece(const float* x) {
 // A rotated pair: turns per position, less whole ones, in units of 2^-64, and 2 pi / 2^32; that is NaN where the frequency is infinite
 // or no number, for which fixed point has nothing.
 struct __align__(16) Turn { unsigned long long per; float unit; };
-// Cosine and sine of an angle of a / 2^32 turns (unit: 2 pi / 2^32): less the nearest quarter turn, an angle |y| <= pi / 4 is left, of which the
-// Taylor polynomials of degree 9 and 10 are off by y^11 / 11! = 1.8e-9 and y^12 / 12! = 1.1e-10, less than 32 bits hold.
+// Cosine and sine of an angle of a / 2^32 turns (unit: 2 pi / 2^32): less the nearest quarter turn, an angle |y| <= pi / 4 is
+// left, of which the Taylor polynomials of degree 9 and 10 are off by y^11 / 11! = 1.8e-9 and y^12 / 12! = 1.1e-10, less than 32 bits hold.
 // (sincospif took about 125 instructions of a pair, two thirds of the kernel's.)
 __device__ __forceinline__ void turn_cos_sin(uint32_t a, float unit, float& cs, float& sn) {
   const uint32_t quarter = a + 0x20000000u;                  // its top two bits: the quarter
